@@ -41,6 +41,10 @@ EXPORTED_LAYER = ("mla_proj_workspace_bytes", "mla_pre_attn", "mla_post_attn", "
 # mla_layer_tune knobs (include/mla_layer.h)
 TUNE_GEMM_BM, TUNE_GEMM_BN, TUNE_GEMM_DEPTH, TUNE_MHA_MIN_ROWS, TUNE_MHA_PAIRS = range(5)
 HIDDEN = 2048
+# include/mla_cache.h
+EXPORTED_CACHE = ("mla_cache8_scale_bytes", "append_latent_kv_rope", "append_latent_kv8", "mixed_step_attn8_workspace_bytes",
+                  "mixed_step_attn_window_workspace_bytes", "mixed_step_attn8", "mixed_step_attn_window")
+MLA_CACHE8_BLOCK = 16
 
 
 class MlaError(RuntimeError):
@@ -75,6 +79,14 @@ class mla_proj_weights(ctypes.Structure):
         ("rms_eps", ctypes.c_float),
         ("rope_base", ctypes.c_float),
     ]
+
+
+class mla_cache8(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class mla_window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
 _lib = None
@@ -130,6 +142,18 @@ def lib() -> ctypes.CDLL:
         L.mla_attention_layer.restype = ctypes.c_int
         L.mla_layer_tune.argtypes = [i32, i32]
         L.mla_layer_tune.restype = ctypes.c_int
+        bp, cp, np_ = ctypes.POINTER(mla_batch), ctypes.POINTER(mla_cache8), ctypes.POINTER(mla_window)
+        L.mla_cache8_scale_bytes.argtypes = [i32, i32]
+        L.append_latent_kv_rope.argtypes = [bp, vp, ctypes.c_float, vp, vp]
+        L.append_latent_kv8.argtypes = [bp, vp, ctypes.c_float, cp, vp]
+        L.mixed_step_attn8.argtypes = [bp, vp, cp, np_, ctypes.c_float, vp, i32, vp, vp, sz, vp]
+        L.mixed_step_attn_window.argtypes = [bp, vp, vp, np_, ctypes.c_float, vp, i32, vp, vp, sz, vp]
+        for f in (L.append_latent_kv_rope, L.append_latent_kv8, L.mixed_step_attn8, L.mixed_step_attn_window):
+            f.restype = ctypes.c_int
+        for f in (L.mixed_step_attn8_workspace_bytes, L.mixed_step_attn_window_workspace_bytes):
+            f.argtypes = [bp, np_]
+            f.restype = sz
+        L.mla_cache8_scale_bytes.restype = sz
         _lib = L
     return _lib
 
@@ -346,3 +370,119 @@ class tuned:
         for k in self.settings:
             layer_tune(k, -1)
         return False
+
+
+# --------------------------------------------------------------------------
+# The compact latent cache (include/mla_cache.h)
+# --------------------------------------------------------------------------
+class LatentCache8:
+    """A paged latent cache held in 8 bits: `data`, uint8 e4m3 codes
+    [num_pages][P][576], and `scales`, bf16 [num_pages][P / 16][2].
+
+    LatentCache8(num_pages=n, page_size=P) allocates both (every code 0, every
+    scale 1); LatentCache8(data=.., scales=..) takes a program's own tensors, whose
+    scales must be allocated to a multiple of 16 bytes."""
+
+    def __init__(self, num_pages: Optional[int] = None, page_size: Optional[int] = None, device="cuda", *, data=None, scales=None):
+        import torch
+        if data is None:
+            n = int(lib().mla_cache8_scale_bytes(int(num_pages), int(page_size)))
+            if n == 0:
+                raise ValueError("need num_pages >= 1 and a page size that is a power of two in [16, 1024]")
+            data = torch.zeros((num_pages, page_size, D_QK), dtype=torch.uint8, device=device)
+            # 4 bytes a block of 16 tokens, rounded up to 16
+            whole = torch.ones(n // 2, dtype=torch.bfloat16, device=device)
+            scales = whole[:num_pages * (page_size // MLA_CACHE8_BLOCK) * 2].view(num_pages, page_size // MLA_CACHE8_BLOCK, 2)
+        if data.element_size() != 1 or data.dim() != 3 or data.shape[2] != D_QK or not data.is_contiguous():
+            raise ValueError("data must be contiguous uint8 [num_pages][P][576]")
+        if (scales.element_size() != 2 or tuple(scales.shape) != (data.shape[0], data.shape[1] // MLA_CACHE8_BLOCK, 2) or
+                not scales.is_contiguous()):
+            raise ValueError("scales must be contiguous bf16 [num_pages][P / 16][2]")
+        self.data, self.scales = data, scales
+        self.num_pages, self.page_size = int(data.shape[0]), int(data.shape[1])
+        self.c = mla_cache8(data=_ptr(data), scales=_ptr(scales))
+
+
+def _window(window):
+    """(window, sinks) -> a pointer for the C ABI (None: no window)."""
+    return None if window is None else ctypes.byref(mla_window(int(window[0]), int(window[1])))
+
+
+def _cache8(batch: DeviceBatch, cache: LatentCache8):
+    if cache.page_size != batch.page_size or cache.num_pages < batch.num_pages:
+        raise ValueError("the cache's pages do not match the batch's")
+    _dev(cache.data, "the cache's data", tuple(cache.data.shape), (1,))
+    return ctypes.byref(cache.c)
+
+
+def _dev(t, name, shape, itemsizes):
+    """Address of a contiguous device tensor of that shape, on the current device."""
+    import torch
+    if t.element_size() not in itemsizes or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {' or '.join(map(str, itemsizes))}-byte values")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+    return t.data_ptr()
+
+
+def _attend_args(batch: DeviceBatch, softmax_scale, out, lse, workspace):
+    T = batch.num_rows
+    if workspace is not None:
+        _dev(workspace, "workspace", tuple(workspace.shape), (workspace.element_size(),))
+    return (float(softmax_scale), _dev(out, "out", (T, NUM_HEADS, D_V), (2, 4)), _out_mode(out),
+            0 if lse is None else _dev(lse, "lse", (T, NUM_HEADS), (4,)), _ptr(workspace), _nbytes(workspace))
+
+
+def _queries(batch: DeviceBatch, q):
+    return _dev(q, "q", (batch.num_rows, NUM_HEADS, D_QK), (2,))
+
+
+def _pool(batch: DeviceBatch, kv_cache):
+    if kv_cache.shape[0] < batch.num_pages:
+        raise ValueError(f"kv_cache has {kv_cache.shape[0]} pages, the batch's pool {batch.num_pages}")
+    return _dev(kv_cache, "kv_cache", (kv_cache.shape[0], batch.page_size, D_QK), (2,))
+
+
+def append_latent_kv_rope(batch: DeviceBatch, new_latents, rope_base: float, kv_cache, stream=None) -> None:
+    """append_latent_kv of bf16 latents [T][576] whose 64 rope dims are rotated to their positions on the way."""
+    _check(lib().append_latent_kv_rope(ctypes.byref(batch.c), _dev(new_latents, "new_latents", (batch.num_rows, D_QK), (2,)),
+                                       float(rope_base), _pool(batch, kv_cache), _stream(stream)))
+
+
+def append_latent_kv8(batch: DeviceBatch, new_latents, cache: LatentCache8, rope_base: float = 0.0, stream=None) -> None:
+    """Append bf16 latents [T][576] into the 8-bit cache; rope_base 0: they are rotated already."""
+    _check(lib().append_latent_kv8(ctypes.byref(batch.c), _dev(new_latents, "new_latents", (batch.num_rows, D_QK), (2,)),
+                                   float(rope_base), _cache8(batch, cache), _stream(stream)))
+
+
+def mixed_step_attn8(batch: DeviceBatch, q, cache: LatentCache8, softmax_scale: float, out, lse=None, workspace=None,
+                     window=None, stream=None) -> None:
+    """mixed_step_attn over the 8-bit cache; window: (window, sinks) or None."""
+    _check(lib().mixed_step_attn8(ctypes.byref(batch.c), _queries(batch, q), _cache8(batch, cache), _window(window),
+                                  *_attend_args(batch, softmax_scale, out, lse, workspace), _stream(stream)))
+
+
+def mixed_step_attn_window(batch: DeviceBatch, q, kv_cache, window, softmax_scale: float, out, lse=None, workspace=None,
+                           stream=None) -> None:
+    """mixed_step_attn through a window of keys and a few first tokens, (window, sinks)."""
+    _check(lib().mixed_step_attn_window(ctypes.byref(batch.c), _queries(batch, q), _pool(batch, kv_cache), _window(window),
+                                        *_attend_args(batch, softmax_scale, out, lse, workspace), _stream(stream)))
+
+
+def _workspace(query, batch: DeviceBatch, window, device):
+    import torch
+    n = int(query(ctypes.byref(batch.c), _window(window)))
+    err = lib().mla_last_error().decode()
+    if n == 0 and err:
+        raise MlaError(MLA_ERR_INVALID_ARG, err)
+    return torch.zeros(n, dtype=torch.uint8, device=device) if n > 0 else None
+
+
+def workspace_for_cache8(batch: DeviceBatch, window=None, device="cuda"):
+    """A zeroed workspace for mixed_step_attn8 (None if it needs none)."""
+    return _workspace(lib().mixed_step_attn8_workspace_bytes, batch, window, device)
+
+
+def workspace_for_window(batch: DeviceBatch, window, device="cuda"):
+    """A zeroed workspace for mixed_step_attn_window (None if it needs none)."""
+    return _workspace(lib().mixed_step_attn_window_workspace_bytes, batch, window, device)

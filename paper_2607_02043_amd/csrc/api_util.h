@@ -1,9 +1,28 @@
 // Error reporting and batch checks shared by the entry points of libmlastep.
 #pragma once
 #include "mla_step.h"
+
+#include <hip/hip_runtime.h>
 #include "chunk_route.h"
 
 namespace mla {
+
+// What a call uses of the cache, for check mode: writes in blocks of `block`
+// tokens, and, with a window (0: none), no key in [sinks, p - window].
+struct CheckUse {
+    long long block = 1, window = 0, sinks = 0;
+};
+
+// Status and message of a failed HIP call.
+int hip_error(hipError_t e, const char *what);
+
+// Host checks of a batch, its rows and log2 of its page size (set only if there are requests).
+int batch_shape(const mla_batch *batch, int *num_rows, int *log2_page);
+
+// Check mode's tests before and after a launch; MLA_OK at once when it is off.
+int check_before(const mla_batch *batch, const CheckUse &use, void *stream);
+int check_after(const char *what, void *stream);
+
 
 // Sets the thread's mla_last_error message (printf format) and returns code.
 int set_error(int code, const char *fmt, ...);

@@ -841,8 +841,9 @@ int make_plan(const mla_batch *b, const Shape &sh, Plan *pl, mla::ChunkRoute rou
 // host ones, every block-table entry a request uses lies in the pool, and no
 // slot a request writes is written or read by another request (or twice by
 // one).  Synchronises the stream first (the device arrays may be produced on
-// it).
-int check_device_batch(const mla_batch *b, const Shape &sh, hipStream_t s) {
+// it).  use.block > 1: slots are written in blocks of that many tokens (the
+// 8-bit cache).  use.window > 0: keys that no row of the step sees are not used.
+int check_device_batch(const mla_batch *b, const Shape &sh, hipStream_t s, const mla::CheckUse &use = {}) {
     hipError_t e = hipStreamSynchronize(s);
     if (e != hipSuccess) return hip_fail(e, "check mode: hipStreamSynchronize");
     const size_t R = sh.R, mp = b->max_pages_per_req;
@@ -863,9 +864,12 @@ int check_device_batch(const mla_batch *b, const Shape &sh, hipStream_t s) {
         }
     }
     const long long P = b->page_size;
+    // keys [sinks, hidden_to) of request r are seen by none of its rows
+    const auto hidden_to = [&](size_t r) { return use.window > 0 ? (long long)b->prefix_lens[r] - use.window + 1 : 0; };
     for (size_t r = 0; r < R; ++r) {
         const long long n = ceil_div_ll((long long)b->prefix_lens[r] + b->q_lens[r], P);
         for (long long j = 0; j < n; ++j) {
+            if (j * P >= use.sinks && (j + 1) * P <= hidden_to(r)) continue;
             const int32_t id = bt[r * mp + j];
             if (id < 0 || id >= b->num_pages)
                 return fail(MLA_ERR_INVALID_ARG,
@@ -873,24 +877,25 @@ int check_device_batch(const mla_batch *b, const Shape &sh, hipStream_t s) {
                             b->num_pages);
         }
     }
-    const long long slots = (long long)b->num_pages * P;
+    const long long B = use.block, slots = (long long)b->num_pages * P;
     if (slots <= (1LL << 28)) {
-        std::vector<int32_t> writer(slots, -1);
+        std::vector<int32_t> writer(slots / B, -1);
         for (size_t r = 0; r < R; ++r)
-            for (long long t = b->prefix_lens[r]; t < (long long)b->prefix_lens[r] + b->q_lens[r]; ++t) {
+            for (long long t = b->prefix_lens[r] / B * B; t < (long long)b->prefix_lens[r] + b->q_lens[r]; t += B) {
                 const long long sl = (long long)bt[r * mp + t / P] * P + t % P;
-                if (writer[sl] >= 0)
+                if (writer[sl / B] >= 0)
                     return fail(MLA_ERR_INVALID_ARG, "check mode: slot %lld is written by requests %d and %zu", sl,
-                                writer[sl], r);
-                writer[sl] = (int32_t)r;
+                                writer[sl / B], r);
+                writer[sl / B] = (int32_t)r;
             }
         for (size_t r = 0; r < R; ++r)
-            for (long long t = 0; t < b->prefix_lens[r]; ++t) {
+            for (long long t = 0; t < b->prefix_lens[r] / B * B; ++t) {
+                if (t >= use.sinks && t < hidden_to(r)) continue;
                 const long long sl = (long long)bt[r * mp + t / P] * P + t % P;
-                if (writer[sl] >= 0)
+                if (writer[sl / B] >= 0)
                     return fail(MLA_ERR_INVALID_ARG,
                                 "check mode: request %zu reads key %lld from slot %lld, which request %d writes", r, t,
-                                sl, writer[sl]);
+                                sl, writer[sl / B]);
             }
     }
     return MLA_OK;
@@ -931,6 +936,27 @@ int attn_workspace(const mla_batch *batch, size_t *bytes, ChunkRoute route) {
     st = make_plan(batch, sh, &pl, route);
     if (st == MLA_OK) *bytes = pl.bytes;
     return st;
+}
+
+int hip_error(hipError_t e, const char *what) { return hip_fail(e, what); }
+
+int batch_shape(const mla_batch *batch, int *num_rows, int *log2_page) {
+    Shape sh;
+    const int st = check_batch(batch, &sh);
+    *num_rows = st == MLA_OK ? sh.T : 0;
+    *log2_page = sh.log2_page;
+    return st;
+}
+
+int check_before(const mla_batch *batch, const CheckUse &use, void *stream) {
+    if (!check_mode()) return MLA_OK;
+    Shape sh;
+    sh.R = batch->num_reqs;
+    return check_device_batch(batch, sh, static_cast<hipStream_t>(stream), use);
+}
+
+int check_after(const char *what, void *stream) {
+    return check_mode() ? check_after_launch(static_cast<hipStream_t>(stream), what) : MLA_OK;
 }
 
 int batch_rows(const mla_batch *batch, int *num_rows) {

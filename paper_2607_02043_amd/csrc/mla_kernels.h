@@ -64,6 +64,10 @@ struct AttnArgs {
     int32_t out_bf16;
     int32_t spin_limit;        // sleeps of a bounded wait before it gives up (kSpinLimit)
     ChunkRoute route;          // chunk requests it sends to the multi-head path are left out of this launch
+    // forms of mla_cache.h: the 8-bit cache (in place of kv), and the window (0: none) with its sinks
+    const uint8_t *kv8;
+    const uint16_t *kv8_scales;
+    int32_t window, sinks;
 };
 
 // The fixed first items of the attention launch's G workgroups (G at most the
@@ -108,7 +112,27 @@ struct AppendArgs {
     int32_t num_pages;
 };
 
+struct Append8Args {
+    const uint16_t *src;
+    uint8_t *data;
+    uint16_t *scales;
+    const int32_t *cu_q;
+    const int32_t *prefix;
+    const int32_t *bt;
+    double log2_base;  // of the rotation; 0: none
+    int32_t num_reqs;
+    int32_t num_rows;
+    int32_t num_blocks;  // workgroups: blocks of 16 tokens that the rows touch
+    int32_t log2_page;
+    int32_t page_size;
+    int32_t max_pages;
+    int32_t num_pages;
+};
+
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);
+hipError_t launch_append_rope(const AppendArgs &a, double log2_base, hipStream_t s);
+hipError_t launch_append8(const Append8Args &a, hipStream_t s);
+hipError_t launch_rows(const AttnArgs &a, hipStream_t s);
 // Reads the device's sticky kernel error flags (kFlag*), and clears them if asked.
 hipError_t read_flags(int *flags, bool clear);
 // Device address of the current device's no-allocation scratch

@@ -1660,6 +1660,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     if (lane < kChunksPerRow - 64) dst[64 + lane] = vb;
 }
 
+#include "cache_append.h"
+#include "cache_attend.h"
+
 }  // namespace
 
 #ifdef MLA_TRACE
@@ -1703,6 +1706,28 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t s) {
     const int grid = (a.num_rows + rows_per_block - 1) / rows_per_block;
     if (grid == 0) return hipSuccess;
     hipLaunchKernelGGL(append_kernel, dim3(grid), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_append_rope(const AppendArgs &a, double log2_base, hipStream_t s) {
+    const int rows_per_block = kThreads / 64;
+    const int grid = (a.num_rows + rows_per_block - 1) / rows_per_block;
+    if (grid == 0) return hipSuccess;
+    hipLaunchKernelGGL(append_rope_kernel, dim3(grid), dim3(kThreads), 0, s, a, log2_base);
+    return hipGetLastError();
+}
+
+hipError_t launch_append8(const Append8Args &a, hipStream_t s) {
+    if (a.num_blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL(append8_kernel, dim3(a.num_blocks), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_rows(const AttnArgs &a, hipStream_t s) {
+    if (a.kv8 != nullptr)
+        hipLaunchKernelGGL(rows_kernel<true>, dim3(a.num_rows), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL(rows_kernel<false>, dim3(a.num_rows), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -1,0 +1,574 @@
+"""The compact latent cache on the GPU against the 64-bit oracle: appends with the
+rotation on the way, the 8-bit cache, attention over it and through windows."""
+import numpy as np
+import pytest
+
+import cache_cases as C
+import paper_2607_02043_amd as mla
+from harness import from_dev_u16, log, to_dev
+from oracle import cache_oracle as CO
+from paper_2607_02043_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+SCALE, BASE = W.SOFTMAX_SCALE, 10000.0
+
+
+@pytest.fixture(autouse=True)
+def flags():
+    mla.device_flags(clear=True)
+    yield
+    for k in (mla.MLA_DEBUG_CHECK, mla.MLA_DEBUG_CHUNK_KEYS, mla.MLA_DEBUG_DEC_UNIT, mla.MLA_DEBUG_DEC_FIRST):
+        mla.debug_set(k, -1 if k != mla.MLA_DEBUG_CHECK else 0)
+    mla.device_flags(clear=True)
+
+
+def up8(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def dev_cache(data, scales):
+    """A LatentCache8 of these arrays."""
+    import torch
+    c = mla.LatentCache8(num_pages=data.shape[0], page_size=data.shape[1])
+    c.data.copy_(up8(data))
+    c.scales.view(torch.int16).copy_(to_dev(scales))
+    return c
+
+
+def down8(c):
+    import torch
+    return c.data.cpu().numpy(), c.scales.view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+class Attend:
+    """One attention call and its check: 8-bit (data, scales) or bf16 (pool)."""
+
+    def __init__(self, b, q, data=None, scales=None, pool=None, window=None, bf16=False):
+        import torch
+        self.b, self.q, self.window = b, q, window
+        self.db = mla.DeviceBatch.from_batch(b)
+        self.qd = to_dev(q.reshape(-1, 16, 576))
+        self.out = torch.full((b.num_rows, 16, 512), float("nan"), dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda")
+        self.lse = torch.full((b.num_rows, 16), float("nan"), dtype=torch.float32, device="cuda")
+        self.bf16, self.eight = bf16, data is not None
+        if self.eight:
+            self.data, self.scales, self.cache = data, scales, dev_cache(data, scales)
+            self.ws = mla.workspace_for_cache8(self.db, window=window)
+            self.keys = lambda r, n: CO.keys8(b, r, n, data, scales)
+        else:
+            self.cache = to_dev(pool)
+            self.ws = mla.workspace_for_window(self.db, window)
+            self.keys = lambda r, n: CO.keys16(b, r, n, pool)
+
+    def run(self, stream=None):
+        if self.eight:
+            mla.mixed_step_attn8(self.db, self.qd, self.cache, SCALE, self.out, self.lse, self.ws, window=self.window, stream=stream)
+        else:
+            mla.mixed_step_attn_window(self.db, self.qd, self.cache, self.window, SCALE, self.out, self.lse, self.ws, stream=stream)
+        return self
+
+    def results(self):
+        import torch
+        torch.cuda.synchronize()
+        return self.out.double().cpu().numpy(), self.lse.double().cpu().numpy()
+
+    def check(self, what, rows=None):
+        out, lse = self.results()
+        b, (w, s) = self.b, self.window or (0, 0)
+        q = CO.bf16_value(self.q).reshape(-1, 16, 576)
+        cu, worst = b.cu_q, [0.0, 0.0]
+        keys, at = None, -1
+        for row in range(b.num_rows) if rows is None else rows:
+            r = int(np.searchsorted(cu, row, side="right")) - 1
+            if r != at:
+                keys, at = self.keys(r, int(b.prefix_lens[r] + b.q_lens[r])), r
+            pos = int(b.prefix_lens[r]) + row - int(cu[r])
+            ro, rl = CO.attend_row(q[row], keys, pos, SCALE, w, s)
+            to, tl = C.bounds(q[row], keys, pos, SCALE, w, s, b.q_lens[r] > 1, not self.bf16, ro, rl)
+            eo, el = np.abs(out[row] - ro), np.abs(lse[row] - rl)
+            worst = [max(worst[0], float((eo / to).max())), max(worst[1], float((el / tl).max()))]
+            assert (eo <= to).all() and (el <= tl).all(), (what, row, pos, float((eo / to).max()), float((el / tl).max()))
+        log(f"  {what}: errors over their bounds: out {worst[0]:.3f} lse {worst[1]:.3f}")
+        return self
+
+
+# ------------------------------------------------------------------- appends
+APPENDS = [  # prefix, rows, page
+    ([0], [1], 1), ([0], [1], 64), ([5, 0, 31], [1, 2, 1], 16), ([15, 16, 17, 0], [1, 1, 18, 47], 32), ([100, 63, 64, 127], [130, 1, 64, 3], 64),
+    ([1023, 0], [2, 1500], 1024), ([7, 9, 8], [3, 20, 9], 2), (list(range(70)), [1] * 69 + [40], 16), ([3] * 300, [1] * 300, 16),
+]
+
+
+def ids(v):
+    return f"{v[:4]}x{len(v)}".replace(" ", "") if isinstance(v, list) else str(v)
+
+
+@pytest.mark.parametrize("prefix,rows,page", APPENDS, ids=ids)
+def test_rotated_append(prefix, rows, page):
+    log(f"[gpu] rotated append {len(rows)} requests, page {page}")
+    b = C.batch(prefix, rows, page, seed=page)
+    new = C.new_latents(b, seed=page)
+    rng = np.random.default_rng(page)
+    pool = rng.integers(0, 1 << 16, (b.num_pages, page, 576), dtype=np.uint16)
+    dev, db = to_dev(pool), mla.DeviceBatch.from_batch(b)
+    mla.append_latent_kv_rope(db, to_dev(new), BASE, dev)
+    got = from_dev_u16(dev).reshape(-1, 576)
+    want = pool.reshape(-1, 576).copy()
+    for r, x in enumerate(CO.rows(b, new, BASE)):
+        for i, v in enumerate(x):
+            s, row = CO.slot(b, r, int(b.prefix_lens[r]) + i), int(b.cu_q[r]) + i
+            want[s, :512] = new[row, :512]
+            # rounded once, of an fp32 value: cos and sin within 2^-22 (the angle's fraction rounds at 2^-25
+            # turns), two products and a sum of 2^-24 each, of |x0| + |x1| at most
+            m = np.repeat(np.abs(CO.bf16_value(new[row, 512:])).reshape(32, 2).sum(1), 2)
+            err = np.abs(CO.bf16_value(got[s, 512:]) - v[512:])
+            assert (err <= np.abs(v[512:]) * 2.0 ** -8 + m * 2.0 ** -21).all(), (r, i)
+            want[s, 512:] = got[s, 512:]
+    np.testing.assert_array_equal(got, want)  # compressed dims copied, other slots as they were
+    assert mla.device_flags() == 0
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_far_positions(eight):
+    """Positions near 2^30: the table's other entries point at page 0."""
+    P, p, c = 1024, (1 << 30) - 5, 5
+    table = np.zeros((1, -(-(p + c) // P)), dtype=np.int32)
+    table[0, -1] = 2
+    b = W.Batch(P, np.array([p], np.int32), np.array([c], np.int32), table, 3)
+    new, db = C.new_latents(b, 1), mla.DeviceBatch.from_batch(b)
+    x = CO.rows(b, new, BASE)[0]
+    at = [2 * P + (p + i) % P for i in range(c)]
+    m = np.repeat(np.abs(CO.bf16_value(new[:, 512:])).reshape(c, 32, 2).sum(2), 2, axis=1)
+    if eight:
+        cache = mla.LatentCache8(num_pages=3, page_size=P)
+        mla.append_latent_kv8(db, to_dev(new), cache, rope_base=BASE)
+        got = CO.keys8(W.Batch(P, np.zeros(1, np.int32), np.ones(1, np.int32), np.arange(3, dtype=np.int32)[None], 3), 0, 3 * P, *down8(cache))
+        # the block holds 11 earlier tokens (2^30 - 5 = 11 mod 16) under the new cache's scale of 1, which stays: 9 2^-5
+        # would do for the new ones, but a block's scale never shrinks, so the smallest half step is 2^-10
+        half = np.maximum(2.0 ** -4 * np.abs(x[:, 512:]), 2.0 ** -10)
+    else:
+        pool = to_dev(np.zeros((3, P, 576), np.uint16))
+        mla.append_latent_kv_rope(db, to_dev(new), BASE, pool)
+        got, half = CO.bf16_value(from_dev_u16(pool)).reshape(-1, 576), 2.0 ** -8 * np.abs(x[:, 512:])
+    # (the 64-bit angle itself is off by 2^30 2^-53 turns at most)
+    assert (np.abs(got[at, 512:] - x[:, 512:]) <= half + m * 2.0 ** -20).all()
+
+
+def special_rows(b, seed):
+    """Zeros, tiny, huge, NaN and infinite values among ordinary rows."""
+    new = C.new_latents(b, seed).copy()
+    f = W.bf16_bits_to_f32(new)
+    rng = np.random.default_rng(seed)
+    for i in range(b.num_rows):
+        k = rng.integers(0, 9)
+        if k == 0:
+            f[i] = 0
+        elif k == 1:
+            f[i] *= np.float32(2.0 ** -70)
+        elif k == 2:
+            f[i, rng.integers(0, 576, 5)] = np.float32(3e38)
+        elif k == 3:
+            f[i, rng.integers(0, 576, 4)] = np.nan
+        elif k == 4:
+            f[i, rng.integers(0, 576, 3)] = -np.inf
+        elif k == 5:
+            f[i] *= np.float32(2.0 ** rng.integers(-12, 13))
+    return W.f32_to_bf16_bits(f)
+
+
+@pytest.mark.parametrize("special", [False, True])
+@pytest.mark.parametrize("base", [0.0, BASE])
+@pytest.mark.parametrize("prefix,rows,page", [a for a in APPENDS if a[2] >= 16], ids=ids)
+def test_append8(prefix, rows, page, base, special):
+    log(f"[gpu] 8-bit append {len(rows)} requests, page {page}, base {base}, special {special}")
+    b = C.batch(prefix, rows, page, seed=page)
+    new = special_rows(b, page) if special else C.new_latents(b, page)
+    data, scales = C.cache8(b, page)
+    cache, db = dev_cache(data, scales), mla.DeviceBatch.from_batch(b)
+    mla.append_latent_kv8(db, to_dev(new), cache, rope_base=base)
+    got, gs = down8(cache)
+    want, ws, touched = CO.append8(b, new, base, data, scales)
+    got, gs = got.reshape(-1, 576), gs.reshape(-1, 2)
+    same = want.copy()
+    if base:  # rotated dims: fp32 against 64 bits, so a value next to a border may go the other way
+        for r, x in enumerate(CO.rows(b, new, base)):
+            for i, v in enumerate(x):
+                s, row = CO.slot(b, r, int(b.prefix_lens[r]) + i), int(b.cu_q[r]) + i
+                pairs = CO.bf16_value(new[row, 512:]).reshape(32, 2)
+                m = np.repeat(np.where(np.isfinite(pairs), np.abs(pairs), 0).sum(1), 2)
+                sc = CO.scale_value(gs[s // 16, 1])
+                g = CO.TABLE[got[s, 512:]] * sc
+                fine = np.isfinite(v[512:])
+                assert (np.isnan(g) == ~fine).all(), (r, i)
+                lim = np.abs(v[512:]) * 2.0 ** -4 + sc * 2.0 ** -10 + m * 2.0 ** -21
+                assert (np.abs(g - v[512:]) <= lim)[fine].all(), (r, i)
+                same[s, 512:] = got[s, 512:]
+        rope_ok = np.isfinite(CO.scale_value(ws[:, 1]))
+        # a maximum within 2^-21 of 448 2^e may take the scale next to it
+        assert (np.abs(np.log2(CO.scale_value(gs[rope_ok, 1])) - np.log2(CO.scale_value(ws[rope_ok, 1]))) <= 1).all()
+        np.testing.assert_array_equal(gs[:, 0], ws[:, 0])
+        assert (gs[:, 1] != ws[:, 1]).mean() <= 0.01
+    else:
+        np.testing.assert_array_equal(gs, ws)
+    nan = np.isnan(CO.TABLE[same])
+    np.testing.assert_array_equal(np.isnan(CO.TABLE[got]), nan)
+    if base:  # earlier tokens of a block whose rope scale went the other way, if any
+        odd = np.repeat(gs[:, 1] != ws[:, 1], 16)
+        same[odd, 512:] = got[odd, 512:]
+    np.testing.assert_array_equal(np.where(nan, 0, got), np.where(nan, 0, same))
+    assert mla.device_flags() == 0
+
+
+def test_append8_twice_is_the_same():
+    b = C.batch([21, 0, 40], [1, 33, 5], 16, seed=3)
+    data, scales = C.cache8(b, 3)
+    cache, db, new = dev_cache(data, scales), mla.DeviceBatch.from_batch(b), to_dev(C.new_latents(b, 3, spread=40.0))
+    mla.append_latent_kv8(db, new, cache, rope_base=BASE)
+    first = down8(cache)
+    mla.append_latent_kv8(db, new, cache, rope_base=BASE)
+    for x, y in zip(first, down8(cache)):
+        np.testing.assert_array_equal(x, y)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_append_with_a_bad_page(eight):
+    b = C.batch([20, 0], [1, 40], 16, seed=5)
+    b.block_table = b.block_table.copy()
+    b.block_table[1, 1] = b.num_pages + 3  # tokens 16 .. 31 of the chunk
+    new, db = C.new_latents(b, 5), mla.DeviceBatch.from_batch(b)
+    if eight:
+        data, scales = C.cache8(b, 5, upto=lambda r: 20 if r == 0 else 0)
+        cache = dev_cache(data, scales)
+        mla.append_latent_kv8(db, to_dev(new), cache)
+        got = down8(cache)[0]
+        changed = (got != data).reshape(-1, 576).any(1)
+    else:
+        pool = np.zeros((b.num_pages, 16, 576), np.uint16)
+        dev = to_dev(pool)
+        mla.append_latent_kv_rope(db, to_dev(new), BASE, dev)
+        changed = (from_dev_u16(dev) != 0).reshape(-1, 576).any(1)
+    assert mla.device_flags() & mla.MLA_FLAG_BAD_PAGE
+    want = np.zeros(b.num_pages * 16, bool)
+    for t in [*range(16), *range(32, 40)]:
+        want[CO.slot(b, 1, t)] = True
+    want[CO.slot(b, 0, 20)] = True
+    if eight:  # (earlier tokens of request 0's block may be rounded again)
+        for t in range(16, 20):
+            changed[CO.slot(b, 0, t)] = want[CO.slot(b, 0, t)] = False
+    np.testing.assert_array_equal(changed, want)
+
+
+# ----------------------------------------------------------------- attention
+BATCHES = {  # prefix, rows, page
+    "one key": ([0], [1], 16),
+    "tile edges": ([15, 16, 30, 31, 32, 33, 62, 63, 64, 65], [1] * 10, 16),
+    "chunks of 2 to 40": ([0, 0, 5, 31, 64, 100], [2, 9, 3, 17, 8, 40], 32),
+    "mixed": ([200, 0, 333, 70, 1, 47], [1, 65, 1, 33, 1, 2], 16),
+    "wide pages": ([1500, 700], [1, 70], 1024),
+    "many requests": (list(range(0, 140, 2)), [1] * 66 + [2, 3, 4, 5], 64),
+}
+WINDOWS = [None, (1, 0), (1, 5), (7, 0), (32, 32), (33, 1), (100, 4), (64, 70), (1 << 30, 0), (5, 1 << 30)]
+
+
+@pytest.mark.parametrize("window", WINDOWS, ids=str)
+@pytest.mark.parametrize("name", BATCHES)
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_attention(name, window, eight):
+    if not eight and window is None:
+        pytest.skip("mixed_step_attn, tested by its own")
+    prefix, rows, page = BATCHES[name]
+    log(f"[gpu] {name}, window {window}, 8-bit {eight}")
+    b = C.batch(prefix, rows, page, seed=len(rows))
+    q = C.queries(b, 1)
+    if eight:
+        data, scales = C.cache8(b, 2, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+        a = Attend(b, q, data, scales, window=window)
+    else:
+        a = Attend(b, q, pool=filled16(b, 2), window=window)
+    a.run().check(name)
+    assert mla.device_flags() == 0
+
+
+def filled16(b, seed, fill=C.NAN16):
+    """A bf16 pool with all of every request's tokens; the other slots hold NaN."""
+    rng = np.random.default_rng([seed, 4])
+    pool = np.full((b.num_pages * b.page_size, 576), fill, dtype=np.uint16)
+    for r in range(b.num_reqs):
+        n = int(b.prefix_lens[r] + b.q_lens[r])
+        t = np.arange(n)
+        s = b.block_table[r, t // b.page_size].astype(np.int64) * b.page_size + t % b.page_size
+        pool[s] = W.f32_to_bf16_bits(rng.standard_normal((n, 576), dtype=np.float32))
+    return pool.reshape(b.num_pages, b.page_size, 576)
+
+
+@pytest.mark.parametrize("page", [1, 2, 8])
+@pytest.mark.parametrize("window", [(1, 0), (9, 3), (40, 33)], ids=str)
+def test_window_on_small_pages(page, window):
+    b = C.batch([100, 0, 60, 3], [1, 20, 30, 1], page, seed=page)
+    Attend(b, C.queries(b, 1), pool=filled16(b, page), window=window).run().check(f"page {page}")
+
+
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_bf16_output(eight):
+    b = C.batch([130, 20, 9], [1, 30, 1], 16, seed=9)
+    if eight:
+        data, scales = C.cache8(b, 2, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+        Attend(b, C.queries(b, 1), data, scales, bf16=True).run().check("bf16 out")
+    else:
+        Attend(b, C.queries(b, 1), pool=filled16(b, 3), window=(50, 2), bf16=True).run().check("bf16 out")
+
+
+def sampled(b, n, seed=0):
+    """Rows to check at size: chunk starts, ends and block borders, and random ones."""
+    rng = np.random.default_rng(seed)
+    rows = set(rng.choice(b.num_rows, size=min(b.num_rows, n), replace=False).tolist())
+    for r in range(b.num_reqs):
+        if b.q_lens[r] > 1:
+            c0 = int(b.cu_q[r])
+            rows |= {c0 + i for i in (0, 1, 7, 8, int(b.q_lens[r]) - 1) if i < b.q_lens[r]}
+    return sorted(rows)
+
+
+LARGE = [  # prefix, rows, page, window, forced chunk keys, decode unit, decode-first workgroups
+    ([5000, 12000, 300, 40, 2000], [1, 1, 1, 1, 300], 64, None, 0, 0, -1),
+    ([3000, 2000, 2500], [1, 260, 1], 32, None, 192, 2, 5),
+    ([100000], [1], 64, None, 0, 0, -1),
+    ([20000, 15000, 9000], [1, 1, 500], 64, (2000, 64), 0, 0, -1),
+    ([9000, 4000, 4100], [1, 200, 1], 16, (513, 37), 128, 3, 64),
+    ([70000, 30000], [1, 40], 64, (30000, 0), 0, 0, -1),
+    ([900] * 90 + [100], [1] * 90 + [700], 128, (300, 4), 0, 0, 0),
+]
+
+
+@pytest.mark.parametrize("prefix,rows,page,window,keys,unit,first", LARGE, ids=ids)
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_split_rows(prefix, rows, page, window, keys, unit, first, eight):
+    if not eight and window is None:
+        pytest.skip("mixed_step_attn, tested by its own")
+    log(f"[gpu] split rows {rows[:6]}, window {window}, 8-bit {eight}")
+    b = C.batch(prefix, rows, page, seed=7)
+    for k, v in ((mla.MLA_DEBUG_CHUNK_KEYS, keys), (mla.MLA_DEBUG_DEC_UNIT, unit), (mla.MLA_DEBUG_DEC_FIRST, first)):
+        mla.debug_set(k, v)
+    if eight:
+        data, scales = C.cache8(b, 2, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+        a = Attend(b, C.queries(b, 1), data, scales, window=window)
+    else:
+        a = Attend(b, C.queries(b, 1), pool=filled16(b, 2), window=window)
+    a.run().check("split", sampled(b, 40))
+    first_out = a.results()
+    a.run()
+    for x, y in zip(first_out, a.results()):
+        np.testing.assert_array_equal(x, y)
+    assert mla.device_flags() == 0
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_nan_and_bad_pages_where_no_row_looks(eight, page):
+    """Pages that no row of the step sees: NaN values, then entries outside the pool."""
+    window = (40, 5)
+    b = C.batch([700, 400, 90], [1, 33, 1], page, seed=11)
+    q, upto = C.queries(b, 1), lambda r: int(b.prefix_lens[r] + b.q_lens[r])
+    data, scales = C.cache8(b, 2, upto=upto)
+    pool = filled16(b, 2)
+    a = Attend(b, q, data, scales, window=window) if eight else Attend(b, q, pool=pool, window=window)
+    a.run().check("before")
+    want = a.results()
+    import torch
+    for r in range(b.num_reqs):
+        for t in range(int(b.prefix_lens[r])):
+            if t >= window[1] and t <= int(b.prefix_lens[r]) - window[0]:
+                s = CO.slot(b, r, t)
+                if eight:
+                    a.cache.data.view(-1, 576)[s] = C.NAN8
+                else:
+                    a.cache.view(-1, 576)[s] = C.NAN16
+    a.run()
+    for x, y in zip(want, a.results()):
+        np.testing.assert_array_equal(x, y)
+    bt = b.block_table.copy()
+    for r in range(b.num_reqs):
+        for lp in range(bt.shape[1]):
+            k0, k1 = lp * page, lp * page + page - 1
+            if k0 >= window[1] and k1 <= int(b.prefix_lens[r]) - window[0]:
+                bt[r, lp] = (-7, b.num_pages + 9, 1 << 30)[lp % 3]
+    a.db.bt_dev.copy_(torch.from_numpy(bt))
+    for check in (0, 1):
+        mla.debug_set(mla.MLA_DEBUG_CHECK, check)
+        a.run()
+        for x, y in zip(want, a.results()):
+            np.testing.assert_array_equal(x, y)
+    assert mla.device_flags() == 0
+
+
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_a_nan_key_reaches_the_rows_that_see_it_alone(eight):
+    b = C.batch([50, 20, 33], [1, 40, 1], 32, seed=12)
+    window = (16, 2)
+    data, scales = C.cache8(b, 2, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+    pool = filled16(b, 2)
+    q = C.queries(b, 1)
+    a = Attend(b, q, data, scales, window=window) if eight else Attend(b, q, pool=pool, window=window)
+    a.run().check("before")
+    want = a.results()[0]
+    bad = {(0, 45), (1, 30), (1, 41), (2, 3)}  # (request, key)
+    for r, t in bad:
+        s = CO.slot(b, r, t)
+        if eight:
+            a.cache.data.view(-1, 576)[s, 100] = C.NAN8
+        else:
+            a.cache.view(-1, 576)[s, 100] = C.NAN16
+    got = a.run().results()[0]
+    for row in range(b.num_rows):
+        r = int(np.searchsorted(b.cu_q, row, side="right")) - 1
+        pos = int(b.prefix_lens[r]) + row - int(b.cu_q[r])
+        hit = any(k in CO.visible(pos, *window) for rr, k in bad if rr == r)
+        if hit:
+            assert np.isnan(got[row]).all(), (r, pos)
+        else:
+            np.testing.assert_array_equal(got[row], want[row], err_msg=str((r, pos)))
+
+
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_bad_page_is_not_followed(eight):
+    b = C.batch([200, 100], [1, 30], 16, seed=13)
+    data, scales = C.cache8(b, 2, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+    a = Attend(b, C.queries(b, 1), data, scales) if eight else Attend(b, C.queries(b, 1), pool=filled16(b, 2), window=(1 << 20, 0))
+    a.db.bt_dev[0, 3] = b.num_pages
+    a.db.bt_dev[1, 2] = -1
+    a.run().results()
+    assert mla.device_flags() & mla.MLA_FLAG_BAD_PAGE
+
+
+def test_scores_far_above_the_first_tiles():
+    """Chunk rows whose later scores exceed the first tile's by far more than fp16 holds, and rows that see
+    nothing of a block's first tile."""
+    b = C.batch([64, 0], [60, 90], 16, seed=14)
+    pool = filled16(b, 2)
+    f = W.bf16_bits_to_f32(pool).reshape(-1, 576)
+    for r in range(2):
+        for t in range(40, 60):
+            f[CO.slot(b, r, t)] *= 12
+    pool = W.f32_to_bf16_bits(f).reshape(pool.shape)
+    for window in ((30, 0), (30, 3), (1000, 0)):
+        Attend(b, C.queries(b, 1), pool=pool, window=window).run().check(str(window))
+
+
+def test_window_over_everything_is_plain_attention():
+    import torch
+    b = C.batch([300, 64, 17], [1, 90, 1], 64, seed=15)
+    pool, q = filled16(b, 2), C.queries(b, 1)
+    a = Attend(b, q, pool=pool, window=(1 << 30, 0)).run()
+    out, lse = torch.empty_like(a.out), torch.empty_like(a.lse)
+    mla.mixed_step_attn(a.db, a.qd, a.cache, SCALE, out, lse, mla.workspace_for(a.db))
+    got, gl = a.results()
+    assert np.abs(got - out.double().cpu().numpy()).max() <= 2e-3 and np.abs(gl - lse.double().cpu().numpy()).max() <= 1e-5
+
+
+# ------------------------------------------------------------------ together
+@pytest.mark.parametrize("window", [None, (48, 4)], ids=str)
+def test_serving_steps_on_the_8_bit_cache(window):
+    """A prompt in chunks beside decodes, then all of them decoding: append, then attention, step after step, with
+    blocks that grow a token at a time; the attention of each step against the values the cache then holds."""
+    import torch
+    P, n_req = 16, 4
+    lens = np.array([0, 37, 0, 90])
+    table = np.random.default_rng(3).permutation(64).astype(np.int32).reshape(n_req, 16)
+    first = W.Batch(P, lens.astype(np.int32), np.ones(n_req, np.int32), table, 64)
+    data, scales = C.cache8(first, 4)
+    cache = dev_cache(data, scales)
+    for step, rows in enumerate([[33, 1, 20, 1], [40, 1, 1, 1], [1, 1, 1, 1], [1, 1, 1, 1], [1, 2, 1, 9]]):
+        b = W.Batch(P, lens.astype(np.int32), np.array(rows, np.int32), table, 64)
+        new = C.new_latents(b, 100 + step, spread=2.0 ** (step - 2))
+        db = mla.DeviceBatch.from_batch(b)
+        mla.append_latent_kv8(db, to_dev(new), cache, rope_base=BASE)
+        data, scales = down8(cache)
+        a = Attend(b, C.queries(b, step), data, scales, window=window)
+        mla.mixed_step_attn8(db, a.qd, cache, SCALE, a.out, a.lse, a.ws, window=window)
+        a.check(f"step {step}")
+        lens = lens + np.array(rows)
+    assert mla.device_flags() == 0
+
+
+def test_rotated_append_then_window_attention():
+    b = C.batch([100, 30], [1, 45], 32, seed=16)
+    pool = filled16(b, 3)
+    new = C.new_latents(b, 6)
+    a = Attend(b, C.queries(b, 2), pool=pool, window=(60, 2))
+    mla.append_latent_kv_rope(a.db, to_dev(new), BASE, a.cache)
+    after = from_dev_u16(a.cache)
+    a.keys = lambda r, n: CO.keys16(b, r, n, after)
+    a.run().check("append, window")
+
+
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_captured_and_replayed(eight):
+    """Both operators in a captured graph, replayed with eager work between; each replay equals the eager result."""
+    import torch
+    b = C.batch([2000, 300, 40], [1, 50, 1], 64, seed=17)
+    mla.debug_set(mla.MLA_DEBUG_DEC_UNIT, 4)
+    upto = lambda r: int(b.prefix_lens[r] + b.q_lens[r])
+    data, scales = C.cache8(b, 2, upto=upto)
+    q, new = C.queries(b, 1), to_dev(C.new_latents(b, 8))
+    a = Attend(b, q, data, scales) if eight else Attend(b, q, pool=filled16(b, 2), window=(700, 4))
+
+    def both():
+        if eight:
+            mla.append_latent_kv8(a.db, new, a.cache, rope_base=BASE)
+        else:
+            mla.append_latent_kv_rope(a.db, new, BASE, a.cache)
+        a.run()
+
+    both()
+    want = a.results()
+    s = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        both()
+    for _ in range(3):
+        a.out.fill_(float("nan"))
+        a.lse.fill_(float("nan"))
+        g.replay()
+        for x, y in zip(want, a.results()):
+            np.testing.assert_array_equal(x, y)
+        both()
+        for x, y in zip(want, a.results()):
+            np.testing.assert_array_equal(x, y)
+
+
+def test_two_streams_at_once():
+    import torch
+    made = []
+    for seed, window in ((20, None), (21, (200, 4))):
+        b = C.batch([4000, 900, 100], [1, 100, 1], 64, seed=seed)
+        data, scales = C.cache8(b, seed, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+        made.append(Attend(b, C.queries(b, seed), data, scales, window=window))
+    want = [a.run().results() for a in made]
+    streams = [torch.cuda.Stream() for _ in made]
+    for a in made:
+        a.out.fill_(float("nan"))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for a, s in zip(made, streams):
+            a.run(stream=s)
+    for a, w in zip(made, want):
+        for x, y in zip(w, a.results()):
+            np.testing.assert_array_equal(x, y)
+
+
+def test_check_mode():
+    mla.debug_set(mla.MLA_DEBUG_CHECK, 1)
+    b = C.batch([20, 30], [1, 1], 32, seed=22)
+    data, scales = C.cache8(b, 2)
+    cache, new = dev_cache(data, scales), to_dev(C.new_latents(b, 1))
+    mla.append_latent_kv8(mla.DeviceBatch.from_batch(b), new, cache)
+    b.block_table = b.block_table.copy()
+    b.block_table[1] = b.block_table[0]  # tokens 20 and 30: other slots, the same block
+    db = mla.DeviceBatch.from_batch(b)
+    pool = to_dev(filled16(b, 1))
+    with pytest.raises(mla.MlaError, match="written by requests"):
+        mla.append_latent_kv8(db, new, cache)
+    b.block_table[1, 0] = b.num_pages
+    with pytest.raises(mla.MlaError, match="outside"):
+        mla.append_latent_kv_rope(mla.DeviceBatch.from_batch(b), new, BASE, pool)
