@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 #include "chunk_route.h"
+#include "mla_kernels.h"
 
 namespace mla {
 
@@ -34,7 +35,11 @@ int batch_rows(const mla_batch *batch, int *num_rows);
 // Workspace bytes of the attention launch for this batch (mixed_step_workspace_bytes
 // with the status of the checks and the planning), leaving out the chunk
 // requests that `route` sends to the multi-head path.
-int attn_workspace(const mla_batch *batch, size_t *bytes, ChunkRoute route = kAbsorbAll);
+int attn_workspace(const mla_batch *batch, size_t *bytes, ChunkRoute route = kAbsorbAll, const Form &form = {});
+
+// mixed_step_attn in a form of mla_cache.h, whose own arguments are checked already.
+int attend_form(const mla_batch *batch, const uint16_t *q, const uint16_t *kv_cache, const Form &form, float softmax_scale,
+                void *out, int32_t out_dtype, float *lse, void *workspace, size_t workspace_bytes, void *stream, const char *what);
 
 // mixed_step (no lse) over every row except those of the chunk requests that
 // `route` sends to the multi-head path, which are left untouched: neither

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "api_util.h"
@@ -29,10 +30,7 @@ int check_window(const mla_window *w, bool null_ok) {
     return MLA_OK;
 }
 
-int check_cache8(const mla_batch *b, const mla_cache8 *c) {
-    if (b->page_size < MLA_CACHE8_BLOCK)
-        return set_error(MLA_ERR_UNSUPPORTED, "page_size = %d: the 8-bit cache needs pages of at least %d tokens", b->page_size,
-                         MLA_CACHE8_BLOCK);
+int check_cache8(const mla_cache8 *c) {
     if (!c || !c->data || !c->scales) return set_error(MLA_ERR_INVALID_ARG, "the cache, its data or its scales are NULL");
     if (misaligned(c->data) || misaligned(c->scales))
         return set_error(MLA_ERR_INVALID_ARG, "cache data / scales must be 16-byte aligned");
@@ -45,54 +43,39 @@ int check_new(const uint16_t *new_latents) {
     return MLA_OK;
 }
 
-// Attention of both forms: exactly one of kv and cache is set.
-int attend(const mla_batch *b, const uint16_t *q, const uint16_t *kv, const mla_cache8 *cache, const mla_window *win, float scale,
-           void *out, int32_t out_dtype, float *lse, void *stream, const char *what) {
-    int T = 0, log2_page = 0;
-    int st = mla::batch_shape(b, &T, &log2_page);
-    if (st != MLA_OK || b->num_reqs == 0) return st;
-    if (!q || !out) return set_error(MLA_ERR_INVALID_ARG, "q / out is NULL");
-    if (misaligned(q) || misaligned(out)) return set_error(MLA_ERR_INVALID_ARG, "q / out must be 16-byte aligned");
-    if (reinterpret_cast<uintptr_t>(lse) & 3) return set_error(MLA_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-    if (out_dtype != MLA_OUT_F32 && out_dtype != MLA_OUT_BF16)
-        return set_error(MLA_ERR_INVALID_ARG, "out_dtype = %d is neither MLA_OUT_F32 nor MLA_OUT_BF16", out_dtype);
-    if (!std::isfinite(scale) || scale <= 0.f) return set_error(MLA_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
-    mla::AttnArgs a{};
-    a.q = q;
-    a.kv = kv;
-    a.kv8 = cache ? cache->data : nullptr;
-    a.kv8_scales = cache ? cache->scales : nullptr;
-    a.window = win ? win->window : 0;
-    a.sinks = win ? win->sinks : 0;
-    a.cu_q = b->cu_q_dev;
-    a.prefix = b->prefix_lens_dev;
-    a.bt = b->block_table_dev;
-    a.out = out;
-    a.lse = lse;
-    a.num_reqs = b->num_reqs;
-    a.num_rows = T;
-    a.page_size = b->page_size;
-    a.log2_page = log2_page;
-    a.max_pages = b->max_pages_per_req;
-    a.num_pages = b->num_pages;
-    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-    a.out_bf16 = out_dtype == MLA_OUT_BF16 ? 1 : 0;
-    const mla::CheckUse use{cache ? MLA_CACHE8_BLOCK : 1, a.window, a.sinks};
-    if ((st = mla::check_before(b, use, stream)) != MLA_OK) return st;
-    const hipError_t e = mla::launch_rows(a, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return mla::hip_error(e, "attention kernel launch");
-    return mla::check_after(what, stream);
+// The window as the planner and the kernels take it: beyond 2^30 keys, more than a
+// request may have, nothing changes any more.
+mla::Band band_of(const mla_window *w) {
+    mla::Band b{};
+    if (!w) return b;
+    const long long most = 1LL << 30;
+    b.window = (int32_t)std::min<long long>(w->window, most);
+    b.sinks = (int32_t)std::min<long long>(w->sinks, most);
+    const long long sink_keys = ((long long)b.sinks + mla::kKeysPerTile - 1) / mla::kKeysPerTile * mla::kKeysPerTile;
+    b.sink_keys = (int32_t)sink_keys;
+    b.span = (int32_t)std::min(most, sink_keys + b.window + mla::kChunkBlockTokens + mla::kKeysPerTile - 2);
+    return b;
 }
 
-size_t workspace(const mla_batch *b, const mla_window *win, bool eight) {
-    int T = 0, log2_page = 0;
-    if (mla::batch_shape(b, &T, &log2_page) != MLA_OK || b->num_reqs == 0) return 0;
-    if (check_window(win, eight) != MLA_OK) return 0;
-    if (eight && b->page_size < MLA_CACHE8_BLOCK) {
-        set_error(MLA_ERR_UNSUPPORTED, "page_size = %d: the 8-bit cache needs pages of at least %d tokens", b->page_size, MLA_CACHE8_BLOCK);
-        return 0;
-    }
-    return 0;
+// Checks what the form adds to a batch's own arguments, and makes the form, without the 8-bit cache's pointers.
+int make_form(const mla_batch *batch, bool eight, const mla_window *window, mla::Form *form) {
+    if (eight && batch->page_size < MLA_CACHE8_BLOCK)
+        return set_error(MLA_ERR_UNSUPPORTED, "page_size = %d: the 8-bit cache needs pages of at least %d tokens", batch->page_size,
+                         MLA_CACHE8_BLOCK);
+    const int st = check_window(window, eight);
+    if (st != MLA_OK) return st;
+    form->eight = eight;
+    form->band = band_of(window);
+    return MLA_OK;
+}
+
+size_t workspace(const mla_batch *batch, const mla_window *window, bool eight) {
+    int T = 0;
+    mla::Form form;
+    if (mla::batch_rows(batch, &T) != MLA_OK || batch->num_reqs == 0) return 0;
+    if (make_form(batch, eight, window, &form) != MLA_OK) return 0;
+    size_t bytes = 0;
+    return mla::attn_workspace(batch, &bytes, mla::kAbsorbAll, form) == MLA_OK ? bytes : 0;
 }
 
 }  // namespace
@@ -133,8 +116,9 @@ int append_latent_kv8(const mla_batch *batch, const uint16_t *new_latents, float
     int T = 0, log2_page = 0;
     int st = mla::batch_shape(batch, &T, &log2_page);
     if (st != MLA_OK || batch->num_reqs == 0) return st;
-    if ((st = check_cache8(batch, cache)) != MLA_OK || (st = check_new(new_latents)) != MLA_OK ||
-        (st = check_base(rope_base, true)) != MLA_OK)
+    mla::Form form;
+    if ((st = make_form(batch, true, nullptr, &form)) != MLA_OK || (st = check_cache8(cache)) != MLA_OK ||
+        (st = check_new(new_latents)) != MLA_OK || (st = check_base(rope_base, true)) != MLA_OK)
         return st;
     long long blocks = 0;
     for (int r = 0; r < batch->num_reqs; ++r) {
@@ -172,22 +156,27 @@ size_t mixed_step_attn_window_workspace_bytes(const mla_batch *batch, const mla_
 int mixed_step_attn8(const mla_batch *batch, const uint16_t *q, const mla_cache8 *cache, const mla_window *window,
                      float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace, size_t workspace_bytes,
                      void *stream) {
-    int T = 0, log2_page = 0;
-    int st = mla::batch_shape(batch, &T, &log2_page);
+    int T = 0;
+    mla::Form form;
+    int st = mla::batch_rows(batch, &T);
     if (st != MLA_OK || batch->num_reqs == 0) return st;
-    if ((st = check_cache8(batch, cache)) != MLA_OK || (st = check_window(window, true)) != MLA_OK) return st;
-    return attend(batch, q, nullptr, cache, window, softmax_scale, out, out_dtype, lse, stream, "mixed_step_attn8");
+    if ((st = make_form(batch, true, window, &form)) != MLA_OK || (st = check_cache8(cache)) != MLA_OK) return st;
+    form.kv8 = cache->data;
+    form.kv8_scales = cache->scales;
+    return mla::attend_form(batch, q, nullptr, form, softmax_scale, out, out_dtype, lse, workspace, workspace_bytes, stream,
+                            "mixed_step_attn8");
 }
 
 int mixed_step_attn_window(const mla_batch *batch, const uint16_t *q, const uint16_t *kv_cache, const mla_window *window,
                            float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace, size_t workspace_bytes,
                            void *stream) {
-    int T = 0, log2_page = 0;
-    int st = mla::batch_shape(batch, &T, &log2_page);
+    int T = 0;
+    mla::Form form;
+    int st = mla::batch_rows(batch, &T);
     if (st != MLA_OK || batch->num_reqs == 0) return st;
-    if (!kv_cache || misaligned(kv_cache)) return set_error(MLA_ERR_INVALID_ARG, "kv_cache is NULL or not 16-byte aligned");
-    if ((st = check_window(window, false)) != MLA_OK) return st;
-    return attend(batch, q, kv_cache, nullptr, window, softmax_scale, out, out_dtype, lse, stream, "mixed_step_attn_window");
+    if ((st = make_form(batch, false, window, &form)) != MLA_OK) return st;
+    return mla::attend_form(batch, q, kv_cache, form, softmax_scale, out, out_dtype, lse, workspace, workspace_bytes, stream,
+                            "mixed_step_attn_window");
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// Attention over the 8-bit cache and through a window (include/mla_cache.h):
+// Attention over the 8-bit cache (include/mla_cache.h):
 // device code, part of mla_kernels.hip (its helpers and namespace).
 #pragma once
 
@@ -6,15 +6,14 @@
 // threads form the 16 x 16 scores, and each thread accumulates two value dims
 // of all heads under a running max and sum per head.  Invisible keys are zeros in
 // LDS and never touched in memory.
-template <bool KV8>
-__global__ __launch_bounds__(kThreads) void rows_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads) void rows8_kernel(AttnArgs a) {
     constexpr int kT = 16, kStride = kDqk + 4;
     __shared__ float s_q[kHeads][kStride], s_k[kT][kStride], s_p[kHeads][kT], s_c[kHeads], s_m[kHeads], s_l[kHeads];
     const int tid = threadIdx.x, row = blockIdx.x;
     const int r = find_request(a.cu_q, a.num_reqs, row, tid & 63);
     const int p = a.prefix[r] + row - a.cu_q[r];
     if (p < 0 || row >= a.cu_q[a.num_reqs]) return;
-    const int W = a.window > 0 ? a.window : INT_MAX;
+    const int W = a.band.window > 0 ? a.band.window : INT_MAX;
     for (int u = tid; u < kHeads * kDqk; u += kThreads)
         s_q[u / kDqk][u % kDqk] = bf16_bits_to_float(a.q[(size_t)row * kHeads * kDqk + u]);
     if (tid < kHeads) {
@@ -24,11 +23,11 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(AttnArgs a) {
     float acc[kHeads][2] = {};
     const int lo = max(p - W + 1, 0);
     for (int k0 = 0; k0 <= p; k0 += kT) {
-        if (k0 >= a.sinks && k0 + kT <= lo) {
+        if (k0 >= a.band.sinks && k0 + kT <= lo) {
             k0 = (lo & -kT) - kT;
             continue;
         }
-        const auto seen = [&](int key) { return key <= p && (key >= lo || key < a.sinks); };
+        const auto seen = [&](int key) { return key <= p && (key >= lo || key < a.band.sinks); };
         __syncthreads();
         for (int u = tid; u < kT * kDqk; u += kThreads) {
             const int key = k0 + u / kDqk, d = u % kDqk;
@@ -41,12 +40,8 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(AttnArgs a) {
                     page = 0;
                 }
                 const size_t slot = (size_t)page * a.page_size + (key & (a.page_size - 1));
-                if constexpr (KV8) {
-                    const float sc = bf16_bits_to_float(a.kv8_scales[slot / kBlock8 * 2 + (d >= kDv)]);
-                    v = __builtin_amdgcn_cvt_f32_fp8(a.kv8[slot * kDqk + d], 0) * sc;
-                } else {
-                    v = bf16_bits_to_float(a.kv[slot * kDqk + d]);
-                }
+                const float sc = bf16_bits_to_float(a.kv8_scales[slot / kBlock8 * 2 + (d >= kDv)]);
+                v = __builtin_amdgcn_cvt_f32_fp8(a.kv8[slot * kDqk + d], 0) * sc;
             }
             s_k[u / kDqk][d] = v;
         }

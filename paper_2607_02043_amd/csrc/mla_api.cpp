@@ -1,6 +1,7 @@
 // C ABI of libmlastep: argument checks, work planning and launches.
 // The entry points and their contracts are declared in include/mla_step.h.
 #include "mla_step.h"
+#include "mla_cache.h"
 
 #include <hip/hip_runtime.h>
 
@@ -156,6 +157,10 @@ constexpr double kEmptyItemUs = 1.5;    // a chunk item past its block's causal 
 constexpr double kDecTileUs = 3.5;      // one decode tile of a unit (the two units of an item run side by side)
 constexpr double kDecUnitUs = 8.0;      // decode item start-up
 constexpr double kDecTileLoUs = 2.65;   // a decode tile when few workgroups stream (per-CU rate bound)
+// the same over the 8-bit cache
+constexpr double kChunk8TileUs = 2.1;
+constexpr double kDec8TileUs = 1.8;
+constexpr double kDec8TileLoUs = 1.3;
 constexpr double kTwoQueueGain = 0.03;  // decode-first workgroups only for at least this much less time
 constexpr double kTwoQueueMinUs = 5.0;  // and at least this many microseconds less
 constexpr double kMergeGBs = 3000.0;    // partial rows written and merged, whole chip
@@ -169,12 +174,12 @@ struct DecReq {
 // Does a decode unit of S tiles respect the kernel's limits (segments and
 // page-window entries per unit)?
 bool dec_share_fits(const std::vector<DecReq> &reqs, long long total, long long S, int page_size,
-                    long long min_tiles) {
+                    long long min_tiles, const mla::Band &band) {
     // a unit of S tiles touches at most S / min_tiles + 2 requests (min_tiles:
     // the shortest request's tiles) and, per request, at most its keys /
-    // page_size + 2 pages
-    const long long segs = std::min(S, S / std::max(1LL, min_tiles) + 2);
-    if (segs <= mla::kMaxDecSegments && S * mla::kKeysPerTile / page_size + 2 * segs <= mla::kPageWindow) return true;
+    // page_size + 2 pages, twice those 2 with a gap behind the sinks
+    const long long segs = std::min(S, S / std::max(1LL, min_tiles) + 2), ends = band.window > 0 ? 4 : 2;
+    if (segs <= mla::kMaxDecSegments && S * mla::kKeysPerTile / page_size + ends * segs <= mla::kPageWindow) return true;
     const int lg = __builtin_ctz((unsigned)page_size);  // page_size is a power of two
     size_t k = 0;
     for (long long R0 = 0; R0 < total; R0 += S) {
@@ -184,9 +189,13 @@ bool dec_share_fits(const std::vector<DecReq> &reqs, long long total, long long 
         for (size_t j = k; j < reqs.size() && reqs[j].first_tile < R1; ++j) {
             const long long t0 = std::max(R0 - reqs[j].first_tile, 0LL);
             const long long t1 = std::min(R1 - reqs[j].first_tile, reqs[j].tiles);
-            const long long k0 = t0 * mla::kKeysPerTile;
-            const long long klast = std::min(t1 * mla::kKeysPerTile, reqs[j].p + 1) - 1;
+            const long long shift = band.window > 0 ? mla::band_shift(band, (int)reqs[j].p) : 0;
+            const auto key = [&](long long v) { return v + (v >= band.sink_keys ? shift : 0); };
+            const long long k0 = key(t0 * mla::kKeysPerTile);
+            const long long klast = std::min(key(t1 * mla::kKeysPerTile - 1), reqs[j].p);
             pages += (klast >> lg) - (k0 >> lg) + 1;
+            if (shift > 0 && t0 * mla::kKeysPerTile < band.sink_keys && t1 * mla::kKeysPerTile > band.sink_keys)
+                pages -= ((band.sink_keys + shift) >> lg) - ((band.sink_keys - 1) >> lg) - 1;  // those in the gap
             ++segs;
         }
         if (segs > mla::kMaxDecSegments || pages > mla::kPageWindow) return false;
@@ -362,10 +371,21 @@ double fill_units(const std::vector<LoadRun> &runs, long long n, double u) {
 // bound can still win), with the decode fill of each unit size evaluated
 // exactly until a lower bound rules the rest out.
 int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkRoute route, Plan *pl,
-                       const Plan *warm = nullptr) {
+                       const Plan *warm = nullptr, const mla::Form &form = {}) {
     const long long P = b->page_size;
-    long long cap = ((long long)(mla::kPageWindow - 1) * P) / 64 * 64;  // keys per chunk item
+    const mla::Band &band = form.band;
+    const bool windowed = band.window > 0;
+    // keys per chunk item (a gap behind the sinks may cut two more pages)
+    long long cap = ((long long)(mla::kPageWindow - (windowed ? 3 : 1)) * P) / 64 * 64;
     if (cap < 64) cap = 64;
+    const double kDecTileUs = form.eight ? kDec8TileUs : ::kDecTileUs, kDecTileLoUs = form.eight ? kDec8TileLoUs : ::kDecTileLoUs;
+    const double kChunkTileUs = form.eight ? kChunk8TileUs : ::kChunkTileUs;
+    // (virtual) keys of a chunk request's longest block, and of its block rb
+    const auto span = [&](long long p, long long c) { return windowed ? (long long)mla::band_span(band, (int)p, (int)c) : p + c; };
+    const auto block_keys = [&](long long p, long long c, long long rb) {
+        return p + std::min(c, (rb + 1) * mla::kChunkBlockTokens) -
+               (windowed ? mla::band_shift(band, (int)(p + rb * mla::kChunkBlockTokens)) : 0);
+    };
     const int BM = mla::kChunkBlockTokens, KT = mla::kKeysPerTile;
 
     std::vector<DecReq> dec;
@@ -375,7 +395,7 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
     for (int r = 0; r < sh.R; ++r) {
         const long long c = b->q_lens[r], p = b->prefix_lens[r];
         if (c == 1) {
-            const long long nt = ceil_div_ll(p + 1, KT);
+            const long long nt = ceil_div_ll(p + 1 - (windowed ? mla::band_shift(band, (int)p) : 0), KT);
             dec.push_back(DecReq{dec_total, nt, p});
             dec_total += nt;
         } else if (!route.multi_head(p, c)) {
@@ -390,8 +410,11 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
     double chunk_pairs = 0.0;
     long long chunk_keys_max = 0;
     for (const auto &pc : chunks) {
-        chunk_pairs += (double)pc.second * ((double)pc.first + 0.5 * (double)(pc.second + 1));
-        chunk_keys_max = std::max(chunk_keys_max, pc.first + pc.second);
+        if (windowed)
+            for (long long rb = 0; rb * BM < pc.second; ++rb) chunk_pairs += (double)BM * (double)block_keys(pc.first, pc.second, rb);
+        else
+            chunk_pairs += (double)pc.second * ((double)pc.first + 0.5 * (double)(pc.second + 1));
+        chunk_keys_max = std::max(chunk_keys_max, span(pc.first, pc.second));
     }
     // large items first: number the chunk requests from the last one when
     // its items are the larger ones
@@ -411,7 +434,7 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
                         near((double)dec_total, (double)warm->dec_total_tiles) && near(chunk_pairs, warm->chunk_pairs) &&
                         near((double)chunk_keys_max, (double)warm->chunk_keys_max) &&
                         warm->ks_chunk >= 64 && warm->ks_chunk <= cap &&
-                        (dec_total == 0 || (U >= 1 && U <= dec_total && dec_share_fits(dec, dec_total, U, (int)P, min_tiles)));
+                        (dec_total == 0 || (U >= 1 && U <= dec_total && dec_share_fits(dec, dec_total, U, (int)P, min_tiles, band)));
         if (!ok) warm = nullptr;
     }
 
@@ -430,17 +453,27 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
         double split_rows = 0.0;
         for (const auto &pc : chunks) {
             const long long p = pc.first, c = pc.second;
-            const long long nrb = ceil_div_ll(c, BM), nks = ceil_div_ll(p + c, ks);
+            const long long nrb = ceil_div_ll(c, BM), nks = ceil_div_ll(span(p, c), ks);
             // sum over blocks of their tiles: limits p + 8, p + 16, .., p + c
-            const double keys = (double)nrb * (double)p + 4.0 * (double)(nrb - 1) * (double)nrb + (double)c;
+            double keys = (double)nrb * (double)p + 4.0 * (double)(nrb - 1) * (double)nrb + (double)c;
+            long long cut_rows = -1;  // with a window: rows of the blocks with more than ks keys
+            if (windowed) {
+                keys = 0.0;
+                cut_rows = 0;
+                for (long long rb = 0; rb < nrb; ++rb) {
+                    const long long n = block_keys(p, c, rb);
+                    keys += (double)n;
+                    if (n > ks) cut_rows += std::min<long long>(BM, c - rb * BM);
+                }
+            }
             const double tiles = keys / KT + 0.5 * (double)nrb * (double)nks;  // + rounding of each range
             e.total += tiles * kChunkTileUs + (double)(nrb * nks) * kChunkItemUs;
-            const long long kp = ceil_div_ll(ceil_div_ll(p + c, nks), 64) * 64;
+            const long long kp = ceil_div_ll(ceil_div_ll(span(p, c), nks), 64) * 64;
             e.max_item = std::max(e.max_item, kChunkItemUs + kChunkTileUs * (double)ceil_div_ll(kp, KT));
             if (nks > 1) {
                 // rows of the blocks whose keys span more than one range
                 const double first_split = std::max(0.0, (double)(ks - p) / BM);  // blocks within ks keys
-                split_rows += (double)(2 * nks) * std::max(0.0, (double)c - first_split * BM);
+                split_rows += (double)(2 * nks) * (cut_rows >= 0 ? (double)cut_rows : std::max(0.0, (double)c - first_split * BM));
             }
             e.items += nrb * nks;
         }
@@ -456,13 +489,23 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
         const uint32_t k32 = (uint32_t)ks;
         size_t n = 0;
         for (const auto &pc : chunks)
-            n += (size_t)(((uint32_t)pc.second + BM - 1) / BM) * (((uint32_t)(pc.first + pc.second) + k32 - 1) / k32);
+            n += (size_t)(((uint32_t)pc.second + BM - 1) / BM) * (((uint32_t)span(pc.first, pc.second) + k32 - 1) / k32);
         items.resize(n);
         double *out = items.data();
         for (size_t i = 0; i < chunks.size(); ++i) {
             const auto &pc = chunks[rev ? chunks.size() - 1 - i : i];
             const uint32_t p = (uint32_t)pc.first, c = (uint32_t)pc.second;
-            const uint32_t nrb = (c + BM - 1) / BM, nks = (p + c + k32 - 1) / k32;
+            const uint32_t nrb = (c + BM - 1) / BM, nks = ((uint32_t)span(p, c) + k32 - 1) / k32;
+            if (windowed) {
+                for (uint32_t rb = nrb; rb-- > 0;) {
+                    const uint32_t n = (uint32_t)block_keys(p, c, rb), cuts = (n + k32 - 1) / k32;
+                    const uint32_t kp = ((n + cuts - 1) / cuts + 63) / 64 * 64, full = n / kp, rest = n - full * kp;
+                    out = std::fill_n(out, full, kChunkItemUs + kChunkTileUs * (double)((kp + KT - 1) / KT));
+                    if (rest > 0) *out++ = kChunkItemUs + kChunkTileUs * (double)((rest + KT - 1) / KT);
+                    out = std::fill_n(out, nks - full - (rest > 0), kEmptyItemUs);
+                }
+                continue;
+            }
             // klim falls by at most BM keys a block, so nr = ceil(klim / ks)
             // and q = ceil(klim / (64 nr)) (kp = 64 q) are stepped down
             // rather than divided out again
@@ -490,7 +533,7 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
     auto fit_unit = [&](long long U) {
         U = std::max(1LL, std::min(U, dec_total));
         bool fits;
-        while (!(fits = dec_share_fits(dec, dec_total, U, (int)P, min_tiles)) && U > 1) U = std::max(1LL, U * 3 / 4);
+        while (!(fits = dec_share_fits(dec, dec_total, U, (int)P, min_tiles, band)) && U > 1) U = std::max(1LL, U * 3 / 4);
         return fits ? U : 0LL;
     };
     // Decode units: the candidate sizes (tiles) that respect those limits.
@@ -735,7 +778,7 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
     const long long n_units = dec_total > 0 ? ceil_div_ll(dec_total, U) : 0;
     long long nci = 0, chunk_parts = 1;
     for (const auto &pc : chunks) {
-        const long long p = pc.first, c = pc.second, parts = ceil_div_ll(p + c, ks_best);
+        const long long p = pc.first, c = pc.second, parts = ceil_div_ll(span(p, c), ks_best);
         nci += ceil_div_ll(c, BM) * parts;
         if (parts > 1) pl->n_split_chunk_rows += (int)c;
         chunk_parts = std::max(chunk_parts, parts);
@@ -795,17 +838,18 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
 // the last one is kept per thread so a steady stream of identical steps
 // plans once.  The last full plan is kept too, as the warm start of batches
 // with nearly the same work (MLA_DEBUG_WARM_PLAN = 0 turns that off).
-int make_plan(const mla_batch *b, const Shape &sh, Plan *pl, mla::ChunkRoute route = mla::kAbsorbAll) {
+int make_plan(const mla_batch *b, const Shape &sh, Plan *pl, mla::ChunkRoute route = mla::kAbsorbAll, const mla::Form &form = {}) {
     *pl = Plan{};
     if (sh.R == 0) return MLA_OK;
     int st = MLA_OK;
     const int ncu = cu_count(&st);
     if (st != MLA_OK) return st;
-    constexpr size_t kHdr = 9;
+    constexpr size_t kHdr = 12;
     const int32_t hdr[kHdr] = {b->page_size, ncu, sh.R, b->max_pages_per_req, route.min_rows, route.pair_keys,
                                debug_value(MLA_DEBUG_CHUNK_KEYS).load(std::memory_order_relaxed),
                                debug_value(MLA_DEBUG_DEC_UNIT).load(std::memory_order_relaxed),
-                               debug_value(MLA_DEBUG_DEC_FIRST).load(std::memory_order_relaxed)};
+                               debug_value(MLA_DEBUG_DEC_FIRST).load(std::memory_order_relaxed),
+                               form.eight ? 1 : 0, form.band.window, form.band.sinks};
     const size_t qbytes = (size_t)sh.R * sizeof(int32_t);
     // key: header, query lengths, prefix lengths
     thread_local std::vector<int32_t> key;
@@ -822,7 +866,7 @@ int make_plan(const mla_batch *b, const Shape &sh, Plan *pl, mla::ChunkRoute rou
     const bool warm = debug_value(MLA_DEBUG_WARM_PLAN).load(std::memory_order_relaxed) != 0 && have_anchor &&
                       std::memcmp(anchor_hdr, hdr, 2 * sizeof(int32_t)) == 0 &&
                       std::memcmp(anchor_hdr + 3, hdr + 3, (kHdr - 3) * sizeof(int32_t)) == 0;
-    st = make_plan_uncached(b, sh, ncu, route, pl, warm ? &anchor : nullptr);
+    st = make_plan_uncached(b, sh, ncu, route, pl, warm ? &anchor : nullptr, form);
     if (st != MLA_OK) return st;
     key.resize(kHdr + 2 * (size_t)sh.R);
     std::memcpy(key.data(), hdr, sizeof hdr);
@@ -927,13 +971,13 @@ int set_error(int code, const char *fmt, ...) {
     return code;
 }
 
-int attn_workspace(const mla_batch *batch, size_t *bytes, ChunkRoute route) {
+int attn_workspace(const mla_batch *batch, size_t *bytes, ChunkRoute route, const Form &form) {
     *bytes = 0;
     Shape sh;
     int st = check_batch(batch, &sh);
     if (st != MLA_OK || sh.R == 0) return st;
     Plan pl;
-    st = make_plan(batch, sh, &pl, route);
+    st = make_plan(batch, sh, &pl, route, form);
     if (st == MLA_OK) *bytes = pl.bytes;
     return st;
 }
@@ -1046,14 +1090,15 @@ int mla_debug_set(int32_t knob, int32_t value) {
 
 namespace {
 
-// Shared by mixed_step_attn (new_latents == NULL) and mixed_step (fused append).
+// Shared by mixed_step_attn (new_latents == NULL), mixed_step (fused append) and the forms of
+// mla_cache.h (no fused append; with an 8-bit cache kv_cache is not read).
 int attend(const mla_batch *batch, const uint16_t *q, const uint16_t *new_latents, uint16_t *kv_cache,
            float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace, size_t workspace_bytes,
-           void *stream, mla::ChunkRoute route = mla::kAbsorbAll) {
+           void *stream, mla::ChunkRoute route = mla::kAbsorbAll, const mla::Form &form = {}, const char *what = nullptr) {
     Shape sh;
     int st = check_batch(batch, &sh);
     if (st != MLA_OK || sh.R == 0) return st;
-    if (!q || !kv_cache || !out) return fail(MLA_ERR_INVALID_ARG, "q / kv_cache / out is NULL");
+    if (!q || !(kv_cache || form.eight) || !out) return fail(MLA_ERR_INVALID_ARG, "q / kv_cache / out is NULL");
     if (reinterpret_cast<uintptr_t>(new_latents) & 15)
         return fail(MLA_ERR_INVALID_ARG, "new_latents must be 16-byte aligned");
     if (out_dtype != MLA_OUT_F32 && out_dtype != MLA_OUT_BF16)
@@ -1065,7 +1110,7 @@ int attend(const mla_batch *batch, const uint16_t *q, const uint16_t *new_latent
         return fail(MLA_ERR_INVALID_ARG, "q / kv_cache / out / workspace must be 16-byte aligned");
     if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(MLA_ERR_INVALID_ARG, "lse must be 4-byte aligned");
     Plan pl;
-    st = make_plan(batch, sh, &pl, route);
+    st = make_plan(batch, sh, &pl, route, form);
     if (st != MLA_OK) return st;
     if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes))
         return fail(MLA_ERR_WORKSPACE, "workspace of %zu bytes at %p; this batch needs %zu", workspace_bytes,
@@ -1108,21 +1153,31 @@ int attend(const mla_batch *batch, const uint16_t *q, const uint16_t *new_latent
     a.out_bf16 = out_dtype == MLA_OUT_BF16 ? 1 : 0;
     a.spin_limit = debug_value(MLA_DEBUG_SPIN_LIMIT).load(std::memory_order_relaxed);
     a.route = route;
+    a.kv8 = form.kv8;
+    a.kv8_scales = form.kv8_scales;
+    a.band = form.band;
+    const mla::CheckUse use{form.eight ? MLA_CACHE8_BLOCK : 1, form.band.window, form.band.sinks};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool chk = check_mode();
-    if (chk && (st = check_device_batch(batch, sh, s)) != MLA_OK) return st;
+    if (chk && (st = check_device_batch(batch, sh, s, use)) != MLA_OK) return st;
     hipError_t e = mla::launch_attention(a, s);
     if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
     if (pl.chunk_split || pl.dec_split) {
         e = mla::launch_combine(a, s);
         if (e != hipSuccess) return hip_fail(e, "merge kernel launch");
     }
-    return chk ? check_after_launch(s, new_latents ? "mixed_step" : "mixed_step_attn") : MLA_OK;
+    return chk ? check_after_launch(s, what ? what : new_latents ? "mixed_step" : "mixed_step_attn") : MLA_OK;
 }
 
 }  // namespace
 
 namespace mla {
+
+int attend_form(const mla_batch *batch, const uint16_t *q, const uint16_t *kv_cache, const Form &form, float softmax_scale,
+                void *out, int32_t out_dtype, float *lse, void *workspace, size_t workspace_bytes, void *stream, const char *what) {
+    return attend(batch, q, nullptr, const_cast<uint16_t *>(kv_cache), softmax_scale, out, out_dtype, lse, workspace,
+                  workspace_bytes, stream, kAbsorbAll, form, what);
+}
 
 int attend_rows(const mla_batch *batch, const uint16_t *q, const uint16_t *new_latents, uint16_t *kv_cache,
                 float softmax_scale, void *out, int32_t out_dtype, void *workspace, size_t workspace_bytes, void *stream,

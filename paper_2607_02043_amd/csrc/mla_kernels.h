@@ -24,6 +24,38 @@ constexpr int kSpinLimit = 1 << 16;   // sleeps of a bounded wait before it give
 constexpr size_t kNoAllocScratchBytes = size_t(128) << 20;  // scratch of mixed_step_noalloc, per device
 constexpr int kMaxDevices = 64;
 
+// A window of keys with sinks (mla_cache.h): the row at position t sees the keys
+// j <= t with j > t - window or j < sinks.  A decode row, or a block of 8 chunk rows
+// from position t on, reads its keys as one range of virtual keys: the sinks,
+// rounded up to whole tiles (sink_keys), then everything from the window's first
+// key, rounded down to a tile.  Virtual key v is key v in the first part and
+// v + band_shift(t) behind it, so tiles stay tiles.
+struct Band {
+    int32_t window, sinks;  // window 0: none
+    int32_t sink_keys;      // sinks rounded up to a multiple of kKeysPerTile
+    int32_t span;           // no block of rows of a request reads more virtual keys than this
+};
+__host__ __device__ inline int band_shift(const Band &b, int t) {
+    const int first = t - b.window + 1, lo = (first > 0 ? first : 0) & -kKeysPerTile;
+    return lo > b.sink_keys ? lo - b.sink_keys : 0;
+}
+// Virtual keys of the longest block of rows p .. p + c - 1: with lo the window's
+// first tile, p + i1 - lo <= window - 1 + 8 + 31, and the sink tiles in front.
+__host__ __device__ inline int band_span(const Band &b, int p, int c) { return p + c < b.span ? p + c : b.span; }
+
+// The cache that a call attends and its window: what the planner needs to know
+// beside the lengths, and the 8-bit cache's arrays at launch.
+struct Form {
+    bool eight = false;
+    Band band{};
+    const uint8_t *kv8 = nullptr;
+    const uint16_t *kv8_scales = nullptr;
+};
+
+// Forms of the attention launch (bits).
+constexpr int kPlain = 0;
+constexpr int kWindow = 1;  // through AttnArgs::band
+
 struct AttnArgs {
     const uint16_t *q;
     const uint16_t *kv;
@@ -67,7 +99,7 @@ struct AttnArgs {
     // forms of mla_cache.h: the 8-bit cache (in place of kv), and the window (0: none) with its sinks
     const uint8_t *kv8;
     const uint16_t *kv8_scales;
-    int32_t window, sinks;
+    Band band;
 };
 
 // The fixed first items of the attention launch's G workgroups (G at most the
@@ -132,7 +164,6 @@ struct Append8Args {
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);
 hipError_t launch_append_rope(const AppendArgs &a, double log2_base, hipStream_t s);
 hipError_t launch_append8(const Append8Args &a, hipStream_t s);
-hipError_t launch_rows(const AttnArgs &a, hipStream_t s);
 // Reads the device's sticky kernel error flags (kFlag*), and clears them if asked.
 hipError_t read_flags(int *flags, bool clear);
 // Device address of the current device's no-allocation scratch

@@ -305,16 +305,28 @@ __device__ bool locate_item(int target, int num_reqs, const ReqLens &rl, CountFn
     return found;
 }
 
+// Virtual keys of a chunk request's longest block (form F), which its key ranges cut.
+template <int F>
+__device__ __forceinline__ int chunk_span(const Band &band, int p, int c) {
+    if constexpr ((F & kWindow) != 0)
+        return band_span(band, p, c);
+    else
+        return p + c;
+}
+
+template <int F>
 struct ChunkCount {
     int ks;
     ChunkRoute route;
+    const Band &band;
     __device__ int operator()(int p, int c) const {
-        return c > 1 && !route.multi_head(p, c) ? ceil_div(c, kChunkBlockTokens) * ceil_div(p + c, ks) : 0;
+        return c > 1 && !route.multi_head(p, c) ? ceil_div(c, kChunkBlockTokens) * ceil_div(chunk_span<F>(band, p, c), ks) : 0;
     }
 };
 
 struct ChunkItem {
-    int r, p, c, row0, i0, i1, k0, k1, ks, nks_eff;
+    int r, p, c, row0, i0, i1, k0, k1, ks, nks_eff;  // keys k0 .. k1 - 1: virtual ones with a window
+    int shift;  // window: band_shift of the block's first row
 };
 
 // Item `local` of a chunk request: every block of 8 query tokens (the
@@ -323,6 +335,7 @@ struct ChunkItem {
 // ceil(klim / ks_chunk) ranges of equal length, rounded up to a multiple of
 // 64 keys (at most ks_chunk); the remaining slots are empty items.  A block
 // whose keys fit one range writes its rows directly.
+template <int F>
 __device__ __forceinline__ ChunkItem decode_chunk_item(const AttnArgs &a, const Located &lc) {
     ChunkItem it;
     it.r = lc.r;
@@ -330,12 +343,13 @@ __device__ __forceinline__ ChunkItem decode_chunk_item(const AttnArgs &a, const 
     it.row0 = lc.row0;
     it.c = lc.c;
     const int nrb = ceil_div(it.c, kChunkBlockTokens);
-    const int nks = ceil_div(it.p + it.c, a.ks_chunk);
+    const int nks = ceil_div(chunk_span<F>(a.band, it.p, it.c), a.ks_chunk);
     const int rb = nrb - 1 - lc.local / nks;  // longest rows first
     it.ks = lc.local % nks;
     it.i0 = rb * kChunkBlockTokens;
     it.i1 = min(it.i0 + kChunkBlockTokens, it.c);
-    const int klim = it.p + it.i1;
+    it.shift = (F & kWindow) != 0 ? band_shift(a.band, it.p + it.i0) : 0;
+    const int klim = it.p + it.i1 - it.shift;
     const int kp = ceil_div(ceil_div(klim, ceil_div(klim, a.ks_chunk)), 64) * 64;  // keys per range (<= ks_chunk)
     it.nks_eff = ceil_div(klim, kp);
     it.k0 = it.ks * kp;
@@ -558,6 +572,22 @@ __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
 // over all 32 keys.  A request spread over several units leaves fp32
 // partials (slot 2 v for unit v's first segment, 2 v + 1 for its last) that
 // the merge kernel combines.
+// Whether the row at position t sees a key, or any key of a logical page (rows t and later).
+template <int F>
+__device__ __forceinline__ bool row_sees(const AttnArgs &a, int key, int t) {
+    if constexpr ((F & kWindow) != 0)
+        return key <= t && (key > t - a.band.window || key < a.band.sinks);
+    else
+        return key <= t;
+}
+template <int F>
+__device__ __forceinline__ bool page_seen(const AttnArgs &a, int lp, int t) {
+    if constexpr ((F & kWindow) != 0)
+        return (lp << a.log2_page) < a.band.sinks || ((lp + 1) << a.log2_page) - 1 > t - a.band.window;
+    else
+        return true;
+}
+
 constexpr int kMaxSeg = kMaxDecSegments;
 constexpr int kXStride = 20;  // floats per head row of a partial score block (16 + pad)
 
@@ -565,12 +595,50 @@ struct DecSeg {
     int r, p, row, t0, t1, pw, lp0;  // tiles t0 .. t1-1 of request r; page window offset / first page
 };
 
-__device__ __forceinline__ int dec_tiles(int p, int c) { return c == 1 ? ceil_div(p + 1, kDecKeys) : 0; }
+template <int F>
+__device__ __forceinline__ int dec_tiles(const AttnArgs &a, int p, int c) {
+    const int shift = (F & kWindow) != 0 ? band_shift(a.band, p) : 0;
+    return c == 1 ? ceil_div(p + 1 - shift, kDecKeys) : 0;
+}
+
+// Keys and pages of a segment.  Its tiles are consecutive, and so are its pages;
+// with a window (tiles of virtual keys) there may be a gap behind the sinks:
+// the page window then holds the pages up to the gap and those behind it.
+template <int F>
+struct SegKeys {
+    __device__ SegKeys(const AttnArgs &, const DecSeg &) {}
+    __device__ int key(int v) const { return v; }
+    __device__ int window_entry(const DecSeg &sg, int key, int log2_page) const { return sg.pw + (key >> log2_page) - sg.lp0; }
+    __device__ int logical_page(const DecSeg &sg, int i) const { return sg.lp0 + i; }
+    __device__ int pages(const AttnArgs &a, const DecSeg &sg) const {
+        return ((min(sg.t1 * kDecKeys, sg.p + 1) - 1) >> a.log2_page) - sg.lp0 + 1;
+    }
+};
+template <>
+struct SegKeys<kWindow> {
+    int sink_keys, shift, before, lpw;  // pages before the gap; logical page of entry i behind it, less i
+    __device__ SegKeys(const AttnArgs &a, const DecSeg &sg) : sink_keys(a.band.sink_keys), shift(band_shift(a.band, sg.p)) {
+        before = 0;
+        lpw = sg.lp0;
+        if (shift > 0 && sg.t0 * kDecKeys < sink_keys && sg.t1 * kDecKeys > sink_keys) {
+            before = ((sink_keys - 1) >> a.log2_page) - sg.lp0 + 1;
+            lpw = ((sink_keys + shift) >> a.log2_page) - before;
+        }
+    }
+    __device__ int key(int v) const { return v + (v >= sink_keys ? shift : 0); }
+    __device__ int window_entry(const DecSeg &sg, int key, int log2_page) const {
+        return sg.pw + (key >> log2_page) - (key >= sink_keys + shift ? lpw : sg.lp0);
+    }
+    __device__ int logical_page(const DecSeg &sg, int i) const { return i + (i < before ? sg.lp0 : lpw); }
+    __device__ int pages(const AttnArgs &a, const DecSeg &sg) const {
+        return (min(key(sg.t1 * kDecKeys - 1), sg.p) >> a.log2_page) - lpw + 1;
+    }
+};
 
 // Segments (request order) of the decode tile range [R0, R1), with the page
 // window each needs; returns their count.  Every wavefront of a group finds
 // them by itself (as a lookup does) and `writer` stores them.
-template <int Q>
+template <int Q, int F>
 __device__ __forceinline__ int find_unit_in(const AttnArgs &a, int R0, int R1, DecSeg *s_seg, bool writer) {
     const int lane = item_tid() & 63;
     int running = 0, nseg = 0, pages = 0;
@@ -588,7 +656,7 @@ __device__ __forceinline__ int find_unit_in(const AttnArgs &a, int R0, int R1, D
         for (int q = 0; q < Q; ++q) {
             // rows outside [0, T) only arise from device lengths that disagree with the host's
             const bool row_ok = base + 64 * q + lane < a.num_reqs && cur[q].p >= 0 && cur[q].row0 >= 0 && cur[q].row0 < a.num_rows;
-            nt[q] = row_ok ? dec_tiles(cur[q].p, cur[q].next - cur[q].row0) : 0;
+            nt[q] = row_ok ? dec_tiles<F>(a, cur[q].p, cur[q].next - cur[q].row0) : 0;
             inc[q] = wave_scan(nt[q]);
         }
 #pragma unroll
@@ -598,8 +666,14 @@ __device__ __forceinline__ int find_unit_in(const AttnArgs &a, int R0, int R1, D
             const uint64_t m = __builtin_amdgcn_ballot_w64(ov);
             if (m != 0) {
                 const int t0 = max(R0 - T, 0), t1 = min(R1 - T, nt[q]);
-                const int lp0 = (t0 * kDecKeys) >> a.log2_page;
-                const int np = ov ? ((min(t1 * kDecKeys, cur[q].p + 1) - 1) >> a.log2_page) - lp0 + 1 : 0;
+                int lp0 = (t0 * kDecKeys) >> a.log2_page, np;
+                if constexpr ((F & kWindow) != 0) {
+                    DecSeg sg{0, cur[q].p, 0, t0, t1, 0, 0};
+                    lp0 = sg.lp0 = SegKeys<kWindow>(a, sg).key(t0 * kDecKeys) >> a.log2_page;
+                    np = ov ? SegKeys<kWindow>(a, sg).pages(a, sg) : 0;
+                } else {
+                    np = ov ? ((min(t1 * kDecKeys, cur[q].p + 1) - 1) >> a.log2_page) - lp0 + 1 : 0;
+                }
                 const int pend = pages + wave_scan(np);
                 const int j = nseg + __builtin_popcountll(m & ((1ull << lane) - 1));
                 if (ov && writer && j < kMaxSeg)
@@ -615,8 +689,9 @@ __device__ __forceinline__ int find_unit_in(const AttnArgs &a, int R0, int R1, D
     }
     return min(nseg, kMaxSeg);
 }
+template <int F>
 __device__ int find_unit(const AttnArgs &a, int R0, int R1, DecSeg *s_seg, bool writer) {
-    const int nseg = a.num_reqs <= 64 ? find_unit_in<1>(a, R0, R1, s_seg, writer) : find_unit_in<kLookupQ>(a, R0, R1, s_seg, writer);
+    const int nseg = a.num_reqs <= 64 ? find_unit_in<1, F>(a, R0, R1, s_seg, writer) : find_unit_in<kLookupQ, F>(a, R0, R1, s_seg, writer);
     end_lookup();
     return nseg;
 }
@@ -648,14 +723,18 @@ __device__ __forceinline__ void advance(Cursor &c, const DecSeg *s_seg, int nseg
 // DMA of one stream unit into a 36 KB ring slot.  A query block (16 heads x
 // 576 dims, 18 KB) is copied twice over so every unit takes 9 DMA rounds.  A
 // full tile inside one page uses the uniform-base form (offsets `dma_off`).
+template <int F>
 __device__ __forceinline__ void issue_unit(const AttnArgs &a, const DecSeg &sg, int t, const int *s_pages,
                                            uint32_t slot, int wv, int lane,
                                            const uint32_t (&dma_off)[(kTileDma + 1) / 2]) {
     constexpr int kDma = kDecTileBytes / (kThreads * 16);  // 9
-    const int kbase = t * kDecKeys;
-    const int last_cached = a.new_kv != nullptr ? sg.p - 1 : sg.p;  // key p is the new latent when fused
+    const SegKeys<F> sk(a, sg);
+    const int kbase = sk.key(t * kDecKeys);
+    // key p is the new latent when fused (the plain form only)
+    const bool fused = F == kPlain && a.new_kv != nullptr;
+    const int last_cached = fused ? sg.p - 1 : sg.p;
     if (t >= 0 && a.page_size >= kDecKeys && kbase + kDecKeys - 1 <= last_cached) {
-        const int page = s_pages[min(sg.pw + (kbase >> a.log2_page) - sg.lp0, kPageWindow - 1)];
+        const int page = s_pages[min(sk.window_entry(sg, kbase, a.log2_page), kPageWindow - 1)];
         const char *src = reinterpret_cast<const char *>(a.kv) +
                           ((size_t)__builtin_amdgcn_readfirstlane(page) * a.page_size + (kbase & (a.page_size - 1))) *
                               kRowBytes;
@@ -665,6 +744,8 @@ __device__ __forceinline__ void issue_unit(const AttnArgs &a, const DecSeg &sg, 
                             __builtin_amdgcn_readfirstlane(slot + (i * 4 + wv) * 1024));
         return;
     }
+    // (the window form has no registers for nine addresses of this path kept across the units)
+    if constexpr (F != kPlain) asm volatile("" : "+v"(lane));
     const char *src[kDma];
     if (t < 0) {
         const char *qb = reinterpret_cast<const char *>(a.q + (size_t)sg.row * kHeads * kDqk);
@@ -682,8 +763,8 @@ __device__ __forceinline__ void issue_unit(const AttnArgs &a, const DecSeg &sg, 
             const int kk = u / kChunksPerRow;
             const int c = (u - kk * kChunksPerRow) ^ (kk & 7);
             const int key = min(kbase + kk, klast);
-            const int page = s_pages[min(sg.pw + (key >> a.log2_page) - sg.lp0, kPageWindow - 1)];
-            src[i] = (a.new_kv != nullptr && key == klast)
+            const int page = s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)];
+            src[i] = (fused && key == klast)
                          ? reinterpret_cast<const char *>(a.new_kv) + (size_t)sg.row * kRowBytes + c * 16
                          : kv + ((size_t)page * a.page_size + (key & (a.page_size - 1))) * kRowBytes + c * 16;
         }
@@ -716,6 +797,24 @@ __device__ __forceinline__ void group_barrier(int *ctr, int &epoch, int spin_lim
 // Barrier of the workgroup for LDS contents only: loads may stay in flight.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Values that no row may read: a masked key has probability 0, but 0 times an
+// infinity or NaN is NaN.  The forms of mla_cache.h zero such values and leave it to
+// the key's score, which is not finite either, to reach the rows that see it.
+// (Two bf16 values a word.)
+__device__ __forceinline__ uint32_t finite_bf16x2(uint32_t w) {
+    if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+    if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+    return w;
+}
+// Whether any of a wavefront's raw scores of a tile is not finite (a sum that overflows only costs time).
+__device__ __forceinline__ bool any_not_finite(const f32x4 (&x)[2]) {
+    const float t = ((x[0][0] + x[0][1]) + (x[0][2] + x[0][3])) + ((x[1][0] + x[1][1]) + (x[1][2] + x[1][3]));
+    return __builtin_amdgcn_ballot_w64(!(fabsf(t) < INFINITY)) != 0;
+}
+// A partial's max: a part whose visible scores were all NaN must not look empty to the merge.
+__device__ __forceinline__ float partial_max(float m, float l) { return l != l ? 0.f : m; }
+
+template <int F>
 __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)[kPageWindow],
                           DecSeg (*s_seg_g)[kMaxSeg], int *s_gbar) {
     const int tid = item_tid(), lane = tid & 63;
@@ -731,7 +830,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
     const int R0 = v * S, R1 = min(R0 + S, a.dec_total_tiles);
     DecSeg *const s_seg = s_seg_g[grp];
     int *const s_pages = s_pages_g[grp];
-    const int nseg = R0 < R1 ? find_unit(a, R0, R1, s_seg, gw == 0) : 0;
+    const int nseg = R0 < R1 ? find_unit<F>(a, R0, R1, s_seg, gw == 0) : 0;
     const int n_units = nseg > 0 ? nseg + (R1 - R0) : 0;
     if (tid < 2) s_gbar[tid] = 0;
     TRACE(1);
@@ -744,7 +843,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
     if (n_units > 0) prod.sg = load_seg(s_seg, 0);
     Cursor cons = prod;
     if (n_units > 0) {
-        issue_unit(a, prod.sg, -1, s_pages, ring, gw, lane, dma_off);  // the first query block
+        issue_unit<F>(a, prod.sg, -1, s_pages, ring, gw, lane, dma_off);  // the first query block
         advance(prod, s_seg, nseg);
         // page window: entry gtid belongs to the last segment that starts at or before it
         static_assert(kPageWindow == kThreads, "one window entry per thread of the group");
@@ -752,24 +851,25 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
         for (int k = 1; k < nseg; ++k) j = s_seg[k].pw <= gtid ? k : j;
         const DecSeg sg = s_seg[j];
         const int i = gtid - sg.pw;
-        if (i < ((min(sg.t1 * kDecKeys, sg.p + 1) - 1) >> a.log2_page) - sg.lp0 + 1) {
-            const int lp = sg.lp0 + i;
+        const SegKeys<F> sk(a, sg);
+        if (i < sk.pages(a, sg)) {
+            const int lp = sk.logical_page(sg, i);
             const int pg = lp < a.max_pages ? a.bt[(size_t)sg.r * a.max_pages + lp] : 0;
             const bool ok = (unsigned)pg < (unsigned)a.num_pages;
-            if (!ok) raise_flag(kFlagBadPage);
+            if (!ok && page_seen<F>(a, lp, sg.p)) raise_flag(kFlagBadPage);
             s_pages[gtid] = ok ? pg : 0;
         }
     }
     __syncthreads();
     if (n_units == 0) return;  // this group has no unit (the other one may)
     if (n_units > 1) {
-        issue_unit(a, prod.sg, prod.t, s_pages, ring + kDecTileBytes, gw, lane, dma_off);
+        issue_unit<F>(a, prod.sg, prod.t, s_pages, ring + kDecTileBytes, gw, lane, dma_off);
         advance(prod, s_seg, nseg);
     }
-    if (a.new_kv != nullptr) {  // fused append: the group holding a request's last tile writes its latent
+    if (F == kPlain && a.new_kv != nullptr) {  // fused append: the group holding a request's last tile writes its latent
         for (int j = 0; j < nseg; ++j) {
             const DecSeg sg = s_seg[j];
-            if (sg.t1 == dec_tiles(sg.p, 1)) append_rows_group(a, sg.r, sg.p, sg.row, 1, gtid);
+            if (sg.t1 == dec_tiles<F>(a, sg.p, 1)) append_rows_group(a, sg.r, sg.p, sg.row, 1, gtid);
         }
     }
     int epoch = 0;
@@ -799,7 +899,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
         const char *slot = smem + grp * kDecGroupBytes + (u % kDecRing) * kDecTileBytes;
         {
             if (u > 0 && prod.j < nseg) {
-                issue_unit(a, prod.sg, prod.t, s_pages, ring + ((u + 1) % kDecRing) * kDecTileBytes, gw, lane, dma_off);
+                issue_unit<F>(a, prod.sg, prod.t, s_pages, ring + ((u + 1) % kDecRing) * kDecTileBytes, gw, lane, dma_off);
                 advance(prod, s_seg, nseg);
             }
             if (cons.t < 0) {  // a new request: its query block
@@ -827,7 +927,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
         if (!tile_unit) continue;
         group_barrier(gbar, epoch, a.spin_limit);  // partial score blocks complete
         TRACE_TILE(u, 12);
-        const int kbase = cons.t * kDecKeys;
+        const int kbase = SegKeys<F>(a, sg).key(cons.t * kDecKeys);
         // full scores of this lane's head: x[kt][i] = key 16 kt + 4 g + i (kt = 0, 1)
         f32x4 x[2];
 #pragma unroll
@@ -836,12 +936,14 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
             const f32x4 hi = *reinterpret_cast<const f32x4 *>(s_X + ((kt + 2) * kHeads + h) * kXStride + 4 * g);
             x[kt] = lo + hi;
         }
+        bool careful = false;
+        if constexpr (F != kPlain) careful = any_not_finite(x);
         float mt = kNegInf;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                x[kt][i] = (kbase + 16 * kt + 4 * g + i <= sg.p) ? x[kt][i] * a.scale_log2 : kNegInf;
+                x[kt][i] = row_sees<F>(a, kbase + 16 * kt + 4 * g + i, sg.p) ? x[kt][i] * a.scale_log2 : kNegInf;
                 mt = fmaxf(mt, x[kt][i]);
             }
         }
@@ -884,6 +986,14 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
             const u32x2 hi = lds_read_tr16(slot + tile_off(tr_key + 16, dv >> 3) + byte);
             vop[mt2] = u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
+        if constexpr (F != kPlain) {
+            if (careful) {
+#pragma unroll
+                for (int mt2 = 0; mt2 < 8; ++mt2)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vop[mt2][i] = finite_bf16x2(vop[mt2][i]);
+            }
+        }
         const u32x4 opb_h = {bh[0], bh[1], bh[2], bh[3]};
         const u32x4 opb_l = {bl[0], bl[1], bl[2], bl[3]};
 #pragma unroll
@@ -896,7 +1006,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
         advance(cons, s_seg, nseg);
         if (cons.j != jseg) {  // the segment's last tile: finish it
             const float l_tot = wave_sum16(l_run);
-            if (sg.t0 == 0 && sg.t1 == dec_tiles(sg.p, 1)) {
+            if (sg.t0 == 0 && sg.t1 == dec_tiles<F>(a, sg.p, 1)) {
                 const float inv = 1.f / l_tot;
 #pragma unroll
                 for (int mt2 = 0; mt2 < 8; ++mt2)
@@ -909,7 +1019,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
                 for (int mt2 = 0; mt2 < 8; ++mt2)
                     *reinterpret_cast<f32x4 *>(po + gw * 128 + mt2 * 16 + 4 * g) = acc[mt2];
                 if (gw == 0 && g == 0) {
-                    a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 0] = m_ref;
+                    a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 0] = F == kPlain ? m_ref : partial_max(m_ref, l_tot);
                     a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 1] = l_tot;
                 }
             }
@@ -928,7 +1038,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
 struct SplitRow {
     int row, T, nt;  // output row, decode tiles before its own, its own
 };
-template <int Q>
+template <int Q, int F>
 __device__ __forceinline__ bool find_split_in(const AttnArgs &a, int k, SplitRow &sr) {
     const int lane = threadIdx.x & 63, S = a.dec_unit_tiles;
     int tiles = 0, splits = 0;  // of the requests before this step's
@@ -945,7 +1055,7 @@ __device__ __forceinline__ bool find_split_in(const AttnArgs &a, int k, SplitRow
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const bool row_ok = base + 64 * q + lane < a.num_reqs && cur[q].p >= 0 && cur[q].row0 >= 0 && cur[q].row0 < a.num_rows;
-            nt[q] = row_ok ? dec_tiles(cur[q].p, cur[q].next - cur[q].row0) : 0;
+            nt[q] = row_ok ? dec_tiles<F>(a, cur[q].p, cur[q].next - cur[q].row0) : 0;
             inc[q] = wave_scan(nt[q]);
         }
 #pragma unroll
@@ -972,10 +1082,10 @@ __device__ __forceinline__ bool find_split_in(const AttnArgs &a, int k, SplitRow
 }
 
 // Workgroup `part` of split row k merges its share of the heads.
-template <bool MANY>
+template <bool MANY, int F>
 __device__ void decode_merge(const AttnArgs &a, int k, int part, float *s_o, float *s_ml) {
     SplitRow sr;
-    if (!(a.num_reqs <= 64 ? find_split_in<1>(a, k, sr) : find_split_in<kLookupQ>(a, k, sr))) return;
+    if (!(a.num_reqs <= 64 ? find_split_in<1, F>(a, k, sr) : find_split_in<kLookupQ, F>(a, k, sr))) return;
     end_lookup();
     const int S = a.dec_unit_tiles, T = sr.T, row = sr.row;
     const int w0 = T / S, w1 = (T + sr.nt - 1) / S;
@@ -998,11 +1108,11 @@ struct ChunkRow {
     Located lc;  // local: the row's index in its request
     int items;
 };
-template <int Q>
+template <int Q, int F>
 __device__ __forceinline__ bool find_chunk_row_in(const AttnArgs &a, int k, ChunkRow &cr) {
     const int lane = threadIdx.x & 63;
     const auto req = [&](int i) { return a.chunk_rev != 0 ? a.num_reqs - 1 - i : i; };
-    const ChunkCount count{a.ks_chunk, a.route};
+    const ChunkCount<F> count{a.ks_chunk, a.route, a.band};
     int rows = 0, items = 0;  // of the requests before this step's
     LenRow cur[Q];
 #pragma unroll
@@ -1045,16 +1155,16 @@ __device__ __forceinline__ bool find_chunk_row_in(const AttnArgs &a, int k, Chun
 }
 
 // Workgroup `part` of row k of the split chunk requests.
-template <bool MANY>
+template <bool MANY, int F>
 __device__ void chunk_merge(const AttnArgs &a, int k, int part, float *s_o, float *s_ml) {
     ChunkRow cr;
-    if (!(a.num_reqs <= 64 ? find_chunk_row_in<1>(a, k, cr) : find_chunk_row_in<kLookupQ>(a, k, cr))) return;
+    if (!(a.num_reqs <= 64 ? find_chunk_row_in<1, F>(a, k, cr) : find_chunk_row_in<kLookupQ, F>(a, k, cr))) return;
     end_lookup();
     // the row's block: its item of key range 0, and ranges 1, 2, .. behind it
     Located lc = cr.lc;
-    const int nks = ceil_div(lc.p + lc.c, a.ks_chunk), j = lc.local % kChunkBlockTokens;
+    const int nks = ceil_div(chunk_span<F>(a.band, lc.p, lc.c), a.ks_chunk), j = lc.local % kChunkBlockTokens;
     lc.local = (ceil_div(lc.c, kChunkBlockTokens) - 1 - lc.local / kChunkBlockTokens) * nks;
-    const ChunkItem it = decode_chunk_item(a, lc);
+    const ChunkItem it = decode_chunk_item<F>(a, lc);
     const int item = cr.items + lc.local;
     if (it.nks_eff <= 1 || item + it.nks_eff > a.n_chunk_items) return;
     if (it.p < 0 || it.row0 < 0 || it.row0 + it.i1 > a.num_rows) return;
@@ -1118,11 +1228,16 @@ __device__ __forceinline__ uint32_t f16x2_bits(float a, float b) {
 
 constexpr int kCT = kChunkBlockTokens;                 // 8 tokens per item, one per wave
 constexpr int kQSteps = kDqk / 32;                     // 18 query operands of 32 dims
-constexpr int kQRegSteps = 16;                         // the first 16 stay in registers, the rope ones in LDS
+// The first of them stay in registers, the others (the rope ones) in LDS: with a
+// window the masks take the four registers of one more.
+template <int F>
+constexpr int q_reg_steps = F == kPlain ? 16 : 15;
 constexpr int kChunkRing = 3;
 constexpr int kPTile = kCT * 64 * 16;                  // fp16 P of one tile: [token][lane] 16 bytes
-constexpr int kQLdsBytes = (kQSteps - kQRegSteps) * kCT * 64 * 16;  // rope query operands: [step][token][lane]
-constexpr int kChunkLds = kChunkRing * kChunkTileBytes + 2 * kPTile + kQLdsBytes + 2 * kCT * kHeads * 4 + 16;
+template <int F>
+constexpr int q_lds_bytes = (kQSteps - q_reg_steps<F>) * kCT * 64 * 16;  // query operands in LDS: [step][token][lane]
+template <int F>
+constexpr int chunk_lds = kChunkRing * kChunkTileBytes + 2 * kPTile + q_lds_bytes<F> + 2 * kCT * kHeads * 4 + 16;
 // Largest exponent (log2 units) a probability may take against the reference
 // max: 2^15 stays inside fp16.
 constexpr float kMaxPExp = 15.f;
@@ -1157,6 +1272,34 @@ __device__ __forceinline__ void lds_dma16_sbase_imm(const void *sbase, uint32_t 
         : "memory");
 }
 
+// Keys and pages of a chunk item's range, as SegKeys for a decode segment: tile t
+// starts at key base + 32 t, `skip` keys further from tile `gap` on.
+template <int F>
+struct ChunkKeys {
+    int base, lp0, log2_page;
+    __device__ ChunkKeys(const AttnArgs &a, const ChunkItem &it) : base(it.k0), lp0(it.k0 >> a.log2_page), log2_page(a.log2_page) {}
+    __device__ int tile(int t) const { return base + t * kChunkKeys; }
+    __device__ int entry(int key) const { return (key >> log2_page) - lp0; }
+    __device__ int logical_page(int i) const { return lp0 + i; }
+};
+template <>
+struct ChunkKeys<kWindow> {
+    int base, lp0, log2_page, gap, skip, gap_pages;  // gap_pages: logical pages that have no entry
+    __device__ ChunkKeys(const AttnArgs &a, const ChunkItem &it) : log2_page(a.log2_page), gap(0), skip(0), gap_pages(0) {
+        const int sink_keys = a.band.sink_keys;
+        base = it.k0 + (it.k0 >= sink_keys ? it.shift : 0);
+        lp0 = base >> log2_page;
+        if (it.shift > 0 && it.k0 < sink_keys && it.k1 > sink_keys) {
+            gap = (sink_keys - it.k0) / kChunkKeys;
+            skip = it.shift;
+            gap_pages = ((sink_keys + skip) >> log2_page) - ((sink_keys - 1) >> log2_page) - 1;
+        }
+    }
+    __device__ int tile(int t) const { return base + t * kChunkKeys + (t >= gap ? skip : 0); }
+    __device__ int entry(int key) const { return (key >> log2_page) - lp0 - (key >= tile(gap) ? gap_pages : 0); }
+    __device__ int logical_page(int i) const { return lp0 + i + (i > ((tile(gap) - skip - 1) >> log2_page) - lp0 ? gap_pages : 0); }
+};
+
 // Passes of a chunk item.  The reference max of each row is fixed for the
 // whole key range, so the accumulators are never rescaled:
 //   main    reference = max of the first tile.  Each lane also tracks the max
@@ -1167,10 +1310,11 @@ __device__ __forceinline__ void lds_dma16_sbase_imm(const void *sbase, uint32_t 
 
 // Returns true when the main pass was abandoned: the caller then runs the
 // item again with exact = true (the exact maxima wait in LDS).
+template <int F>
 __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages, bool exact) {
     Located lc;
-    if (!locate_item(item, a.num_reqs, ReqLens{a.cu_q, a.prefix, a.chunk_rev != 0}, ChunkCount{a.ks_chunk, a.route}, lc)) return false;
-    const ChunkItem it = decode_chunk_item(a, lc);
+    if (!locate_item(item, a.num_reqs, ReqLens{a.cu_q, a.prefix, a.chunk_rev != 0}, ChunkCount<F>{a.ks_chunk, a.route, a.band}, lc)) return false;
+    const ChunkItem it = decode_chunk_item<F>(a, lc);
     TRACE(1);
     const int r = it.r;
     if (it.k0 >= it.k1) return false;  // key range past this block's causal limit
@@ -1181,7 +1325,10 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     const int g = lane >> 4, hd = lane & 15;
     const int nt = it.i1 - it.i0;  // tokens of this block (1 .. 8)
     const int ntiles = ceil_div(it.k1 - it.k0, kChunkKeys);
-    const int lp0 = it.k0 >> a.log2_page;
+    // keys and pages of the item's range: consecutive, with a window perhaps a gap behind the sinks
+    const ChunkKeys<F> ck(a, it);
+    int k_end = it.k1;  // its last key, plus 1
+    if constexpr (F != kPlain) k_end = ck.tile((it.k1 - 1 - it.k0) / kChunkKeys) + (it.k1 - 1 - it.k0) % kChunkKeys + 1;
     // This wave's token (an idle token repeats the last one; its results are
     // not stored).  Query operands: lane l holds dims 32 s + 8 g .. + 7 of
     // head hd, s = 0..17.
@@ -1189,10 +1336,11 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // Page ids (needed first, by the tile DMAs), then the queries go out, and
     // the DMAs follow while the queries are still on their way: one round trip
     // less before an item's first tile (32 + 512 rows 43.1 -> 42.3 us).
-    const int npages = ((it.k1 - 1) >> a.log2_page) - lp0 + 1;
+    const int npages = ck.entry(k_end - 1) + 1;
     static_assert(kPageWindow <= kAttnThreads, "one window entry per thread");
     int pg = 0;
-    if (tid < min(npages, kPageWindow) && lp0 + tid < a.max_pages) pg = a.bt[(size_t)r * a.max_pages + lp0 + tid];
+    if (tid < min(npages, kPageWindow) && ck.logical_page(tid) < a.max_pages) pg = a.bt[(size_t)r * a.max_pages + ck.logical_page(tid)];
+    constexpr int kQRegSteps = q_reg_steps<F>;
     u32x4 qreg[kQRegSteps], qr[kQSteps - kQRegSteps];
     char *const s_q = smem + kChunkRing * kChunkTileBytes + 2 * kPTile;  // rope query operands
     {
@@ -1204,7 +1352,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     }
     if (tid < min(npages, kPageWindow)) {
         const bool ok = (unsigned)pg < (unsigned)a.num_pages;
-        if (!ok) raise_flag(kFlagBadPage);
+        if (!ok && page_seen<F>(a, ck.logical_page(tid), it.p + it.i0)) raise_flag(kFlagBadPage);
         s_pages[tid] = ok ? pg : 0;
     }
     TRACE(2);
@@ -1212,13 +1360,14 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
 
     const uint32_t ring = lds_addr(smem);
     char *const s_pbuf = smem + kChunkRing * kChunkTileBytes;           // [2][token][lane] 16 bytes
-    float *const s_l = reinterpret_cast<float *>(s_q + kQLdsBytes);     // [token][head] row sums
+    float *const s_l = reinterpret_cast<float *>(s_q + q_lds_bytes<F>);     // [token][head] row sums
     float *const s_mx = s_l + kCT * kHeads;                            // [token][head] exact maxima
     int *const s_abort = reinterpret_cast<int *>(s_mx + kCT * kHeads);
 
     // Causal limit of this wave's token (absolute key index, clipped to the
     // item's key range); wave-uniform.
-    const int lim = __builtin_amdgcn_readfirstlane(min(it.p + it.i0 + tk, it.k1 - 1));
+    const int pos = it.p + it.i0 + tk;
+    const int lim = __builtin_amdgcn_readfirstlane(min(pos, k_end - 1));
 
     // K operand of key block kb, step s (keys 16 kb + hd, dims 32 s + 8 g ..):
     // chunk 4 s + g, at kq_off[s & 1] + 2048 kb + 4096 (s >> 1).
@@ -1247,12 +1396,13 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     const int dkey = 8 * dw + (lane >> 3);  // this lane's key in every round of this wave
     const uint32_t dvoff = dkey * kRowBytes + 16 * ((lane & 7) ^ ((lane >> 3) & 7));
     const bool in_page = a.page_size >= kChunkKeys;
-    const int cached_end = a.new_kv != nullptr ? min(it.k1, it.p) : it.k1;
+    const bool fused = F == kPlain && a.new_kv != nullptr;
+    const int cached_end = fused ? min(k_end, it.p) : k_end;
     auto page_of = [&](int t) {
-        return s_pages[min(((it.k0 + t * kChunkKeys) >> a.log2_page) - lp0, kPageWindow - 1)];
+        return s_pages[min(ck.entry(ck.tile(t)), kPageWindow - 1)];
     };
     auto issue = [&](int t, int slot, int page) {
-        const int kbase = it.k0 + t * kChunkKeys;
+        const int kbase = ck.tile(t);
         const uint32_t dst = ring + slot * kChunkTileBytes + dw * 1024;  // round r = dw + 4 r'
         if (in_page && kbase + kChunkKeys <= cached_end) {
             const char *src = reinterpret_cast<const char *>(a.kv) +
@@ -1264,16 +1414,18 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
 #undef MLA_CHUNK_DMA_S
         } else {
             // keys past the item's range repeat its last key (a finite cached latent)
-            const int key = min(kbase + dkey, it.k1 - 1);
+            const int key = min(kbase + dkey, k_end - 1);
             const char *gs;
-            if (a.new_kv != nullptr && key >= it.p) {
+            if (fused && key >= it.p) {
                 gs = reinterpret_cast<const char *>(a.new_kv) + (size_t)(it.row0 + key - it.p) * kRowBytes;
             } else {
-                const int pg = s_pages[min((key >> a.log2_page) - lp0, kPageWindow - 1)];
+                const int pg = s_pages[min(ck.entry(key), kPageWindow - 1)];
                 gs = reinterpret_cast<const char *>(a.kv) +
                      ((size_t)pg * a.page_size + (key & (a.page_size - 1))) * kRowBytes;
             }
-            gs += 16 * ((lane & 7) ^ ((lane >> 3) & 7));
+            int ln = lane;
+            if constexpr (F != kPlain) asm volatile("" : "+v"(ln));  // (or an address is kept across the tiles, in scratch)
+            gs += 16 * ((ln & 7) ^ ((ln >> 3) & 7));
 #define MLA_CHUNK_DMA_V(r) lds_dma16_imm<128 * (r)>(gs, __builtin_amdgcn_readfirstlane(dst + 4096 * (r)))
             MLA_CHUNK_DMA_V(0); MLA_CHUNK_DMA_V(1); MLA_CHUNK_DMA_V(2); MLA_CHUNK_DMA_V(3); MLA_CHUNK_DMA_V(4);
             MLA_CHUNK_DMA_V(5); MLA_CHUNK_DMA_V(6); MLA_CHUNK_DMA_V(7); MLA_CHUNK_DMA_V(8);
@@ -1281,6 +1433,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
     };
 
+    const bool main_pass = !exact;
     float m_ref = kNegInf, m_lane = kNegInf, l_run = 0.f;
     f32x4 acc[kCT][4];  // [token][value block db]
 
@@ -1317,8 +1470,19 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     };
     // masked raw scores of tile t
     auto masked = [&](int t, const f32x4 (&s)[2], float (&x)[8]) {
-        const int kbase = it.k0 + t * kChunkKeys;
-        if (kbase + kChunkKeys - 1 <= lim) {
+        const int kbase = ck.tile(t);
+        if constexpr ((F & kWindow) != 0) {
+            if (kbase + kChunkKeys - 1 <= lim && (kbase > pos - a.band.window || kbase + kChunkKeys <= a.band.sinks)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int key = kbase + 4 * g + 16 * (e >> 2) + (e & 3);
+                    x[e] = key <= lim && row_sees<F>(a, key, pos) ? s[e >> 2][e & 3] : kNegInf;
+                }
+            }
+        } else if (kbase + kChunkKeys - 1 <= lim) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3];
         } else {
@@ -1334,6 +1498,14 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         float x[8];
         masked(t, s, x);
         m_lane = lane_max(x, m_lane);
+        if constexpr ((F & kWindow) != 0) {
+            // a row that saw nothing so far: its reference is the max of the first tile that it sees (with no
+            // probability behind it yet, nothing is rescaled)
+            if (main_pass && __builtin_amdgcn_ballot_w64(m_ref == kNegInf) != 0) {
+                const float m = wave_max16(lane_max(x, kNegInf) * a.scale_log2);
+                m_ref = m_ref == kNegInf ? m : m_ref;
+            }
+        }
         // the scaled score is rounded before the max is subtracted, so the max
         // key gets p = 1 exactly; masked scores give p = 0
         const float mref = m_ref == kNegInf ? 0.f : m_ref;
@@ -1361,7 +1533,15 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto vconv = [&] {
+    auto vconv = [&](bool careful) {
+        if constexpr (F != kPlain) {
+            if (careful) {
+#pragma unroll
+                for (int db = 0; db < 4; ++db)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) av[db][i] = finite_bf16x2(av[db][i]);
+            }
+        }
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -1386,7 +1566,6 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     };
 
     TRACE(3);
-    const bool main_pass = !exact;
     if (exact) m_ref = s_mx[wv * kHeads + hd];
     if (tid == 0) *s_abort = 0;
     lds_barrier();  // page window and abort flag ready; the ring is idle
@@ -1425,7 +1604,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         vload(0);
         softmax(0, 0, s0);
-        vconv();
+        vconv(F != kPlain && any_not_finite(s0));
     }
     int slot = 0;  // ring slot of tile t (t % 3)
     // steady state: after the barrier, P*V of tile t and the scores of t + 1,
@@ -1447,7 +1626,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             scores(slot1, s1);
             vload(slot1);
             softmax(t + 1, (t + 1) & 1, s1);
-            vconv();
+            vconv(F != kPlain && any_not_finite(s1));
         }
         slot = slot1;
         TRACE_TILE(t, 13);
@@ -1496,18 +1675,19 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             if (a.lse) a.lse[(size_t)row * kHeads + hd] = (m_ref + log2f(l)) * kLn2;
         } else {
             const size_t prow = (size_t)item * kCT + wv;
-            a.ws_chunk_ml[(prow * kHeads + hd) * 2 + 0] = m_ref;
+            a.ws_chunk_ml[(prow * kHeads + hd) * 2 + 0] = F == kPlain ? m_ref : partial_max(m_ref, l);
             a.ws_chunk_ml[(prow * kHeads + hd) * 2 + 1] = l;
         }
     }
     // fused append: split 0 of a block writes the block's own new latents
     // (nothing in this launch reads those slots, so it can come last)
-    if (a.new_kv != nullptr && it.ks == 0) append_rows(a, r, it.p + it.i0, it.row0 + it.i0, it.i1 - it.i0);
+    if (F == kPlain && a.new_kv != nullptr && it.ks == 0) append_rows(a, r, it.p + it.i0, it.row0 + it.i0, it.i1 - it.i0);
     TRACE(5);
     return false;
 }
 
-constexpr int kMainLds = kDecLds > kChunkLds ? kDecLds : kChunkLds;
+template <int F>
+constexpr int main_lds = kDecLds > chunk_lds<F> ? kDecLds : chunk_lds<F>;
 
 // Persistent workgroups (one per CU) take work items from two counters in
 // the workspace, one per queue: the chunk items (largest blocks first) and
@@ -1524,8 +1704,9 @@ constexpr int kMainLds = kDecLds > kChunkLds ? kDecLds : kChunkLds;
 // waited for up to five round trips to memory.  With the shorter decode
 // start-up: 4 decode rows of 842 to 3569 keys 28.6 -> 19.6 us, 68 rows of about
 // 205 keys 31.3 -> 23.6, 256 rows of up to 16384 keys 475 -> 465.)
+template <int F>
 __global__ __launch_bounds__(kAttnThreads, 1) void attention_kernel(AttnArgs a) {
-    __shared__ __attribute__((aligned(16))) char smem[kMainLds];
+    __shared__ __attribute__((aligned(16))) char smem[main_lds<F>];
     __shared__ int s_pages[2][kPageWindow];  // chunk items use the first window
     __shared__ DecSeg s_seg[2][kMaxSeg];
     __shared__ int s_gbar[2];
@@ -1537,12 +1718,12 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attention_kernel(AttnArgs a) 
         if (item < a.n_chunk_items) {
             // a second, exact pass only if the main one was abandoned
             for (int pass = 0; pass < 2; ++pass) {
-                if (!chunk_item(a, item, smem, s_pages[0], pass != 0)) break;
+                if (!chunk_item<F>(a, item, smem, s_pages[0], pass != 0)) break;
                 __syncthreads();
             }
         }
         else
-            decode_wg(a, item - a.n_chunk_items, smem, s_pages, s_seg, s_gbar);
+            decode_wg<F>(a, item - a.n_chunk_items, smem, s_pages, s_seg, s_gbar);
         TRACE(7);
         int grid = a.grid;
         asm volatile("" : "+s"(grid));  // (computed again per item: kept across the items it would take registers from their loops)
@@ -1589,16 +1770,16 @@ __host__ __device__ __forceinline__ int merge_dec_wgs(const AttnArgs &a) {
 // partial visible): first merge_wgs workgroups per split decode row, then
 // chunk_merge_wgs per row of the split chunk requests.  MANY: some rows take a
 // workgroup per head.
-template <bool MANY>
+template <bool MANY, int F>
 __global__ __launch_bounds__(kThreads, MANY ? 4 : 5) void combine_kernel(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) float s_o[4 * kDv];
     __shared__ float s_ml[8];
     const int b = blockIdx.x;
     const int n_dec = merge_dec_wgs(a);
     if (b < n_dec)
-        decode_merge<MANY>(a, b / merge_wgs(a), b % merge_wgs(a), s_o, s_ml);
+        decode_merge<MANY, F>(a, b / merge_wgs(a), b % merge_wgs(a), s_o, s_ml);
     else
-        chunk_merge<MANY>(a, (b - n_dec) / a.chunk_merge_wgs, (b - n_dec) % a.chunk_merge_wgs, s_o, s_ml);
+        chunk_merge<MANY, F>(a, (b - n_dec) / a.chunk_merge_wgs, (b - n_dec) % a.chunk_merge_wgs, s_o, s_ml);
 }
 
 // ----------------------------------------------------------------- append
@@ -1723,19 +1904,24 @@ hipError_t launch_append8(const Append8Args &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_rows(const AttnArgs &a, hipStream_t s) {
-    if (a.kv8 != nullptr)
-        hipLaunchKernelGGL(rows_kernel<true>, dim3(a.num_rows), dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL(rows_kernel<false>, dim3(a.num_rows), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
-}
-
 hipError_t launch_attention(const AttnArgs &a, hipStream_t s) {
     const int grid = a.grid;
     if (grid == 0) return hipSuccess;
-    hipLaunchKernelGGL(attention_kernel, dim3(grid), dim3(kAttnThreads), 0, s, a);
+    if (a.kv8 != nullptr)
+        hipLaunchKernelGGL(rows8_kernel, dim3(a.num_rows), dim3(kThreads), 0, s, a);
+    else if (a.band.window > 0)
+        hipLaunchKernelGGL(attention_kernel<kWindow>, dim3(grid), dim3(kAttnThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL(attention_kernel<kPlain>, dim3(grid), dim3(kAttnThreads), 0, s, a);
     return hipGetLastError();
+}
+
+template <int F>
+static void launch_merge(const AttnArgs &a, int grid, hipStream_t s) {
+    if (a.merge_many || a.chunk_merge_wgs == kHeads)
+        hipLaunchKernelGGL((combine_kernel<true, F>), dim3(grid), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((combine_kernel<false, F>), dim3(grid), dim3(kThreads), 0, s, a);
 }
 
 hipError_t launch_combine(const AttnArgs &a, hipStream_t s) {
@@ -1744,11 +1930,11 @@ hipError_t launch_combine(const AttnArgs &a, hipStream_t s) {
         (long long)merge_dec_wgs(a) + (a.ws_chunk_o != nullptr ? (long long)a.n_split_chunk_rows * a.chunk_merge_wgs : 0);
     if (grid_ll > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const int grid = (int)grid_ll;
-    if (grid == 0) return hipSuccess;
-    if (a.merge_many || a.chunk_merge_wgs == kHeads)
-        hipLaunchKernelGGL(combine_kernel<true>, dim3(grid), dim3(kThreads), 0, s, a);
+    if (grid == 0 || a.kv8 != nullptr) return hipSuccess;
+    if (a.band.window > 0)
+        launch_merge<kWindow>(a, grid, s);
     else
-        hipLaunchKernelGGL(combine_kernel<false>, dim3(grid), dim3(kThreads), 0, s, a);
+        launch_merge<kPlain>(a, grid, s);
     return hipGetLastError();
 }
 
