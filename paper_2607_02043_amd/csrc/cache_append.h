@@ -54,7 +54,6 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendArgs a, dou
 // smallest integer in [kMinExp8, kMaxExp8] for which amax 2^-E <= 448 = 1.75 2^8.
 // amax = m 2^e with m in [1, 2) gives E = e - 8, one more if m > 1.75, which is
 // when 0x1fffff added to the bits carries into the exponent field.
-constexpr int kBlock8 = 16;  // MLA_CACHE8_BLOCK
 constexpr int kMinExp8 = -100, kMaxExp8 = 120;
 __device__ __forceinline__ int block_exponent(float amax) {
     const int e = (int)((__float_as_uint(amax) + 0x1fffffu) >> 23) - 127 - 8;

@@ -55,6 +55,12 @@ struct Form {
 // Forms of the attention launch (bits).
 constexpr int kPlain = 0;
 constexpr int kWindow = 1;  // through AttnArgs::band
+constexpr int kEight = 2;   // over the 8-bit cache, AttnArgs::kv8
+template <int F>
+inline constexpr bool has_window = (F & kWindow) != 0;
+template <int F>
+inline constexpr bool has_eight = (F & kEight) != 0;
+constexpr int kBlock8 = 16;  // tokens that share a pair of scales (MLA_CACHE8_BLOCK)
 
 struct AttnArgs {
     const uint16_t *q;

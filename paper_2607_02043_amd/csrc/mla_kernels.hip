@@ -60,6 +60,13 @@ constexpr int kDecGroupBytes = kDecRing * kDecTileBytes;
 constexpr int kDecXBytes = 4 * kHeads * 20 * 4;               // partial score blocks of a group
 constexpr int kDecLds = 2 * kDecGroupBytes + 2 * kDecXBytes;  // two groups: rings, then score blocks
 // chunk path
+constexpr int kDec8Ring = 4;                            // over the 8-bit cache: ring slots, bytes of one
+constexpr int kDec8TileBytes = kDecKeys * kDqk;         // 18432, also a query block's
+constexpr int kDec8GroupBytes = kDec8Ring * kDec8TileBytes;
+constexpr int kDec8XBytes = 4 * 64 * 16;                // partial score blocks of a group
+constexpr int kDec8ScaleBytes = kDec8Ring * 32;         // two 16-byte pieces of the scales a tile
+constexpr int kDec8Lds = 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes);
+static_assert(kDec8TileBytes == kHeads * kRowBytes, "a query block fills a slot");
 constexpr int kChunkKeys = kKeysPerTile;  // 32
 constexpr int kChunkTileBytes = kChunkKeys * kRowBytes;  // 36864
 
@@ -308,7 +315,7 @@ __device__ bool locate_item(int target, int num_reqs, const ReqLens &rl, CountFn
 // Virtual keys of a chunk request's longest block (form F), which its key ranges cut.
 template <int F>
 __device__ __forceinline__ int chunk_span(const Band &band, int p, int c) {
-    if constexpr ((F & kWindow) != 0)
+    if constexpr (has_window<F>)
         return band_span(band, p, c);
     else
         return p + c;
@@ -348,7 +355,7 @@ __device__ __forceinline__ ChunkItem decode_chunk_item(const AttnArgs &a, const 
     it.ks = lc.local % nks;
     it.i0 = rb * kChunkBlockTokens;
     it.i1 = min(it.i0 + kChunkBlockTokens, it.c);
-    it.shift = (F & kWindow) != 0 ? band_shift(a.band, it.p + it.i0) : 0;
+    it.shift = has_window<F> ? band_shift(a.band, it.p + it.i0) : 0;
     const int klim = it.p + it.i1 - it.shift;
     const int kp = ceil_div(ceil_div(klim, ceil_div(klim, a.ks_chunk)), 64) * 64;  // keys per range (<= ks_chunk)
     it.nks_eff = ceil_div(klim, kp);
@@ -575,14 +582,14 @@ __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
 // Whether the row at position t sees a key, or any key of a logical page (rows t and later).
 template <int F>
 __device__ __forceinline__ bool row_sees(const AttnArgs &a, int key, int t) {
-    if constexpr ((F & kWindow) != 0)
+    if constexpr (has_window<F>)
         return key <= t && (key > t - a.band.window || key < a.band.sinks);
     else
         return key <= t;
 }
 template <int F>
 __device__ __forceinline__ bool page_seen(const AttnArgs &a, int lp, int t) {
-    if constexpr ((F & kWindow) != 0)
+    if constexpr (has_window<F>)
         return (lp << a.log2_page) < a.band.sinks || ((lp + 1) << a.log2_page) - 1 > t - a.band.window;
     else
         return true;
@@ -597,14 +604,14 @@ struct DecSeg {
 
 template <int F>
 __device__ __forceinline__ int dec_tiles(const AttnArgs &a, int p, int c) {
-    const int shift = (F & kWindow) != 0 ? band_shift(a.band, p) : 0;
+    const int shift = has_window<F> ? band_shift(a.band, p) : 0;
     return c == 1 ? ceil_div(p + 1 - shift, kDecKeys) : 0;
 }
 
 // Keys and pages of a segment.  Its tiles are consecutive, and so are its pages;
 // with a window (tiles of virtual keys) there may be a gap behind the sinks:
 // the page window then holds the pages up to the gap and those behind it.
-template <int F>
+template <bool WINDOW>
 struct SegKeys {
     __device__ SegKeys(const AttnArgs &, const DecSeg &) {}
     __device__ int key(int v) const { return v; }
@@ -615,7 +622,7 @@ struct SegKeys {
     }
 };
 template <>
-struct SegKeys<kWindow> {
+struct SegKeys<true> {
     int sink_keys, shift, before, lpw;  // pages before the gap; logical page of entry i behind it, less i
     __device__ SegKeys(const AttnArgs &a, const DecSeg &sg) : sink_keys(a.band.sink_keys), shift(band_shift(a.band, sg.p)) {
         before = 0;
@@ -667,10 +674,10 @@ __device__ __forceinline__ int find_unit_in(const AttnArgs &a, int R0, int R1, D
             if (m != 0) {
                 const int t0 = max(R0 - T, 0), t1 = min(R1 - T, nt[q]);
                 int lp0 = (t0 * kDecKeys) >> a.log2_page, np;
-                if constexpr ((F & kWindow) != 0) {
+                if constexpr (has_window<F>) {
                     DecSeg sg{0, cur[q].p, 0, t0, t1, 0, 0};
-                    lp0 = sg.lp0 = SegKeys<kWindow>(a, sg).key(t0 * kDecKeys) >> a.log2_page;
-                    np = ov ? SegKeys<kWindow>(a, sg).pages(a, sg) : 0;
+                    lp0 = sg.lp0 = SegKeys<true>(a, sg).key(t0 * kDecKeys) >> a.log2_page;
+                    np = ov ? SegKeys<true>(a, sg).pages(a, sg) : 0;
                 } else {
                     np = ov ? ((min(t1 * kDecKeys, cur[q].p + 1) - 1) >> a.log2_page) - lp0 + 1 : 0;
                 }
@@ -728,7 +735,7 @@ __device__ __forceinline__ void issue_unit(const AttnArgs &a, const DecSeg &sg, 
                                            uint32_t slot, int wv, int lane,
                                            const uint32_t (&dma_off)[(kTileDma + 1) / 2]) {
     constexpr int kDma = kDecTileBytes / (kThreads * 16);  // 9
-    const SegKeys<F> sk(a, sg);
+    const SegKeys<has_window<F>> sk(a, sg);
     const int kbase = sk.key(t * kDecKeys);
     // key p is the new latent when fused (the plain form only)
     const bool fused = F == kPlain && a.new_kv != nullptr;
@@ -851,7 +858,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
         for (int k = 1; k < nseg; ++k) j = s_seg[k].pw <= gtid ? k : j;
         const DecSeg sg = s_seg[j];
         const int i = gtid - sg.pw;
-        const SegKeys<F> sk(a, sg);
+        const SegKeys<has_window<F>> sk(a, sg);
         if (i < sk.pages(a, sg)) {
             const int lp = sk.logical_page(sg, i);
             const int pg = lp < a.max_pages ? a.bt[(size_t)sg.r * a.max_pages + lp] : 0;
@@ -927,7 +934,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
         if (!tile_unit) continue;
         group_barrier(gbar, epoch, a.spin_limit);  // partial score blocks complete
         TRACE_TILE(u, 12);
-        const int kbase = SegKeys<F>(a, sg).key(cons.t * kDecKeys);
+        const int kbase = SegKeys<has_window<F>>(a, sg).key(cons.t * kDecKeys);
         // full scores of this lane's head: x[kt][i] = key 16 kt + 4 g + i (kt = 0, 1)
         f32x4 x[2];
 #pragma unroll
@@ -1030,6 +1037,18 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
         }
     }
     TRACE(4);
+}
+
+#include "cache_decode.h"
+
+// A decode item in form F.
+template <int F>
+__device__ __forceinline__ void decode_item(const AttnArgs &a, int w, char *smem, int (*s_pages_g)[kPageWindow],
+                                            DecSeg (*s_seg_g)[kMaxSeg], int *s_gbar) {
+    if constexpr (has_eight<F>)
+        decode8_wg<F>(a, w, smem, s_pages_g, s_seg_g, s_gbar);
+    else
+        decode_wg<F>(a, w, smem, s_pages_g, s_seg_g, s_gbar);
 }
 
 // Merge kernel side.  A decode row is split when its tiles span several decode
@@ -1229,15 +1248,21 @@ __device__ __forceinline__ uint32_t f16x2_bits(float a, float b) {
 constexpr int kCT = kChunkBlockTokens;                 // 8 tokens per item, one per wave
 constexpr int kQSteps = kDqk / 32;                     // 18 query operands of 32 dims
 // The first of them stay in registers, the others (the rope ones) in LDS: with a
-// window the masks take the four registers of one more.
+// window the masks take the four registers of one more, and over the 8-bit cache
+// the conversion of the next tile.
 template <int F>
 constexpr int q_reg_steps = F == kPlain ? 16 : 15;
 constexpr int kChunkRing = 3;
 constexpr int kPTile = kCT * 64 * 16;                  // fp16 P of one tile: [token][lane] 16 bytes
+constexpr int kChunk8Raw = 2 * kChunkTileBytes;      // 8-bit cache: two converted tiles, then two raw ones (half the size)
+constexpr int kChunk8RawBytes = kChunkKeys * kDqk;   // 18432
+static_assert(kChunk8Raw + 2 * kChunk8RawBytes == kChunkRing * kChunkTileBytes, "both rings take the same space");
+constexpr int kChunk8ScaleBytes = 2 * 8 * 16;        // [raw slot][wave]: the piece of the scales that its rows need
 template <int F>
 constexpr int q_lds_bytes = (kQSteps - q_reg_steps<F>) * kCT * 64 * 16;  // query operands in LDS: [step][token][lane]
 template <int F>
-constexpr int chunk_lds = kChunkRing * kChunkTileBytes + 2 * kPTile + q_lds_bytes<F> + 2 * kCT * kHeads * 4 + 16;
+constexpr int chunk_lds = kChunkRing * kChunkTileBytes + 2 * kPTile + q_lds_bytes<F> + 2 * kCT * kHeads * 4 + 16 +
+                          (has_eight<F> ? kChunk8ScaleBytes : 0);
 // Largest exponent (log2 units) a probability may take against the reference
 // max: 2^15 stays inside fp16.
 constexpr float kMaxPExp = 15.f;
@@ -1274,7 +1299,7 @@ __device__ __forceinline__ void lds_dma16_sbase_imm(const void *sbase, uint32_t 
 
 // Keys and pages of a chunk item's range, as SegKeys for a decode segment: tile t
 // starts at key base + 32 t, `skip` keys further from tile `gap` on.
-template <int F>
+template <bool WINDOW>
 struct ChunkKeys {
     int base, lp0, log2_page;
     __device__ ChunkKeys(const AttnArgs &a, const ChunkItem &it) : base(it.k0), lp0(it.k0 >> a.log2_page), log2_page(a.log2_page) {}
@@ -1283,7 +1308,7 @@ struct ChunkKeys {
     __device__ int logical_page(int i) const { return lp0 + i; }
 };
 template <>
-struct ChunkKeys<kWindow> {
+struct ChunkKeys<true> {
     int base, lp0, log2_page, gap, skip, gap_pages;  // gap_pages: logical pages that have no entry
     __device__ ChunkKeys(const AttnArgs &a, const ChunkItem &it) : log2_page(a.log2_page), gap(0), skip(0), gap_pages(0) {
         const int sink_keys = a.band.sink_keys;
@@ -1326,7 +1351,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     const int nt = it.i1 - it.i0;  // tokens of this block (1 .. 8)
     const int ntiles = ceil_div(it.k1 - it.k0, kChunkKeys);
     // keys and pages of the item's range: consecutive, with a window perhaps a gap behind the sinks
-    const ChunkKeys<F> ck(a, it);
+    const ChunkKeys<has_window<F>> ck(a, it);
     int k_end = it.k1;  // its last key, plus 1
     if constexpr (F != kPlain) k_end = ck.tile((it.k1 - 1 - it.k0) / kChunkKeys) + (it.k1 - 1 - it.k0) % kChunkKeys + 1;
     // This wave's token (an idle token repeats the last one; its results are
@@ -1401,6 +1426,11 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     auto page_of = [&](int t) {
         return s_pages[min(ck.entry(ck.tile(t)), kPageWindow - 1)];
     };
+    [[maybe_unused]] const auto opaque_lane = [&] {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
     auto issue = [&](int t, int slot, int page) {
         const int kbase = ck.tile(t);
         const uint32_t dst = ring + slot * kChunkTileBytes + dw * 1024;  // round r = dw + 4 r'
@@ -1423,13 +1453,60 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
                 gs = reinterpret_cast<const char *>(a.kv) +
                      ((size_t)pg * a.page_size + (key & (a.page_size - 1))) * kRowBytes;
             }
-            int ln = lane;
-            if constexpr (F != kPlain) asm volatile("" : "+v"(ln));  // (or an address is kept across the tiles, in scratch)
+            const int ln = F == kPlain ? lane : opaque_lane();  // (or an address is kept across the tiles, in scratch)
             gs += 16 * ((ln & 7) ^ ((ln >> 3) & 7));
 #define MLA_CHUNK_DMA_V(r) lds_dma16_imm<128 * (r)>(gs, __builtin_amdgcn_readfirstlane(dst + 4096 * (r)))
             MLA_CHUNK_DMA_V(0); MLA_CHUNK_DMA_V(1); MLA_CHUNK_DMA_V(2); MLA_CHUNK_DMA_V(3); MLA_CHUNK_DMA_V(4);
             MLA_CHUNK_DMA_V(5); MLA_CHUNK_DMA_V(6); MLA_CHUNK_DMA_V(7); MLA_CHUNK_DMA_V(8);
 #undef MLA_CHUNK_DMA_V
+        }
+    };
+
+    // Over the 8-bit cache a wave loads and converts the same 16-byte pieces of every tile: round r of wave wv is dims
+    // 64 (wv / 2 + 4 r) .. + 63 of the 16 keys of half wv & 1, four lanes a key (r = 2, the rope dims, on waves 0 and 1
+    // alone).  Raw tiles pass through LDS, so a load in flight holds no registers; a lane then takes its 16 codes out, converts them
+    // with their block's scale (exact) and writes two chunks of the bf16 tile.
+    // (Lanes are opaque in both: their addresses, kept across the tiles, would be kept in scratch.)
+    [[maybe_unused]] const int rounds8 = wv < 2 ? 3 : 2;
+    [[maybe_unused]] char *const s_scale8 = reinterpret_cast<char *>(s_abort) + 16 + 16 * wv;  // + 128 raw slot
+    [[maybe_unused]] auto issue8 = [&](int t) {
+        const int kbase = ck.tile(t);
+        const uint32_t dst = ring + kChunk8Raw + (t & 1) * kChunk8RawBytes + wv * 1024;
+        const int ln = opaque_lane(), key8 = 16 * (wv & 1) + (ln >> 2), part = 16 * (ln & 3) + 64 * (wv >> 1);
+        if (in_page && kbase + kChunkKeys <= k_end) {
+            const uint8_t *src = a.kv8 + ((size_t)__builtin_amdgcn_readfirstlane(page_of(t)) * a.page_size + (kbase & (a.page_size - 1))) * kDqk;
+            const uint32_t voff = key8 * kDqk + part;
+            lds_dma16_sbase_imm<0>(src, voff, __builtin_amdgcn_readfirstlane(dst));
+            lds_dma16_sbase_imm<256>(src, voff, __builtin_amdgcn_readfirstlane(dst + 8192));
+            if (rounds8 == 3) lds_dma16_sbase_imm<512>(src, voff, __builtin_amdgcn_readfirstlane(dst + 16384));
+        } else {
+            const int key = min(kbase + key8, k_end - 1);
+            const int pg = s_pages[min(ck.entry(key), kPageWindow - 1)];
+            const uint8_t *src = a.kv8 + ((size_t)pg * a.page_size + (key & (a.page_size - 1))) * kDqk + part;
+            lds_dma16_imm<0>(src, __builtin_amdgcn_readfirstlane(dst));
+            lds_dma16_imm<256>(src, __builtin_amdgcn_readfirstlane(dst + 8192));
+            if (rounds8 == 3) lds_dma16_imm<512>(src, __builtin_amdgcn_readfirstlane(dst + 16384));
+        }
+        const uint32_t sdst = lds_addr(s_scale8) + 128 * (t & 1);
+        const size_t entry = scale_entry(a, s_pages[min(ck.entry(min(kbase + 16 * (wv & 1), k_end - 1)), kPageWindow - 1)],
+                                         min(kbase + 16 * (wv & 1), k_end - 1));
+        if (lane == 0) lds_dma16(reinterpret_cast<const char *>(a.kv8_scales) + (entry * 4 & ~size_t(15)), __builtin_amdgcn_readfirstlane(sdst));
+    };
+    // the raw tile t (this wave's part, landed) -> bf16 slot t & 1
+    [[maybe_unused]] auto convert8 = [&](int t) {
+        const int key0 = min(ck.tile(t) + 16 * (wv & 1), k_end - 1);
+        const int pg = a.page_size >= 64 ? 0 : s_pages[min(ck.entry(key0), kPageWindow - 1)];
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(s_scale8 + 128 * (t & 1) + 4 * (scale_entry(a, pg, key0) & 3));
+        const float sc = __uint_as_float(w << 16), sr = __uint_as_float(w & 0xffff0000u);
+        const int ln = opaque_lane(), key8 = 16 * (wv & 1) + (ln >> 2);
+        const char *raw = smem + kChunk8Raw + (t & 1) * kChunk8RawBytes + wv * 1024 + ln * 16;
+        char *tile = smem + (t & 1) * kChunkTileBytes + 4096 * (wv >> 1) + 128 * key8;
+        for (int r = 0; r < rounds8; ++r) {
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(raw + 8192 * r);
+            const float s = r == 2 ? sr : sc;
+            const int c = 2 * (ln & 3);
+            *reinterpret_cast<u32x4 *>(tile + 16384 * r + 16 * (c ^ (key8 & 7))) = bf16_of_e4m3x8(v[0], v[1], s);
+            *reinterpret_cast<u32x4 *>(tile + 16384 * r + 16 * ((c + 1) ^ (key8 & 7))) = bf16_of_e4m3x8(v[2], v[3], s);
         }
     };
 
@@ -1471,7 +1548,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // masked raw scores of tile t
     auto masked = [&](int t, const f32x4 (&s)[2], float (&x)[8]) {
         const int kbase = ck.tile(t);
-        if constexpr ((F & kWindow) != 0) {
+        if constexpr (has_window<F>) {
             if (kbase + kChunkKeys - 1 <= lim && (kbase > pos - a.band.window || kbase + kChunkKeys <= a.band.sinks)) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3];
@@ -1498,7 +1575,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         float x[8];
         masked(t, s, x);
         m_lane = lane_max(x, m_lane);
-        if constexpr ((F & kWindow) != 0) {
+        if constexpr (has_window<F>) {
             // a row that saw nothing so far: its reference is the max of the first tile that it sees (with no
             // probability behind it yet, nothing is rescaled)
             if (main_pass && __builtin_amdgcn_ballot_w64(m_ref == kNegInf) != 0) {
@@ -1576,13 +1653,24 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // waits for anyway, and tile 1 stays in flight across it.  (Both tiles from
     // waves 4..7, the queries awaited behind them: 5 + 32 rows 22.6 -> 22.3 us, 32 +
     // 512 rows 41.0 -> 40.4, ragged chunks in two calls 85.0 -> 84.1.)
-    if (!dma_wave) issue(0, 0, page_of(0));
+    if constexpr (has_eight<F>) {
+        issue8(0);
+        if (ntiles > 1) issue8(1);
+    } else {
+        if (!dma_wave) issue(0, 0, page_of(0));
+    }
 #pragma unroll
     for (int s = 0; s < kQRegSteps; ++s) asm volatile("" : "+v"(qreg[s]));
 #pragma unroll
     for (int s = 0; s < kQSteps - kQRegSteps; ++s) asm volatile("" : "+v"(qr[s]));
     wait_dma_all();
-    if (dma_wave && ntiles > 1) issue(1, 1, page_of(1));
+    if constexpr (has_eight<F>) {
+        convert8(0);
+        if (ntiles > 1) convert8(1);
+        if (ntiles > 2) issue8(2);
+    } else {
+        if (dma_wave && ntiles > 1) issue(1, 1, page_of(1));
+    }
 #pragma unroll
     for (int s = 0; s < kQSteps - kQRegSteps; ++s)
         *reinterpret_cast<u32x4 *>(s_q + ((s * kCT + wv) * 64 + lane) * 16) = qr[s];
@@ -1611,6 +1699,25 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // then the softmax of t + 1
     for (int t = 0; t < ntiles; ++t) {
         TRACE_TILE(t, 11);
+        if constexpr (has_eight<F>) {
+            // Tile t + 1 was converted before this barrier (two bf16 slots: tile t's, whose V is in registers, takes tile
+            // t + 2), raw tile t + 2 is in flight.
+            __syncthreads();
+            pv(t & 1);
+            if (t + 2 < ntiles) {
+                wait_dma_all();  // raw tile t + 2 (this wave's part)
+                if (t + 3 < ntiles) issue8(t + 3);
+                convert8(t + 2);
+            }
+            if (t + 1 < ntiles) {
+                f32x4 s1[2];
+                scores((t + 1) & 1, s1);
+                vload((t + 1) & 1);
+                softmax(t + 1, (t + 1) & 1, s1);
+                vconv(any_not_finite(s1));
+            }
+            continue;
+        }
         const int next_page = page_of(min(t + 2, ntiles - 1));
         if (t + 1 < ntiles) wait_dma_all();  // tile t + 1 (this wave's part)
         __syncthreads();  // tile t + 1 and P of tile t complete; slot (t + 2) % 3 and P buffer (t + 1) & 1 free
@@ -1652,6 +1759,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     }
     __syncthreads();
     TRACE(6);
+    const int ge = has_eight<F> ? (item_tid() & 63) >> 4 : g;  // (kept across the tiles it would be kept in scratch)
     // acc[tb][db] element i: value dim 64 wv + 16 db + 4 g + i of token tb, head hd
 #pragma unroll
     for (int tb = 0; tb < kCT; ++tb) {
@@ -1660,10 +1768,10 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         if (it.nks_eff == 1) {
             const float inv = 1.f / s_l[tb * kHeads + hd];
 #pragma unroll
-            for (int db = 0; db < 4; ++db) store_out4(a, row, hd, 64 * wv + 16 * db + 4 * g, acc[tb][db] * inv);
+            for (int db = 0; db < 4; ++db) store_out4(a, row, hd, 64 * wv + 16 * db + 4 * ge, acc[tb][db] * inv);
         } else {
             const size_t prow = (size_t)item * kCT + tb;
-            float *po = a.ws_chunk_o + (prow * kHeads + hd) * kDv + 64 * wv + 4 * g;
+            float *po = a.ws_chunk_o + (prow * kHeads + hd) * kDv + 64 * wv + 4 * ge;
 #pragma unroll
             for (int db = 0; db < 4; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = acc[tb][db];
         }
@@ -1687,7 +1795,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
 }
 
 template <int F>
-constexpr int main_lds = kDecLds > chunk_lds<F> ? kDecLds : chunk_lds<F>;
+constexpr int dec_lds = has_eight<F> ? kDec8Lds : kDecLds;
+template <int F>
+constexpr int main_lds = dec_lds<F> > chunk_lds<F> ? dec_lds<F> : chunk_lds<F>;
 
 // Persistent workgroups (one per CU) take work items from two counters in
 // the workspace, one per queue: the chunk items (largest blocks first) and
@@ -1723,7 +1833,7 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attention_kernel(AttnArgs a) 
             }
         }
         else
-            decode_wg<F>(a, item - a.n_chunk_items, smem, s_pages, s_seg, s_gbar);
+            decode_item<F>(a, item - a.n_chunk_items, smem, s_pages, s_seg, s_gbar);
         TRACE(7);
         int grid = a.grid;
         asm volatile("" : "+s"(grid));  // (computed again per item: kept across the items it would take registers from their loops)
@@ -1842,7 +1952,6 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 }
 
 #include "cache_append.h"
-#include "cache_attend.h"
 
 }  // namespace
 
@@ -1907,12 +2016,15 @@ hipError_t launch_append8(const Append8Args &a, hipStream_t s) {
 hipError_t launch_attention(const AttnArgs &a, hipStream_t s) {
     const int grid = a.grid;
     if (grid == 0) return hipSuccess;
-    if (a.kv8 != nullptr)
-        hipLaunchKernelGGL(rows8_kernel, dim3(a.num_rows), dim3(kThreads), 0, s, a);
-    else if (a.band.window > 0)
-        hipLaunchKernelGGL(attention_kernel<kWindow>, dim3(grid), dim3(kAttnThreads), 0, s, a);
+    const dim3 wgs(grid), threads(kAttnThreads);
+    if (a.kv8 == nullptr && a.band.window == 0)
+        hipLaunchKernelGGL(attention_kernel<kPlain>, wgs, threads, 0, s, a);
+    else if (a.kv8 == nullptr)
+        hipLaunchKernelGGL(attention_kernel<kWindow>, wgs, threads, 0, s, a);
+    else if (a.band.window == 0)
+        hipLaunchKernelGGL(attention_kernel<kEight>, wgs, threads, 0, s, a);
     else
-        hipLaunchKernelGGL(attention_kernel<kPlain>, dim3(grid), dim3(kAttnThreads), 0, s, a);
+        hipLaunchKernelGGL((attention_kernel<kEight | kWindow>), wgs, threads, 0, s, a);
     return hipGetLastError();
 }
 
@@ -1930,7 +2042,7 @@ hipError_t launch_combine(const AttnArgs &a, hipStream_t s) {
         (long long)merge_dec_wgs(a) + (a.ws_chunk_o != nullptr ? (long long)a.n_split_chunk_rows * a.chunk_merge_wgs : 0);
     if (grid_ll > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const int grid = (int)grid_ll;
-    if (grid == 0 || a.kv8 != nullptr) return hipSuccess;
+    if (grid == 0) return hipSuccess;
     if (a.band.window > 0)
         launch_merge<kWindow>(a, grid, s);
     else
