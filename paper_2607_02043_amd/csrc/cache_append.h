@@ -54,15 +54,10 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendArgs a, dou
 // smallest integer in [kMinExp8, kMaxExp8] for which amax 2^-E <= 448 = 1.75 2^8.
 // amax = m 2^e with m in [1, 2) gives E = e - 8, one more if m > 1.75, which is
 // when 0x1fffff added to the bits carries into the exponent field.
-constexpr int kMinExp8 = -100, kMaxExp8 = 120;
 __device__ __forceinline__ int block_exponent(float amax) {
     const int e = (int)((__float_as_uint(amax) + 0x1fffffu) >> 23) - 127 - 8;
     return min(max(e, kMinExp8), kMaxExp8);
 }
-__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
-// The exponent of a stored scale (bf16 bits of a power of two).
-__device__ __forceinline__ int scale_exponent(uint32_t bf16) { return (int)((bf16 >> 7) & 0xff) - 127; }
-
 // |x|, and 0 for NaN and infinities, which do not count for a scale.
 __device__ __forceinline__ float finite_abs(float x) {
     const float v = fabsf(x);
@@ -157,10 +152,10 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
             if (e[k] == was[k]) continue;
             uint32_t *const w = reinterpret_cast<uint32_t *>(blk) + u;
             const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)*w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)*w, true);
-            *w = pack_e4m3(lo[0], lo[1], hi[0], hi[1], pow2f(max(was[k] - e[k], -126)));
+            *w = pack_e4m3(lo[0], lo[1], hi[0], hi[1], exp2_bits(max(was[k] - e[k], -126)));
         }
     }
-    const float sc = pow2f(-e[0]), sr = pow2f(-e[1]);
+    const float sc = exp2_bits(-e[0]), sr = exp2_bits(-e[1]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (4 * i + wv >= n) break;

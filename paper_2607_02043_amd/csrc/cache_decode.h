@@ -2,107 +2,35 @@
 // mla_kernels.hip (its helpers and namespace).
 #pragma once
 
-// Index of the pair of scales (4 bytes) of a key in a pool page.
-__device__ __forceinline__ size_t scale_entry(const AttnArgs &a, int page, int key) {
-    return (size_t)page * (a.page_size / kBlock8) + (size_t)((key & (a.page_size - 1)) / kBlock8);
-}
-
-// Eight e4m3 codes (two words) times a power of two as bf16: exact.
-__device__ __forceinline__ u32x4 bf16_of_e4m3x8(uint32_t w0, uint32_t w1, float scale) {
-    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true))};
-}
-
-// Transposing LDS read of 8-bit elements: inside each 16-lane group, lane i receives
-// element (i & 7) of the 8 bytes read by lane 2 j + (i >> 3), j = 0..7: of the 8
-// rows of 16 that two lanes each read, lane i gets column i.
-__device__ __forceinline__ u32x2 lds_read_tr8(const char *p) {
-    typedef int i32x2 __attribute__((ext_vector_type(2)));
-    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(p));
-    return __builtin_bit_cast(u32x2, v);
-}
-
-// NaN codes (0x7f, 0xff) of four to zero.
-__device__ __forceinline__ uint32_t finite_e4m3x4(uint32_t w) {
-    const uint32_t nan = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bit 7 of every NaN byte
-    return w & ~((nan >> 7) * 0xffu);
-}
-
-// A tile in LDS: 32 keys of 36 16-byte pieces, row-major; piece positions are
-// xor-swizzled inside aligned groups of four.  Rows are 9 x 64 bytes, so four
-// consecutive keys cover the 64 banks at one piece: bits 2 and 3 of the key spread
-// the 16 keys of a score operand, bit 4 the two key halves of a value operand.
-constexpr int kPieces8 = kDqk / 16;  // 36
-__device__ __forceinline__ int swz8(int k) { return ((k >> 2) & 3) ^ ((k >> 3) & 2); }
-__device__ __forceinline__ int tile8_off(int k, int c) { return (k * kPieces8 + (c ^ swz8(k))) * 16; }
-
-// A unit (query block or tile: 18 rounds of 1 KB) takes five DMA instructions of
-// each wave, so that what is in flight can be counted: rounds wv, wv + 4, ..; the
-// fifth of waves 2 and 3 loads the scales of key half wv - 2 (of a query block:
-// their first round again).
-constexpr int kDma8 = 5;
-__device__ __forceinline__ void dma8_offsets(int wv, int lane, uint32_t (&off)[3]) {
-#pragma unroll
-    for (int w = 0; w < 3; ++w) off[w] = 0;
-#pragma unroll
-    for (int i = 0; i < kDma8; ++i) {
-        const int u = (i * 4 + wv) * 64 + lane, kk = u / kPieces8, c = (u - kk * kPieces8) ^ swz8(kk);
-        if (u < kDecKeys * kPieces8) off[i / 2] |= (uint32_t)(kk * kDqk + c * 16) << (16 * (i & 1));
-    }
-}
-// Until only the DMAs of the last `units` units are in flight.  (Loads complete in
-// order; a store in between only makes the wait longer.)
-__device__ __forceinline__ void wait_dma8(int units) {
-    if (units >= 2)
-        asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
-    else if (units == 1)
-        asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
-    else
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-}
-
+// DMA of one stream unit of a group: a tile with its scales, or (t < 0) a query
+// block, 18 rounds too (waves 2 and 3 take their first one twice, for the count).
 template <int F>
 __device__ __forceinline__ void issue_unit8(const AttnArgs &a, const DecSeg &sg, int t, const int *s_pages, uint32_t slot,
-                                            uint32_t scale_slot, int wv, int lane, const uint32_t (&off)[3]) {
-    const auto lds = [&](int i) { return __builtin_amdgcn_readfirstlane(slot + (i * 4 + wv) * 1024); };
-    asm volatile("" : "+v"(lane));  // (nothing of the rare paths is kept across the units)
+                                            uint32_t scale_slot, int wv, int lane) {
+    asm volatile("" : "+v"(lane));  // (no address is kept across the units)
     if (t < 0) {
         const char *qb = reinterpret_cast<const char *>(a.q + (size_t)sg.row * kHeads * kDqk) + lane * 16;
 #pragma unroll
         for (int i = 0; i < kDma8; ++i) {
-            const int j = i == 4 && wv >= 2 ? 0 : i;
-            lds_dma16(qb + (j * 4 + wv) * 1024, lds(j));
+            const int j = (i == 4 && wv >= 2 ? 0 : i) * 4 + wv;
+            lds_dma16(qb + j * 1024, __builtin_amdgcn_readfirstlane(slot + j * 1024));
         }
         return;
     }
     const SegKeys<has_window<F>> sk(a, sg);
     const int kbase = sk.key(t * kDecKeys);
-    const auto page_of = [&](int key) { return s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)]; };
+    const auto slot_of = [&](int key) {  // pool slot
+        const int k = min(key, sg.p);
+        return (size_t)s_pages[min(sk.window_entry(sg, k, a.log2_page), kPageWindow - 1)] * a.page_size + (k & (a.page_size - 1));
+    };
     if (a.page_size >= kDecKeys && kbase + kDecKeys - 1 <= sg.p) {
-        const int page = __builtin_amdgcn_readfirstlane(page_of(kbase));
-        const uint8_t *src = a.kv8 + ((size_t)page * a.page_size + (kbase & (a.page_size - 1))) * kDqk;
-#pragma unroll
-        for (int i = 0; i < kDma8; ++i)
-            if (i < 4 || wv < 2) lds_dma16_sbase(src, (off[i / 2] >> (16 * (i & 1))) & 0xffffu, lds(i));
+        const int page = s_pages[min(sk.window_entry(sg, kbase, a.log2_page), kPageWindow - 1)];
+        const size_t first = (size_t)__builtin_amdgcn_readfirstlane(page) * a.page_size + (kbase & (a.page_size - 1));
+        dma_tile8(a.kv8 + first * kDqk, tile8_key(wv, lane) * kDqk + tile8_dims(wv, lane), slot, wv);
     } else {
-#pragma unroll
-        for (int i = 0; i < kDma8; ++i) {
-            if (i == 4 && wv >= 2) break;
-            const int u = (i * 4 + wv) * 64 + lane, kk = u / kPieces8, c = (u - kk * kPieces8) ^ swz8(kk);
-            const int key = min(kbase + kk, sg.p);
-            lds_dma16(a.kv8 + ((size_t)page_of(key) * a.page_size + (key & (a.page_size - 1))) * kDqk + c * 16, lds(i));
-        }
+        dma_tile8(a.kv8 + slot_of(kbase + tile8_key(wv, lane)) * kDqk + tile8_dims(wv, lane), slot, wv);
     }
-    if (wv >= 2) {
-        const int key = min(kbase + 16 * (wv - 2), sg.p);
-        const size_t entry = scale_entry(a, page_of(key), key);
-        if (lane == 0)
-            lds_dma16(reinterpret_cast<const char *>(a.kv8_scales) + (entry * 4 & ~size_t(15)),
-                      __builtin_amdgcn_readfirstlane(scale_slot + 16 * (wv - 2)));
-    }
+    if (wv >= 2) dma_scales8(a, slot_of(kbase + 16 * (wv - 2)), scale_slot + 16 * (wv - 2), lane);
 }
 
 // decode_wg over the 8-bit cache.  Half the bytes a key: HBM-bound at 578 B a key,
@@ -129,8 +57,6 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     if (tid < 2) s_gbar[tid] = 0;
     TRACE(1);
     __syncthreads();
-    uint32_t off[3];
-    dma8_offsets(gw, lane, off);
     char *const slots = smem + grp * kDec8GroupBytes;
     char *const s_X = smem + 2 * kDec8GroupBytes + grp * kDec8XBytes;
     char *const s_scale = smem + 2 * (kDec8GroupBytes + kDec8XBytes) + grp * kDec8ScaleBytes;
@@ -139,7 +65,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     if (n_units > 0) prod.sg = load_seg(s_seg, 0);
     Cursor cons = prod;
     const auto issue = [&](int u) {
-        issue_unit8<F>(a, prod.sg, prod.t, s_pages, ring + (u % kDec8Ring) * kDec8TileBytes, scales + (u % kDec8Ring) * 32, gw, lane, off);
+        issue_unit8<F>(a, prod.sg, prod.t, s_pages, ring + (u % kDec8Ring) * kTile8Bytes, scales + (u % kDec8Ring) * 32, gw, lane);
         advance(prod, s_seg, nseg);
     };
     if (n_units > 0) {
@@ -185,7 +111,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         wait_dma8(min(2, n_units - 1 - u));        // unit u
         group_barrier(gbar, epoch, a.spin_limit);  // landed for all four waves; slot (u + 3) % 4 is free
         if (u + 3 < n_units) issue(u + 3);
-        const char *slot = slots + (u % kDec8Ring) * kDec8TileBytes;
+        const char *slot = slots + (u % kDec8Ring) * kTile8Bytes;
         if (cons.t < 0) {  // a new request: its query block
             const char *q = slot + h * kRowBytes;
 #pragma unroll
@@ -207,7 +133,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         for (int kt = 0; kt < 2; ++kt) {
             const int key = min(kbase + 16 * kt, sg.p);
             const int pg = a.page_size >= 64 ? 0 : s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)];
-            const uint32_t wd = *reinterpret_cast<const uint32_t *>(s_scale + (u % kDec8Ring) * 32 + 16 * kt + 4 * (scale_entry(a, pg, key) & 3));
+            const uint32_t wd = *reinterpret_cast<const uint32_t *>(s_scale + (u % kDec8Ring) * 32 + 16 * kt + 4 * scale_piece8(a, pg, key));
             // (a half that no row sees may have anything for a scale: 0 times it would be NaN)
             sc[kt] = (wd & 0x7f80u) == 0x7f80u ? 0.f : __uint_as_float(wd << 16);
             sr[kt] = __uint_as_float(wd & 0xffff0000u);
@@ -217,8 +143,8 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
             const float kc = (gw & 1) ? sc[1] : sc[0], kr = hf ? ((gw & 1) ? sr[1] : sr[0]) : kc;
             u32x4 av[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) av[j] = *reinterpret_cast<const u32x4 *>(slot + tile8_off(kq, gbase / 16 + 4 * j + g));
-            const u32x2 as = *reinterpret_cast<const u32x2 *>(slot + tile8_off(kq, sbase / 16 + (g >> 1)) + 8 * (g & 1));
+            for (int j = 0; j < 4; ++j) av[j] = *reinterpret_cast<const u32x4 *>(slot + kQuad8 * (gbase / 64 + j) + tile8_off(kq, g));
+            const u32x2 as = *reinterpret_cast<const u32x2 *>(slot + kQuad8 * 4 + tile8_off(kq, 2 * hf + (g >> 1)) + 8 * (g & 1));
             f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -232,7 +158,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         // values of this wave's 128 dims, before the scores are complete
         u32x2 vraw[8];
 #pragma unroll
-        for (int mt2 = 0; mt2 < 8; ++mt2) vraw[mt2] = lds_read_tr8(slot + tile8_off(tr_key, gw * 8 + mt2) + 8 * (lane & 1));
+        for (int mt2 = 0; mt2 < 8; ++mt2) vraw[mt2] = lds_read_tr8(slot + kQuad8 * (2 * gw + (mt2 >> 2)) + tile8_off(tr_key, mt2 & 3) + 8 * (lane & 1));
         u32x4 vop[8];
 #pragma unroll
         for (int mt2 = 0; mt2 < 8; ++mt2) vop[mt2] = bf16_of_e4m3x8(vraw[mt2][0], vraw[mt2][1], 1.f);
@@ -247,7 +173,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         if (any_not_finite(x)) {
 #pragma unroll
             for (int mt2 = 0; mt2 < 8; ++mt2) {
-                const u32x2 raw = lds_read_tr8(slot + tile8_off(tr_key, gw * 8 + mt2) + 8 * (lane & 1));
+                const u32x2 raw = lds_read_tr8(slot + kQuad8 * (2 * gw + (mt2 >> 2)) + tile8_off(tr_key, mt2 & 3) + 8 * (lane & 1));
                 vop[mt2] = bf16_of_e4m3x8(finite_e4m3x4(raw[0]), finite_e4m3x4(raw[1]), 1.f);
             }
         }

@@ -1,0 +1,94 @@
+// Tiles of the 8-bit cache (include/mla_cache.h): device code, part of
+// mla_kernels.hip (its helpers and namespace).
+#pragma once
+
+// Scales are powers of two, handled as exponents where that is cheaper.
+constexpr int kMinExp8 = -100, kMaxExp8 = 120;
+__device__ __forceinline__ float exp2_bits(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+// The exponent of a stored scale (bf16 bits of a power of two; 128 if it is no number).
+__device__ __forceinline__ int scale_exponent(uint32_t bf16) { return (int)((bf16 >> 7) & 0xff) - 127; }
+
+// The scales of a block of 16 tokens are 4 bytes, loaded in aligned pieces of 16:
+// which of its four entries a key's is (the page matters below 64 tokens a page only).
+__device__ __forceinline__ int scale_piece8(const AttnArgs &a, int page, int key) {
+    return (page * (a.page_size / kBlock8) + (key & (a.page_size - 1)) / kBlock8) & 3;
+}
+
+// Eight e4m3 codes (two words) times a power of two as bf16: exact.
+__device__ __forceinline__ u32x4 bf16_of_e4m3x8(uint32_t w0, uint32_t w1, float scale) {
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true))};
+}
+// The same as fp16, the two words with scales of their own (rounded to nearest; exact unless below 2^-24).
+__device__ __forceinline__ u32x4 f16_of_e4m3x8(uint32_t w0, uint32_t w1, float s0, float s1) {
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, s0, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, s0, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, s1, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, s1, true))};
+}
+
+// Transposing LDS read of 8-bit elements: inside each 16-lane group, lane i receives
+// element (i & 7) of the 8 bytes read by lane 2 j + (i >> 3), j = 0..7: of the 8
+// rows of 16 that two lanes each read, lane i gets column i.
+__device__ __forceinline__ u32x2 lds_read_tr8(const char *p) {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(p));
+    return __builtin_bit_cast(u32x2, v);
+}
+
+// NaN codes (0x7f, 0xff) of four to zero.
+__device__ __forceinline__ uint32_t finite_e4m3x4(uint32_t w) {
+    const uint32_t nan = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bit 7 of every NaN byte
+    return w & ~((nan >> 7) * 0xffu);
+}
+
+// A tile in LDS: nine quads of 64 dims, each 32 keys of four 16-byte pieces.  Four
+// consecutive keys cover the 64 banks at one piece; pieces are xor-swizzled so that
+// bits 2 and 3 of the key spread the 16 keys of a score operand, and bit 4 the two
+// key halves of a value operand.  Piece p of quad 0 of key k is at tile8_off(k, p).
+constexpr int kQuad8 = kKeysPerTile * 64;  // 2048 bytes
+__device__ __forceinline__ int swz8(int k) { return ((k >> 2) & 3) ^ ((k >> 3) & 2); }
+__device__ __forceinline__ int tile8_off(int k, int p) { return 64 * k + 16 * (p ^ swz8(k)); }
+
+// DMA of a tile (18 rounds of 1 KB) by four waves, five instructions each, so that
+// what is in flight can be counted.  Round j is keys 16 (j & 1) .. + 15 of quad j / 2;
+// wave w takes rounds w, w + 4, ..: a lane has one key, and its source moves by two
+// quads a round.  The fifth instruction of waves 2 and 3 loads the scales of key half
+// w - 2.  (The instruction offset moves source and destination alike.)
+constexpr int kDma8 = 5;
+__device__ __forceinline__ int tile8_key(int w, int lane) { return 16 * (w & 1) + (lane >> 2); }
+__device__ __forceinline__ int tile8_dims(int w, int lane) {
+    return 64 * (w >> 1) + 16 * ((lane & 3) ^ swz8(tile8_key(w, lane)));
+}
+__device__ __forceinline__ void dma_tile8(const uint8_t *src, uint32_t voff, uint32_t slot, int w) {  // uniform src, a page's keys
+    const uint32_t dst = slot + 1024 * w;
+#define MLA_DMA8(i) lds_dma16_sbase_imm<128 * (i)>(src, voff, __builtin_amdgcn_readfirstlane(dst + 4096 * (i)))
+    MLA_DMA8(0); MLA_DMA8(1); MLA_DMA8(2); MLA_DMA8(3);
+    if (w < 2) MLA_DMA8(4);
+#undef MLA_DMA8
+}
+__device__ __forceinline__ void dma_tile8(const uint8_t *src, uint32_t slot, int w) {  // src per lane
+    const uint32_t dst = slot + 1024 * w;
+#define MLA_DMA8(i) lds_dma16_imm<128 * (i)>(src, __builtin_amdgcn_readfirstlane(dst + 4096 * (i)))
+    MLA_DMA8(0); MLA_DMA8(1); MLA_DMA8(2); MLA_DMA8(3);
+    if (w < 2) MLA_DMA8(4);
+#undef MLA_DMA8
+}
+// The piece with the scales of a pool slot's block, to 16 bytes at `dst` (one lane; counts as an instruction).
+__device__ __forceinline__ void dma_scales8(const AttnArgs &a, size_t pool_slot, uint32_t dst, int lane) {
+    const char *src = reinterpret_cast<const char *>(a.kv8_scales) + (pool_slot / kBlock8 * 4 & ~size_t(15));
+    if (lane == 0) lds_dma16(src, __builtin_amdgcn_readfirstlane(dst));
+}
+// Until only the DMAs of the last `units` units are in flight.  (Loads complete in
+// order; a store in between only makes the wait longer.)
+__device__ __forceinline__ void wait_dma8(int units) {
+    if (units >= 2)
+        asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+    else if (units == 1)
+        asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+    else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}

@@ -60,13 +60,13 @@ constexpr int kDecGroupBytes = kDecRing * kDecTileBytes;
 constexpr int kDecXBytes = 4 * kHeads * 20 * 4;               // partial score blocks of a group
 constexpr int kDecLds = 2 * kDecGroupBytes + 2 * kDecXBytes;  // two groups: rings, then score blocks
 // chunk path
-constexpr int kDec8Ring = 4;                            // over the 8-bit cache: ring slots, bytes of one
-constexpr int kDec8TileBytes = kDecKeys * kDqk;         // 18432, also a query block's
-constexpr int kDec8GroupBytes = kDec8Ring * kDec8TileBytes;
+constexpr int kTile8Bytes = kKeysPerTile * kDqk;        // 18432: a tile of the 8-bit cache, also a query block
+constexpr int kDec8Ring = 4;                            // its decode path: ring slots of each wave group
+constexpr int kDec8GroupBytes = kDec8Ring * kTile8Bytes;
 constexpr int kDec8XBytes = 4 * 64 * 16;                // partial score blocks of a group
 constexpr int kDec8ScaleBytes = kDec8Ring * 32;         // two 16-byte pieces of the scales a tile
 constexpr int kDec8Lds = 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes);
-static_assert(kDec8TileBytes == kHeads * kRowBytes, "a query block fills a slot");
+static_assert(kTile8Bytes == kHeads * kRowBytes, "a query block fills a slot");
 constexpr int kChunkKeys = kKeysPerTile;  // 32
 constexpr int kChunkTileBytes = kChunkKeys * kRowBytes;  // 36864
 
@@ -391,6 +391,27 @@ __device__ __forceinline__ void lds_dma16_sbase(const void *sbase, uint32_t voff
         : "memory");
 }
 
+// The instruction offset OFF moves the LDS destination as well as the
+// global source, so M0 is set to lds_base - OFF.
+template <int OFF>
+__device__ __forceinline__ void lds_dma16_imm(const void *gsrc, uint32_t lds_base) {
+    asm volatile(
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, off offset:%2\n\t"
+        :
+        : "{m0}"(lds_base - OFF), "v"(gsrc), "i"(OFF)
+        : "memory");
+}
+template <int OFF>
+__device__ __forceinline__ void lds_dma16_sbase_imm(const void *sbase, uint32_t voff, uint32_t lds_base) {
+    asm volatile(
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %0, %1 offset:%3\n\t"
+        :
+        : "v"(voff), "s"(sbase), "{m0}"(lds_base - OFF), "i"(OFF)
+        : "memory");
+}
+
 // Fused append: copy n new latents (rows row0 .. of a.new_kv, keys key0 .. of
 // request r) into their cache slots; the whole workgroup takes part.  Slots
 // with a page id outside the pool are skipped.
@@ -564,6 +585,8 @@ __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
         store_merged(a, row, hh, lane, o, M, den);
     }
 }
+
+#include "cache_tile.h"
 
 // ------------------------------------------------------------ decode path
 // The 32-key tiles of all decode requests, request after request, form one
@@ -1249,20 +1272,22 @@ constexpr int kCT = kChunkBlockTokens;                 // 8 tokens per item, one
 constexpr int kQSteps = kDqk / 32;                     // 18 query operands of 32 dims
 // The first of them stay in registers, the others (the rope ones) in LDS: with a
 // window the masks take the four registers of one more, and over the 8-bit cache
-// the conversion of the next tile.
+// the conversion of the keys.
 template <int F>
 constexpr int q_reg_steps = F == kPlain ? 16 : 15;
 constexpr int kChunkRing = 3;
 constexpr int kPTile = kCT * 64 * 16;                  // fp16 P of one tile: [token][lane] 16 bytes
-constexpr int kChunk8Raw = 2 * kChunkTileBytes;      // 8-bit cache: two converted tiles, then two raw ones (half the size)
-constexpr int kChunk8RawBytes = kChunkKeys * kDqk;   // 18432
-static_assert(kChunk8Raw + 2 * kChunk8RawBytes == kChunkRing * kChunkTileBytes, "both rings take the same space");
-constexpr int kChunk8ScaleBytes = 2 * 8 * 16;        // [raw slot][wave]: the piece of the scales that its rows need
+template <int F>
+constexpr int chunk_tile_bytes = has_eight<F> ? kTile8Bytes : kChunkTileBytes;
+// Forms other than the plain one raise a row's reference max as they go (see softmax): the factors [P buffer][token][head],
+// the tile that each was raised at [P buffer][token]; the 8-bit cache's scales, two 16-byte pieces a ring slot.
+constexpr int kRaiseBytes = 2 * kCT * kHeads * 4 + 2 * kCT * 4;
+constexpr int kChunk8ScaleBytes = kChunkRing * 32;
 template <int F>
 constexpr int q_lds_bytes = (kQSteps - q_reg_steps<F>) * kCT * 64 * 16;  // query operands in LDS: [step][token][lane]
 template <int F>
-constexpr int chunk_lds = kChunkRing * kChunkTileBytes + 2 * kPTile + q_lds_bytes<F> + 2 * kCT * kHeads * 4 + 16 +
-                          (has_eight<F> ? kChunk8ScaleBytes : 0);
+constexpr int chunk_lds = kChunkRing * chunk_tile_bytes<F> + 2 * kPTile + q_lds_bytes<F> + 2 * kCT * kHeads * 4 + 16 +
+                          (F != kPlain ? kRaiseBytes + kChunk8ScaleBytes : 0);
 // Largest exponent (log2 units) a probability may take against the reference
 // max: 2^15 stays inside fp16.
 constexpr float kMaxPExp = 15.f;
@@ -1276,27 +1301,6 @@ constexpr float kMaxPExp = 15.f;
 // row-major tile (conflict-free).  Round j fills octet j >> 2, keys
 // 8 (j & 3) .. + 7: lane l loads chunk 8 (j >> 2) + ((l & 7) ^ ((l >> 3) & 7))
 // of key 8 (j & 3) + (l >> 3).
-// The instruction offset OFF moves the LDS destination as well as the
-// global source, so M0 is set to lds_base - OFF.
-template <int OFF>
-__device__ __forceinline__ void lds_dma16_imm(const void *gsrc, uint32_t lds_base) {
-    asm volatile(
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, off offset:%2\n\t"
-        :
-        : "{m0}"(lds_base - OFF), "v"(gsrc), "i"(OFF)
-        : "memory");
-}
-template <int OFF>
-__device__ __forceinline__ void lds_dma16_sbase_imm(const void *sbase, uint32_t voff, uint32_t lds_base) {
-    asm volatile(
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %0, %1 offset:%3\n\t"
-        :
-        : "v"(voff), "s"(sbase), "{m0}"(lds_base - OFF), "i"(OFF)
-        : "memory");
-}
-
 // Keys and pages of a chunk item's range, as SegKeys for a decode segment: tile t
 // starts at key base + 32 t, `skip` keys further from tile `gap` on.
 template <bool WINDOW>
@@ -1332,6 +1336,9 @@ struct ChunkKeys<true> {
 //           more than 2^15, the pass still runs to the end and its products
 //           are discarded;
 //   exact   then the item runs again against the exact max.
+// (Scores of a standard deviation of 2.6 take the second pass in most items of
+// 8192 keys.  The forms of mla_cache.h have the main pass alone and raise the
+// reference in it: 2048 rows over 8192 keys of such scores RAISE_FIGURES.)
 
 // Returns true when the main pass was abandoned: the caller then runs the
 // item again with exact = true (the exact maxima wait in LDS).
@@ -1356,7 +1363,8 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     if constexpr (F != kPlain) k_end = ck.tile((it.k1 - 1 - it.k0) / kChunkKeys) + (it.k1 - 1 - it.k0) % kChunkKeys + 1;
     // This wave's token (an idle token repeats the last one; its results are
     // not stored).  Query operands: lane l holds dims 32 s + 8 g .. + 7 of
-    // head hd, s = 0..17.
+    // head hd, s = 0..17 (over the 8-bit cache 64 (s / 2) + 16 g + 8 (s & 1) .. + 7:
+    // a lane's 16-byte piece of a key feeds two steps).
     const int tk = min(wv, nt - 1);
     // Page ids (needed first, by the tile DMAs), then the queries go out, and
     // the DMAs follow while the queries are still on their way: one round trip
@@ -1367,13 +1375,14 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     if (tid < min(npages, kPageWindow) && ck.logical_page(tid) < a.max_pages) pg = a.bt[(size_t)r * a.max_pages + ck.logical_page(tid)];
     constexpr int kQRegSteps = q_reg_steps<F>;
     u32x4 qreg[kQRegSteps], qr[kQSteps - kQRegSteps];
-    char *const s_q = smem + kChunkRing * kChunkTileBytes + 2 * kPTile;  // rope query operands
+    char *const s_q = smem + kChunkRing * chunk_tile_bytes<F> + 2 * kPTile;  // rope query operands
     {
-        const uint16_t *qp = a.q + ((size_t)(it.row0 + it.i0 + tk) * kHeads + hd) * kDqk + 8 * g;
+        const uint16_t *qp = a.q + ((size_t)(it.row0 + it.i0 + tk) * kHeads + hd) * kDqk + (has_eight<F> ? 16 : 8) * g;
+        const auto dim = [](int s) { return has_eight<F> ? 64 * (s / 2) + 8 * (s & 1) : 32 * s; };
 #pragma unroll
-        for (int s = 0; s < kQRegSteps; ++s) qreg[s] = *reinterpret_cast<const u32x4 *>(qp + 32 * s);
+        for (int s = 0; s < kQRegSteps; ++s) qreg[s] = *reinterpret_cast<const u32x4 *>(qp + dim(s));
 #pragma unroll
-        for (int s = kQRegSteps; s < kQSteps; ++s) qr[s - kQRegSteps] = *reinterpret_cast<const u32x4 *>(qp + 32 * s);
+        for (int s = kQRegSteps; s < kQSteps; ++s) qr[s - kQRegSteps] = *reinterpret_cast<const u32x4 *>(qp + dim(s));
     }
     if (tid < min(npages, kPageWindow)) {
         const bool ok = (unsigned)pg < (unsigned)a.num_pages;
@@ -1384,10 +1393,13 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     TRACE_VAL(8, 1000000ull * 1 + ntiles);
 
     const uint32_t ring = lds_addr(smem);
-    char *const s_pbuf = smem + kChunkRing * kChunkTileBytes;           // [2][token][lane] 16 bytes
+    char *const s_pbuf = smem + kChunkRing * chunk_tile_bytes<F>;       // [2][token][lane] 16 bytes
     float *const s_l = reinterpret_cast<float *>(s_q + q_lds_bytes<F>);     // [token][head] row sums
     float *const s_mx = s_l + kCT * kHeads;                            // [token][head] exact maxima
     int *const s_abort = reinterpret_cast<int *>(s_mx + kCT * kHeads);
+    [[maybe_unused]] float *const s_raise = reinterpret_cast<float *>(s_abort + 4);                          // [P buffer][token][head]
+    [[maybe_unused]] int *const s_raised = reinterpret_cast<int *>(s_raise + 2 * kCT * kHeads);              // [P buffer][token]
+    [[maybe_unused]] char *const s_scale = reinterpret_cast<char *>(s_raised + 2 * kCT);                     // [ring slot] 32 bytes
 
     // Causal limit of this wave's token (absolute key index, clipped to the
     // item's key range); wave-uniform.
@@ -1462,61 +1474,108 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
     };
 
-    // Over the 8-bit cache a wave loads and converts the same 16-byte pieces of every tile: round r of wave wv is dims
-    // 64 (wv / 2 + 4 r) .. + 63 of the 16 keys of half wv & 1, four lanes a key (r = 2, the rope dims, on waves 0 and 1
-    // alone).  Raw tiles pass through LDS, so a load in flight holds no registers; a lane then takes its 16 codes out, converts them
-    // with their block's scale (exact) and writes two chunks of the bf16 tile.
-    // (Lanes are opaque in both: their addresses, kept across the tiles, would be kept in scratch.)
-    [[maybe_unused]] const int rounds8 = wv < 2 ? 3 : 2;
-    [[maybe_unused]] char *const s_scale8 = reinterpret_cast<char *>(s_abort) + 16 + 16 * wv;  // + 128 raw slot
-    [[maybe_unused]] auto issue8 = [&](int t) {
-        const int kbase = ck.tile(t);
-        const uint32_t dst = ring + kChunk8Raw + (t & 1) * kChunk8RawBytes + wv * 1024;
-        const int ln = opaque_lane(), key8 = 16 * (wv & 1) + (ln >> 2), part = 16 * (ln & 3) + 64 * (wv >> 1);
+    // the same over the 8-bit cache: five DMAs of each of the four waves, the scales among them
+    [[maybe_unused]] auto issue8 = [&](int t, int slot, int page) {
+        const int kbase = ck.tile(t), ln = opaque_lane();
+        const uint32_t dst = ring + slot * kTile8Bytes;
+        const auto slot_of = [&](int key) {  // pool slot
+            const int k = min(key, k_end - 1);
+            return (size_t)s_pages[min(ck.entry(k), kPageWindow - 1)] * a.page_size + (k & (a.page_size - 1));
+        };
         if (in_page && kbase + kChunkKeys <= k_end) {
-            const uint8_t *src = a.kv8 + ((size_t)__builtin_amdgcn_readfirstlane(page_of(t)) * a.page_size + (kbase & (a.page_size - 1))) * kDqk;
-            const uint32_t voff = key8 * kDqk + part;
-            lds_dma16_sbase_imm<0>(src, voff, __builtin_amdgcn_readfirstlane(dst));
-            lds_dma16_sbase_imm<256>(src, voff, __builtin_amdgcn_readfirstlane(dst + 8192));
-            if (rounds8 == 3) lds_dma16_sbase_imm<512>(src, voff, __builtin_amdgcn_readfirstlane(dst + 16384));
+            const size_t first = (size_t)__builtin_amdgcn_readfirstlane(page) * a.page_size + (kbase & (a.page_size - 1));
+            dma_tile8(a.kv8 + first * kDqk, tile8_key(dw, ln) * kDqk + tile8_dims(dw, ln), dst, dw);
         } else {
-            const int key = min(kbase + key8, k_end - 1);
-            const int pg = s_pages[min(ck.entry(key), kPageWindow - 1)];
-            const uint8_t *src = a.kv8 + ((size_t)pg * a.page_size + (key & (a.page_size - 1))) * kDqk + part;
-            lds_dma16_imm<0>(src, __builtin_amdgcn_readfirstlane(dst));
-            lds_dma16_imm<256>(src, __builtin_amdgcn_readfirstlane(dst + 8192));
-            if (rounds8 == 3) lds_dma16_imm<512>(src, __builtin_amdgcn_readfirstlane(dst + 16384));
+            dma_tile8(a.kv8 + slot_of(kbase + tile8_key(dw, ln)) * kDqk + tile8_dims(dw, ln), dst, dw);
         }
-        const uint32_t sdst = lds_addr(s_scale8) + 128 * (t & 1);
-        const size_t entry = scale_entry(a, s_pages[min(ck.entry(min(kbase + 16 * (wv & 1), k_end - 1)), kPageWindow - 1)],
-                                         min(kbase + 16 * (wv & 1), k_end - 1));
-        if (lane == 0) lds_dma16(reinterpret_cast<const char *>(a.kv8_scales) + (entry * 4 & ~size_t(15)), __builtin_amdgcn_readfirstlane(sdst));
+        if (dw >= 2) dma_scales8(a, slot_of(kbase + 16 * (dw - 2)), lds_addr(s_scale) + slot * 32 + 16 * (dw - 2), ln);
     };
-    // the raw tile t (this wave's part, landed) -> bf16 slot t & 1
-    [[maybe_unused]] auto convert8 = [&](int t) {
-        const int key0 = min(ck.tile(t) + 16 * (wv & 1), k_end - 1);
-        const int pg = a.page_size >= 64 ? 0 : s_pages[min(ck.entry(key0), kPageWindow - 1)];
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(s_scale8 + 128 * (t & 1) + 4 * (scale_entry(a, pg, key0) & 3));
-        const float sc = __uint_as_float(w << 16), sr = __uint_as_float(w & 0xffff0000u);
-        const int ln = opaque_lane(), key8 = 16 * (wv & 1) + (ln >> 2);
-        const char *raw = smem + kChunk8Raw + (t & 1) * kChunk8RawBytes + wv * 1024 + ln * 16;
-        char *tile = smem + (t & 1) * kChunkTileBytes + 4096 * (wv >> 1) + 128 * key8;
-        for (int r = 0; r < rounds8; ++r) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(raw + 8192 * r);
-            const float s = r == 2 ? sr : sc;
-            const int c = 2 * (ln & 3);
-            *reinterpret_cast<u32x4 *>(tile + 16384 * r + 16 * (c ^ (key8 & 7))) = bf16_of_e4m3x8(v[0], v[1], s);
-            *reinterpret_cast<u32x4 *>(tile + 16384 * r + 16 * ((c + 1) ^ (key8 & 7))) = bf16_of_e4m3x8(v[2], v[3], s);
-        }
+    // page of tile t, and its DMA into a ring slot
+    auto issue_tile = [&](int t, int slot, int page) {
+        if constexpr (has_eight<F>)
+            issue8(t, slot, page);
+        else
+            issue(t, slot, page);
     };
 
     const bool main_pass = !exact;
-    float m_ref = kNegInf, m_lane = kNegInf, l_run = 0.f;
+    float m_ref = kNegInf, l_run = 0.f;
+    [[maybe_unused]] float m_lane = kNegInf;
+    // 8-bit cache: exponents of the scales of the tile being read, [key half], of the compressed and the rope dims; values are
+    // held relative to 2^v_exp, the accumulators too
+    constexpr int kNoExp = -1000;  // no block read yet
+    [[maybe_unused]] int ec[2] = {0, 0}, er[2] = {0, 0}, v_exp = kNoExp;
     f32x4 acc[kCT][4];  // [token][value block db]
 
+    // Over the 8-bit cache: one 16-byte piece of a key a lane feeds two steps, converted on the way (exactly, scale
+    // included).
+    [[maybe_unused]] auto scores8 = [&](const char *tile, f32x4 (&s)[2]) {
+        s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int D = 2, kGroups = kDqk / 64;  // groups of 64 dims, those whose pieces are in flight
+        u32x4 av[D][2];
+        int kq[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) kq[kb] = tile8_off(16 * kb + hd, g);
+#pragma unroll
+        for (int j = 0; j < D; ++j)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) av[j][kb] = *reinterpret_cast<const u32x4 *>(tile + kq[kb] + kQuad8 * j);
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+            const u32x4 cur[2] = {av[j % D][0], av[j % D][1]};
+            if (j + D < kGroups) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) av[j % D][kb] = *reinterpret_cast<const u32x4 *>(tile + kq[kb] + kQuad8 * (j + D));
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int st = 2 * j + e;
+                u32x4 qb;
+                if (st < kQRegSteps)
+                    qb = qreg[st];
+                else
+                    qb = *reinterpret_cast<const u32x4 *>(s_q + (((st - kQRegSteps) * kCT + wv) * 64 + lane) * 16);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+                    s[kb] = mfma_bf16(bf16_of_e4m3x8(cur[kb][2 * e], cur[kb][2 * e + 1], exp2_bits(j < kGroups - 1 ? ec[kb] : er[kb])), qb, s[kb]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // Scales of tile t in ring slot `slot`: the exponents, and the reference of the values raised (rarely) to what fp16
+    // holds; a key half that no row of the block sees has no say.
+    [[maybe_unused]] auto scales8 = [&](int t, int slot) {
+        const int kbase = ck.tile(t);
+        int most = kNoExp;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int key = min(kbase + 16 * kb, k_end - 1);
+            const int pg = a.page_size >= 64 ? 0 : s_pages[min(ck.entry(key), kPageWindow - 1)];
+            const uint32_t w = __builtin_amdgcn_readfirstlane(
+                *reinterpret_cast<const int *>(s_scale + slot * 32 + 16 * kb + 4 * scale_piece8(a, pg, key)));
+            ec[kb] = scale_exponent(w);
+            er[kb] = scale_exponent(w >> 16);
+            if (ec[kb] <= kMaxExp8 && (!has_window<F> || kbase + 16 * kb < a.band.sinks || kbase + 16 * kb + 15 > it.p + it.i0 - a.band.window))
+                most = max(most, ec[kb]);
+        }
+        if (v_exp == kNoExp) {
+            v_exp = most;
+        } else if (most > v_exp + 7) {  // 448 2^7 = 57344
+            const float f = exp2_bits(max(v_exp - most, -126));
+            v_exp = most;
+#pragma unroll
+            for (int tb = 0; tb < kCT; ++tb)
+#pragma unroll
+                for (int db = 0; db < 4; ++db) acc[tb][db] = acc[tb][db] * f;
+        }
+    };
     // S^T of tile t for this wave's token: lane l, element i of block kb =
     // key 16 kb + 4 g + i of the tile, head hd.  Two accumulation chains.
     auto scores = [&](int slot, f32x4 (&s)[2]) {
+        if constexpr (has_eight<F>) {
+            scores8(smem + __builtin_amdgcn_readfirstlane(slot * kTile8Bytes), s);
+            return;
+        }
         const char *tile = smem + __builtin_amdgcn_readfirstlane(slot * kChunkTileBytes);
         s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
         constexpr int D = 2;  // steps whose K operands are in flight
@@ -1574,13 +1633,21 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     auto softmax = [&](int t, int pbuf, const f32x4 (&s)[2]) {
         float x[8];
         masked(t, s, x);
-        m_lane = lane_max(x, m_lane);
-        if constexpr (has_window<F>) {
-            // a row that saw nothing so far: its reference is the max of the first tile that it sees (with no
-            // probability behind it yet, nothing is rescaled)
-            if (main_pass && __builtin_amdgcn_ballot_w64(m_ref == kNegInf) != 0) {
-                const float m = wave_max16(lane_max(x, kNegInf) * a.scale_log2);
-                m_ref = m_ref == kNegInf ? m : m_ref;
+        if constexpr (F == kPlain) {
+            m_lane = lane_max(x, m_lane);
+        } else {
+            // The reference max is raised as soon as a score exceeds it by more than fp16 holds (also from nothing: rows
+            // may see their first key late); the factor of what is accumulated goes with P to the waves that hold it.
+            const float tm = lane_max(x, kNegInf) * a.scale_log2;
+            if (__builtin_amdgcn_ballot_w64(tm > m_ref + kMaxPExp) != 0) {
+                const float m_new = fmaxf(m_ref, wave_max16(tm));
+                const float f = m_ref == kNegInf ? 0.f : exp2f(m_ref - m_new);
+                l_run *= f;
+                m_ref = m_new;
+                if (t > 0) {
+                    if (g == 0) s_raise[(pbuf * kCT + wv) * kHeads + hd] = f;
+                    if (lane == 0) s_raised[pbuf * kCT + wv] = t;
+                }
             }
         }
         // the scaled score is rounded before the max is subtracted, so the max
@@ -1601,6 +1668,17 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // that only the P reads stand between it and the first product.
     u32x4 av[4];
     auto vload = [&](int slot) {
+        if constexpr (has_eight<F>) {
+            const char *tile = smem + __builtin_amdgcn_readfirstlane(slot * kTile8Bytes) + kQuad8 * wv + 8 * (lane & 1);
+            const int tr = (lane & 15) >> 1, key = 4 * g + (tr & 3) + 16 * (tr >> 2);
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                const u32x2 v = lds_read_tr8(tile + tile8_off(key, db));
+                av[db] = u32x4{v[0], v[1], 0u, 0u};
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            return;
+        }
         const char *tile = smem + __builtin_amdgcn_readfirstlane(slot * kChunkTileBytes);
 #pragma unroll
         for (int db = 0; db < 4; ++db) {
@@ -1611,6 +1689,19 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         __builtin_amdgcn_sched_barrier(0);
     };
     auto vconv = [&](bool careful) {
+        if constexpr (has_eight<F>) {
+            // (half kt of the keys in word kt; a half whose scale is no number is not seen, or its scores are none either)
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                if (careful) {
+                    av[db][0] = finite_e4m3x4(av[db][0]);
+                    av[db][1] = finite_e4m3x4(av[db][1]);
+                }
+                av[db] = f16_of_e4m3x8(av[db][0], av[db][1], exp2_bits(min(max(ec[0] - v_exp, -126), 7)),
+                                       exp2_bits(min(max(ec[1] - v_exp, -126), 7)));
+            }
+            return;
+        }
         if constexpr (F != kPlain) {
             if (careful) {
 #pragma unroll
@@ -1625,7 +1716,20 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             for (int i = 0; i < 4; ++i) av[db][i] = bf16x2_to_f16x2(av[db][i]);
     };
     // O^T += V^T P^T for tile t (P from buffer t & 1)
-    auto pv = [&](int pbuf) {
+    auto pv = [&](int t) {
+        const int pbuf = t & 1;
+        if constexpr (F != kPlain) {
+            const uint64_t raised = __builtin_amdgcn_ballot_w64(s_raised[pbuf * kCT + (lane & 7)] == t) & 0xff;
+            if (raised != 0) {
+#pragma unroll
+                for (int tb = 0; tb < kCT; ++tb) {
+                    if ((raised >> tb & 1) == 0) continue;
+                    const float f = s_raise[(pbuf * kCT + tb) * kHeads + hd];
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) acc[tb][db] = acc[tb][db] * f;
+                }
+            }
+        }
         const char *pb = s_pbuf + __builtin_amdgcn_readfirstlane(pbuf * kPTile) + lane * 16;
         constexpr int PD = 3;  // P operands in flight
         u32x4 bp[PD];
@@ -1645,6 +1749,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     TRACE(3);
     if (exact) m_ref = s_mx[wv * kHeads + hd];
     if (tid == 0) *s_abort = 0;
+    if (F != kPlain && tid < 2 * kCT) s_raised[tid] = -1;
     lds_barrier();  // page window and abort flag ready; the ring is idle
     // Waves 0..3 issue tile 0 at once, beside their queries; waves 4..7 issue
     // tile 1 when theirs have landed.  The compiler does not count the
@@ -1653,24 +1758,13 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // waits for anyway, and tile 1 stays in flight across it.  (Both tiles from
     // waves 4..7, the queries awaited behind them: 5 + 32 rows 22.6 -> 22.3 us, 32 +
     // 512 rows 41.0 -> 40.4, ragged chunks in two calls 85.0 -> 84.1.)
-    if constexpr (has_eight<F>) {
-        issue8(0);
-        if (ntiles > 1) issue8(1);
-    } else {
-        if (!dma_wave) issue(0, 0, page_of(0));
-    }
+    if (!dma_wave) issue_tile(0, 0, page_of(0));
 #pragma unroll
     for (int s = 0; s < kQRegSteps; ++s) asm volatile("" : "+v"(qreg[s]));
 #pragma unroll
     for (int s = 0; s < kQSteps - kQRegSteps; ++s) asm volatile("" : "+v"(qr[s]));
     wait_dma_all();
-    if constexpr (has_eight<F>) {
-        convert8(0);
-        if (ntiles > 1) convert8(1);
-        if (ntiles > 2) issue8(2);
-    } else {
-        if (dma_wave && ntiles > 1) issue(1, 1, page_of(1));
-    }
+    if (dma_wave && ntiles > 1) issue_tile(1, 1, page_of(1));
 #pragma unroll
     for (int s = 0; s < kQSteps - kQRegSteps; ++s)
         *reinterpret_cast<u32x4 *>(s_q + ((s * kCT + wv) * 64 + lane) * 16) = qr[s];
@@ -1684,8 +1778,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     TRACE_TILE(0, 11);
     {
         f32x4 s0[2];
+        if constexpr (has_eight<F>) scales8(0, 0);
         scores(0, s0);
-        if (main_pass) {
+        if (F == kPlain && main_pass) {
             float x[8];
             masked(0, s0, x);
             m_ref = wave_max16(lane_max(x, kNegInf) * a.scale_log2);
@@ -1699,37 +1794,19 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // then the softmax of t + 1
     for (int t = 0; t < ntiles; ++t) {
         TRACE_TILE(t, 11);
-        if constexpr (has_eight<F>) {
-            // Tile t + 1 was converted before this barrier (two bf16 slots: tile t's, whose V is in registers, takes tile
-            // t + 2), raw tile t + 2 is in flight.
-            __syncthreads();
-            pv(t & 1);
-            if (t + 2 < ntiles) {
-                wait_dma_all();  // raw tile t + 2 (this wave's part)
-                if (t + 3 < ntiles) issue8(t + 3);
-                convert8(t + 2);
-            }
-            if (t + 1 < ntiles) {
-                f32x4 s1[2];
-                scores((t + 1) & 1, s1);
-                vload((t + 1) & 1);
-                softmax(t + 1, (t + 1) & 1, s1);
-                vconv(any_not_finite(s1));
-            }
-            continue;
-        }
         const int next_page = page_of(min(t + 2, ntiles - 1));
         if (t + 1 < ntiles) wait_dma_all();  // tile t + 1 (this wave's part)
         __syncthreads();  // tile t + 1 and P of tile t complete; slot (t + 2) % 3 and P buffer (t + 1) & 1 free
         TRACE_TILE(t, 12);
         const int slot1 = slot == kChunkRing - 1 ? 0 : slot + 1;
         const int slot2 = slot1 == kChunkRing - 1 ? 0 : slot1 + 1;
-        if (dma_wave && t + 2 < ntiles) issue(t + 2, slot2, next_page);
+        if (dma_wave && t + 2 < ntiles) issue_tile(t + 2, slot2, next_page);
         TRACE_TILE(t, 14);
-        pv(t & 1);
+        pv(t);
         TRACE_TILE(t, 15);
         if (t + 1 < ntiles) {
             f32x4 s1[2];
+            if constexpr (has_eight<F>) scales8(t + 1, slot1);
             scores(slot1, s1);
             vload(slot1);
             softmax(t + 1, (t + 1) & 1, s1);
@@ -1740,10 +1817,12 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     }
     // a score that exceeds the reference by more than P may hold (also a first
     // visible key after the first tile): the products are discarded
-    m_lane *= a.scale_log2;
-    if (main_pass && __builtin_amdgcn_ballot_w64(m_lane - m_ref > kMaxPExp) != 0 && lane == 0) *s_abort = 1;
+    if constexpr (F == kPlain) {
+        m_lane *= a.scale_log2;
+        if (main_pass && __builtin_amdgcn_ballot_w64(m_lane - m_ref > kMaxPExp) != 0 && lane == 0) *s_abort = 1;
+    }
     __syncthreads();  // every wave's flag write and P*V reads are done
-    if (main_pass && __builtin_amdgcn_readfirstlane(*s_abort) != 0) {
+    if (F == kPlain && main_pass && __builtin_amdgcn_readfirstlane(*s_abort) != 0) {
         // abandoned: publish the exact maxima for the exact pass
         const float mx = wave_max16(m_lane);
         if (g == 0) s_mx[wv * kHeads + hd] = mx;
@@ -1766,14 +1845,14 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         if (tb >= nt) break;
         const int row = it.row0 + it.i0 + tb;
         if (it.nks_eff == 1) {
-            const float inv = 1.f / s_l[tb * kHeads + hd];
+            const float inv = (has_eight<F> ? exp2_bits(max(v_exp, -126)) : 1.f) / s_l[tb * kHeads + hd];
 #pragma unroll
             for (int db = 0; db < 4; ++db) store_out4(a, row, hd, 64 * wv + 16 * db + 4 * ge, acc[tb][db] * inv);
         } else {
             const size_t prow = (size_t)item * kCT + tb;
             float *po = a.ws_chunk_o + (prow * kHeads + hd) * kDv + 64 * wv + 4 * ge;
 #pragma unroll
-            for (int db = 0; db < 4; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = acc[tb][db];
+            for (int db = 0; db < 4; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = has_eight<F> ? acc[tb][db] * exp2_bits(max(v_exp, -126)) : acc[tb][db];
         }
     }
     if (g == 0 && wv < nt) {
@@ -1827,7 +1906,7 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attention_kernel(AttnArgs a) 
         TRACE_ITEM(item);
         if (item < a.n_chunk_items) {
             // a second, exact pass only if the main one was abandoned
-            for (int pass = 0; pass < 2; ++pass) {
+            for (int pass = 0; pass < (F == kPlain ? 2 : 1); ++pass) {
                 if (!chunk_item<F>(a, item, smem, s_pages[0], pass != 0)) break;
                 __syncthreads();
             }
