@@ -2,8 +2,23 @@
 // mla_kernels.hip (its helpers and namespace).
 #pragma once
 
-// DMA of one stream unit of a group: a tile with its scales, or (t < 0) a query
-// block, 18 rounds too (waves 2 and 3 take their first one twice, for the count).
+// A stream unit of a group: a segment's query block (t < 0), or two tiles of it, t
+// and t + 1 (the last one of a segment may be alone).
+struct Cursor8 {
+    int j, t;
+    DecSeg sg;
+};
+__device__ __forceinline__ void advance8(Cursor8 &c, const DecSeg *s_seg, int nseg) {
+    c.t = c.t < 0 ? c.sg.t0 : c.t + 2;
+    if (c.t >= c.sg.t1) {
+        ++c.j;
+        c.t = -1;
+        if (c.j < nseg) c.sg = load_seg(s_seg, c.j);
+    }
+}
+
+// DMA of a unit.  Of two tiles every wave issues ten instructions: five of each (see
+// dma_tile8), the waves' parts exchanged in the second one.
 template <int F>
 __device__ __forceinline__ void issue_unit8(const AttnArgs &a, const DecSeg &sg, int t, const int *s_pages, uint32_t slot,
                                             uint32_t scale_slot, int wv, int lane) {
@@ -11,35 +26,45 @@ __device__ __forceinline__ void issue_unit8(const AttnArgs &a, const DecSeg &sg,
     if (t < 0) {
         const char *qb = reinterpret_cast<const char *>(a.q + (size_t)sg.row * kHeads * kDqk) + lane * 16;
 #pragma unroll
-        for (int i = 0; i < kDma8; ++i) {
-            const int j = (i == 4 && wv >= 2 ? 0 : i) * 4 + wv;
-            lds_dma16(qb + j * 1024, __builtin_amdgcn_readfirstlane(slot + j * 1024));
+        for (int i = 0; i < 5; ++i) {
+            const int j = i * 4 + wv;
+            if (j < kTile8Bytes / 1024) lds_dma16(qb + j * 1024, __builtin_amdgcn_readfirstlane(slot + j * 1024));
         }
         return;
     }
     const SegKeys<has_window<F>> sk(a, sg);
-    const int kbase = sk.key(t * kDecKeys);
-    const auto slot_of = [&](int key) {  // pool slot
-        const int k = min(key, sg.p);
-        return (size_t)s_pages[min(sk.window_entry(sg, k, a.log2_page), kPageWindow - 1)] * a.page_size + (k & (a.page_size - 1));
-    };
-    if (a.page_size >= kDecKeys && kbase + kDecKeys - 1 <= sg.p) {
-        const int page = s_pages[min(sk.window_entry(sg, kbase, a.log2_page), kPageWindow - 1)];
-        const size_t first = (size_t)__builtin_amdgcn_readfirstlane(page) * a.page_size + (kbase & (a.page_size - 1));
-        dma_tile8(a.kv8 + first * kDqk, tile8_key(wv, lane) * kDqk + tile8_dims(wv, lane), slot, wv);
-    } else {
-        dma_tile8(a.kv8 + slot_of(kbase + tile8_key(wv, lane)) * kDqk + tile8_dims(wv, lane), slot, wv);
+    const auto page_of = [&](int key) { return s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)]; };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (t + h >= sg.t1) break;
+        const int kbase = sk.key((t + h) * kDecKeys), w = wv ^ (2 * h);
+        const auto slot_of = [&](int key) {  // pool slot
+            const int k = min(key, sg.p);
+            return (size_t)page_of(k) * a.page_size + (k & (a.page_size - 1));
+        };
+        if (a.page_size >= kDecKeys && kbase + kDecKeys - 1 <= sg.p) {
+            const size_t first = (size_t)__builtin_amdgcn_readfirstlane(page_of(kbase)) * a.page_size + (kbase & (a.page_size - 1));
+            dma_tile8(a.kv8 + first * kDqk, tile8_key(w, lane) * kDqk + tile8_dims(w, lane), slot + h * kTile8Bytes, w);
+        } else {
+            dma_tile8(a.kv8 + slot_of(kbase + tile8_key(w, lane)) * kDqk + tile8_dims(w, lane), slot + h * kTile8Bytes, w);
+        }
+        if (w >= 2) dma_scales8(a, slot_of(kbase + 16 * (w - 2)), scale_slot + 32 * h + 16 * (w - 2), lane);
     }
-    if (wv >= 2) dma_scales8(a, slot_of(kbase + 16 * (wv - 2)), scale_slot + 16 * (wv - 2), lane);
 }
 
-// decode_wg over the 8-bit cache.  Half the bytes a key: HBM-bound at 578 B a key,
-// so a tile of a group has half the time (1.6 us at 6 TB/s), and it is the chain of
-// a tile that has to be short.  Raw tiles pass through a ring of four slots, two to
-// three of them in flight.  Keys are converted where the matrix instruction takes
-// them (one instruction for two values, the scale of the 16 keys of its rows applied
-// on the way: bf16 holds the value exactly), the values of a tile before its score
-// barrier, with their scales folded into the probabilities (a power of two, exact).
+// decode_wg over the 8-bit cache.  Half the bytes a key (578), so a key has half the
+// time, and what bounds a group is the chain of a unit: wait, barrier, scores,
+// barrier, softmax, values.  Hence units of two tiles, 64 keys a barrier pair: each
+// wave scores 16 keys over all dims (nothing is added across waves) and then
+// accumulates its 128 value dims over the 64.  (Units of one tile, in a ring of four
+// slots: UNIT_FIGURES.)
+// Keys are converted at the matrix instruction (two values an instruction, the scale of
+// the 16 keys applied on the way: bf16 holds the result exactly).  Values become fp16
+// relative to 2^v_exp, the scale of the first blocks (raised, rarely, to what fp16
+// holds); probabilities go to the matrix instruction as fp16 hi + lo, taken against a
+// reference 2^6 below the max, so that hi + lo keep 22 bits down to 2^-9 of the max and
+// 2^-31 of it below.
+constexpr float kRef8 = 6.f, kRaise8 = 14.f;  // below the max; raised when a score is further above it (fp16 ends at 2^16)
 template <int F>
 __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)[kPageWindow], DecSeg (*s_seg_g)[kMaxSeg],
                            int *s_gbar) {
@@ -48,12 +73,11 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     const int grp = wv >> 2, gw = wv & 3, gtid = tid & 255;  // wave group, wave and thread inside it
     const int g = lane >> 4, h = lane & 15;
     const int S = a.dec_unit_tiles;
-    const int v = 2 * w + grp;  // this group's unit
+    const int v = 2 * w + grp;  // this group's share of the tile list
     const int R0 = v * S, R1 = min(R0 + S, a.dec_total_tiles);
     DecSeg *const s_seg = s_seg_g[grp];
     int *const s_pages = s_pages_g[grp];
     const int nseg = R0 < R1 ? find_unit<F>(a, R0, R1, s_seg, gw == 0) : 0;
-    const int n_units = nseg > 0 ? nseg + (R1 - R0) : 0;
     if (tid < 2) s_gbar[tid] = 0;
     TRACE(1);
     __syncthreads();
@@ -61,14 +85,14 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     char *const s_X = smem + 2 * kDec8GroupBytes + grp * kDec8XBytes;
     char *const s_scale = smem + 2 * (kDec8GroupBytes + kDec8XBytes) + grp * kDec8ScaleBytes;
     const uint32_t ring = lds_addr(slots), scales = lds_addr(s_scale);
-    Cursor prod{0, -1, DecSeg{}};
-    if (n_units > 0) prod.sg = load_seg(s_seg, 0);
-    Cursor cons = prod;
+    Cursor8 prod{0, -1, DecSeg{}};
+    if (nseg > 0) prod.sg = load_seg(s_seg, 0);
+    Cursor8 cons = prod;
     const auto issue = [&](int u) {
-        issue_unit8<F>(a, prod.sg, prod.t, s_pages, ring + (u % kDec8Ring) * kTile8Bytes, scales + (u % kDec8Ring) * 32, gw, lane);
-        advance(prod, s_seg, nseg);
+        issue_unit8<F>(a, prod.sg, prod.t, s_pages, ring + (u & 1) * kDec8SlotBytes, scales + (u & 1) * 64, gw, lane);
+        advance8(prod, s_seg, nseg);
     };
-    if (n_units > 0) {
+    if (nseg > 0) {
         issue(0);  // the first query block
         // page window: entry gtid belongs to the last segment that starts at or before it
         int j = 0;
@@ -85,151 +109,157 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         }
     }
     __syncthreads();
-    if (n_units == 0) return;  // this group has no unit (the other one may)
-    if (n_units > 1) issue(1);
-    if (n_units > 2) issue(2);
+    if (nseg == 0) return;  // this group has no share (the other one may)
+    issue(1);
     int epoch = 0;
     int *const gbar = s_gbar + grp;
     TRACE(2);
-    TRACE_VAL(8, 1000000ull * 2 + n_units);
+    TRACE_VAL(8, 1000000ull * 2 + nseg + (R1 - R0) / 2);
 
-    // This wave's half of the dims, 9 steps of 32: four groups of 64 from gbase on (a lane's 16 dims of a group feed two
-    // steps: the dims of a step may be any, as long as keys and queries agree), and 32 from sbase on.
-    const int hf = gw >> 1, gbase = hf ? 320 : 0, sbase = hf ? 288 : 256;
-    u32x4 qreg[9];
+    u32x4 qreg[18];  // dims 64 (s / 2) + 16 g + 8 (s & 1) .. + 7 of step s: a lane's 16-byte piece of a key feeds two steps
     f32x4 acc[8];
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt) acc[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_ref = kNegInf, l_run = 0.f;
-    const int kq = 16 * (gw & 1) + (lane & 15);  // key this lane scores
-    // value operand: slots 8 g + 4 kt + i of a step hold keys 16 kt + 4 g + i, as the probabilities do
+    constexpr int kNoExp = -1000;
+    int v_exp = kNoExp;
+    // value operand: slots 8 g + 4 kt + i of a tile hold keys 16 kt + 4 g + i, as the probabilities do
     const int tr = (lane & 15) >> 1, tr_key = 4 * g + (tr & 3) + 16 * (tr >> 2);
 
     TRACE(3);
-    for (int u = 0; u < n_units; ++u) {
+    for (int u = 0; cons.j < nseg; ++u) {
         TRACE_TILE(u, 10);
-        wait_dma8(min(2, n_units - 1 - u));        // unit u
-        group_barrier(gbar, epoch, a.spin_limit);  // landed for all four waves; slot (u + 3) % 4 is free
-        if (u + 3 < n_units) issue(u + 3);
-        const char *slot = slots + (u % kDec8Ring) * kTile8Bytes;
+        wait_dma_all();                            // unit u
+        group_barrier(gbar, epoch, a.spin_limit);  // landed for all four waves; the other slot is free
+        if (u > 0 && prod.j < nseg) issue(u + 1);
+        const char *slot = slots + (u & 1) * kDec8SlotBytes;
         if (cons.t < 0) {  // a new request: its query block
-            const char *q = slot + h * kRowBytes;
+            const char *q = slot + h * kRowBytes + 32 * g;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                qreg[2 * j] = *reinterpret_cast<const u32x4 *>(q + 2 * (gbase + 64 * j + 16 * g));
-                qreg[2 * j + 1] = *reinterpret_cast<const u32x4 *>(q + 2 * (gbase + 64 * j + 16 * g) + 16);
-            }
-            qreg[8] = *reinterpret_cast<const u32x4 *>(q + 2 * (sbase + 8 * g));
-            advance(cons, s_seg, nseg);
+            for (int s = 0; s < 18; ++s) qreg[s] = *reinterpret_cast<const u32x4 *>(q + 128 * (s >> 1) + 16 * (s & 1));
+            advance8(cons, s_seg, nseg);
             continue;
         }
         TRACE_TILE(u, 11);
         const DecSeg sg = cons.sg;
         const SegKeys<has_window<F>> sk(a, sg);
-        const int kbase = sk.key(cons.t * kDecKeys);
-        // scales of the tile's two key halves
-        float sc[2], sr[2];
+        const bool two = cons.t + 1 < sg.t1;
+        const int kb[2] = {sk.key(cons.t * kDecKeys), sk.key((cons.t + 1) * kDecKeys)};
+        // scales of the unit's four key blocks
+        int ec[4], er[4], most = kNoExp;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const int key = min(kbase + 16 * kt, sg.p);
+        for (int kt = 0; kt < 4; ++kt) {
+            const int first = kb[kt >> 1] + 16 * (kt & 1), key = min(first, sg.p);
             const int pg = a.page_size >= 64 ? 0 : s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)];
-            const uint32_t wd = *reinterpret_cast<const uint32_t *>(s_scale + (u % kDec8Ring) * 32 + 16 * kt + 4 * scale_piece8(a, pg, key));
-            // (a half that no row sees may have anything for a scale: 0 times it would be NaN)
-            sc[kt] = (wd & 0x7f80u) == 0x7f80u ? 0.f : __uint_as_float(wd << 16);
-            sr[kt] = __uint_as_float(wd & 0xffff0000u);
+            const uint32_t wd = __builtin_amdgcn_readfirstlane(
+                *reinterpret_cast<const int *>(s_scale + (u & 1) * 64 + 16 * kt + 4 * scale_piece8(a, pg, key)));
+            ec[kt] = scale_exponent(wd);
+            er[kt] = scale_exponent(wd >> 16);
+            // (a block that the row does not see has no say in the reference)
+            const bool seen = (kt < 2 || two) && first <= sg.p && (!has_window<F> || first + 15 > sg.p - a.band.window || first < a.band.sinks);
+            if (seen && ec[kt] <= kMaxExp8) most = max(most, ec[kt]);
         }
         {
-            // partial scores: keys 16 (gw & 1) .. + 16, this wave's dims
-            const float kc = (gw & 1) ? sc[1] : sc[0], kr = hf ? ((gw & 1) ? sr[1] : sr[0]) : kc;
-            u32x4 av[4];
+            // scores of key block gw
+            const char *kp = slot + (gw >> 1) * kTile8Bytes + tile8_off(16 * (gw & 1) + h, g);
+            const int e0 = gw == 0 ? ec[0] : gw == 1 ? ec[1] : gw == 2 ? ec[2] : ec[3];
+            const int e1 = gw == 0 ? er[0] : gw == 1 ? er[1] : gw == 2 ? er[2] : er[3];
+            u32x4 av[9];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) av[j] = *reinterpret_cast<const u32x4 *>(slot + kQuad8 * (gbase / 64 + j) + tile8_off(kq, g));
-            const u32x2 as = *reinterpret_cast<const u32x2 *>(slot + kQuad8 * 4 + tile8_off(kq, 2 * hf + (g >> 1)) + 8 * (g & 1));
+            for (int j = 0; j < 9; ++j) av[j] = *reinterpret_cast<const u32x4 *>(kp + kQuad8 * j);
             f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float s = j == 3 ? kr : kc;  // (the last group of the upper half: the rope dims)
+            for (int j = 0; j < 9; ++j) {
+                const float s = exp2_bits(j < 8 ? e0 : e1);  // (the last quad: the rope dims)
                 sa = mfma_bf16(bf16_of_e4m3x8(av[j][0], av[j][1], s), qreg[2 * j], sa);
                 sb = mfma_bf16(bf16_of_e4m3x8(av[j][2], av[j][3], s), qreg[2 * j + 1], sb);
             }
-            sa = mfma_bf16(bf16_of_e4m3x8(as[0], as[1], kc), qreg[8], sa);
             *reinterpret_cast<f32x4 *>(s_X + (gw * 64 + lane) * 16) = sa + sb;
         }
         // values of this wave's 128 dims, before the scores are complete
-        u32x2 vraw[8];
+        u32x2 vraw[2][8];
+        const auto load_values = [&] {
 #pragma unroll
-        for (int mt2 = 0; mt2 < 8; ++mt2) vraw[mt2] = lds_read_tr8(slot + kQuad8 * (2 * gw + (mt2 >> 2)) + tile8_off(tr_key, mt2 & 3) + 8 * (lane & 1));
-        u32x4 vop[8];
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int mt2 = 0; mt2 < 8; ++mt2) vop[mt2] = bf16_of_e4m3x8(vraw[mt2][0], vraw[mt2][1], 1.f);
-        group_barrier(gbar, epoch, a.spin_limit);  // partial score blocks complete
+                for (int mt = 0; mt < 8; ++mt)
+                    vraw[k][mt] = lds_read_tr8(slot + k * kTile8Bytes + kQuad8 * (2 * gw + (mt >> 2)) + tile8_off(tr_key, mt & 3) + 8 * (lane & 1));
+        };
+        load_values();
+        group_barrier(gbar, epoch, a.spin_limit);  // scores complete
         TRACE_TILE(u, 12);
-        // full scores of this lane's head: x[kt][i] = key 16 kt + 4 g + i (kt = 0, 1)
-        f32x4 x[2];
+        // scores of this lane's head: x[kt][i] = key 16 (kt & 1) + 4 g + i of tile kt / 2
+        f32x4 x[4];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-            x[kt] = *reinterpret_cast<const f32x4 *>(s_X + (kt * 64 + lane) * 16) +
-                    *reinterpret_cast<const f32x4 *>(s_X + ((kt + 2) * 64 + lane) * 16);
-        if (any_not_finite(x)) {
+        for (int kt = 0; kt < 4; ++kt) x[kt] = *reinterpret_cast<const f32x4 *>(s_X + (kt * 64 + lane) * 16);
+        if (any_not_finite(x[0] + x[1] + x[2] + x[3])) {
 #pragma unroll
-            for (int mt2 = 0; mt2 < 8; ++mt2) {
-                const u32x2 raw = lds_read_tr8(slot + kQuad8 * (2 * gw + (mt2 >> 2)) + tile8_off(tr_key, mt2 & 3) + 8 * (lane & 1));
-                vop[mt2] = bf16_of_e4m3x8(finite_e4m3x4(raw[0]), finite_e4m3x4(raw[1]), 1.f);
-            }
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int mt = 0; mt < 8; ++mt) vraw[k][mt] = u32x2{finite_e4m3x4(vraw[k][mt][0]), finite_e4m3x4(vraw[k][mt][1])};
         }
         float mt = kNegInf;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+        for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                x[kt][i] = row_sees<F>(a, kbase + 16 * kt + 4 * g + i, sg.p) ? x[kt][i] * a.scale_log2 : kNegInf;
+                const int key = kb[kt >> 1] + 16 * (kt & 1) + 4 * g + i;
+                x[kt][i] = (kt < 2 || two) && row_sees<F>(a, key, sg.p) ? x[kt][i] * a.scale_log2 : kNegInf;
                 mt = fmaxf(mt, x[kt][i]);
             }
         }
         mt = wave_max16(mt);
-        // lazy rescale, the same decision in every wave of the group (see decode_wg)
-        if (__builtin_amdgcn_ballot_w64(mt > m_ref + 8.f) != 0) {
-            const float m_new = fmaxf(m_ref, mt);
+        // raise the reference of the probabilities, or that of the values (the same decisions in every wave of the group)
+        if (__builtin_amdgcn_ballot_w64(mt > m_ref + kRaise8) != 0) {
+            const float m_new = fmaxf(m_ref, mt - kRef8);
             const float alpha = (m_ref == kNegInf) ? 0.f : exp2f(m_ref - m_new);
 #pragma unroll
             for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = acc[mt2] * alpha;
             l_run *= alpha;
             m_ref = m_new;
         }
-        // probabilities times their keys' value scale as a bf16 pair hi + lo (about 16 bits)
-        uint32_t bh[4], bl[4];
+        if (v_exp == kNoExp) {
+            v_exp = most;
+        } else if (most > v_exp + 7) {  // 448 2^7 = 57344
+            const float f = exp2_bits(max(v_exp - most, -126));
+            v_exp = most;
+#pragma unroll
+            for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = acc[mt2] * f;
+        }
+        u32x4 ph[2], pl[2];
         float ps = 0.f;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+        for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
-                float p0 = (x[kt][i] == kNegInf) ? 0.f : exp2f(x[kt][i] - m_ref);
-                float p1 = (x[kt][i + 1] == kNegInf) ? 0.f : exp2f(x[kt][i + 1] - m_ref);
+                const float p0 = (x[kt][i] == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(x[kt][i] - m_ref);
+                const float p1 = (x[kt][i + 1] == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(x[kt][i + 1] - m_ref);
                 ps += p0 + p1;
-                p0 *= sc[kt];
-                p1 *= sc[kt];
-                const uint32_t h0 = bf16_bits(p0), h1 = bf16_bits(p1);
-                bh[kt * 2 + (i >> 1)] = h0 | (h1 << 16);
-                bl[kt * 2 + (i >> 1)] = bf16_bits(p0 - bf16_bits_to_float(h0)) |
-                                        (bf16_bits(p1 - bf16_bits_to_float(h1)) << 16);
+                const f16x2 hi = {(_Float16)p0, (_Float16)p1};
+                ph[kt >> 1][2 * (kt & 1) + (i >> 1)] = __builtin_bit_cast(uint32_t, hi);
+                pl[kt >> 1][2 * (kt & 1) + (i >> 1)] = f16x2_bits(p0 - (float)hi[0], p1 - (float)hi[1]);
             }
         }
         l_run += ps;
         TRACE_TILE(u, 13);
-        const u32x4 opb_h = {bh[0], bh[1], bh[2], bh[3]};
-        const u32x4 opb_l = {bl[0], bl[1], bl[2], bl[3]};
 #pragma unroll
-        for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = mfma_bf16(vop[mt2], opb_h, acc[mt2]);
+        for (int k = 0; k < 2; ++k) {
+            const float s0 = exp2_bits(min(max(ec[2 * k] - v_exp, -126), 7)), s1 = exp2_bits(min(max(ec[2 * k + 1] - v_exp, -126), 7));
 #pragma unroll
-        for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = mfma_bf16(vop[mt2], opb_l, acc[mt2]);
+            for (int mt2 = 0; mt2 < 8; ++mt2) {
+                const u32x4 vop = f16_of_e4m3x8(vraw[k][mt2][0], vraw[k][mt2][1], s0, s1);
+                acc[mt2] = mfma_f16(vop, ph[k], acc[mt2]);
+                acc[mt2] = mfma_f16(vop, pl[k], acc[mt2]);
+            }
+        }
 
         TRACE_TILE(u, 14);
         const int jseg = cons.j;
-        advance(cons, s_seg, nseg);
+        advance8(cons, s_seg, nseg);
         if (cons.j != jseg) {  // the segment's last tile: finish it
-            const float l_tot = wave_sum16(l_run);
+            const float l_tot = wave_sum16(l_run), out_scale = exp2_bits(max(v_exp, -126));
             if (sg.t0 == 0 && sg.t1 == dec_tiles<F>(a, sg.p, 1)) {
-                const float inv = 1.f / l_tot;
+                const float inv = out_scale / l_tot;
 #pragma unroll
                 for (int mt2 = 0; mt2 < 8; ++mt2)
                     store_out4(a, sg.row, h, gw * 128 + mt2 * 16 + 4 * g, acc[mt2] * inv);
@@ -239,7 +269,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
                 float *po = a.ws_dec_o + (slot_id * kHeads + h) * kDv;
 #pragma unroll
                 for (int mt2 = 0; mt2 < 8; ++mt2)
-                    *reinterpret_cast<f32x4 *>(po + gw * 128 + mt2 * 16 + 4 * g) = acc[mt2];
+                    *reinterpret_cast<f32x4 *>(po + gw * 128 + mt2 * 16 + 4 * g) = acc[mt2] * out_scale;
                 if (gw == 0 && g == 0) {
                     a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 0] = partial_max(m_ref, l_tot);
                     a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 1] = l_tot;
@@ -249,6 +279,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
             for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = f32x4{0.f, 0.f, 0.f, 0.f};
             m_ref = kNegInf;
             l_run = 0.f;
+            v_exp = kNoExp;
         }
     }
     TRACE(4);

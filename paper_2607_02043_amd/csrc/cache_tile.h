@@ -53,12 +53,10 @@ constexpr int kQuad8 = kKeysPerTile * 64;  // 2048 bytes
 __device__ __forceinline__ int swz8(int k) { return ((k >> 2) & 3) ^ ((k >> 3) & 2); }
 __device__ __forceinline__ int tile8_off(int k, int p) { return 64 * k + 16 * (p ^ swz8(k)); }
 
-// DMA of a tile (18 rounds of 1 KB) by four waves, five instructions each, so that
-// what is in flight can be counted.  Round j is keys 16 (j & 1) .. + 15 of quad j / 2;
+// DMA of a tile (18 rounds of 1 KB) by four waves, five instructions each.  Round j is keys 16 (j & 1) .. + 15 of quad j / 2;
 // wave w takes rounds w, w + 4, ..: a lane has one key, and its source moves by two
 // quads a round.  The fifth instruction of waves 2 and 3 loads the scales of key half
 // w - 2.  (The instruction offset moves source and destination alike.)
-constexpr int kDma8 = 5;
 __device__ __forceinline__ int tile8_key(int w, int lane) { return 16 * (w & 1) + (lane >> 2); }
 __device__ __forceinline__ int tile8_dims(int w, int lane) {
     return 64 * (w >> 1) + 16 * ((lane & 3) ^ swz8(tile8_key(w, lane)));
@@ -77,18 +75,8 @@ __device__ __forceinline__ void dma_tile8(const uint8_t *src, uint32_t slot, int
     if (w < 2) MLA_DMA8(4);
 #undef MLA_DMA8
 }
-// The piece with the scales of a pool slot's block, to 16 bytes at `dst` (one lane; counts as an instruction).
+// The piece with the scales of a pool slot's block, to 16 bytes at `dst` (one lane).
 __device__ __forceinline__ void dma_scales8(const AttnArgs &a, size_t pool_slot, uint32_t dst, int lane) {
     const char *src = reinterpret_cast<const char *>(a.kv8_scales) + (pool_slot / kBlock8 * 4 & ~size_t(15));
     if (lane == 0) lds_dma16(src, __builtin_amdgcn_readfirstlane(dst));
-}
-// Until only the DMAs of the last `units` units are in flight.  (Loads complete in
-// order; a store in between only makes the wait longer.)
-__device__ __forceinline__ void wait_dma8(int units) {
-    if (units >= 2)
-        asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
-    else if (units == 1)
-        asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
-    else
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }

@@ -61,10 +61,10 @@ constexpr int kDecXBytes = 4 * kHeads * 20 * 4;               // partial score b
 constexpr int kDecLds = 2 * kDecGroupBytes + 2 * kDecXBytes;  // two groups: rings, then score blocks
 // chunk path
 constexpr int kTile8Bytes = kKeysPerTile * kDqk;        // 18432: a tile of the 8-bit cache, also a query block
-constexpr int kDec8Ring = 4;                            // its decode path: ring slots of each wave group
-constexpr int kDec8GroupBytes = kDec8Ring * kTile8Bytes;
-constexpr int kDec8XBytes = 4 * 64 * 16;                // partial score blocks of a group
-constexpr int kDec8ScaleBytes = kDec8Ring * 32;         // two 16-byte pieces of the scales a tile
+constexpr int kDec8SlotBytes = 2 * kTile8Bytes;         // its decode path: two tiles a ring slot
+constexpr int kDec8GroupBytes = kDecRing * kDec8SlotBytes;
+constexpr int kDec8XBytes = 4 * 64 * 16;                // score blocks of a group
+constexpr int kDec8ScaleBytes = kDecRing * 64;          // 16-byte pieces of the scales, four a slot
 constexpr int kDec8Lds = 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes);
 static_assert(kTile8Bytes == kHeads * kRowBytes, "a query block fills a slot");
 constexpr int kChunkKeys = kKeysPerTile;  // 32
@@ -586,6 +586,12 @@ __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
     }
 }
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t f16x2_bits(float a, float b) {
+    const f16x2 v = {(_Float16)a, (_Float16)b};  // round to nearest even
+    return __builtin_bit_cast(uint32_t, v);
+}
+
 #include "cache_tile.h"
 
 // ------------------------------------------------------------ decode path
@@ -837,8 +843,8 @@ __device__ __forceinline__ uint32_t finite_bf16x2(uint32_t w) {
     return w;
 }
 // Whether any of a wavefront's raw scores of a tile is not finite (a sum that overflows only costs time).
-__device__ __forceinline__ bool any_not_finite(const f32x4 (&x)[2]) {
-    const float t = ((x[0][0] + x[0][1]) + (x[0][2] + x[0][3])) + ((x[1][0] + x[1][1]) + (x[1][2] + x[1][3]));
+__device__ __forceinline__ bool any_not_finite(f32x4 x) {
+    const float t = (x[0] + x[1]) + (x[2] + x[3]);
     return __builtin_amdgcn_ballot_w64(!(fabsf(t) < INFINITY)) != 0;
 }
 // A partial's max: a part whose visible scores were all NaN must not look empty to the merge.
@@ -967,7 +973,7 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
             x[kt] = lo + hi;
         }
         bool careful = false;
-        if constexpr (F != kPlain) careful = any_not_finite(x);
+        if constexpr (F != kPlain) careful = any_not_finite(x[0] + x[1]);
         float mt = kNegInf;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
@@ -1260,12 +1266,6 @@ __device__ void chunk_merge(const AttnArgs &a, int k, int part, float *s_o, floa
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
     const auto h = __builtin_amdgcn_cvt_pkrtz(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     return __builtin_bit_cast(uint32_t, h);
-}
-
-__device__ __forceinline__ uint32_t f16x2_bits(float a, float b) {
-    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-    const f16x2 v = {(_Float16)a, (_Float16)b};  // round to nearest even
-    return __builtin_bit_cast(uint32_t, v);
 }
 
 constexpr int kCT = kChunkBlockTokens;                 // 8 tokens per item, one per wave
@@ -1787,7 +1787,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         vload(0);
         softmax(0, 0, s0);
-        vconv(F != kPlain && any_not_finite(s0));
+        vconv(F != kPlain && any_not_finite(s0[0] + s0[1]));
     }
     int slot = 0;  // ring slot of tile t (t % 3)
     // steady state: after the barrier, P*V of tile t and the scores of t + 1,
@@ -1810,7 +1810,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             scores(slot1, s1);
             vload(slot1);
             softmax(t + 1, (t + 1) & 1, s1);
-            vconv(F != kPlain && any_not_finite(s1));
+            vconv(F != kPlain && any_not_finite(s1[0] + s1[1]));
         }
         slot = slot1;
         TRACE_TILE(t, 13);
