@@ -54,10 +54,11 @@ __device__ __forceinline__ void issue_unit8(const AttnArgs &a, const DecSeg &sg,
 
 // decode_wg over the 8-bit cache.  Half the bytes a key (578), so a key has half the
 // time, and what bounds a group is the chain of a unit: wait, barrier, scores,
-// barrier, softmax, values.  Hence units of two tiles, 64 keys a barrier pair: each
-// wave scores 16 keys over all dims (nothing is added across waves) and then
-// accumulates its 128 value dims over the 64.  (Units of one tile, in a ring of four
-// slots: UNIT_FIGURES.)
+// barrier, values.  Hence units of two tiles, 64 keys a barrier pair; each wave scores
+// 16 keys over all dims, takes their probabilities against the reference so far and
+// passes those on (not the scores, whose softmax every wave would repeat: HALF_FIGURES),
+// and then accumulates its 128 value dims over the 64 keys.  (Units of one tile, in a
+// ring of four slots: UNIT_FIGURES.)
 // Keys are converted at the matrix instruction (two values an instruction, the scale of
 // the 16 keys applied on the way: bf16 holds the result exactly).  Values become fp16
 // relative to 2^v_exp, the scale of the first blocks (raised, rarely, to what fp16
@@ -84,6 +85,8 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     char *const slots = smem + grp * kDec8GroupBytes;
     char *const s_X = smem + 2 * kDec8GroupBytes + grp * kDec8XBytes;
     char *const s_scale = smem + 2 * (kDec8GroupBytes + kDec8XBytes) + grp * kDec8ScaleBytes;
+    float *const s_stat = reinterpret_cast<float *>(smem + 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes) + grp * kDec8StatBytes);
+    int *const s_sign = reinterpret_cast<int *>(s_stat + 4 * kHeads);  // [wave]: 1 a score far above the reference, 2 one not finite
     const uint32_t ring = lds_addr(slots), scales = lds_addr(s_scale);
     Cursor8 prod{0, -1, DecSeg{}};
     if (nseg > 0) prod.sg = load_seg(s_seg, 0);
@@ -131,12 +134,12 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         TRACE_TILE(u, 10);
         wait_dma_all();                            // unit u
         group_barrier(gbar, epoch, a.spin_limit);  // landed for all four waves; the other slot is free
-        if (u > 0 && prod.j < nseg) issue(u + 1);
         const char *slot = slots + (u & 1) * kDec8SlotBytes;
         if (cons.t < 0) {  // a new request: its query block
             const char *q = slot + h * kRowBytes + 32 * g;
 #pragma unroll
             for (int s = 0; s < 18; ++s) qreg[s] = *reinterpret_cast<const u32x4 *>(q + 128 * (s >> 1) + 16 * (s & 1));
+            if (u > 0 && prod.j < nseg) issue(u + 1);
             advance8(cons, s_seg, nseg);
             continue;
         }
@@ -145,111 +148,123 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         const SegKeys<has_window<F>> sk(a, sg);
         const bool two = cons.t + 1 < sg.t1;
         const int kb[2] = {sk.key(cons.t * kDecKeys), sk.key((cons.t + 1) * kDecKeys)};
-        // scales of the unit's four key blocks
-        int ec[4], er[4], most = kNoExp;
+        // this wave's 16 keys (block gw) and the scales of the unit's four blocks, in flight over the next unit's DMAs
+        const char *const kp = slot + (gw >> 1) * kTile8Bytes + tile8_off(16 * (gw & 1) + h, g);
+        u32x4 av[9];
+#pragma unroll
+        for (int j = 0; j < 9; ++j) av[j] = *reinterpret_cast<const u32x4 *>(kp + kQuad8 * j);
+        int wd[4];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
-            const int first = kb[kt >> 1] + 16 * (kt & 1), key = min(first, sg.p);
+            const int key = min(kb[kt >> 1] + 16 * (kt & 1), sg.p);
             const int pg = a.page_size >= 64 ? 0 : s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)];
-            const uint32_t wd = __builtin_amdgcn_readfirstlane(
-                *reinterpret_cast<const int *>(s_scale + (u & 1) * 64 + 16 * kt + 4 * scale_piece8(a, pg, key)));
-            ec[kt] = scale_exponent(wd);
-            er[kt] = scale_exponent(wd >> 16);
+            wd[kt] = *reinterpret_cast<const int *>(s_scale + (u & 1) * 64 + 16 * kt + 4 * scale_piece8(a, pg, key));
+        }
+        if (u > 0 && prod.j < nseg) issue(u + 1);
+        int ec[4], e_mine = 0, r_mine = 0, most = kNoExp;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            const uint32_t w2 = __builtin_amdgcn_readfirstlane(wd[kt]);
+            const int first = kb[kt >> 1] + 16 * (kt & 1);
+            ec[kt] = scale_exponent(w2);
+            e_mine = kt == gw ? ec[kt] : e_mine;
+            r_mine = kt == gw ? scale_exponent(w2 >> 16) : r_mine;
             // (a block that the row does not see has no say in the reference)
             const bool seen = (kt < 2 || two) && first <= sg.p && (!has_window<F> || first + 15 > sg.p - a.band.window || first < a.band.sinks);
             if (seen && ec[kt] <= kMaxExp8) most = max(most, ec[kt]);
         }
-        {
-            // scores of key block gw
-            const char *kp = slot + (gw >> 1) * kTile8Bytes + tile8_off(16 * (gw & 1) + h, g);
-            const int e0 = gw == 0 ? ec[0] : gw == 1 ? ec[1] : gw == 2 ? ec[2] : ec[3];
-            const int e1 = gw == 0 ? er[0] : gw == 1 ? er[1] : gw == 2 ? er[2] : er[3];
-            u32x4 av[9];
+        // scores x[i]: key 16 gw + 4 g + i of the unit, head h
+        f32x4 x, sb = {0.f, 0.f, 0.f, 0.f};
+        x = sb;
 #pragma unroll
-            for (int j = 0; j < 9; ++j) av[j] = *reinterpret_cast<const u32x4 *>(kp + kQuad8 * j);
-            f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 9; ++j) {
-                const float s = exp2_bits(j < 8 ? e0 : e1);  // (the last quad: the rope dims)
-                sa = mfma_bf16(bf16_of_e4m3x8(av[j][0], av[j][1], s), qreg[2 * j], sa);
-                sb = mfma_bf16(bf16_of_e4m3x8(av[j][2], av[j][3], s), qreg[2 * j + 1], sb);
-            }
-            *reinterpret_cast<f32x4 *>(s_X + (gw * 64 + lane) * 16) = sa + sb;
+        for (int j = 0; j < 9; ++j) {
+            const float s = exp2_bits(j < 8 ? e_mine : r_mine);  // (the last quad: the rope dims)
+            x = mfma_bf16(bf16_of_e4m3x8(av[j][0], av[j][1], s), qreg[2 * j], x);
+            sb = mfma_bf16(bf16_of_e4m3x8(av[j][2], av[j][3], s), qreg[2 * j + 1], sb);
         }
-        // values of this wave's 128 dims, before the scores are complete
-        u32x2 vraw[2][8];
-        const auto load_values = [&] {
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int mt = 0; mt < 8; ++mt)
-                    vraw[k][mt] = lds_read_tr8(slot + k * kTile8Bytes + kQuad8 * (2 * gw + (mt >> 2)) + tile8_off(tr_key, mt & 3) + 8 * (lane & 1));
-        };
-        load_values();
-        group_barrier(gbar, epoch, a.spin_limit);  // scores complete
-        TRACE_TILE(u, 12);
-        // scores of this lane's head: x[kt][i] = key 16 (kt & 1) + 4 g + i of tile kt / 2
-        f32x4 x[4];
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) x[kt] = *reinterpret_cast<const f32x4 *>(s_X + (kt * 64 + lane) * 16);
-        if (any_not_finite(x[0] + x[1] + x[2] + x[3])) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int mt = 0; mt < 8; ++mt) vraw[k][mt] = u32x2{finite_e4m3x4(vraw[k][mt][0]), finite_e4m3x4(vraw[k][mt][1])};
-        }
+        x = x + sb;
+        bool careful = any_not_finite(x);
         float mt = kNegInf;
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = kb[kt >> 1] + 16 * (kt & 1) + 4 * g + i;
-                x[kt][i] = (kt < 2 || two) && row_sees<F>(a, key, sg.p) ? x[kt][i] * a.scale_log2 : kNegInf;
-                mt = fmaxf(mt, x[kt][i]);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int key = kb[gw >> 1] + 16 * (gw & 1) + 4 * g + i;
+            x[i] = (gw < 2 || two) && row_sees<F>(a, key, sg.p) ? x[i] * a.scale_log2 : kNegInf;
+            mt = fmaxf(mt, x[i]);
         }
-        mt = wave_max16(mt);
-        // raise the reference of the probabilities, or that of the values (the same decisions in every wave of the group)
-        if (__builtin_amdgcn_ballot_w64(mt > m_ref + kRaise8) != 0) {
+        // probabilities of this wave's keys against the reference so far, hi and lo, for all four waves
+        float ps = 0.f;
+        const auto probabilities = [&] {
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = x[i] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(x[i] - m_ref);
+            ps = (p[0] + p[1]) + (p[2] + p[3]);
+            const f16x2 h0 = {(_Float16)p[0], (_Float16)p[1]}, h1 = {(_Float16)p[2], (_Float16)p[3]};
+            *reinterpret_cast<u32x4 *>(s_X + (gw * 64 + lane) * 16) =
+                u32x4{__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1),
+                      f16x2_bits(p[0] - (float)h0[0], p[1] - (float)h0[1]), f16x2_bits(p[2] - (float)h1[0], p[3] - (float)h1[1])};
+        };
+        probabilities();
+        const bool above = __builtin_amdgcn_ballot_w64(mt > m_ref + kRaise8) != 0;
+        if (lane == 0) s_sign[gw] = (above ? 1 : 0) | (careful ? 2 : 0);
+        // values of this wave's 128 dims, before the probabilities are complete
+        u32x2 vraw[2][8];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+                vraw[k][m] = lds_read_tr8(slot + k * kTile8Bytes + kQuad8 * (2 * gw + (m >> 2)) + tile8_off(tr_key, m & 3) + 8 * (lane & 1));
+        group_barrier(gbar, epoch, a.spin_limit);  // probabilities complete
+        TRACE_TILE(u, 12);
+        int signs = s_sign[0] | s_sign[1] | s_sign[2] | s_sign[3];
+        u32x4 pb[4];  // of block kt: hi (two words), lo
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) pb[kt] = *reinterpret_cast<const u32x4 *>(s_X + (kt * 64 + lane) * 16);
+        signs = __builtin_amdgcn_readfirstlane(signs);
+        if ((signs & 1) != 0) {
+            // a score far above the reference (rarely; always at a segment's start): raised for all four waves, from their
+            // maxima, and the probabilities once more
+            mt = wave_max16(mt);
+            if (g == 0) s_stat[gw * kHeads + h] = mt;
+            group_barrier(gbar, epoch, a.spin_limit);
+            mt = fmaxf(fmaxf(s_stat[h], s_stat[kHeads + h]), fmaxf(s_stat[2 * kHeads + h], s_stat[3 * kHeads + h]));
             const float m_new = fmaxf(m_ref, mt - kRef8);
             const float alpha = (m_ref == kNegInf) ? 0.f : exp2f(m_ref - m_new);
 #pragma unroll
-            for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = acc[mt2] * alpha;
+            for (int m = 0; m < 8; ++m) acc[m] = acc[m] * alpha;
             l_run *= alpha;
             m_ref = m_new;
+            probabilities();
+            group_barrier(gbar, epoch, a.spin_limit);
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) pb[kt] = *reinterpret_cast<const u32x4 *>(s_X + (kt * 64 + lane) * 16);
         }
+        l_run += ps;
+        if ((signs & 2) != 0) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int m = 0; m < 8; ++m) vraw[k][m] = u32x2{finite_e4m3x4(vraw[k][m][0]), finite_e4m3x4(vraw[k][m][1])};
+        }
+        // the reference of the values (the same decision in every wave)
         if (v_exp == kNoExp) {
             v_exp = most;
         } else if (most > v_exp + 7) {  // 448 2^7 = 57344
             const float f = exp2_bits(max(v_exp - most, -126));
             v_exp = most;
 #pragma unroll
-            for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = acc[mt2] * f;
+            for (int m = 0; m < 8; ++m) acc[m] = acc[m] * f;
         }
-        u32x4 ph[2], pl[2];
-        float ps = 0.f;
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                const float p0 = (x[kt][i] == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(x[kt][i] - m_ref);
-                const float p1 = (x[kt][i + 1] == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(x[kt][i + 1] - m_ref);
-                ps += p0 + p1;
-                const f16x2 hi = {(_Float16)p0, (_Float16)p1};
-                ph[kt >> 1][2 * (kt & 1) + (i >> 1)] = __builtin_bit_cast(uint32_t, hi);
-                pl[kt >> 1][2 * (kt & 1) + (i >> 1)] = f16x2_bits(p0 - (float)hi[0], p1 - (float)hi[1]);
-            }
-        }
-        l_run += ps;
         TRACE_TILE(u, 13);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const float s0 = exp2_bits(min(max(ec[2 * k] - v_exp, -126), 7)), s1 = exp2_bits(min(max(ec[2 * k + 1] - v_exp, -126), 7));
+            const u32x4 ph = {pb[2 * k][0], pb[2 * k][1], pb[2 * k + 1][0], pb[2 * k + 1][1]};
+            const u32x4 pl = {pb[2 * k][2], pb[2 * k][3], pb[2 * k + 1][2], pb[2 * k + 1][3]};
 #pragma unroll
-            for (int mt2 = 0; mt2 < 8; ++mt2) {
-                const u32x4 vop = f16_of_e4m3x8(vraw[k][mt2][0], vraw[k][mt2][1], s0, s1);
-                acc[mt2] = mfma_f16(vop, ph[k], acc[mt2]);
-                acc[mt2] = mfma_f16(vop, pl[k], acc[mt2]);
+            for (int m = 0; m < 8; ++m) {
+                const u32x4 vop = f16_of_e4m3x8(vraw[k][m][0], vraw[k][m][1], s0, s1);
+                acc[m] = mfma_f16(vop, ph, acc[m]);
+                acc[m] = mfma_f16(vop, pl, acc[m]);
             }
         }
 
@@ -257,7 +272,11 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         const int jseg = cons.j;
         advance8(cons, s_seg, nseg);
         if (cons.j != jseg) {  // the segment's last tile: finish it
-            const float l_tot = wave_sum16(l_run), out_scale = exp2_bits(max(v_exp, -126));
+            l_run = wave_sum16(l_run);  // of this wave's keys
+            if (g == 0) s_stat[gw * kHeads + h] = l_run;
+            group_barrier(gbar, epoch, a.spin_limit);
+            const float l_tot = (s_stat[h] + s_stat[kHeads + h]) + (s_stat[2 * kHeads + h] + s_stat[3 * kHeads + h]);
+            const float out_scale = exp2_bits(max(v_exp, -126));
             if (sg.t0 == 0 && sg.t1 == dec_tiles<F>(a, sg.p, 1)) {
                 const float inv = out_scale / l_tot;
 #pragma unroll

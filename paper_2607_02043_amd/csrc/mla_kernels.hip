@@ -65,7 +65,8 @@ constexpr int kDec8SlotBytes = 2 * kTile8Bytes;         // its decode path: two 
 constexpr int kDec8GroupBytes = kDecRing * kDec8SlotBytes;
 constexpr int kDec8XBytes = 4 * 64 * 16;                // score blocks of a group
 constexpr int kDec8ScaleBytes = kDecRing * 64;          // 16-byte pieces of the scales, four a slot
-constexpr int kDec8Lds = 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes);
+constexpr int kDec8StatBytes = 4 * kHeads * 4 + 16;     // a float of each wave and head, a word of each wave
+constexpr int kDec8Lds = 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes + kDec8StatBytes);
 static_assert(kTile8Bytes == kHeads * kRowBytes, "a query block fills a slot");
 constexpr int kChunkKeys = kKeysPerTile;  // 32
 constexpr int kChunkTileBytes = kChunkKeys * kRowBytes;  // 36864
