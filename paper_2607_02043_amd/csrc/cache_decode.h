@@ -17,39 +17,53 @@ __device__ __forceinline__ void advance8(Cursor8 &c, const DecSeg *s_seg, int ns
     }
 }
 
-// DMA of a unit.  Of two tiles every wave issues ten instructions: five of each (see
-// dma_tile8), the waves' parts exchanged in the second one.
+// Sources of a unit's DMAs, found while the unit before it is still computed, so that
+// only the DMAs themselves stand in a unit's chain.  A tile's rounds are dealt to the
+// waves as dma_tile8 says, with the waves' parts exchanged in the second tile: ten
+// instructions of each wave.
+struct Source8 {
+    const uint8_t *src[2];  // per lane: this wave's part of each tile; of a query block src[0]
+    const char *scale;      // of the tile whose scales this wave loads (lane 0)
+    int tiles;              // 0: a query block
+};
 template <int F>
-__device__ __forceinline__ void issue_unit8(const AttnArgs &a, const DecSeg &sg, int t, const int *s_pages, uint32_t slot,
-                                            uint32_t scale_slot, int wv, int lane) {
-    asm volatile("" : "+v"(lane));  // (no address is kept across the units)
-    if (t < 0) {
-        const char *qb = reinterpret_cast<const char *>(a.q + (size_t)sg.row * kHeads * kDqk) + lane * 16;
-#pragma unroll
-        for (int i = 0; i < 5; ++i) {
-            const int j = i * 4 + wv;
-            if (j < kTile8Bytes / 1024) lds_dma16(qb + j * 1024, __builtin_amdgcn_readfirstlane(slot + j * 1024));
-        }
-        return;
+__device__ __forceinline__ Source8 find_source8(const AttnArgs &a, const Cursor8 &c, const int *s_pages, int wv, int lane) {
+    const DecSeg &sg = c.sg;
+    Source8 s;
+    s.src[1] = nullptr;
+    s.scale = nullptr;
+    if (c.t < 0) {
+        s.tiles = 0;
+        s.src[0] = reinterpret_cast<const uint8_t *>(a.q + (size_t)sg.row * kHeads * kDqk) + wv * 1024 + lane * 16;
+        return s;
     }
     const SegKeys<has_window<F>> sk(a, sg);
-    const auto page_of = [&](int key) { return s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)]; };
+    s.tiles = min(sg.t1 - c.t, 2);
+    const auto slot_of = [&](int key) {  // pool slot
+        const int k = min(key, sg.p), page = s_pages[min(sk.window_entry(sg, k, a.log2_page), kPageWindow - 1)];
+        return (size_t)page * a.page_size + (k & (a.page_size - 1));
+    };
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (t + h >= sg.t1) break;
-        const int kbase = sk.key((t + h) * kDecKeys), w = wv ^ (2 * h);
-        const auto slot_of = [&](int key) {  // pool slot
-            const int k = min(key, sg.p);
-            return (size_t)page_of(k) * a.page_size + (k & (a.page_size - 1));
-        };
-        if (a.page_size >= kDecKeys && kbase + kDecKeys - 1 <= sg.p) {
-            const size_t first = (size_t)__builtin_amdgcn_readfirstlane(page_of(kbase)) * a.page_size + (kbase & (a.page_size - 1));
-            dma_tile8(a.kv8 + first * kDqk, tile8_key(w, lane) * kDqk + tile8_dims(w, lane), slot + h * kTile8Bytes, w);
-        } else {
-            dma_tile8(a.kv8 + slot_of(kbase + tile8_key(w, lane)) * kDqk + tile8_dims(w, lane), slot + h * kTile8Bytes, w);
-        }
-        if (w >= 2) dma_scales8(a, slot_of(kbase + 16 * (w - 2)), scale_slot + 32 * h + 16 * (w - 2), lane);
+    for (int h = 0; h < 2; ++h) {  // (past the segment's end the second tile repeats its last key and is not loaded)
+        const int w = wv ^ (2 * h);
+        s.src[h] = a.kv8 + slot_of(sk.key((c.t + h) * kDecKeys) + tile8_key(w, lane)) * kDqk + tile8_dims(w, lane);
     }
+    const int h = wv >= 2 ? 0 : 1;
+    s.scale = reinterpret_cast<const char *>(a.kv8_scales) +
+              (slot_of(sk.key((c.t + h) * kDecKeys) + 16 * (wv & 1)) / kBlock8 * 4 & ~size_t(15));
+    return s;
+}
+__device__ __forceinline__ void issue8(const Source8 &s, uint32_t slot, uint32_t scale_slot, int wv, int lane) {
+    if (s.tiles == 0) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i)
+            if (i < 4 || wv < 2) lds_dma16(s.src[0] + 4096 * i, __builtin_amdgcn_readfirstlane(slot + 1024 * wv + 4096 * i));
+        return;
+    }
+    dma_tile8(s.src[0], slot, wv);
+    if (s.tiles == 2) dma_tile8(s.src[1], slot + kTile8Bytes, wv ^ 2);
+    if ((wv >= 2 || s.tiles == 2) && lane == 0)
+        lds_dma16(s.scale, __builtin_amdgcn_readfirstlane(scale_slot + (wv >= 2 ? 0 : 32) + 16 * (wv & 1)));
 }
 
 // decode_wg over the 8-bit cache.  Half the bytes a key (578), so a key has half the
@@ -61,7 +75,7 @@ __device__ __forceinline__ void issue_unit8(const AttnArgs &a, const DecSeg &sg,
 // ring of four slots: UNIT_FIGURES.)
 // Keys are converted at the matrix instruction (two values an instruction, the scale of
 // the 16 keys applied on the way: bf16 holds the result exactly).  Values become fp16
-// relative to 2^v_exp, the scale of the first blocks (raised, rarely, to what fp16
+// relative to v_ref, the scale of the first blocks (raised, rarely, to what fp16
 // holds); probabilities go to the matrix instruction as fp16 hi + lo, taken against a
 // reference 2^6 below the max, so that hi + lo keep 22 bits down to 2^-9 of the max and
 // 2^-31 of it below.
@@ -91,11 +105,14 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     Cursor8 prod{0, -1, DecSeg{}};
     if (nseg > 0) prod.sg = load_seg(s_seg, 0);
     Cursor8 cons = prod;
+    Source8 next{};  // of unit u + 1 while unit u is computed (if prod is inside the share)
+    const auto find_next = [&] { next = find_source8<F>(a, prod, s_pages, gw, lane); };
     const auto issue = [&](int u) {
-        issue_unit8<F>(a, prod.sg, prod.t, s_pages, ring + (u & 1) * kDec8SlotBytes, scales + (u & 1) * 64, gw, lane);
+        issue8(next, ring + (u & 1) * kDec8SlotBytes, scales + (u & 1) * 64, gw, lane);
         advance8(prod, s_seg, nseg);
     };
     if (nseg > 0) {
+        find_next();
         issue(0);  // the first query block
         // page window: entry gtid belongs to the last segment that starts at or before it
         int j = 0;
@@ -113,7 +130,9 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     }
     __syncthreads();
     if (nseg == 0) return;  // this group has no share (the other one may)
+    find_next();
     issue(1);
+    if (prod.j < nseg) find_next();
     int epoch = 0;
     int *const gbar = s_gbar + grp;
     TRACE(2);
@@ -124,8 +143,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt) acc[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_ref = kNegInf, l_run = 0.f;
-    constexpr int kNoExp = -1000;
-    int v_exp = kNoExp;
+    float v_ref = 0.f, v_inv = 0.f;  // 0: no block read yet
     // value operand: slots 8 g + 4 kt + i of a tile hold keys 16 kt + 4 g + i, as the probabilities do
     const int tr = (lane & 15) >> 1, tr_key = 4 * g + (tr & 3) + 16 * (tr >> 2);
 
@@ -139,7 +157,10 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
             const char *q = slot + h * kRowBytes + 32 * g;
 #pragma unroll
             for (int s = 0; s < 18; ++s) qreg[s] = *reinterpret_cast<const u32x4 *>(q + 128 * (s >> 1) + 16 * (s & 1));
-            if (u > 0 && prod.j < nseg) issue(u + 1);
+            if (u > 0 && prod.j < nseg) {
+                issue(u + 1);
+                if (prod.j < nseg) find_next();
+            }
             advance8(cons, s_seg, nseg);
             continue;
         }
@@ -153,32 +174,34 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         u32x4 av[9];
 #pragma unroll
         for (int j = 0; j < 9; ++j) av[j] = *reinterpret_cast<const u32x4 *>(kp + kQuad8 * j);
-        int wd[4];
+        uint32_t wd[4];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
             const int key = min(kb[kt >> 1] + 16 * (kt & 1), sg.p);
             const int pg = a.page_size >= 64 ? 0 : s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)];
-            wd[kt] = *reinterpret_cast<const int *>(s_scale + (u & 1) * 64 + 16 * kt + 4 * scale_piece8(a, pg, key));
+            wd[kt] = *reinterpret_cast<const uint32_t *>(s_scale + (u & 1) * 64 + 16 * kt + 4 * scale_piece8(a, pg, key));
         }
-        if (u > 0 && prod.j < nseg) issue(u + 1);
-        int ec[4], e_mine = 0, r_mine = 0, most = kNoExp;
+        const bool issued = u > 0 && prod.j < nseg;
+        if (issued) issue(u + 1);
+        // scales of the values, and the largest of the blocks that the row sees (a scale that is no number counts for none: its
+        // block is not seen, or its scores are not finite; a tile that is not there has any bits, a sign among them)
+        float sc[4], most = 0.f;
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
-            const uint32_t w2 = __builtin_amdgcn_readfirstlane(wd[kt]);
             const int first = kb[kt >> 1] + 16 * (kt & 1);
-            ec[kt] = scale_exponent(w2);
-            e_mine = kt == gw ? ec[kt] : e_mine;
-            r_mine = kt == gw ? scale_exponent(w2 >> 16) : r_mine;
-            // (a block that the row does not see has no say in the reference)
-            const bool seen = (kt < 2 || two) && first <= sg.p && (!has_window<F> || first + 15 > sg.p - a.band.window || first < a.band.sinks);
-            if (seen && ec[kt] <= kMaxExp8) most = max(most, ec[kt]);
+            sc[kt] = __uint_as_float(wd[kt] << 16 & 0x7fffffffu);
+            sc[kt] = sc[kt] < INFINITY ? sc[kt] : 0.f;
+            const bool seen = (kt < 2 || two) && (!has_window<F> || first + 15 > sg.p - a.band.window || first < a.band.sinks);
+            most = fmaxf(most, seen ? sc[kt] : 0.f);
         }
+        const uint32_t w_mine = gw == 0 ? wd[0] : gw == 1 ? wd[1] : gw == 2 ? wd[2] : wd[3];
+        const float e_mine = __uint_as_float(w_mine << 16), r_mine = __uint_as_float(w_mine & 0xffff0000u);
         // scores x[i]: key 16 gw + 4 g + i of the unit, head h
         f32x4 x, sb = {0.f, 0.f, 0.f, 0.f};
         x = sb;
 #pragma unroll
         for (int j = 0; j < 9; ++j) {
-            const float s = exp2_bits(j < 8 ? e_mine : r_mine);  // (the last quad: the rope dims)
+            const float s = j < 8 ? e_mine : r_mine;  // (the last quad: the rope dims)
             x = mfma_bf16(bf16_of_e4m3x8(av[j][0], av[j][1], s), qreg[2 * j], x);
             sb = mfma_bf16(bf16_of_e4m3x8(av[j][2], av[j][3], s), qreg[2 * j + 1], sb);
         }
@@ -246,18 +269,17 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
                 for (int m = 0; m < 8; ++m) vraw[k][m] = u32x2{finite_e4m3x4(vraw[k][m][0]), finite_e4m3x4(vraw[k][m][1])};
         }
         // the reference of the values (the same decision in every wave)
-        if (v_exp == kNoExp) {
-            v_exp = most;
-        } else if (most > v_exp + 7) {  // 448 2^7 = 57344
-            const float f = exp2_bits(max(v_exp - most, -126));
-            v_exp = most;
+        if (__builtin_amdgcn_ballot_w64(most > 128.f * v_ref) != 0) {  // 448 2^7 = 57344
+            const float f = v_ref / most;  // (0 at a segment's start)
+            v_ref = most;
+            v_inv = 1.f / most;
 #pragma unroll
             for (int m = 0; m < 8; ++m) acc[m] = acc[m] * f;
         }
         TRACE_TILE(u, 13);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const float s0 = exp2_bits(min(max(ec[2 * k] - v_exp, -126), 7)), s1 = exp2_bits(min(max(ec[2 * k + 1] - v_exp, -126), 7));
+            const float s0 = fminf(sc[2 * k] * v_inv, 128.f), s1 = fminf(sc[2 * k + 1] * v_inv, 128.f);
             const u32x4 ph = {pb[2 * k][0], pb[2 * k][1], pb[2 * k + 1][0], pb[2 * k + 1][1]};
             const u32x4 pl = {pb[2 * k][2], pb[2 * k][3], pb[2 * k + 1][2], pb[2 * k + 1][3]};
 #pragma unroll
@@ -267,6 +289,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
                 acc[m] = mfma_f16(vop, pl, acc[m]);
             }
         }
+        if (issued && prod.j < nseg) find_next();  // (beside the last products)
 
         TRACE_TILE(u, 14);
         const int jseg = cons.j;
@@ -276,9 +299,8 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
             if (g == 0) s_stat[gw * kHeads + h] = l_run;
             group_barrier(gbar, epoch, a.spin_limit);
             const float l_tot = (s_stat[h] + s_stat[kHeads + h]) + (s_stat[2 * kHeads + h] + s_stat[3 * kHeads + h]);
-            const float out_scale = exp2_bits(max(v_exp, -126));
             if (sg.t0 == 0 && sg.t1 == dec_tiles<F>(a, sg.p, 1)) {
-                const float inv = out_scale / l_tot;
+                const float inv = v_ref / l_tot;
 #pragma unroll
                 for (int mt2 = 0; mt2 < 8; ++mt2)
                     store_out4(a, sg.row, h, gw * 128 + mt2 * 16 + 4 * g, acc[mt2] * inv);
@@ -288,7 +310,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
                 float *po = a.ws_dec_o + (slot_id * kHeads + h) * kDv;
 #pragma unroll
                 for (int mt2 = 0; mt2 < 8; ++mt2)
-                    *reinterpret_cast<f32x4 *>(po + gw * 128 + mt2 * 16 + 4 * g) = acc[mt2] * out_scale;
+                    *reinterpret_cast<f32x4 *>(po + gw * 128 + mt2 * 16 + 4 * g) = acc[mt2] * v_ref;
                 if (gw == 0 && g == 0) {
                     a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 0] = partial_max(m_ref, l_tot);
                     a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 1] = l_tot;
@@ -298,7 +320,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
             for (int mt2 = 0; mt2 < 8; ++mt2) acc[mt2] = f32x4{0.f, 0.f, 0.f, 0.f};
             m_ref = kNegInf;
             l_run = 0.f;
-            v_exp = kNoExp;
+            v_ref = 0.f;
         }
     }
     TRACE(4);
