@@ -157,10 +157,11 @@ constexpr double kEmptyItemUs = 1.5;    // a chunk item past its block's causal 
 constexpr double kDecTileUs = 3.5;      // one decode tile of a unit (the two units of an item run side by side)
 constexpr double kDecUnitUs = 8.0;      // decode item start-up
 constexpr double kDecTileLoUs = 2.65;   // a decode tile when few workgroups stream (per-CU rate bound)
-// the same over the 8-bit cache
-constexpr double kChunk8TileUs = 2.1;
-constexpr double kDec8TileUs = 1.8;
-constexpr double kDec8TileLoUs = 1.3;
+// the same over the 8-bit cache (two tiles a barrier pair: an item's start and end weigh more)
+constexpr double kChunk8TileUs = 2.5;
+constexpr double kDec8TileUs = 2.0;
+constexpr double kDec8UnitUs = 12.0;
+constexpr double kDec8TileLoUs = 1.6;
 constexpr double kTwoQueueGain = 0.03;  // decode-first workgroups only for at least this much less time
 constexpr double kTwoQueueMinUs = 5.0;  // and at least this many microseconds less
 constexpr double kMergeGBs = 3000.0;    // partial rows written and merged, whole chip
@@ -379,7 +380,7 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
     long long cap = ((long long)(mla::kPageWindow - (windowed ? 3 : 1)) * P) / 64 * 64;
     if (cap < 64) cap = 64;
     const double kDecTileUs = form.eight ? kDec8TileUs : ::kDecTileUs, kDecTileLoUs = form.eight ? kDec8TileLoUs : ::kDecTileLoUs;
-    const double kChunkTileUs = form.eight ? kChunk8TileUs : ::kChunkTileUs;
+    const double kChunkTileUs = form.eight ? kChunk8TileUs : ::kChunkTileUs, kDecUnitUs = form.eight ? kDec8UnitUs : ::kDecUnitUs;
     // (virtual) keys of a chunk request's longest block, and of its block rb
     const auto span = [&](long long p, long long c) { return windowed ? (long long)mla::band_span(band, (int)p, (int)c) : p + c; };
     const auto block_keys = [&](long long p, long long c, long long rb) {
