@@ -23,6 +23,18 @@ int check_base(float base, bool zero_ok) {
     return MLA_OK;
 }
 
+// The last base's table is kept per thread (64 powers of 2, a microsecond).
+const mla::RopeTable &rope_table(float base) {
+    thread_local mla::RopeTable t;
+    thread_local float of = 0.f;
+    if (of != base) {
+        const double log2_base = std::log2((double)base);
+        for (int i = 0; i < 32; ++i) t.turns[i] = std::exp2(-(double)i / 32.0 * log2_base) * 0.15915494309189533577;
+        of = base;
+    }
+    return t;
+}
+
 int check_window(const mla_window *w, bool null_ok) {
     if (!w) return null_ok ? MLA_OK : set_error(MLA_ERR_INVALID_ARG, "window is NULL");
     if (w->window < 1) return set_error(MLA_ERR_INVALID_ARG, "window of %d keys < 1", w->window);
@@ -107,7 +119,7 @@ int append_latent_kv_rope(const mla_batch *batch, const uint16_t *new_latents, f
     a.max_pages = batch->max_pages_per_req;
     a.num_pages = batch->num_pages;
     if ((st = mla::check_before(batch, {}, stream)) != MLA_OK) return st;
-    const hipError_t e = mla::launch_append_rope(a, std::log2((double)rope_base), static_cast<hipStream_t>(stream));
+    const hipError_t e = mla::launch_append_rope(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return mla::hip_error(e, "append kernel launch");
     return mla::check_after("append_latent_kv_rope", stream);
 }
@@ -132,7 +144,7 @@ int append_latent_kv8(const mla_batch *batch, const uint16_t *new_latents, float
     a.cu_q = batch->cu_q_dev;
     a.prefix = batch->prefix_lens_dev;
     a.bt = batch->block_table_dev;
-    a.log2_base = rope_base == 0.f ? 0.0 : std::log2((double)rope_base);
+    a.rotate = rope_base != 0.f;
     a.num_reqs = batch->num_reqs;
     a.num_rows = T;
     a.num_blocks = (int)blocks;  // at most one per row
@@ -142,7 +154,7 @@ int append_latent_kv8(const mla_batch *batch, const uint16_t *new_latents, float
     a.num_pages = batch->num_pages;
     const mla::CheckUse use{MLA_CACHE8_BLOCK, 0, 0};
     if ((st = mla::check_before(batch, use, stream)) != MLA_OK) return st;
-    const hipError_t e = mla::launch_append8(a, static_cast<hipStream_t>(stream));
+    const hipError_t e = mla::launch_append8(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return mla::hip_error(e, "8-bit append kernel launch");
     return mla::check_after("append_latent_kv8", stream);
 }

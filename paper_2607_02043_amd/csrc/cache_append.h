@@ -5,13 +5,11 @@
 // ------------------------------------------------------- rotation on the way
 // Sine and cosine of position t times base^(-2 i / 64): the angle in turns, in
 // 64 bits, so that only its fraction is rounded to fp32 (2^-25 turns, 2e-7 rad, at
-// any position); the rest is fp32.
+// any position); the rest is fp32.  The turns per position of the 32 pairs come with
+// the launch (RopeTable): their powers in 64 bits would be half of a small append.
 struct SinCos {
     float sn, cs;
 };
-__device__ __forceinline__ double rope_turns(int i, double log2_base) {  // per position
-    return exp2(-(double)i / 32.0 * log2_base) * 0.15915494309189533577;
-}
 __device__ __forceinline__ SinCos rope_angle(int t, double turns) {
     const double a = (double)t * turns;
     const float f = (float)(a - floor(a));
@@ -24,7 +22,7 @@ __device__ __forceinline__ SinCos rope_angle(int t, double turns) {
 // One wavefront a row, as append_kernel; lanes 0 .. 31 rotate a pair each.
 // Bound by latency like it: lengths -> page id -> store, with the row's loads and
 // the angles beside them.
-__global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendArgs a, double log2_base) {
+__global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendArgs a, RopeTable rope) {
     const int lane = threadIdx.x & 63;
     const int row = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (row >= a.num_rows) return;
@@ -40,7 +38,7 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendArgs a, dou
         raise_flag(kFlagBadPage);
         return;
     }
-    const SinCos w = rope_angle(t, rope_turns(i, log2_base));
+    const SinCos w = rope_angle(t, rope.turns[i]);
     const float x0 = bf16_bits_to_float(x & 0xffffu), x1 = bf16_bits_to_float(x >> 16);
     uint16_t *dst = a.kv + ((size_t)page * a.page_size + (t & (a.page_size - 1))) * kDqk;
     reinterpret_cast<u32x4 *>(dst)[lane] = va;
@@ -75,21 +73,42 @@ struct Block8Count {
     __device__ int operator()(int p, int c) const { return c > 0 ? ((p + c - 1) >> 4) - (p >> 4) + 1 : 0; }
 };
 
+// Bound by latency: the lengths, then the page id and the rows, then the old scales,
+// then the stores, a round trip each (256 tokens of 256 requests AP8_FIGURES).
 // One workgroup a block: thread (wave w, lane l) takes the compressed chunk l
 // (8 dims) of its rows w, w + 4, .., and the first 128 threads one rope chunk (4
 // pairs) each.  The two maxima meet in LDS; then everything is scaled, rounded and
 // stored, and a block with earlier tokens whose scale grew rounds those again.
-__global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
+__global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a, RopeTable rope_table) {
     __shared__ float s_max[4][2];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rr = tid >> 3, rc = tid & 7;  // rope row and chunk of this thread
+    double turns[4] = {0.0, 0.0, 0.0, 0.0};
+    if (a.rotate) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) turns[k] = rope_table.turns[4 * rc + k];
+    }
     Located lc;
     if (!locate_item(blockIdx.x, a.num_reqs, ReqLens{a.cu_q, a.prefix, false}, Block8Count{}, lc)) return;
     const int b = (lc.p >> 4) + lc.local;                                     // logical block of the request
     const int t0 = max(lc.p, b * kBlock8), t1 = min(lc.p + lc.c, (b + 1) * kBlock8);  // its new tokens
     const int row0 = lc.row0 + t0 - lc.p, n = t1 - t0;
+    if (lc.p < 0 || row0 < 0 || row0 + n > a.num_rows) {  // device lengths that disagree with the host's
+        if (tid == 0) raise_flag(kFlagBadPage);
+        return;
+    }
+    // the page id and the new rows in one round of loads
     const int lp = (b * kBlock8) >> a.log2_page;
     const int page = lp < a.max_pages ? a.bt[(size_t)lc.r * a.max_pages + lp] : -1;
-    if (lc.p < 0 || row0 < 0 || row0 + n > a.num_rows || (unsigned)page >= (unsigned)a.num_pages) {
+    u32x4 vc[4], vr = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        vc[i] = u32x4{0u, 0u, 0u, 0u};
+        if (4 * i + wv < n) vc[i] = reinterpret_cast<const u32x4 *>(a.src + (size_t)(row0 + 4 * i + wv) * kDqk)[lane];
+    }
+    const bool rope = rr < n;  // (n <= 16: threads 0 .. 127)
+    if (rope) vr = reinterpret_cast<const u32x4 *>(a.src + (size_t)(row0 + rr) * kDqk + kDv)[rc];
+    if ((unsigned)page >= (unsigned)a.num_pages) {
         if (tid == 0) raise_flag(kFlagBadPage);
         return;
     }
@@ -98,15 +117,6 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
     uint32_t *const scale = reinterpret_cast<uint32_t *>(a.scales) + slot0 / kBlock8;
     const int held = t0 - b * kBlock8;  // earlier tokens of the block
 
-    u32x4 vc[4], vr = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        vc[i] = u32x4{0u, 0u, 0u, 0u};
-        if (4 * i + wv < n) vc[i] = reinterpret_cast<const u32x4 *>(a.src + (size_t)(row0 + 4 * i + wv) * kDqk)[lane];
-    }
-    const int rr = tid >> 3, rc = tid & 7;  // rope row and chunk of this thread
-    const bool rope = rr < n;               // (n <= 16: threads 0 .. 127)
-    if (rope) vr = reinterpret_cast<const u32x4 *>(a.src + (size_t)(row0 + rr) * kDqk + kDv)[rc];
     const uint32_t old = held > 0 ? *scale : 0u;
 
     float xr[8], mc = 0.f, mr = 0.f;
@@ -115,8 +125,8 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
         const float x0 = bf16_bits_to_float(vr[k] & 0xffffu), x1 = bf16_bits_to_float(vr[k] >> 16);
         xr[2 * k] = x0;
         xr[2 * k + 1] = x1;
-        if (a.log2_base > 0.0 && rope) {
-            const SinCos w = rope_angle(t0 + rr, rope_turns(4 * rc + k, a.log2_base));
+        if (a.rotate && rope) {
+            const SinCos w = rope_angle(t0 + rr, turns[k]);
             xr[2 * k] = x0 * w.cs - x1 * w.sn;
             xr[2 * k + 1] = x0 * w.sn + x1 * w.cs;
         }

@@ -150,6 +150,11 @@ struct AppendArgs {
     int32_t num_pages;
 };
 
+// Turns per position of the 32 rotated pairs, base^(-2 i / 64) / 2 pi.
+struct RopeTable {
+    double turns[32];
+};
+
 struct Append8Args {
     const uint16_t *src;
     uint8_t *data;
@@ -157,7 +162,7 @@ struct Append8Args {
     const int32_t *cu_q;
     const int32_t *prefix;
     const int32_t *bt;
-    double log2_base;  // of the rotation; 0: none
+    int32_t rotate;    // 0: the rope dims are rotated already
     int32_t num_reqs;
     int32_t num_rows;
     int32_t num_blocks;  // workgroups: blocks of 16 tokens that the rows touch
@@ -168,8 +173,8 @@ struct Append8Args {
 };
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);
-hipError_t launch_append_rope(const AppendArgs &a, double log2_base, hipStream_t s);
-hipError_t launch_append8(const Append8Args &a, hipStream_t s);
+hipError_t launch_append_rope(const AppendArgs &a, const RopeTable &rope, hipStream_t s);
+hipError_t launch_append8(const Append8Args &a, const RopeTable &rope, hipStream_t s);
 // Reads the device's sticky kernel error flags (kFlag*), and clears them if asked.
 hipError_t read_flags(int *flags, bool clear);
 // Device address of the current device's no-allocation scratch

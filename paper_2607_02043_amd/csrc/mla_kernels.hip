@@ -2079,17 +2079,17 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_append_rope(const AppendArgs &a, double log2_base, hipStream_t s) {
+hipError_t launch_append_rope(const AppendArgs &a, const RopeTable &rope, hipStream_t s) {
     const int rows_per_block = kThreads / 64;
     const int grid = (a.num_rows + rows_per_block - 1) / rows_per_block;
     if (grid == 0) return hipSuccess;
-    hipLaunchKernelGGL(append_rope_kernel, dim3(grid), dim3(kThreads), 0, s, a, log2_base);
+    hipLaunchKernelGGL(append_rope_kernel, dim3(grid), dim3(kThreads), 0, s, a, rope);
     return hipGetLastError();
 }
 
-hipError_t launch_append8(const Append8Args &a, hipStream_t s) {
+hipError_t launch_append8(const Append8Args &a, const RopeTable &rope, hipStream_t s) {
     if (a.num_blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL(append8_kernel, dim3(a.num_blocks), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(append8_kernel, dim3(a.num_blocks), dim3(kThreads), 0, s, a, rope);
     return hipGetLastError();
 }
 

@@ -27,8 +27,8 @@ static hipError_t harness_get_attribute(int *v, hipDeviceAttribute_t, int) {
 
 namespace mla {
 hipError_t launch_append(const AppendArgs &, hipStream_t) { return hipSuccess; }
-hipError_t launch_append_rope(const AppendArgs &, double, hipStream_t) { return hipSuccess; }
-hipError_t launch_append8(const Append8Args &, hipStream_t) { return hipSuccess; }
+hipError_t launch_append_rope(const AppendArgs &, const RopeTable &, hipStream_t) { return hipSuccess; }
+hipError_t launch_append8(const Append8Args &, const RopeTable &, hipStream_t) { return hipSuccess; }
 hipError_t launch_attention(const AttnArgs &, hipStream_t) { return hipSuccess; }
 hipError_t launch_combine(const AttnArgs &, hipStream_t) { return hipSuccess; }
 hipError_t read_flags(int *flags, bool) {
