@@ -68,11 +68,12 @@ __device__ __forceinline__ void issue8(const Source8 &s, uint32_t slot, uint32_t
 
 // decode_wg over the 8-bit cache.  Half the bytes a key (578), so a key has half the
 // time, and what bounds a group is the chain of a unit: wait, barrier, scores,
-// barrier, values.  Hence units of two tiles, 64 keys a barrier pair; each wave scores
-// 16 keys over all dims, takes their probabilities against the reference so far and
-// passes those on (not the scores, whose softmax every wave would repeat: HALF_FIGURES),
-// and then accumulates its 128 value dims over the 64 keys.  (Units of one tile, in a
-// ring of four slots: UNIT_FIGURES.)
+// barrier, values.  Hence units of two tiles, 64 keys a barrier pair (256 rows of up
+// to 16384 keys, with units of one tile in a ring of four slots 370 us, with two 329);
+// each wave scores 16 keys over all dims, takes their probabilities against the
+// reference so far and passes those on (the scores passed on instead, whose softmax
+// every wave then repeats: 329, so 307), and then accumulates its 128 value dims over
+// the 64 keys.
 // Keys are converted at the matrix instruction (two values an instruction, the scale of
 // the 16 keys applied on the way: bf16 holds the result exactly).  Values become fp16
 // relative to v_ref, the scale of the first blocks (raised, rarely, to what fp16

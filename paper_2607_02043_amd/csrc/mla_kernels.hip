@@ -835,8 +835,9 @@ __device__ __forceinline__ void group_barrier(int *ctr, int &epoch, int spin_lim
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Values that no row may read: a masked key has probability 0, but 0 times an
-// infinity or NaN is NaN.  The forms of mla_cache.h zero such values and leave it to
-// the key's score, which is not finite either, to reach the rows that see it.
+// infinity or NaN is NaN.  Where some row masks a key, the forms of mla_cache.h zero
+// such values and leave it to the key's score, which is not finite either, to reach
+// the rows that see it.
 // (Two bf16 values a word.)
 __device__ __forceinline__ uint32_t finite_bf16x2(uint32_t w) {
     if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
@@ -1271,11 +1272,10 @@ __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
 
 constexpr int kCT = kChunkBlockTokens;                 // 8 tokens per item, one per wave
 constexpr int kQSteps = kDqk / 32;                     // 18 query operands of 32 dims
-// The first of them stay in registers, the others (the rope ones) in LDS: with a
-// window the masks take the four registers of one more, and over the 8-bit cache
-// the conversion of the keys.
+// The first of them stay in registers, the others (the rope ones) in LDS: over a
+// bf16 cache with a window the masks take the four registers of one more.
 template <int F>
-constexpr int q_reg_steps = F == kPlain ? 16 : 15;
+constexpr int q_reg_steps = F == kPlain ? 16 : has_eight<F> ? 16 : 15;
 constexpr int kChunkRing = 3;
 constexpr int kPTile = kCT * 64 * 16;                  // fp16 P of one tile: [token][lane] 16 bytes
 template <int F>
@@ -1339,7 +1339,8 @@ struct ChunkKeys<true> {
 //   exact   then the item runs again against the exact max.
 // (Scores of a standard deviation of 2.6 take the second pass in most items of
 // 8192 keys.  The forms of mla_cache.h have the main pass alone and raise the
-// reference in it: 2048 rows over 8192 keys of such scores RAISE_FIGURES.)
+// reference in it: 2048 rows over 8192 keys of such scores take 741 us in two
+// passes, 506 so; of scores of a deviation of 1.7, 466 here and 504 so.)
 
 // Returns true when the main pass was abandoned: the caller then runs the
 // item again with exact = true (the exact maxima wait in LDS).
@@ -1477,19 +1478,22 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
 
     // the same over the 8-bit cache: five DMAs of each of the four waves, the scales among them
     [[maybe_unused]] auto issue8 = [&](int t, int slot, int page) {
-        const int kbase = ck.tile(t), ln = opaque_lane();
-        const uint32_t dst = ring + slot * kTile8Bytes;
-        const auto slot_of = [&](int key) {  // pool slot
-            const int k = min(key, k_end - 1);
-            return (size_t)s_pages[min(ck.entry(k), kPageWindow - 1)] * a.page_size + (k & (a.page_size - 1));
-        };
+        const int kbase = ck.tile(t);
+        const uint32_t dst = ring + slot * kTile8Bytes, scale_dst = lds_addr(s_scale) + slot * 32 + 16 * (dw - 2);
+        const int ln = opaque_lane();
         if (in_page && kbase + kChunkKeys <= k_end) {
-            const size_t first = (size_t)__builtin_amdgcn_readfirstlane(page) * a.page_size + (kbase & (a.page_size - 1));
-            dma_tile8(a.kv8 + first * kDqk, tile8_key(dw, ln) * kDqk + tile8_dims(dw, ln), dst, dw);
+            const uint32_t pg = __builtin_amdgcn_readfirstlane(page), in = kbase & (a.page_size - 1);
+            dma_tile8(a.kv8 + (size_t)pg * (uint32_t)(a.page_size * kDqk) + in * kDqk,
+                      tile8_key(dw, ln) * kDqk + tile8_dims(dw, ln), dst, dw);
+            if (dw >= 2) dma_scales8(a, (size_t)pg * (uint32_t)a.page_size + in + 16 * (dw - 2), scale_dst, ln);
         } else {
+            const auto slot_of = [&](int key) {  // pool slot
+                const int k = min(key, k_end - 1);
+                return (size_t)s_pages[min(ck.entry(k), kPageWindow - 1)] * a.page_size + (k & (a.page_size - 1));
+            };
             dma_tile8(a.kv8 + slot_of(kbase + tile8_key(dw, ln)) * kDqk + tile8_dims(dw, ln), dst, dw);
+            if (dw >= 2) dma_scales8(a, slot_of(kbase + 16 * (dw - 2)), scale_dst, ln);
         }
-        if (dw >= 2) dma_scales8(a, slot_of(kbase + 16 * (dw - 2)), lds_addr(s_scale) + slot * 32 + 16 * (dw - 2), ln);
     };
     // page of tile t, and its DMA into a ring slot
     auto issue_tile = [&](int t, int slot, int page) {
@@ -1502,10 +1506,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     const bool main_pass = !exact;
     float m_ref = kNegInf, l_run = 0.f;
     [[maybe_unused]] float m_lane = kNegInf;
-    // 8-bit cache: exponents of the scales of the tile being read, [key half], of the compressed and the rope dims; values are
-    // held relative to 2^v_exp, the accumulators too
-    constexpr int kNoExp = -1000;  // no block read yet
-    [[maybe_unused]] int ec[2] = {0, 0}, er[2] = {0, 0}, v_exp = kNoExp;
+    // 8-bit cache: scales of the tile being read, [key half], of the compressed and the rope dims; values (times sv) and
+    // accumulators are held relative to v_ref, the scale of the first blocks
+    [[maybe_unused]] float sc[2], sr[2], sv[2], v_ref = 0.f, v_inv = 0.f;
     f32x4 acc[kCT][4];  // [token][value block db]
 
     // Over the 8-bit cache: one 16-byte piece of a key a lane feeds two steps, converted on the way (exactly, scale
@@ -1538,37 +1541,52 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
                     qb = *reinterpret_cast<const u32x4 *>(s_q + (((st - kQRegSteps) * kCT + wv) * 64 + lane) * 16);
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
-                    s[kb] = mfma_bf16(bf16_of_e4m3x8(cur[kb][2 * e], cur[kb][2 * e + 1], exp2_bits(j < kGroups - 1 ? ec[kb] : er[kb])), qb, s[kb]);
+                    s[kb] = mfma_bf16(bf16_of_e4m3x8(cur[kb][2 * e], cur[kb][2 * e + 1], j < kGroups - 1 ? sc[kb] : sr[kb]), qb, s[kb]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // Scales of tile t in ring slot `slot`: the exponents, and the reference of the values raised (rarely) to what fp16
-    // holds; a key half that no row of the block sees has no say.
-    [[maybe_unused]] auto scales8 = [&](int t, int slot) {
-        const int kbase = ck.tile(t);
-        int most = kNoExp;
+    // Scales of tile t in ring slot `slot`.
+    [[maybe_unused]] auto read_scales8 = [&](int t, int slot, uint32_t (&w)[2]) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const int key = min(kbase + 16 * kb, k_end - 1);
+            const int key = min(ck.tile(t) + 16 * kb, k_end - 1);
             const int pg = a.page_size >= 64 ? 0 : s_pages[min(ck.entry(key), kPageWindow - 1)];
-            const uint32_t w = __builtin_amdgcn_readfirstlane(
-                *reinterpret_cast<const int *>(s_scale + slot * 32 + 16 * kb + 4 * scale_piece8(a, pg, key)));
-            ec[kb] = scale_exponent(w);
-            er[kb] = scale_exponent(w >> 16);
-            if (ec[kb] <= kMaxExp8 && (!has_window<F> || kbase + 16 * kb < a.band.sinks || kbase + 16 * kb + 15 > it.p + it.i0 - a.band.window))
-                most = max(most, ec[kb]);
+            w[kb] = *reinterpret_cast<const uint32_t *>(s_scale + slot * 32 + 16 * kb + 4 * scale_piece8(a, pg, key));
         }
-        if (v_exp == kNoExp) {
-            v_exp = most;
-        } else if (most > v_exp + 7) {  // 448 2^7 = 57344
-            const float f = exp2_bits(max(v_exp - most, -126));
-            v_exp = most;
+    };
+    [[maybe_unused]] auto scales8 = [&](const uint32_t (&w)[2]) {  // (scalar: the vector registers are all taken)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const uint32_t u = __builtin_amdgcn_readfirstlane(w[kb]);
+            sc[kb] = __uint_as_float(u << 16);
+            sr[kb] = __uint_as_float(u & 0xffff0000u);
+            sv[kb] = sc[kb] * v_inv;
+        }
+    };
+    // Raises the reference of the values (rarely; at an item's first tile) to what fp16 holds.  A key half that no row of
+    // the block sees has no say, and its scale may be anything; one that is no number belongs to such a half, or the
+    // scores of its keys are none either.
+    [[maybe_unused]] auto raise8 = [&](int t) {
+        const int kbase = ck.tile(t);
+        float most = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            sc[kb] = fabsf(sc[kb]) < INFINITY ? fabsf(sc[kb]) : 0.f;
+            if (!has_window<F> || kbase + 16 * kb < a.band.sinks || kbase + 16 * kb + 15 > it.p + it.i0 - a.band.window)
+                most = fmaxf(most, sc[kb]);
+        }
+        if (__builtin_amdgcn_ballot_w64(most > 128.f * v_ref) != 0) {  // 448 2^7 = 57344
+            const float f = v_ref / most;
+            v_ref = most;
+            v_inv = 1.f / most;
 #pragma unroll
             for (int tb = 0; tb < kCT; ++tb)
 #pragma unroll
                 for (int db = 0; db < 4; ++db) acc[tb][db] = acc[tb][db] * f;
         }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) sv[kb] = fminf(sc[kb] * v_inv, 128.f);
     };
     // S^T of tile t for this wave's token: lane l, element i of block kb =
     // key 16 kb + 4 g + i of the tile, head hd.  Two accumulation chains.
@@ -1605,6 +1623,12 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // Whether some row of the block does not see all of tile t.
+    [[maybe_unused]] auto hides = [&](int t) {
+        const int kbase = ck.tile(t), last = kbase + kChunkKeys - 1;
+        if (last > it.p + it.i0) return true;
+        return has_window<F> && kbase <= it.p + it.i1 - 1 - a.band.window && last >= a.band.sinks;
+    };
     // masked raw scores of tile t
     auto masked = [&](int t, const f32x4 (&s)[2], float (&x)[8]) {
         const int kbase = ck.tile(t);
@@ -1631,23 +1655,40 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     auto lane_max = [&](const float (&x)[8], float m) {
         return max3(max3(max3(max3(m, x[0], x[1]), x[2], x[3]), x[4], x[5]), x[6], x[7]);
     };
+    u32x4 av[4];  // V^T operands, see vload
     auto softmax = [&](int t, int pbuf, const f32x4 (&s)[2]) {
         float x[8];
         masked(t, s, x);
         if constexpr (F == kPlain) {
             m_lane = lane_max(x, m_lane);
         } else {
-            // The reference max is raised as soon as a score exceeds it by more than fp16 holds (also from nothing: rows
-            // may see their first key late); the factor of what is accumulated goes with P to the waves that hold it.
+            // One branch a tile for what is rare.  The reference max is raised as soon as a score exceeds it by more than
+            // fp16 holds (also from nothing: rows may see their first key late); the factor of what is accumulated goes
+            // with P to the waves that hold it.  In a tile that some row does not see whole, values that are not finite
+            // are zeroed (over a bf16 cache in vconv: here its operands would spill).
             const float tm = lane_max(x, kNegInf) * a.scale_log2;
-            if (__builtin_amdgcn_ballot_w64(tm > m_ref + kMaxPExp) != 0) {
-                const float m_new = fmaxf(m_ref, wave_max16(tm));
-                const float f = m_ref == kNegInf ? 0.f : exp2f(m_ref - m_new);
-                l_run *= f;
-                m_ref = m_new;
-                if (t > 0) {
-                    if (g == 0) s_raise[(pbuf * kCT + wv) * kHeads + hd] = f;
-                    if (lane == 0) s_raised[pbuf * kCT + wv] = t;
+            bool rare = tm > m_ref + kMaxPExp;
+            if constexpr (has_eight<F>) rare = rare || !(fmaxf(sv[0], sv[1]) <= 128.f) || v_ref == 0.f || hides(t);
+            if (__builtin_amdgcn_ballot_w64(rare) != 0) {
+                if constexpr (has_eight<F>) {
+                    raise8(t);
+                    if (hides(t) && any_not_finite(s[0] + s[1])) {
+#pragma unroll
+                        for (int db = 0; db < 4; ++db)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) av[db][i] = finite_e4m3x4(av[db][i]);
+                    }
+                }
+                if (__builtin_amdgcn_ballot_w64(tm > m_ref + kMaxPExp) != 0) {
+                    const float m_new = fmaxf(m_ref, wave_max16(tm));
+                    const float f = m_ref == kNegInf ? 0.f : exp2f(m_ref - m_new);
+                    l_run *= f;
+                    m_ref = m_new;
+                    if (t > 0) {
+                        const int ln = opaque_lane();
+                        if (ln < kHeads) s_raise[(pbuf * kCT + wv) * kHeads + ln] = f;
+                        if (ln == 0) s_raised[pbuf * kCT + wv] = t;
+                    }
                 }
             }
         }
@@ -1667,7 +1708,6 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // V^T operands of a tile for this wave's value dims, converted to fp16.
     // They are read and converted before the barrier that P waits for, so
     // that only the P reads stand between it and the first product.
-    u32x4 av[4];
     auto vload = [&](int slot) {
         if constexpr (has_eight<F>) {
             const char *tile = smem + __builtin_amdgcn_readfirstlane(slot * kTile8Bytes) + kQuad8 * wv + 8 * (lane & 1);
@@ -1694,12 +1734,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             // (half kt of the keys in word kt; a half whose scale is no number is not seen, or its scores are none either)
 #pragma unroll
             for (int db = 0; db < 4; ++db) {
-                if (careful) {
-                    av[db][0] = finite_e4m3x4(av[db][0]);
-                    av[db][1] = finite_e4m3x4(av[db][1]);
-                }
-                av[db] = f16_of_e4m3x8(av[db][0], av[db][1], exp2_bits(min(max(ec[0] - v_exp, -126), 7)),
-                                       exp2_bits(min(max(ec[1] - v_exp, -126), 7)));
+                av[db] = f16_of_e4m3x8(av[db][0], av[db][1], sv[0], sv[1]);
             }
             return;
         }
@@ -1719,8 +1754,16 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // O^T += V^T P^T for tile t (P from buffer t & 1)
     auto pv = [&](int t) {
         const int pbuf = t & 1;
+        const char *pb = s_pbuf + __builtin_amdgcn_readfirstlane(pbuf * kPTile) + lane * 16;
+        constexpr int PD = 3;  // P operands in flight
+        u32x4 bp[PD];
+        [[maybe_unused]] int raised_at = 0;
+        if constexpr (F != kPlain) raised_at = s_raised[pbuf * kCT + (lane & 7)];
+#pragma unroll
+        for (int tb = 0; tb < PD; ++tb) bp[tb] = *reinterpret_cast<const u32x4 *>(pb + tb * 64 * 16);
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (F != kPlain) {
-            const uint64_t raised = __builtin_amdgcn_ballot_w64(s_raised[pbuf * kCT + (lane & 7)] == t) & 0xff;
+            const uint64_t raised = __builtin_amdgcn_ballot_w64(raised_at == t) & 0xff;
             if (raised != 0) {
 #pragma unroll
                 for (int tb = 0; tb < kCT; ++tb) {
@@ -1731,12 +1774,6 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
                 }
             }
         }
-        const char *pb = s_pbuf + __builtin_amdgcn_readfirstlane(pbuf * kPTile) + lane * 16;
-        constexpr int PD = 3;  // P operands in flight
-        u32x4 bp[PD];
-#pragma unroll
-        for (int tb = 0; tb < PD; ++tb) bp[tb] = *reinterpret_cast<const u32x4 *>(pb + tb * 64 * 16);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int tb = 0; tb < kCT; ++tb) {
             const u32x4 cur = bp[tb % PD];
@@ -1779,7 +1816,11 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     TRACE_TILE(0, 11);
     {
         f32x4 s0[2];
-        if constexpr (has_eight<F>) scales8(0, 0);
+        if constexpr (has_eight<F>) {
+            uint32_t w[2];
+            read_scales8(0, 0, w);
+            scales8(w);
+        }
         scores(0, s0);
         if (F == kPlain && main_pass) {
             float x[8];
@@ -1788,14 +1829,19 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         vload(0);
         softmax(0, 0, s0);
-        vconv(F != kPlain && any_not_finite(s0[0] + s0[1]));
+        vconv(F == kWindow && hides(0) && any_not_finite(s0[0] + s0[1]));
     }
     int slot = 0;  // ring slot of tile t (t % 3)
+    [[maybe_unused]] int page_ahead = has_eight<F> ? page_of(min(2, ntiles - 1)) : 0;  // page of tile t + 2
     // steady state: after the barrier, P*V of tile t and the scores of t + 1,
     // then the softmax of t + 1
     for (int t = 0; t < ntiles; ++t) {
         TRACE_TILE(t, 11);
-        const int next_page = page_of(min(t + 2, ntiles - 1));
+        int next_page;
+        if constexpr (has_eight<F>)
+            next_page = page_ahead;
+        else
+            next_page = page_of(min(t + 2, ntiles - 1));
         if (t + 1 < ntiles) wait_dma_all();  // tile t + 1 (this wave's part)
         __syncthreads();  // tile t + 1 and P of tile t complete; slot (t + 2) % 3 and P buffer (t + 1) & 1 free
         TRACE_TILE(t, 12);
@@ -1803,15 +1849,20 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         const int slot2 = slot1 == kChunkRing - 1 ? 0 : slot1 + 1;
         if (dma_wave && t + 2 < ntiles) issue_tile(t + 2, slot2, next_page);
         TRACE_TILE(t, 14);
+        [[maybe_unused]] uint32_t w8[2];  // in flight over the products
+        if constexpr (has_eight<F>) {
+            read_scales8(min(t + 1, ntiles - 1), slot1, w8);
+            page_ahead = page_of(min(t + 3, ntiles - 1));
+        }
         pv(t);
         TRACE_TILE(t, 15);
         if (t + 1 < ntiles) {
             f32x4 s1[2];
-            if constexpr (has_eight<F>) scales8(t + 1, slot1);
+            if constexpr (has_eight<F>) scales8(w8);
             scores(slot1, s1);
             vload(slot1);
             softmax(t + 1, (t + 1) & 1, s1);
-            vconv(F != kPlain && any_not_finite(s1[0] + s1[1]));
+            vconv(F == kWindow && hides(t + 1) && any_not_finite(s1[0] + s1[1]));
         }
         slot = slot1;
         TRACE_TILE(t, 13);
@@ -1846,14 +1897,14 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         if (tb >= nt) break;
         const int row = it.row0 + it.i0 + tb;
         if (it.nks_eff == 1) {
-            const float inv = (has_eight<F> ? exp2_bits(max(v_exp, -126)) : 1.f) / s_l[tb * kHeads + hd];
+            const float inv = (has_eight<F> ? v_ref : 1.f) / s_l[tb * kHeads + hd];
 #pragma unroll
             for (int db = 0; db < 4; ++db) store_out4(a, row, hd, 64 * wv + 16 * db + 4 * ge, acc[tb][db] * inv);
         } else {
             const size_t prow = (size_t)item * kCT + tb;
             float *po = a.ws_chunk_o + (prow * kHeads + hd) * kDv + 64 * wv + 4 * ge;
 #pragma unroll
-            for (int db = 0; db < 4; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = has_eight<F> ? acc[tb][db] * exp2_bits(max(v_exp, -126)) : acc[tb][db];
+            for (int db = 0; db < 4; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = has_eight<F> ? acc[tb][db] * v_ref : acc[tb][db];
         }
     }
     if (g == 0 && wv < nt) {

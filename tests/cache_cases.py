@@ -44,7 +44,7 @@ def cache8(b, seed, upto=None):
     return data.reshape(b.num_pages, b.page_size, 576), scales.reshape(b.num_pages, b.page_size // 16, 2)
 
 
-def bounds(q, keys, pos, scale, window, sinks, fp16_p, fp32_out, ref_out, ref_lse):
+def bounds(q, keys, pos, scale, window, sinks, fp16_p, fp32_out, ref_out, ref_lse, top=0.0):
     """How far a row's out [16][512] and lse [16] may be from the 64-bit ones.
 
     Scores: fp32 sums of 576 exact products, 64 roundings of at most the sum of
@@ -54,6 +54,13 @@ def bounds(q, keys, pos, scale, window, sinks, fp16_p, fp32_out, ref_out, ref_ls
     2 delta max|v| and the log of the sum by delta.
     Probabilities: fp16 (chunk rows): half a step, 2^-11 of p, and 2^-25 where p is
     below fp16's normal range, each key once; a bf16 pair (decode rows) 2^-16.
+    Values of chunk rows over the 8-bit cache: fp16 relative to a reference scale.  A code
+    has 4 significant bits, so it is exact there down to fp16's normal range and a
+    multiple of 2^-24 below it: off by half of that at most, 2^-25 of the reference.
+    The reference is one for the 8 rows that are computed together and at most the
+    largest scale that one of them sees, `top`; a softmax average of such errors is
+    no larger.  (Far-apart scales alone make this term count: beside equal scales it
+    is below 2^-25 / 2^-11 of the fp16 term of the probabilities.)
     Sums of n terms in fp32 on top: n 2^-24 of the sum of magnitudes, by halves
     of the tree at least, 2^-24 (n / 8 + 8).  The output rounds once (2^-24 or 2^-8)."""
     at = CO.visible(pos, window, sinks)
@@ -62,5 +69,5 @@ def bounds(q, keys, pos, scale, window, sinks, fp16_p, fp32_out, ref_out, ref_ls
     delta = 64 * 2.0 ** -24 * scale * float((np.abs(q) @ np.abs(k).T).max())
     sums = 2.0 ** -24 * (n / 8 + 8)
     p = 2.0 ** -11 + n * 2.0 ** -25 if fp16_p else 2.0 ** -16
-    out = v * (2 * delta + p + 2 * sums) + np.abs(ref_out) * (2.0 ** -24 if fp32_out else 2.0 ** -8)
+    out = v * (2 * delta + p + 2 * sums) + 2.0 ** -25 * top + np.abs(ref_out) * (2.0 ** -24 if fp32_out else 2.0 ** -8)
     return out, delta + sums + 2.0 ** -22 * (1 + np.abs(ref_lse))

@@ -73,6 +73,15 @@ class Attend:
         torch.cuda.synchronize()
         return self.out.double().cpu().numpy(), self.lse.double().cpu().numpy()
 
+    def top_scale(self, r, i):
+        """8-bit chunk rows: the largest scale of compressed dims that the rows computed with row i of request r see."""
+        b, (w, s) = self.b, self.window or (0, 0)
+        if not self.eight or b.q_lens[r] == 1:
+            return 0.0
+        first, last = int(b.prefix_lens[r]) + i // 8 * 8, int(b.prefix_lens[r]) + min(i // 8 * 8 + 8, int(b.q_lens[r])) - 1
+        blocks = {k // 16 for k in range(last + 1) if not w or k > first - w or k < s}
+        return max(float(CO.scale_value(self.scales.reshape(-1, 2)[CO.slot(b, r, 16 * i) // 16, 0])) for i in blocks)
+
     def check(self, what, rows=None):
         out, lse = self.results()
         b, (w, s) = self.b, self.window or (0, 0)
@@ -85,7 +94,7 @@ class Attend:
                 keys, at = self.keys(r, int(b.prefix_lens[r] + b.q_lens[r])), r
             pos = int(b.prefix_lens[r]) + row - int(cu[r])
             ro, rl = CO.attend_row(q[row], keys, pos, SCALE, w, s)
-            to, tl = C.bounds(q[row], keys, pos, SCALE, w, s, b.q_lens[r] > 1, not self.bf16, ro, rl)
+            to, tl = C.bounds(q[row], keys, pos, SCALE, w, s, b.q_lens[r] > 1, not self.bf16, ro, rl, self.top_scale(r, row - int(cu[r])))
             eo, el = np.abs(out[row] - ro), np.abs(lse[row] - rl)
             worst = [max(worst[0], float((eo / to).max())), max(worst[1], float((el / tl).max()))]
             assert (eo <= to).all() and (el <= tl).all(), (what, row, pos, float((eo / to).max()), float((el / tl).max()))
@@ -464,6 +473,118 @@ def test_window_over_everything_is_plain_attention():
     mla.mixed_step_attn(a.db, a.qd, a.cache, SCALE, out, lse, mla.workspace_for(a.db))
     got, gl = a.results()
     assert np.abs(got - out.double().cpu().numpy()).max() <= 2e-3 and np.abs(gl - lse.double().cpu().numpy()).max() <= 1e-5
+
+
+def rope_queries(b, seed):
+    """Queries whose compressed dims are zero: scores come from the rope dims alone."""
+    q = C.queries(b, seed).reshape(-1, 16, 576)
+    q[:, :, :512] = 0
+    return q
+
+
+FAR = [([2500, 700, 95], [1, 1, 1], 16), ([300, 0, 61], [60, 33, 2], 16), ([900, 130], [1, 40], 64)]
+
+
+@pytest.mark.parametrize("window", [None, (130, 21)], ids=str)
+@pytest.mark.parametrize("prefix,rows,page", FAR, ids=ids)
+@pytest.mark.parametrize("order", ["rising", "falling", "random"])
+def test_scales_far_apart(prefix, rows, page, window, order):
+    """Compressed scales from 2^-100 to 2^110 among the blocks of a request: the values exceed what fp16 holds
+    beside one another many times over.  Scores come from the rope dims."""
+    b = C.batch(prefix, rows, page, seed=31)
+    data, scales = C.cache8(b, 5, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+    rng = np.random.default_rng(31)
+    flat = scales.reshape(-1, 2)
+    for r in range(b.num_reqs):
+        n = -(-int(b.prefix_lens[r] + b.q_lens[r]) // 16)
+        e = rng.integers(-100, 111, n)
+        e = np.sort(e) if order == "rising" else np.sort(e)[::-1] if order == "falling" else e
+        for i in range(n):
+            flat[CO.slot(b, r, 16 * i) // 16, 0] = CO.scale_bits(np.array([e[i]]))[0]
+    Attend(b, rope_queries(b, 3), data, scales, window=window).run().check(f"scales {order}")
+    assert mla.device_flags() == 0
+
+
+@pytest.mark.parametrize("first", [True, False], ids=["loud first", "loud last"])
+@pytest.mark.parametrize("rows", [1, 30])
+def test_small_values_beside_an_unlikely_loud_block(rows, first):
+    """A block whose values are 2^15 times the others' and whose probability is zero.  Values relative to 2^15 are
+    exact in fp16 (the smallest code, 2^-9, becomes 2^-24), so the rows' bounds are those without the block."""
+    b = C.batch([200], [rows], 16, seed=32)
+    data, scales = C.cache8(b, 6, upto=lambda r: 200 + rows)
+    flat, codes = scales.reshape(-1, 2), data.reshape(-1, 576)
+    loud = 0 if first else 11  # block of 16 keys
+    for i in range(-(-(200 + rows) // 16)):
+        flat[CO.slot(b, 0, 16 * i) // 16, 0] = CO.scale_bits(np.array([9 if i == loud else -6]))[0]
+    q = rope_queries(b, 4)
+    q[:, :, 575] = W.f32_to_bf16_bits(np.array([100.0], np.float32))[0]
+    for t in range(200 + rows):  # the loud block's scores: 100 x -448 x its scale (2^-9 at least) below the others'
+        codes[CO.slot(b, 0, t), 575] = 0xFE if t // 16 == loud else 0
+    flat[CO.slot(b, 0, 16 * loud) // 16, 1] = CO.scale_bits(np.array([4]))[0]
+    a = Attend(b, q, data, scales).run()
+    out, lse = a.results()
+    keys = CO.keys8(b, 0, 200 + rows, data, scales)
+    quiet = np.arange(200 + rows) // 16 != loud
+    qv = CO.bf16_value(q).reshape(-1, 16, 576)
+    for row in range(rows):
+        pos = 200 + row
+        ro, rl = CO.attend_row(qv[row], keys, pos, SCALE, 0, 0)
+        few = keys[quiet]
+        to, tl = C.bounds(qv[row], few, int(quiet[:pos + 1].sum()) - 1, SCALE, 0, 0, rows > 1, True, ro, rl)
+        assert (np.abs(out[row] - ro) <= to).all() and (np.abs(lse[row] - rl) <= tl).all(), (row, float((np.abs(out[row] - ro) / to).max()))
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("bits", [0x7FC0, 0xFFC0, 0x7F80, 0xFF80, 0x7F7F, 0xFF7F, 0x0000, 0x0001])
+def test_any_scale_where_no_row_looks(bits, page):
+    """Blocks that no row sees: any bits as their scales, NaN as their codes, beside seen blocks of the same tile."""
+    window = (50, 5)
+    b = C.batch([700, 405, 93, 1200], [1, 33, 1, 9], page, seed=33)
+    data, scales = C.cache8(b, 2, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+    a = Attend(b, C.queries(b, 1), data, scales, window=window).run()
+    a.check("before")
+    want = a.results()
+    d, s = data.copy().reshape(-1, 576), scales.copy().reshape(-1, 2)
+    for r in range(b.num_reqs):
+        for i in range(int(b.prefix_lens[r]) // 16):
+            if 16 * i >= window[1] and 16 * i + 15 <= int(b.prefix_lens[r]) - window[0]:
+                at = CO.slot(b, r, 16 * i)
+                s[at // 16] = bits
+                d[at:at + 16, ::3] = C.NAN8
+    a.cache.data.copy_(up8(d.reshape(data.shape)))
+    import torch
+    a.cache.scales.view(torch.int16).copy_(to_dev(s.reshape(scales.shape)))
+    for x, y in zip(want, a.run().results()):
+        np.testing.assert_array_equal(x, y)
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Captured one after the other on the same workspace, replayed in both orders, eager calls between."""
+    import torch
+    made = []
+    for seed, rows, window in ((34, [1, 60, 1], None), (35, [1, 1, 17], (300, 3))):
+        b = C.batch([3000, 500, 100], rows, 64, seed=seed)
+        data, scales = C.cache8(b, seed, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r]))
+        made.append(Attend(b, C.queries(b, seed), data, scales, window=window))
+    made[0].ws = made[1].ws = max((a.ws for a in made), key=lambda w: w.numel())
+    want = [a.run().results() for a in made]
+    s, graphs = torch.cuda.Stream(), []
+    for a in made:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            a.run()
+        graphs.append(g)
+    for order in ((0, 1), (1, 0), (0, 0), (1, 1)):
+        for a in made:
+            a.out.fill_(float("nan"))
+        for i in order:
+            graphs[i].replay()
+        for i in set(order):
+            for x, y in zip(want[i], made[i].results()):
+                np.testing.assert_array_equal(x, y)
+            made[i].run()
+            for x, y in zip(want[i], made[i].results()):
+                np.testing.assert_array_equal(x, y)
 
 
 # ------------------------------------------------------------------ together
