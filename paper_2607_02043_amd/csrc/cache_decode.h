@@ -145,6 +145,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     for (int mt = 0; mt < 8; ++mt) acc[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_ref = kNegInf, l_run = 0.f;
     float v_ref = 0.f, v_inv = 0.f;  // 0: no block read yet
+    bool first = true;               // the unit to come is the first of its segment
     // value operand: slots 8 g + 4 kt + i of a tile hold keys 16 kt + 4 g + i, as the probabilities do
     const int tr = (lane & 15) >> 1, tr_key = 4 * g + (tr & 3) + 16 * (tr >> 2);
 
@@ -227,8 +228,18 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
                 u32x4{__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1),
                       f16x2_bits(p[0] - (float)h0[0], p[1] - (float)h0[1]), f16x2_bits(p[2] - (float)h1[0], p[3] - (float)h1[1])};
         };
+        // the reference for all four waves, from their maxima
+        const auto raise = [&] {
+            mt = wave_max16(mt);
+            if (g == 0) s_stat[gw * kHeads + h] = mt;
+            group_barrier(gbar, epoch, a.spin_limit);
+            mt = fmaxf(fmaxf(s_stat[h], s_stat[kHeads + h]), fmaxf(s_stat[2 * kHeads + h], s_stat[3 * kHeads + h]));
+            return fmaxf(m_ref, mt - kRef8);
+        };
+        if (first) m_ref = raise();
         probabilities();
-        const bool above = __builtin_amdgcn_ballot_w64(mt > m_ref + kRaise8) != 0;
+        const bool above = !first && __builtin_amdgcn_ballot_w64(mt > m_ref + kRaise8) != 0;
+        first = false;
         if (lane == 0) s_sign[gw] = (above ? 1 : 0) | (careful ? 2 : 0);
         // values of this wave's 128 dims, before the probabilities are complete
         u32x2 vraw[2][8];
@@ -245,13 +256,8 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         for (int kt = 0; kt < 4; ++kt) pb[kt] = *reinterpret_cast<const u32x4 *>(s_X + (kt * 64 + lane) * 16);
         signs = __builtin_amdgcn_readfirstlane(signs);
         if ((signs & 1) != 0) {
-            // a score far above the reference (rarely; always at a segment's start): raised for all four waves, from their
-            // maxima, and the probabilities once more
-            mt = wave_max16(mt);
-            if (g == 0) s_stat[gw * kHeads + h] = mt;
-            group_barrier(gbar, epoch, a.spin_limit);
-            mt = fmaxf(fmaxf(s_stat[h], s_stat[kHeads + h]), fmaxf(s_stat[2 * kHeads + h], s_stat[3 * kHeads + h]));
-            const float m_new = fmaxf(m_ref, mt - kRef8);
+            // a score far above the reference (rarely): raised, and the probabilities once more
+            const float m_new = raise();
             const float alpha = (m_ref == kNegInf) ? 0.f : exp2f(m_ref - m_new);
 #pragma unroll
             for (int m = 0; m < 8; ++m) acc[m] = acc[m] * alpha;
@@ -322,6 +328,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
             m_ref = kNegInf;
             l_run = 0.f;
             v_ref = 0.f;
+            first = true;
         }
     }
     TRACE(4);

@@ -61,7 +61,7 @@ __device__ __forceinline__ int tile8_key(int w, int lane) { return 16 * (w & 1) 
 __device__ __forceinline__ int tile8_dims(int w, int lane) {
     return 64 * (w >> 1) + 16 * ((lane & 3) ^ swz8(tile8_key(w, lane)));
 }
-__device__ __forceinline__ void dma_tile8(const uint8_t *src, uint32_t voff, uint32_t slot, int w) {  // uniform src, a page's keys
+__device__ __forceinline__ void dma_tile8(const uint8_t *src, uint32_t voff, uint32_t slot, int w) {  // uniform src
     const uint32_t dst = slot + 1024 * w;
 #define MLA_DMA8(i) lds_dma16_sbase_imm<128 * (i)>(src, voff, __builtin_amdgcn_readfirstlane(dst + 4096 * (i)))
     MLA_DMA8(0); MLA_DMA8(1); MLA_DMA8(2); MLA_DMA8(3);

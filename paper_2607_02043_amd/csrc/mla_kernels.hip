@@ -1438,7 +1438,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     const bool fused = F == kPlain && a.new_kv != nullptr;
     const int cached_end = fused ? min(k_end, it.p) : k_end;
     auto page_of = [&](int t) {
-        return s_pages[min(ck.entry(ck.tile(t)), kPageWindow - 1)];
+        return s_pages[min(ck.entry(ck.tile(t) + (has_eight<F> ? 16 * (dw & 1) : 0)), kPageWindow - 1)];
     };
     [[maybe_unused]] const auto opaque_lane = [&] {
         int l = lane;
@@ -1476,16 +1476,17 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
     };
 
-    // the same over the 8-bit cache: five DMAs of each of the four waves, the scales among them
+    // The same over the 8-bit cache: five DMAs of each of the four waves, the scales among them.  A wave's 16 keys are in
+    // one page (16 tokens at least).
     [[maybe_unused]] auto issue8 = [&](int t, int slot, int page) {
         const int kbase = ck.tile(t);
         const uint32_t dst = ring + slot * kTile8Bytes, scale_dst = lds_addr(s_scale) + slot * 32 + 16 * (dw - 2);
         const int ln = opaque_lane();
-        if (in_page && kbase + kChunkKeys <= k_end) {
-            const uint32_t pg = __builtin_amdgcn_readfirstlane(page), in = kbase & (a.page_size - 1);
+        if (kbase + kChunkKeys <= k_end) {
+            const uint32_t pg = __builtin_amdgcn_readfirstlane(page), in = (kbase + 16 * (dw & 1)) & (a.page_size - 1);
             dma_tile8(a.kv8 + (size_t)pg * (uint32_t)(a.page_size * kDqk) + in * kDqk,
-                      tile8_key(dw, ln) * kDqk + tile8_dims(dw, ln), dst, dw);
-            if (dw >= 2) dma_scales8(a, (size_t)pg * (uint32_t)a.page_size + in + 16 * (dw - 2), scale_dst, ln);
+                      (tile8_key(dw, ln) & 15) * kDqk + tile8_dims(dw, ln), dst, dw);
+            if (dw >= 2) dma_scales8(a, (size_t)pg * (uint32_t)a.page_size + in, scale_dst, ln);
         } else {
             const auto slot_of = [&](int key) {  // pool slot
                 const int k = min(key, k_end - 1);
