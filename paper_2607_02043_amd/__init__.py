@@ -402,9 +402,9 @@ class LatentCache8:
             # 4 bytes a block of 16 tokens, rounded up to 16
             whole = torch.ones(n // 2, dtype=torch.bfloat16, device=device)
             scales = whole[:num_pages * (page_size // MLA_CACHE8_BLOCK) * 2].view(num_pages, page_size // MLA_CACHE8_BLOCK, 2)
-        if data.element_size() != 1 or data.dim() != 3 or data.shape[2] != D_QK or not data.is_contiguous():
+        if data.dtype not in (torch.uint8, torch.float8_e4m3fn) or data.dim() != 3 or data.shape[2] != D_QK or not data.is_contiguous():
             raise ValueError("data must be contiguous uint8 [num_pages][P][576]")
-        if (scales.element_size() != 2 or tuple(scales.shape) != (data.shape[0], data.shape[1] // MLA_CACHE8_BLOCK, 2) or
+        if (scales.dtype not in _bf16() or tuple(scales.shape) != (data.shape[0], data.shape[1] // MLA_CACHE8_BLOCK, 2) or
                 not scales.is_contiguous()):
             raise ValueError("scales must be contiguous bf16 [num_pages][P / 16][2]")
         self.data, self.scales = data, scales
@@ -414,68 +414,101 @@ class LatentCache8:
 
 def _window(window):
     """(window, sinks) -> a pointer for the C ABI (None: no window)."""
-    return None if window is None else ctypes.byref(mla_window(int(window[0]), int(window[1])))
+    if window is None:
+        return None
+    w, s = (int(v) for v in window)
+    if max(w, s) >= 1 << 31 or min(w, s) < -(1 << 31):
+        raise ValueError(f"window {w}, sinks {s}: outside 32 bits")
+    return ctypes.byref(mla_window(w, s))
 
 
-def _cache8(batch: DeviceBatch, cache: LatentCache8):
-    if cache.page_size != batch.page_size or cache.num_pages < batch.num_pages:
-        raise ValueError("the cache's pages do not match the batch's")
-    _dev(cache.data, "the cache's data", tuple(cache.data.shape), (1,))
-    return ctypes.byref(cache.c)
-
-
-def _dev(t, name, shape, itemsizes):
-    """Address of a contiguous device tensor of that shape, on the current device."""
-    import torch
-    if t.element_size() not in itemsizes or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {' or '.join(map(str, itemsizes))}-byte values")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+def _dev(t, name, shape, kinds, here):
+    """Address of a contiguous tensor of that shape and one of those types, on device `here`."""
+    if t.dtype not in kinds or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {' or '.join(map(str, kinds))}")
+    _on_device(t, name, here)
     return t.data_ptr()
 
 
-def _attend_args(batch: DeviceBatch, softmax_scale, out, lse, workspace):
+def _here() -> int:
+    """The current device (-2 before the first use of one: then no tensor is on it)."""
+    import torch
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+
+
+def _on_device(t, name, here):
+    if t.get_device() != here:  # (-1: not on a device)
+        raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+
+
+def _bf16():
+    """bf16, or its bits."""
+    import torch
+    return torch.bfloat16, torch.uint16, torch.int16
+
+
+def _batch(batch: DeviceBatch, here):
+    _on_device(batch.bt_dev, "the batch", here)
+    return ctypes.byref(batch.c)
+
+
+def _cache8(batch: DeviceBatch, cache: LatentCache8, here):
+    if cache.page_size != batch.page_size or cache.num_pages < batch.num_pages:
+        raise ValueError("the cache's pages do not match the batch's")
+    _on_device(cache.data, "the cache's data", here)
+    _on_device(cache.scales, "the cache's scales", here)
+    return ctypes.byref(cache.c)
+
+
+def _attend_args(batch: DeviceBatch, softmax_scale, out, lse, workspace, here):
+    import torch
     T = batch.num_rows
     if workspace is not None:
-        _dev(workspace, "workspace", tuple(workspace.shape), (workspace.element_size(),))
-    return (float(softmax_scale), _dev(out, "out", (T, NUM_HEADS, D_V), (2, 4)), _out_mode(out),
-            0 if lse is None else _dev(lse, "lse", (T, NUM_HEADS), (4,)), _ptr(workspace), _nbytes(workspace))
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        _on_device(workspace, "workspace", here)
+    return (float(softmax_scale), _dev(out, "out", (T, NUM_HEADS, D_V), (torch.float32, *_bf16()), here), _out_mode(out),
+            0 if lse is None else _dev(lse, "lse", (T, NUM_HEADS), (torch.float32,), here), _ptr(workspace), _nbytes(workspace))
 
 
-def _queries(batch: DeviceBatch, q):
-    return _dev(q, "q", (batch.num_rows, NUM_HEADS, D_QK), (2,))
+def _queries(batch: DeviceBatch, q, here):
+    return _dev(q, "q", (batch.num_rows, NUM_HEADS, D_QK), _bf16(), here)
 
 
-def _pool(batch: DeviceBatch, kv_cache):
+def _pool(batch: DeviceBatch, kv_cache, here):
     if kv_cache.shape[0] < batch.num_pages:
         raise ValueError(f"kv_cache has {kv_cache.shape[0]} pages, the batch's pool {batch.num_pages}")
-    return _dev(kv_cache, "kv_cache", (kv_cache.shape[0], batch.page_size, D_QK), (2,))
+    return _dev(kv_cache, "kv_cache", (kv_cache.shape[0], batch.page_size, D_QK), _bf16(), here)
 
 
 def append_latent_kv_rope(batch: DeviceBatch, new_latents, rope_base: float, kv_cache, stream=None) -> None:
     """append_latent_kv of bf16 latents [T][576] whose 64 rope dims are rotated to their positions on the way."""
-    _check(lib().append_latent_kv_rope(ctypes.byref(batch.c), _dev(new_latents, "new_latents", (batch.num_rows, D_QK), (2,)),
-                                       float(rope_base), _pool(batch, kv_cache), _stream(stream)))
+    here = _here()
+    _check(lib().append_latent_kv_rope(_batch(batch, here), _dev(new_latents, "new_latents", (batch.num_rows, D_QK), _bf16(), here),
+                                       float(rope_base), _pool(batch, kv_cache, here), _stream(stream)))
 
 
 def append_latent_kv8(batch: DeviceBatch, new_latents, cache: LatentCache8, rope_base: float = 0.0, stream=None) -> None:
     """Append bf16 latents [T][576] into the 8-bit cache; rope_base 0: they are rotated already."""
-    _check(lib().append_latent_kv8(ctypes.byref(batch.c), _dev(new_latents, "new_latents", (batch.num_rows, D_QK), (2,)),
-                                   float(rope_base), _cache8(batch, cache), _stream(stream)))
+    here = _here()
+    _check(lib().append_latent_kv8(_batch(batch, here), _dev(new_latents, "new_latents", (batch.num_rows, D_QK), _bf16(), here),
+                                   float(rope_base), _cache8(batch, cache, here), _stream(stream)))
 
 
 def mixed_step_attn8(batch: DeviceBatch, q, cache: LatentCache8, softmax_scale: float, out, lse=None, workspace=None,
                      window=None, stream=None) -> None:
     """mixed_step_attn over the 8-bit cache; window: (window, sinks) or None."""
-    _check(lib().mixed_step_attn8(ctypes.byref(batch.c), _queries(batch, q), _cache8(batch, cache), _window(window),
-                                  *_attend_args(batch, softmax_scale, out, lse, workspace), _stream(stream)))
+    here = _here()
+    _check(lib().mixed_step_attn8(_batch(batch, here), _queries(batch, q, here), _cache8(batch, cache, here), _window(window),
+                                  *_attend_args(batch, softmax_scale, out, lse, workspace, here), _stream(stream)))
 
 
 def mixed_step_attn_window(batch: DeviceBatch, q, kv_cache, window, softmax_scale: float, out, lse=None, workspace=None,
                            stream=None) -> None:
     """mixed_step_attn through a window of keys and a few first tokens, (window, sinks)."""
-    _check(lib().mixed_step_attn_window(ctypes.byref(batch.c), _queries(batch, q), _pool(batch, kv_cache), _window(window),
-                                        *_attend_args(batch, softmax_scale, out, lse, workspace), _stream(stream)))
+    here = _here()
+    _check(lib().mixed_step_attn_window(_batch(batch, here), _queries(batch, q, here), _pool(batch, kv_cache, here), _window(window),
+                                        *_attend_args(batch, softmax_scale, out, lse, workspace, here), _stream(stream)))
 
 
 def _workspace(query, batch: DeviceBatch, window, device):

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <exception>
 
 #include "api_util.h"
 #include "mla_kernels.h"
@@ -81,13 +82,27 @@ int make_form(const mla_batch *batch, bool eight, const mla_window *window, mla:
     return MLA_OK;
 }
 
+// Runs an entry point's body: an exception (the planner and check mode take host memory) becomes its error.
+template <class Body>
+int guarded(const Body &body) {
+    try {
+        return body();
+    } catch (const std::exception &e) {
+        return set_error(MLA_ERR_HIP, "host side: %s", e.what());
+    }
+}
+
 size_t workspace(const mla_batch *batch, const mla_window *window, bool eight) {
-    int T = 0;
-    mla::Form form;
-    if (mla::batch_rows(batch, &T) != MLA_OK || batch->num_reqs == 0) return 0;
-    if (make_form(batch, eight, window, &form) != MLA_OK) return 0;
     size_t bytes = 0;
-    return mla::attn_workspace(batch, &bytes, mla::kAbsorbAll, form) == MLA_OK ? bytes : 0;
+    const int st = guarded([&]() -> int {
+        int T = 0;
+        mla::Form form;
+        int st = mla::batch_rows(batch, &T);
+        if (st != MLA_OK || batch->num_reqs == 0) return st;
+        if ((st = make_form(batch, eight, window, &form)) != MLA_OK) return st;
+        return mla::attn_workspace(batch, &bytes, mla::kAbsorbAll, form);
+    });
+    return st == MLA_OK ? bytes : 0;
 }
 
 }  // namespace
@@ -101,62 +116,66 @@ size_t mla_cache8_scale_bytes(int32_t num_pages, int32_t page_size) {
 }
 
 int append_latent_kv_rope(const mla_batch *batch, const uint16_t *new_latents, float rope_base, uint16_t *kv_cache, void *stream) {
-    int T = 0, log2_page = 0;
-    int st = mla::batch_shape(batch, &T, &log2_page);
-    if (st != MLA_OK || batch->num_reqs == 0) return st;
-    if ((st = check_new(new_latents)) != MLA_OK || (st = check_base(rope_base, false)) != MLA_OK) return st;
-    if (!kv_cache || misaligned(kv_cache)) return set_error(MLA_ERR_INVALID_ARG, "kv_cache is NULL or not 16-byte aligned");
-    mla::AppendArgs a;
-    a.src = new_latents;
-    a.kv = kv_cache;
-    a.cu_q = batch->cu_q_dev;
-    a.prefix = batch->prefix_lens_dev;
-    a.bt = batch->block_table_dev;
-    a.num_reqs = batch->num_reqs;
-    a.num_rows = T;
-    a.page_size = batch->page_size;
-    a.log2_page = log2_page;
-    a.max_pages = batch->max_pages_per_req;
-    a.num_pages = batch->num_pages;
-    if ((st = mla::check_before(batch, {}, stream)) != MLA_OK) return st;
-    const hipError_t e = mla::launch_append_rope(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return mla::hip_error(e, "append kernel launch");
-    return mla::check_after("append_latent_kv_rope", stream);
+    return guarded([&]() -> int {
+        int T = 0, log2_page = 0;
+        int st = mla::batch_shape(batch, &T, &log2_page);
+        if (st != MLA_OK || batch->num_reqs == 0) return st;
+        if ((st = check_new(new_latents)) != MLA_OK || (st = check_base(rope_base, false)) != MLA_OK) return st;
+        if (!kv_cache || misaligned(kv_cache)) return set_error(MLA_ERR_INVALID_ARG, "kv_cache is NULL or not 16-byte aligned");
+        mla::AppendArgs a;
+        a.src = new_latents;
+        a.kv = kv_cache;
+        a.cu_q = batch->cu_q_dev;
+        a.prefix = batch->prefix_lens_dev;
+        a.bt = batch->block_table_dev;
+        a.num_reqs = batch->num_reqs;
+        a.num_rows = T;
+        a.page_size = batch->page_size;
+        a.log2_page = log2_page;
+        a.max_pages = batch->max_pages_per_req;
+        a.num_pages = batch->num_pages;
+        if ((st = mla::check_before(batch, {}, stream)) != MLA_OK) return st;
+        const hipError_t e = mla::launch_append_rope(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return mla::hip_error(e, "append kernel launch");
+        return mla::check_after("append_latent_kv_rope", stream);
+    });
 }
 
 int append_latent_kv8(const mla_batch *batch, const uint16_t *new_latents, float rope_base, const mla_cache8 *cache, void *stream) {
-    int T = 0, log2_page = 0;
-    int st = mla::batch_shape(batch, &T, &log2_page);
-    if (st != MLA_OK || batch->num_reqs == 0) return st;
-    mla::Form form;
-    if ((st = make_form(batch, true, nullptr, &form)) != MLA_OK || (st = check_cache8(cache)) != MLA_OK ||
-        (st = check_new(new_latents)) != MLA_OK || (st = check_base(rope_base, true)) != MLA_OK)
-        return st;
-    long long blocks = 0;
-    for (int r = 0; r < batch->num_reqs; ++r) {
-        const long long p = batch->prefix_lens[r], last = p + batch->q_lens[r] - 1;
-        blocks += last / MLA_CACHE8_BLOCK - p / MLA_CACHE8_BLOCK + 1;
-    }
-    mla::Append8Args a;
-    a.src = new_latents;
-    a.data = cache->data;
-    a.scales = cache->scales;
-    a.cu_q = batch->cu_q_dev;
-    a.prefix = batch->prefix_lens_dev;
-    a.bt = batch->block_table_dev;
-    a.rotate = rope_base != 0.f;
-    a.num_reqs = batch->num_reqs;
-    a.num_rows = T;
-    a.num_blocks = (int)blocks;  // at most one per row
-    a.log2_page = log2_page;
-    a.page_size = batch->page_size;
-    a.max_pages = batch->max_pages_per_req;
-    a.num_pages = batch->num_pages;
-    const mla::CheckUse use{MLA_CACHE8_BLOCK, 0, 0};
-    if ((st = mla::check_before(batch, use, stream)) != MLA_OK) return st;
-    const hipError_t e = mla::launch_append8(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return mla::hip_error(e, "8-bit append kernel launch");
-    return mla::check_after("append_latent_kv8", stream);
+    return guarded([&]() -> int {
+        int T = 0, log2_page = 0;
+        int st = mla::batch_shape(batch, &T, &log2_page);
+        if (st != MLA_OK || batch->num_reqs == 0) return st;
+        mla::Form form;
+        if ((st = make_form(batch, true, nullptr, &form)) != MLA_OK || (st = check_cache8(cache)) != MLA_OK ||
+            (st = check_new(new_latents)) != MLA_OK || (st = check_base(rope_base, true)) != MLA_OK)
+            return st;
+        long long blocks = 0;
+        for (int r = 0; r < batch->num_reqs; ++r) {
+            const long long p = batch->prefix_lens[r], last = p + batch->q_lens[r] - 1;
+            blocks += last / MLA_CACHE8_BLOCK - p / MLA_CACHE8_BLOCK + 1;
+        }
+        mla::Append8Args a;
+        a.src = new_latents;
+        a.data = cache->data;
+        a.scales = cache->scales;
+        a.cu_q = batch->cu_q_dev;
+        a.prefix = batch->prefix_lens_dev;
+        a.bt = batch->block_table_dev;
+        a.rotate = rope_base != 0.f;
+        a.num_reqs = batch->num_reqs;
+        a.num_rows = T;
+        a.num_blocks = (int)blocks;  // at most one per row
+        a.log2_page = log2_page;
+        a.page_size = batch->page_size;
+        a.max_pages = batch->max_pages_per_req;
+        a.num_pages = batch->num_pages;
+        const mla::CheckUse use{MLA_CACHE8_BLOCK, 0, 0};
+        if ((st = mla::check_before(batch, use, stream)) != MLA_OK) return st;
+        const hipError_t e = mla::launch_append8(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return mla::hip_error(e, "8-bit append kernel launch");
+        return mla::check_after("append_latent_kv8", stream);
+    });
 }
 
 size_t mixed_step_attn8_workspace_bytes(const mla_batch *batch, const mla_window *window) { return workspace(batch, window, true); }
@@ -168,27 +187,31 @@ size_t mixed_step_attn_window_workspace_bytes(const mla_batch *batch, const mla_
 int mixed_step_attn8(const mla_batch *batch, const uint16_t *q, const mla_cache8 *cache, const mla_window *window,
                      float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace, size_t workspace_bytes,
                      void *stream) {
-    int T = 0;
-    mla::Form form;
-    int st = mla::batch_rows(batch, &T);
-    if (st != MLA_OK || batch->num_reqs == 0) return st;
-    if ((st = make_form(batch, true, window, &form)) != MLA_OK || (st = check_cache8(cache)) != MLA_OK) return st;
-    form.kv8 = cache->data;
-    form.kv8_scales = cache->scales;
-    return mla::attend_form(batch, q, nullptr, form, softmax_scale, out, out_dtype, lse, workspace, workspace_bytes, stream,
-                            "mixed_step_attn8");
+    return guarded([&]() -> int {
+        int T = 0;
+        mla::Form form;
+        int st = mla::batch_rows(batch, &T);
+        if (st != MLA_OK || batch->num_reqs == 0) return st;
+        if ((st = make_form(batch, true, window, &form)) != MLA_OK || (st = check_cache8(cache)) != MLA_OK) return st;
+        form.kv8 = cache->data;
+        form.kv8_scales = cache->scales;
+        return mla::attend_form(batch, q, nullptr, form, softmax_scale, out, out_dtype, lse, workspace, workspace_bytes, stream,
+                                "mixed_step_attn8");
+    });
 }
 
 int mixed_step_attn_window(const mla_batch *batch, const uint16_t *q, const uint16_t *kv_cache, const mla_window *window,
                            float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace, size_t workspace_bytes,
                            void *stream) {
-    int T = 0;
-    mla::Form form;
-    int st = mla::batch_rows(batch, &T);
-    if (st != MLA_OK || batch->num_reqs == 0) return st;
-    if ((st = make_form(batch, false, window, &form)) != MLA_OK) return st;
-    return mla::attend_form(batch, q, kv_cache, form, softmax_scale, out, out_dtype, lse, workspace, workspace_bytes, stream,
-                            "mixed_step_attn_window");
+    return guarded([&]() -> int {
+        int T = 0;
+        mla::Form form;
+        int st = mla::batch_rows(batch, &T);
+        if (st != MLA_OK || batch->num_reqs == 0) return st;
+        if ((st = make_form(batch, false, window, &form)) != MLA_OK) return st;
+        return mla::attend_form(batch, q, kv_cache, form, softmax_scale, out, out_dtype, lse, workspace, workspace_bytes, stream,
+                                "mixed_step_attn_window");
+    });
 }
 
 }  // extern "C"

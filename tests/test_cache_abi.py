@@ -177,3 +177,23 @@ def test_python_refuses_other_shapes_and_strides():
             mla.mixed_step_attn8(b, a["q"], c, 0.07, a["out"], a["lse"])
         with pytest.raises((ValueError, TypeError)):
             mla.mixed_step_attn_window(b, a["q"], kv, (4, 0), 0.07, a["out"], a["lse"])
+
+
+def test_python_refuses_other_types_devices_and_windows():
+    b = mla.DeviceBatch([1, 2], [3, 0], np.zeros((2, 1)), 32, 3, device="cpu")
+    c = mla.LatentCache8(num_pages=3, page_size=32, device="cpu")
+    new, q, out = torch.zeros((3, 576), dtype=torch.bfloat16), torch.zeros((3, 16, 576), dtype=torch.bfloat16), torch.zeros((3, 16, 512))
+    with pytest.raises(ValueError, match="batch is on cpu"):
+        mla.append_latent_kv8(b, new, c)
+    with pytest.raises(ValueError, match="float16"):
+        mla._dev(new.half(), "new_latents", (3, 576), mla._bf16(), 0)
+    with pytest.raises(ValueError, match="on cpu"):
+        mla._dev(new, "new_latents", (3, 576), mla._bf16(), 0)
+    for data, scales in ((c.data.bool(), c.scales), (c.data.view(torch.int8), c.scales), (c.data, c.scales.half())):
+        with pytest.raises(ValueError):
+            mla.LatentCache8(data=data, scales=scales)
+    for w in ((1 << 31, 0), ((1 << 32) + 5, 0), (4, 1 << 32), (-(1 << 40), 0)):
+        with pytest.raises(ValueError, match="32 bits"):
+            mla.workspace_for_cache8(b, window=w)
+        with pytest.raises(ValueError, match="32 bits"):
+            mla.workspace_for_window(b, w)

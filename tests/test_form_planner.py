@@ -180,3 +180,15 @@ def test_windows_beyond_every_request(harness, window, sinks):
     (pl, shifts), = plans(harness, [c])
     assert shifts == [0, 0, 0]
     check(dict(c, window=0, sinks=0), pl)
+
+
+def test_entries_survive_a_failed_allocation(tmp_path):
+    cxx = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    if not os.path.exists(cxx):
+        pytest.skip("hipcc not available")
+    exe = str(tmp_path / "throw_harness")
+    inc = [f"-I{os.path.join(ROOT, 'include')}", f"-I{os.path.join(ROOT, 'paper_2607_02043_amd', 'csrc')}"]
+    subprocess.run([cxx, "-O1", "-std=c++17", *inc, os.path.join(ROOT, "tests", "planner", "throw_harness.cpp"), "-o", exe],
+                   check=True, capture_output=True)
+    out = dict(line.split() for line in subprocess.run([exe], capture_output=True, text=True, check=True).stdout.splitlines())
+    assert len(out) == 6 and int(out["mixed_step_attn8"]) > 0 and int(out["mixed_step_attn_window_workspace_bytes"]) > 0, out

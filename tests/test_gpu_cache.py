@@ -587,6 +587,59 @@ def test_two_graphs_that_share_a_workspace():
                 np.testing.assert_array_equal(x, y)
 
 
+def test_tensors_that_are_not_on_the_device():
+    import torch
+    b = C.batch([40], [1], 16)
+    db, c = mla.DeviceBatch.from_batch(b), mla.LatentCache8(num_pages=b.num_pages, page_size=16)
+    new = to_dev(C.new_latents(b, 1))
+    cpu = mla.LatentCache8(data=c.data, scales=c.scales.cpu())
+    for call in (lambda: mla.append_latent_kv8(db, new.cpu(), c), lambda: mla.append_latent_kv8(db, new, cpu),
+                 lambda: mla.append_latent_kv8(mla.DeviceBatch.from_batch(b, device="cpu"), new, c),
+                 lambda: mla.append_latent_kv_rope(db, new, BASE, torch.zeros((b.num_pages, 16, 576), dtype=torch.bfloat16))):
+        with pytest.raises(ValueError, match="on cpu"):
+            call()
+    a = Attend(C.batch([3000], [1], 16), C.queries(b, 1), *C.cache8(C.batch([3000], [1], 16), 2, upto=lambda r: 3001))
+    for out, lse, ws in ((a.out.cpu(), a.lse, a.ws), (a.out, a.lse.cpu(), a.ws), (a.out, a.lse, a.ws.cpu())):
+        with pytest.raises(ValueError, match="on cpu"):
+            mla.mixed_step_attn8(a.db, a.qd, a.cache, SCALE, out, lse, ws)
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_pool_beyond_32_bits(eight, page):
+    """Pages past 2^32 bytes of a pool: what a small pool gives, in appends and attention."""
+    import torch
+    b = C.batch([300, 65, 1000], [1, 40, 1], page, seed=36)
+    upto = lambda r: int(b.prefix_lens[r])
+    far = (1 << 32) // (page * (576 if eight else 1152)) + 3  # first page of the far copy
+    shifted = C.batch([300, 65, 1000], [1, 40, 1], page, seed=36)
+    shifted.block_table = np.where(b.block_table >= 0, b.block_table + far, b.block_table)
+    shifted.num_pages = b.num_pages + far
+    q, new, window = to_dev(C.queries(b, 1).reshape(-1, 16, 576)), to_dev(C.new_latents(b, 3)), (100, 4)
+    results = []
+    for bb, at in ((b, 0), (shifted, far)):
+        db = mla.DeviceBatch.from_batch(bb)
+        out, lse = torch.empty((b.num_rows, 16, 512), device="cuda"), torch.empty((b.num_rows, 16), device="cuda")
+        if eight:
+            data, scales = C.cache8(b, 2, upto=upto)
+            c = mla.LatentCache8(data=torch.empty((bb.num_pages, page, 576), dtype=torch.uint8, device="cuda"),
+                                 scales=torch.empty((bb.num_pages, page // 16, 2), dtype=torch.bfloat16, device="cuda"))
+            c.data[at:].copy_(up8(data))
+            c.scales[at:].view(torch.int16).copy_(to_dev(scales))
+            mla.append_latent_kv8(db, new, c, rope_base=BASE)
+            mla.mixed_step_attn8(db, q, c, SCALE, out, lse, mla.workspace_for_cache8(db))
+            results.append([x.cpu().numpy() for x in (c.data[at:], c.scales[at:].view(torch.int16), out, lse)])
+        else:
+            pool = torch.empty((bb.num_pages, page, 576), dtype=torch.bfloat16, device="cuda")
+            pool[at:].view(torch.int16).copy_(to_dev(filled16(b, 2)))
+            mla.append_latent_kv_rope(db, new, BASE, pool)
+            mla.mixed_step_attn_window(db, q, pool, window, SCALE, out, lse, mla.workspace_for_window(db, window))
+            results.append([x.cpu().numpy() for x in (pool[at:].view(torch.int16), out, lse)])
+    for x, y in zip(*results):
+        np.testing.assert_array_equal(x, y)
+    assert np.isfinite(results[0][-1]).all() and mla.device_flags() == 0
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("window", [None, (48, 4)], ids=str)
 def test_serving_steps_on_the_8_bit_cache(window):
