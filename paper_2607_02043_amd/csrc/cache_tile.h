@@ -46,11 +46,15 @@ __device__ __forceinline__ uint32_t finite_e4m3x4(uint32_t w) {
 }
 
 // A tile in LDS: nine quads of 64 dims, each 32 keys of four 16-byte pieces.  Four
-// consecutive keys cover the 64 banks at one piece; pieces are xor-swizzled so that
-// bits 2 and 3 of the key spread the 16 keys of a score operand, and bit 4 the two
-// key halves of a value operand.  Piece p of quad 0 of key k is at tile8_off(k, p).
+// consecutive keys cover the 64 banks at one piece; pieces are xor-swizzled by bits 2
+// and 3 of the key so that they spread a score operand, and by bit 4 for the two key
+// halves of a value operand.  A score operand's read (piece g of key h for lane
+// 16 g + h) is served 16 lanes at a time, {0 .. 3, 12 .. 15, 20 .. 27} and the other
+// half of 32: keys 0 .. 3 and 12 .. 15 of one piece with keys 4 .. 11 of the next one,
+// which fall on four different pieces with 0, 2, 3, 1 (plain 0, 1, 2, 3, or 0, 2, 1, 3:
+// 4 conflict cycles a read).  Piece p of quad 0 of key k is at tile8_off(k, p).
 constexpr int kQuad8 = kKeysPerTile * 64;  // 2048 bytes
-__device__ __forceinline__ int swz8(int k) { return ((k >> 2) & 3) ^ ((k >> 3) & 2); }
+__device__ __forceinline__ int swz8(int k) { return (((k >> 1) ^ (k >> 2)) & 2) ^ ((k >> 3) & 1) ^ ((k >> 4) & 1); }
 __device__ __forceinline__ int tile8_off(int k, int p) { return 64 * k + 16 * (p ^ swz8(k)); }
 
 // DMA of a tile (18 rounds of 1 KB) by four waves, five instructions each.  Round j is keys 16 (j & 1) .. + 15 of quad j / 2;
