@@ -1372,7 +1372,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // the DMAs follow while the queries are still on their way: one round trip
     // less before an item's first tile (32 + 512 rows 43.1 -> 42.3 us).
     const int npages = ck.entry(k_end - 1) + 1;
-    static_assert(kPageWindow <= kAttnThreads, "one window entry per thread");
+    static_assert(kPageWindow <= kAttnThreads && kPageWindow >= 4 * 64, "one window entry per thread; offsets of four waves");
     int pg = 0;
     if (tid < min(npages, kPageWindow) && ck.logical_page(tid) < a.max_pages) pg = a.bt[(size_t)r * a.max_pages + ck.logical_page(tid)];
     constexpr int kQRegSteps = q_reg_steps<F>;
@@ -1477,7 +1477,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     };
 
     // The same over the 8-bit cache: five DMAs of each of the four waves, the scales among them.  A wave's 16 keys are in
-    // one page (16 tokens at least).
+    // one page (16 tokens at least).  The lanes' offsets wait in the page window that chunk items leave free: computed
+    // for each tile they make 2048 rows over 8192 keys 540 us, not 533, and no register is left to keep one.
+    [[maybe_unused]] int *const s_voff8 = s_pages + kPageWindow;  // [wave of four][lane]
     [[maybe_unused]] auto issue8 = [&](int t, int slot, int page) {
         const int kbase = ck.tile(t);
         const uint32_t dst = ring + slot * kTile8Bytes, scale_dst = lds_addr(s_scale) + slot * 32 + 16 * (dw - 2);
@@ -1485,7 +1487,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         if (kbase + kChunkKeys <= k_end) {
             const uint32_t pg = __builtin_amdgcn_readfirstlane(page), in = (kbase + 16 * (dw & 1)) & (a.page_size - 1);
             dma_tile8(a.kv8 + (size_t)pg * (uint32_t)(a.page_size * kDqk) + in * kDqk,
-                      (tile8_key(dw, ln) & 15) * kDqk + tile8_dims(dw, ln), dst, dw);
+                      (uint32_t)s_voff8[dw * 64 + ln], dst, dw);
             if (dw >= 2) dma_scales8(a, (size_t)pg * (uint32_t)a.page_size + in, scale_dst, ln);
         } else {
             const auto slot_of = [&](int key) {  // pool slot
@@ -1788,6 +1790,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     TRACE(3);
     if (exact) m_ref = s_mx[wv * kHeads + hd];
     if (tid == 0) *s_abort = 0;
+    if (has_eight<F> && tid < 4 * 64) s_voff8[tid] = (tile8_key(dw, lane) & 15) * kDqk + tile8_dims(dw, lane);
     if (F != kPlain && tid < 2 * kCT) s_raised[tid] = -1;
     lds_barrier();  // page window and abort flag ready; the ring is idle
     // Waves 0..3 issue tile 0 at once, beside their queries; waves 4..7 issue

@@ -587,6 +587,21 @@ def test_two_graphs_that_share_a_workspace():
                 np.testing.assert_array_equal(x, y)
 
 
+def test_no_requests():
+    import torch
+    db = mla.DeviceBatch(np.zeros(0), np.zeros(0), np.zeros((0, 4)), 16, 8)
+    c = mla.LatentCache8(num_pages=8, page_size=16)
+    new, q = torch.zeros((0, 576), dtype=torch.bfloat16, device="cuda"), torch.zeros((0, 16, 576), dtype=torch.bfloat16, device="cuda")
+    kv, out = torch.zeros((8, 16, 576), dtype=torch.bfloat16, device="cuda"), torch.zeros((0, 16, 512), device="cuda")
+    assert mla.workspace_for_cache8(db) is None and mla.workspace_for_window(db, (4, 0)) is None
+    mla.append_latent_kv8(db, new, c)
+    mla.append_latent_kv_rope(db, new, BASE, kv)
+    mla.mixed_step_attn8(db, q, c, SCALE, out)
+    mla.mixed_step_attn_window(db, q, kv, (4, 0), SCALE, out)
+    torch.cuda.synchronize()
+    assert (c.data == 0).all() and (kv == 0).all() and mla.device_flags() == 0
+
+
 def test_tensors_that_are_not_on_the_device():
     import torch
     b = C.batch([40], [1], 16)
