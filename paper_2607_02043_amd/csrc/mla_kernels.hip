@@ -25,6 +25,11 @@
 // unnormalised sum, the max and sum in log2 units); a second, small merge
 // kernel combines them in a fixed order.  Results are therefore run-to-run
 // deterministic and do not depend on the physical page order.
+//
+// The attention and merge kernels are templates over the forms of mla_cache.h: plain,
+// through a window of keys with sinks, over a cache held in 8 bits, or both.
+// cache_tile.h holds that cache's tiles, cache_decode.h its decode items and
+// cache_append.h the appends that rotate or round on the way.
 #include "mla_kernels.h"
 
 #include <limits.h>
