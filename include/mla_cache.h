@@ -20,9 +20,7 @@
  *   scales  DEVICE bf16 [num_pages][P / 16][2]: every block of 16 tokens of a
  *           page has one scale for its 512 compressed dims and one for its 64
  *           rope dims, each a power of two in [2^-100, 2^120].  A key's value is
- *           code x scale (exact in bf16).  The array is read in 16-byte pieces:
- *           its allocation is rounded up to a multiple of 16 bytes
- *           (mla_cache8_scale_bytes).
+ *           code x scale (exact in bf16).
  *   The page size P is at least 16.
  * Append (append_latent_kv8) takes the rows' values (rotated, in fp32, if asked)
  * and, for every block that it writes into and each of the two parts, the
@@ -59,8 +57,9 @@ typedef struct mla_window {
     int32_t sinks;  /* S >= 0 */
 } mla_window;
 
-/* Bytes to allocate for the scales of a pool (0 on invalid arguments: num_pages
- * < 1, or a page size that is not a power of two in [16, 1024]). */
+/* Bytes of the scales of a pool, rounded up to a multiple of 16 (0 on invalid
+ * arguments: num_pages < 1, or a page size that is not a power of two in [16,
+ * 1024]).  Nothing outside the scales themselves is read. */
 size_t mla_cache8_scale_bytes(int32_t num_pages, int32_t page_size);
 
 /* append_latent_kv with the rotation applied on the way.

@@ -389,8 +389,7 @@ class LatentCache8:
     [num_pages][P][576], and `scales`, bf16 [num_pages][P / 16][2].
 
     LatentCache8(num_pages=n, page_size=P) allocates both (every code 0, every
-    scale 1); LatentCache8(data=.., scales=..) takes a program's own tensors, whose
-    scales must be allocated to a multiple of 16 bytes."""
+    scale 1); LatentCache8(data=.., scales=..) takes a program's own tensors."""
 
     def __init__(self, num_pages: Optional[int] = None, page_size: Optional[int] = None, device="cuda", *, data=None, scales=None):
         import torch

@@ -23,7 +23,7 @@ __device__ __forceinline__ void advance8(Cursor8 &c, const DecSeg *s_seg, int ns
 // instructions of each wave.
 struct Source8 {
     const uint8_t *src[2];  // per lane: this wave's part of each tile; of a query block src[0]
-    const char *scale;      // of the tile whose scales this wave loads (lane 0)
+    const char *scale;      // of the block of 16 keys whose scales this wave loads (lane 0)
     int tiles;              // 0: a query block
 };
 template <int F>
@@ -49,8 +49,7 @@ __device__ __forceinline__ Source8 find_source8(const AttnArgs &a, const Cursor8
         s.src[h] = a.kv8 + slot_of(sk.key((c.t + h) * kDecKeys) + tile8_key(w, lane)) * kDqk + tile8_dims(w, lane);
     }
     const int h = wv >= 2 ? 0 : 1;
-    s.scale = reinterpret_cast<const char *>(a.kv8_scales) +
-              (slot_of(sk.key((c.t + h) * kDecKeys) + 16 * (wv & 1)) / kBlock8 * 4 & ~size_t(15));
+    s.scale = block_scales8(a, slot_of(sk.key((c.t + h) * kDecKeys) + 16 * (wv & 1)));
     return s;
 }
 __device__ __forceinline__ void issue8(const Source8 &s, uint32_t slot, uint32_t scale_slot, int wv, int lane) {
@@ -62,8 +61,7 @@ __device__ __forceinline__ void issue8(const Source8 &s, uint32_t slot, uint32_t
     }
     dma_tile8(s.src[0], slot, wv);
     if (s.tiles == 2) dma_tile8(s.src[1], slot + kTile8Bytes, wv ^ 2);
-    if ((wv >= 2 || s.tiles == 2) && lane == 0)
-        lds_dma16(s.scale, __builtin_amdgcn_readfirstlane(scale_slot + (wv >= 2 ? 0 : 32) + 16 * (wv & 1)));
+    if (wv >= 2 || s.tiles == 2) dma_scales8(s.scale, scale_slot + (wv >= 2 ? 0 : 8) + 4 * (wv & 1), lane);
 }
 
 // decode_wg over the 8-bit cache.  Half the bytes a key (578), so a key has half the
@@ -109,7 +107,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
     Source8 next{};  // of unit u + 1 while unit u is computed (if prod is inside the share)
     const auto find_next = [&] { next = find_source8<F>(a, prod, s_pages, gw, lane); };
     const auto issue = [&](int u) {
-        issue8(next, ring + (u & 1) * kDec8SlotBytes, scales + (u & 1) * 64, gw, lane);
+        issue8(next, ring + (u & 1) * kDec8SlotBytes, scales + (u & 1) * 16, gw, lane);
         advance8(prod, s_seg, nseg);
     };
     if (nseg > 0) {
@@ -176,13 +174,7 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
         u32x4 av[9];
 #pragma unroll
         for (int j = 0; j < 9; ++j) av[j] = *reinterpret_cast<const u32x4 *>(kp + kQuad8 * j);
-        uint32_t wd[4];
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-            const int key = min(kb[kt >> 1] + 16 * (kt & 1), sg.p);
-            const int pg = a.page_size >= 64 ? 0 : s_pages[min(sk.window_entry(sg, key, a.log2_page), kPageWindow - 1)];
-            wd[kt] = *reinterpret_cast<const uint32_t *>(s_scale + (u & 1) * 64 + 16 * kt + 4 * scale_piece8(a, pg, key));
-        }
+        const u32x4 wd = *reinterpret_cast<const u32x4 *>(s_scale + (u & 1) * 16);
         const bool issued = u > 0 && prod.j < nseg;
         if (issued) issue(u + 1);
         // scales of the values, and the largest of the blocks that the row sees (a scale that is no number counts for none: its

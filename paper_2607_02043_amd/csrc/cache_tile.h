@@ -8,10 +8,14 @@ __device__ __forceinline__ float exp2_bits(int e) { return __uint_as_float((uint
 // The exponent of a stored scale (bf16 bits of a power of two; 128 if it is no number).
 __device__ __forceinline__ int scale_exponent(uint32_t bf16) { return (int)((bf16 >> 7) & 0xff) - 127; }
 
-// The scales of a block of 16 tokens are 4 bytes, loaded in aligned pieces of 16:
-// which of its four entries a key's is (the page matters below 64 tokens a page only).
-__device__ __forceinline__ int scale_piece8(const AttnArgs &a, int page, int key) {
-    return (page * (a.page_size / kBlock8) + (key & (a.page_size - 1)) / kBlock8) & 3;
+// Four bytes of one lane (the others' land behind them), global -> LDS.
+__device__ __forceinline__ void lds_dma4(const void *gsrc, uint32_t lds_base) {
+    asm volatile(
+        "s_nop 0\n\t"
+        "global_load_lds_dword %1, off\n\t"
+        :
+        : "{m0}"(lds_base), "v"(gsrc)
+        : "memory");
 }
 
 // Eight e4m3 codes (two words) times a power of two as bf16: exact.
@@ -79,8 +83,11 @@ __device__ __forceinline__ void dma_tile8(const uint8_t *src, uint32_t slot, int
     if (w < 2) MLA_DMA8(4);
 #undef MLA_DMA8
 }
-// The piece with the scales of a pool slot's block, to 16 bytes at `dst` (one lane).
-__device__ __forceinline__ void dma_scales8(const AttnArgs &a, size_t pool_slot, uint32_t dst, int lane) {
-    const char *src = reinterpret_cast<const char *>(a.kv8_scales) + (pool_slot / kBlock8 * 4 & ~size_t(15));
-    if (lane == 0) lds_dma16(src, __builtin_amdgcn_readfirstlane(dst));
+// Address of the two scales of a pool slot's block, and their DMA to the four bytes at
+// `dst` (one lane: nothing beside them is read, so the array may end there).
+__device__ __forceinline__ const char *block_scales8(const AttnArgs &a, size_t pool_slot) {
+    return reinterpret_cast<const char *>(a.kv8_scales) + pool_slot / kBlock8 * 4;
+}
+__device__ __forceinline__ void dma_scales8(const char *src, uint32_t dst, int lane) {
+    if (lane == 0) lds_dma4(src, __builtin_amdgcn_readfirstlane(dst));
 }

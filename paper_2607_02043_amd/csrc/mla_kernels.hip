@@ -69,7 +69,7 @@ constexpr int kTile8Bytes = kKeysPerTile * kDqk;        // 18432: a tile of the 
 constexpr int kDec8SlotBytes = 2 * kTile8Bytes;         // its decode path: two tiles a ring slot
 constexpr int kDec8GroupBytes = kDecRing * kDec8SlotBytes;
 constexpr int kDec8XBytes = 4 * 64 * 16;                // score blocks of a group
-constexpr int kDec8ScaleBytes = kDecRing * 64;          // 16-byte pieces of the scales, four a slot
+constexpr int kDec8ScaleBytes = kDecRing * 16;          // pairs of scales, four a slot
 constexpr int kDec8StatBytes = 4 * kHeads * 4 + 16;     // a float of each wave and head, a word of each wave
 constexpr int kDec8Lds = 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes + kDec8StatBytes);
 static_assert(kTile8Bytes == kHeads * kRowBytes, "a query block fills a slot");
@@ -1286,9 +1286,9 @@ constexpr int kPTile = kCT * 64 * 16;                  // fp16 P of one tile: [t
 template <int F>
 constexpr int chunk_tile_bytes = has_eight<F> ? kTile8Bytes : kChunkTileBytes;
 // Forms other than the plain one raise a row's reference max as they go (see softmax): the factors [P buffer][token][head],
-// the tile that each was raised at [P buffer][token]; the 8-bit cache's scales, two 16-byte pieces a ring slot.
+// the tile that each was raised at [P buffer][token]; the 8-bit cache's pairs of scales, two a ring slot.
 constexpr int kRaiseBytes = 2 * kCT * kHeads * 4 + 2 * kCT * 4;
-constexpr int kChunk8ScaleBytes = kChunkRing * 32;
+constexpr int kChunk8ScaleBytes = kChunkRing * 8;
 template <int F>
 constexpr int q_lds_bytes = (kQSteps - q_reg_steps<F>) * kCT * 64 * 16;  // query operands in LDS: [step][token][lane]
 template <int F>
@@ -1406,7 +1406,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     int *const s_abort = reinterpret_cast<int *>(s_mx + kCT * kHeads);
     [[maybe_unused]] float *const s_raise = reinterpret_cast<float *>(s_abort + 4);                          // [P buffer][token][head]
     [[maybe_unused]] int *const s_raised = reinterpret_cast<int *>(s_raise + 2 * kCT * kHeads);              // [P buffer][token]
-    [[maybe_unused]] char *const s_scale = reinterpret_cast<char *>(s_raised + 2 * kCT);                     // [ring slot] 32 bytes
+    [[maybe_unused]] char *const s_scale = reinterpret_cast<char *>(s_raised + 2 * kCT);                     // [ring slot][key half] 4 bytes
 
     // Causal limit of this wave's token (absolute key index, clipped to the
     // item's key range); wave-uniform.
@@ -1487,20 +1487,20 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     [[maybe_unused]] int *const s_voff8 = s_pages + kPageWindow;  // [wave of four][lane]
     [[maybe_unused]] auto issue8 = [&](int t, int slot, int page) {
         const int kbase = ck.tile(t);
-        const uint32_t dst = ring + slot * kTile8Bytes, scale_dst = lds_addr(s_scale) + slot * 32 + 16 * (dw - 2);
+        const uint32_t dst = ring + slot * kTile8Bytes, scale_dst = lds_addr(s_scale) + slot * 8 + 4 * (dw - 2);
         const int ln = opaque_lane();
         if (kbase + kChunkKeys <= k_end) {
             const uint32_t pg = __builtin_amdgcn_readfirstlane(page), in = (kbase + 16 * (dw & 1)) & (a.page_size - 1);
             dma_tile8(a.kv8 + (size_t)pg * (uint32_t)(a.page_size * kDqk) + in * kDqk,
                       (uint32_t)s_voff8[dw * 64 + ln], dst, dw);
-            if (dw >= 2) dma_scales8(a, (size_t)pg * (uint32_t)a.page_size + in, scale_dst, ln);
+            if (dw >= 2) dma_scales8(block_scales8(a, (size_t)pg * (uint32_t)a.page_size + in), scale_dst, ln);
         } else {
             const auto slot_of = [&](int key) {  // pool slot
                 const int k = min(key, k_end - 1);
                 return (size_t)s_pages[min(ck.entry(k), kPageWindow - 1)] * a.page_size + (k & (a.page_size - 1));
             };
             dma_tile8(a.kv8 + slot_of(kbase + tile8_key(dw, ln)) * kDqk + tile8_dims(dw, ln), dst, dw);
-            if (dw >= 2) dma_scales8(a, slot_of(kbase + 16 * (dw - 2)), scale_dst, ln);
+            if (dw >= 2) dma_scales8(block_scales8(a, slot_of(kbase + 16 * (dw - 2))), scale_dst, ln);
         }
     };
     // page of tile t, and its DMA into a ring slot
@@ -1555,16 +1555,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // Scales of tile t in ring slot `slot`.
-    [[maybe_unused]] auto read_scales8 = [&](int t, int slot, uint32_t (&w)[2]) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const int key = min(ck.tile(t) + 16 * kb, k_end - 1);
-            const int pg = a.page_size >= 64 ? 0 : s_pages[min(ck.entry(key), kPageWindow - 1)];
-            w[kb] = *reinterpret_cast<const uint32_t *>(s_scale + slot * 32 + 16 * kb + 4 * scale_piece8(a, pg, key));
-        }
-    };
-    [[maybe_unused]] auto scales8 = [&](const uint32_t (&w)[2]) {  // (scalar: the vector registers are all taken)
+    // Scales of the tile in ring slot `slot`.
+    [[maybe_unused]] auto read_scales8 = [&](int slot) { return *reinterpret_cast<const u32x2 *>(s_scale + slot * 8); };
+    [[maybe_unused]] auto scales8 = [&](u32x2 w) {  // (scalar: the vector registers are all taken)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const uint32_t u = __builtin_amdgcn_readfirstlane(w[kb]);
@@ -1827,9 +1820,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     {
         f32x4 s0[2];
         if constexpr (has_eight<F>) {
-            uint32_t w[2];
-            read_scales8(0, 0, w);
-            scales8(w);
+            scales8(read_scales8(0));
         }
         scores(0, s0);
         if (F == kPlain && main_pass) {
@@ -1859,9 +1850,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         const int slot2 = slot1 == kChunkRing - 1 ? 0 : slot1 + 1;
         if (dma_wave && t + 2 < ntiles) issue_tile(t + 2, slot2, next_page);
         TRACE_TILE(t, 14);
-        [[maybe_unused]] uint32_t w8[2];  // in flight over the products
+        [[maybe_unused]] u32x2 w8;  // in flight over the products
         if constexpr (has_eight<F>) {
-            read_scales8(min(t + 1, ntiles - 1), slot1, w8);
+            w8 = read_scales8(slot1);
             page_ahead = page_of(min(t + 3, ntiles - 1));
         }
         pv(t);
