@@ -92,12 +92,13 @@ size_t mixed_step_attn_window_workspace_bytes(const mla_batch *batch, const mla_
 /* mixed_step_attn over the 8-bit cache, which already holds the step's tokens
  * (call append_latent_kv8 first, on the same stream).
  *   window       NULL: every earlier key is visible.
- *   other arguments as for mixed_step_attn.  Value dims (code x scale) go
- *   through fp16 relative to a scale of the blocks read, so no value is too
- *   large; those of a decode row are off by at most 2^-25 of the largest
- *   compressed scale that it sees, those of a chunk row by at most 2^-25 of the
- *   largest that its block of 8 rows sees (rows 8 k .. 8 k + 7 of the request).
- *   Scales at most 2^15 apart lose nothing.
+ *   other arguments as for mixed_step_attn.  Scores are sums in fp32, as there.
+ *   Value dims (code x scale) go through fp16 relative to a scale of the blocks
+ *   read, and rows that are cut into parts keep the parts' averages, so no value
+ *   below 2^128 is too large; those of a decode row are off by at most 2^-25 of
+ *   the largest compressed scale that it sees, those of a chunk row by at most
+ *   2^-25 of the largest that its block of 8 rows sees (rows 8 k .. 8 k + 7 of
+ *   the request).  Scales at most 2^15 apart lose nothing.
  * Errors: as mixed_step_attn, and MLA_ERR_INVALID_ARG for a bad window,
  * MLA_ERR_UNSUPPORTED for a page size below 16. */
 int mixed_step_attn8(const mla_batch *batch, const uint16_t *q, const mla_cache8 *cache, const mla_window *window,

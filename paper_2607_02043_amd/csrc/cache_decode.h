@@ -299,17 +299,18 @@ __device__ void decode8_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g
             group_barrier(gbar, epoch, a.spin_limit);
             const float l_tot = (s_stat[h] + s_stat[kHeads + h]) + (s_stat[2 * kHeads + h] + s_stat[3 * kHeads + h]);
             if (sg.t0 == 0 && sg.t1 == dec_tiles<F>(a, sg.p, 1)) {
-                const float inv = v_ref / l_tot;
+                const float inv = 1.f / l_tot;
 #pragma unroll
                 for (int mt2 = 0; mt2 < 8; ++mt2)
-                    store_out4(a, sg.row, h, gw * 128 + mt2 * 16 + 4 * g, acc[mt2] * inv);
+                    store_out4(a, sg.row, h, gw * 128 + mt2 * 16 + 4 * g, acc[mt2] * inv * v_ref);
                 if (a.lse && gw == 0 && g == 0) a.lse[(size_t)sg.row * kHeads + h] = (m_ref + log2f(l_tot)) * kLn2;
             } else if (a.ws_dec_o != nullptr) {
                 const size_t slot_id = 2 * (size_t)v + (jseg == 0 ? 0 : 1);
                 float *po = a.ws_dec_o + (slot_id * kHeads + h) * kDv;
+                const float inv = inv_sum(l_tot);
 #pragma unroll
                 for (int mt2 = 0; mt2 < 8; ++mt2)
-                    *reinterpret_cast<f32x4 *>(po + gw * 128 + mt2 * 16 + 4 * g) = acc[mt2] * v_ref;
+                    *reinterpret_cast<f32x4 *>(po + gw * 128 + mt2 * 16 + 4 * g) = acc[mt2] * inv * v_ref;
                 if (gw == 0 && g == 0) {
                     a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 0] = partial_max(m_ref, l_tot);
                     a.ws_dec_ml[(slot_id * kHeads + h) * 2 + 1] = l_tot;

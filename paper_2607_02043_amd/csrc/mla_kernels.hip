@@ -22,7 +22,8 @@
 //     units, one per 4-wave group of the workgroup, each streaming its tiles
 //     through its own 2-slot ring.
 // Rows whose keys are split across items leave fp32 partials (the
-// unnormalised sum, the max and sum in log2 units); a second, small merge
+// unnormalised sum, over the 8-bit cache the average; the max and sum in log2
+// units); a second, small merge
 // kernel combines them in a fixed order.  Results are therefore run-to-run
 // deterministic and do not depend on the physical page order.
 //
@@ -490,12 +491,16 @@ __device__ __forceinline__ void store_out4(const AttnArgs &a, int row, int head,
 // parts 62.0 us before, 71.9 with the chain, 7.8 spread; 64 rows of 9 parts 12.6,
 // 15.1 and 6.9; 2048 rows of 7 parts 136.9, 119.7 and 94.3.  Only rows that have
 // partials get workgroups (the chain's launch had one per item and block row).
+//
+// MEAN (the 8-bit cache, whose values may be as large as fp32 holds): o_s is
+// divided by l_s already, and the merge keeps an average with weights of at most 1,
+// so that no step is larger than the largest value.
 struct SplitRef {
     const float *o, *ml;
 };
 
 // o, M, den += splits s0, s0 + SW, .. of head hh (B of them in flight).
-template <int B, int SW, typename Slot>
+template <bool MEAN, int B, int SW, typename Slot>
 __device__ __forceinline__ void merge_splits(int s0, int nsplit, int hh, int lane, Slot slot, f32x4 (&o)[2], float &M,
                                              float &den) {
     for (; s0 < nsplit; s0 += B * SW) {
@@ -518,15 +523,29 @@ __device__ __forceinline__ void merge_splits(int s0, int nsplit, int hh, int lan
         float m_new = M;
 #pragma unroll
         for (int q = 0; q < B; ++q) m_new = fmaxf(m_new, ms[q]);
-        const float c_old = (M == kNegInf) ? 0.f : exp2f(M - m_new);
-        den *= c_old;
+        float c_old = (M == kNegInf) ? 0.f : exp2f(M - m_new);
+        if constexpr (MEAN) {
+            const float d_old = den * c_old;
+            den = d_old;
+#pragma unroll
+            for (int q = 0; q < B; ++q) {
+                ls[q] = ms[q] == kNegInf ? 0.f : ls[q] * exp2f(ms[q] - m_new);  // its weight
+                den += ls[q];
+            }
+            const float r = den == 0.f ? 0.f : 1.f / den;
+            c_old = d_old * r;
+#pragma unroll
+            for (int q = 0; q < B; ++q) ls[q] *= r;
+        } else {
+            den *= c_old;
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k) o[k] = o[k] * c_old;
 #pragma unroll
         for (int q = 0; q < B; ++q) {
             if (ms[q] == kNegInf) continue;  // a split that saw no key of this row
-            const float c = exp2f(ms[q] - m_new);
-            den += ls[q] * c;
+            const float c = MEAN ? ls[q] : exp2f(ms[q] - m_new);
+            if constexpr (!MEAN) den += ls[q] * c;
 #pragma unroll
             for (int k = 0; k < 2; ++k) o[k] = o[k] + v[q][k] * c;
         }
@@ -534,22 +553,23 @@ __device__ __forceinline__ void merge_splits(int s0, int nsplit, int hh, int lan
     }
 }
 
+template <bool MEAN>
 __device__ __forceinline__ void store_merged(const AttnArgs &a, int row, int hh, int lane, const f32x4 (&o)[2], float M,
                                              float den) {
-    const float inv = 1.f / den;
+    const float inv = MEAN ? (den == 0.f ? NAN : 1.f) : 1.f / den;  // (no weight at all: NaN, as 0 / 0)
 #pragma unroll
     for (int k = 0; k < 2; ++k) store_out4(a, row, hh, 4 * lane + 256 * k, o[k] * inv);
     if (a.lse && lane == 0) a.lse[(size_t)row * kHeads + hh] = (M + log2f(den)) * kLn2;
 }
 
 // Heads hh0 .. hh0 + 4 / SW - 1 of a row with many splits; s_o holds 4 x 512 floats, s_ml 4 x 2.
-template <int B, int SW, typename Slot>
+template <bool MEAN, int B, int SW, typename Slot>
 __device__ void merge_heads(const AttnArgs &a, int row, int hh0, int nsplit, Slot slot, float *s_o, float *s_ml) {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     const int hh = hh0 + wv / SW, part = wv % SW;
     f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
     float M = kNegInf, den = 0.f;
-    merge_splits<B, SW>(part, nsplit, hh, lane, slot, o, M, den);
+    merge_splits<MEAN, B, SW>(part, nsplit, hh, lane, slot, o, M, den);
     if constexpr (SW > 1) {
         if (part != 0) {
             f32x4 *dst = reinterpret_cast<f32x4 *>(s_o + wv * kDv) + lane;
@@ -567,19 +587,28 @@ __device__ void merge_heads(const AttnArgs &a, int row, int hh0, int nsplit, Slo
             const float m = s_ml[2 * (wv + w)], l = s_ml[2 * (wv + w) + 1];
             if (m == kNegInf) continue;  // fewer splits than wavefronts
             const float m_new = fmaxf(M, m);
-            const float c_old = (M == kNegInf) ? 0.f : exp2f(M - m_new), c = exp2f(m - m_new);
+            float c_old = (M == kNegInf) ? 0.f : exp2f(M - m_new), c = exp2f(m - m_new);
             const f32x4 *src = reinterpret_cast<const f32x4 *>(s_o + (wv + w) * kDv) + lane;
-            den = den * c_old + l * c;
+            if constexpr (MEAN) {
+                c_old *= den;
+                c *= l;
+                den = c_old + c;
+                const float r = den == 0.f ? 0.f : 1.f / den;
+                c_old *= r;
+                c *= r;
+            } else {
+                den = den * c_old + l * c;
+            }
             o[0] = o[0] * c_old + src[0] * c;
             o[1] = o[1] * c_old + src[64] * c;
             M = m_new;
         }
     }
-    store_merged(a, row, hh, lane, o, M, den);
+    store_merged<MEAN>(a, row, hh, lane, o, M, den);
 }
 
 // A whole row of few parts, four heads per wavefront.
-template <typename Slot>
+template <bool MEAN, typename Slot>
 __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
 #pragma unroll
@@ -587,8 +616,8 @@ __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
         const int hh = wv * (kHeads / 4) + k;
         f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         float M = kNegInf, den = 0.f;
-        merge_splits<2, 1>(0, nsplit, hh, lane, slot, o, M, den);
-        store_merged(a, row, hh, lane, o, M, den);
+        merge_splits<MEAN, 2, 1>(0, nsplit, hh, lane, slot, o, M, den);
+        store_merged<MEAN>(a, row, hh, lane, o, M, den);
     }
 }
 
@@ -854,6 +883,8 @@ __device__ __forceinline__ bool any_not_finite(f32x4 x) {
     const float t = (x[0] + x[1]) + (x[2] + x[3]);
     return __builtin_amdgcn_ballot_w64(!(fabsf(t) < INFINITY)) != 0;
 }
+// What a part of the 8-bit cache's forms divides by: its average is 0 where it saw no key.
+__device__ __forceinline__ float inv_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
 // A partial's max: a part whose visible scores were all NaN must not look empty to the merge.
 __device__ __forceinline__ float partial_max(float m, float l) { return l != l ? 0.f : m; }
 
@@ -1152,9 +1183,9 @@ __device__ void decode_merge(const AttnArgs &a, int k, int part, float *s_o, flo
     };
     const int n = w1 - w0 + 1;
     if (MANY && a.merge_many)
-        merge_heads<8, 4>(a, row, part, n, slot, s_o, s_ml);
+        merge_heads<has_eight<F>, 8, 4>(a, row, part, n, slot, s_o, s_ml);
     else
-        merge_heads<4, 1>(a, row, 4 * part, n, slot, s_o, s_ml);
+        merge_heads<has_eight<F>, 4, 1>(a, row, 4 * part, n, slot, s_o, s_ml);
 }
 
 // The k-th row of the chunk requests whose keys are cut into ranges (requests
@@ -1229,11 +1260,11 @@ __device__ void chunk_merge(const AttnArgs &a, int k, int part, float *s_o, floa
     };
     const int row = it.row0 + it.i0 + j;
     if (MANY && a.chunk_merge_wgs == kHeads)
-        merge_heads<8, 4>(a, row, part, it.nks_eff, slot, s_o, s_ml);
+        merge_heads<has_eight<F>, 8, 4>(a, row, part, it.nks_eff, slot, s_o, s_ml);
     else if (a.chunk_merge_wgs == kHeads / 4)
-        merge_heads<4, 1>(a, row, 4 * part, it.nks_eff, slot, s_o, s_ml);
+        merge_heads<has_eight<F>, 4, 1>(a, row, 4 * part, it.nks_eff, slot, s_o, s_ml);
     else
-        merge_row(a, row, it.nks_eff, slot);
+        merge_row<has_eight<F>>(a, row, it.nks_eff, slot);
 }
 
 // ------------------------------------------------------------- chunk path
@@ -1898,14 +1929,17 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         if (tb >= nt) break;
         const int row = it.row0 + it.i0 + tb;
         if (it.nks_eff == 1) {
-            const float inv = (has_eight<F> ? v_ref : 1.f) / s_l[tb * kHeads + hd];
+            const float inv = 1.f / s_l[tb * kHeads + hd];
 #pragma unroll
-            for (int db = 0; db < 4; ++db) store_out4(a, row, hd, 64 * wv + 16 * db + 4 * ge, acc[tb][db] * inv);
+            for (int db = 0; db < 4; ++db)
+                store_out4(a, row, hd, 64 * wv + 16 * db + 4 * ge, has_eight<F> ? acc[tb][db] * inv * v_ref : acc[tb][db] * inv);
         } else {
             const size_t prow = (size_t)item * kCT + tb;
             float *po = a.ws_chunk_o + (prow * kHeads + hd) * kDv + 64 * wv + 4 * ge;
+            const float inv = has_eight<F> ? inv_sum(s_l[tb * kHeads + hd]) : 1.f;
 #pragma unroll
-            for (int db = 0; db < 4; ++db) *reinterpret_cast<f32x4 *>(po + 16 * db) = has_eight<F> ? acc[tb][db] * v_ref : acc[tb][db];
+            for (int db = 0; db < 4; ++db)
+                *reinterpret_cast<f32x4 *>(po + 16 * db) = has_eight<F> ? acc[tb][db] * inv * v_ref : acc[tb][db];
         }
     }
     if (g == 0 && wv < nt) {
@@ -2175,10 +2209,14 @@ hipError_t launch_combine(const AttnArgs &a, hipStream_t s) {
     if (grid_ll > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const int grid = (int)grid_ll;
     if (grid == 0) return hipSuccess;
-    if (a.band.window > 0)
-        launch_merge<kWindow>(a, grid, s);
-    else
+    if (a.kv8 == nullptr && a.band.window == 0)
         launch_merge<kPlain>(a, grid, s);
+    else if (a.kv8 == nullptr)
+        launch_merge<kWindow>(a, grid, s);
+    else if (a.band.window == 0)
+        launch_merge<kEight>(a, grid, s);
+    else
+        launch_merge<kEight | kWindow>(a, grid, s);
     return hipGetLastError();
 }
 
