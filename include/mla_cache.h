@@ -20,7 +20,8 @@
  *   scales  DEVICE bf16 [num_pages][P / 16][2]: every block of 16 tokens of a
  *           page has one scale for its 512 compressed dims and one for its 64
  *           rope dims, each a power of two in [2^-100, 2^120].  A key's value is
- *           code x scale (exact in bf16).
+ *           code x scale (exact in bf16; of magnitude below 2^128, so at a scale of
+ *           2^120 codes are at most 240).
  *   The page size P is at least 16.
  * Append (append_latent_kv8) takes the rows' values (rotated, in fp32, if asked)
  * and, for every block that it writes into and each of the two parts, the
@@ -28,8 +29,9 @@
  * largest e4m3 value; a block that holds earlier tokens of the request (p_r
  * inside it) keeps its own scale if that is larger, otherwise those earlier
  * tokens are rounded again to the new scale.  Values are rounded to nearest,
- * ties to even, once; NaN and infinities are stored as NaN.  Other tokens of the
- * pool are left as they are.
+ * ties to even, once (at a scale of 2^120 to at most 240, which is within half a
+ * step of every finite bf16: 2^-4 of it); NaN and infinities are stored as NaN.
+ * Other tokens of the pool are left as they are.
  *   What mla_step.h says about written slots holds for blocks here: a block
  *   that one request writes into belongs to it alone in that step.
  *

@@ -63,6 +63,11 @@ def exponent(amax):
     raise ValueError(amax)
 
 
+def largest(e):
+    """Largest e4m3 value that a bf16 holds times 2^e (448, or below 2^(128 - e))."""
+    return max(v for v in TABLE[:127] if v * 2.0 ** e < 2.0 ** 128)
+
+
 def scale_bits(e):
     return np.uint16((e + 127) << 7)
 
@@ -112,7 +117,7 @@ def append8(batch, new_bits, base, data, scales):
                 for t in range(t0, t1):
                     v = new[t - t0]
                     s = slot(batch, r, t)
-                    data[s, d0:d1] = e4m3_code(np.where(np.isfinite(v), v, math.nan) * 2.0 ** -e)
+                    data[s, d0:d1] = e4m3_code(np.clip(np.where(np.isfinite(v), v, math.nan) * 2.0 ** -e, -largest(e), largest(e)))
                     touched.add((s, k))
     return data, scales, touched
 

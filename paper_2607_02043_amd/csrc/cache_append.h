@@ -61,9 +61,12 @@ __device__ __forceinline__ float finite_abs(float x) {
     const float v = fabsf(x);
     return v < INFINITY ? v : 0.f;
 }
-// Four values to e4m3 (nearest even; |x s| <= 448), non-finite ones to NaN.
-__device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, float x3, float s) {
-    const auto f = [&](float x) { return fabsf(x) < INFINITY ? x * s : NAN; };
+// Largest code value at a scale of 2^e: 448, at 2^120 the largest below 2^8 (codes
+// from 256 on stand for 2^128 and more there, which neither bf16 nor fp32 holds).
+__device__ __forceinline__ float largest_code(int e) { return e < kMaxExp8 ? 448.f : 240.f; }
+// Four values to e4m3 (nearest even, none beyond `most`), non-finite ones to NaN.
+__device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, float x3, float s, float most) {
+    const auto f = [&](float x) { return fabsf(x) < INFINITY ? fminf(fmaxf(x * s, -most), most) : NAN; };
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(f(x0), f(x1), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f(x2), f(x3), w, true);
 }
@@ -163,10 +166,10 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a, RopeTa
             if (e[k] == was[k]) continue;
             uint32_t *const w = reinterpret_cast<uint32_t *>(blk) + u;
             const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)*w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)*w, true);
-            *w = pack_e4m3(lo[0], lo[1], hi[0], hi[1], exp2_bits(max(was[k] - e[k], -126)));
+            *w = pack_e4m3(lo[0], lo[1], hi[0], hi[1], exp2_bits(max(was[k] - e[k], -126)), largest_code(e[k]));
         }
     }
-    const float sc = exp2_bits(-e[0]), sr = exp2_bits(-e[1]);
+    const float sc = exp2_bits(-e[0]), sr = exp2_bits(-e[1]), top_c = largest_code(e[0]), top_r = largest_code(e[1]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (4 * i + wv >= n) break;
@@ -177,9 +180,9 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a, RopeTa
             x[2 * k + 1] = bf16_bits_to_float(vc[i][k] >> 16);
         }
         reinterpret_cast<u32x2 *>(blk + (size_t)(held + 4 * i + wv) * kDqk)[lane] =
-            u32x2{pack_e4m3(x[0], x[1], x[2], x[3], sc), pack_e4m3(x[4], x[5], x[6], x[7], sc)};
+            u32x2{pack_e4m3(x[0], x[1], x[2], x[3], sc, top_c), pack_e4m3(x[4], x[5], x[6], x[7], sc, top_c)};
     }
     if (rope)
         reinterpret_cast<u32x2 *>(blk + (size_t)(held + rr) * kDqk + kDv)[rc] =
-            u32x2{pack_e4m3(xr[0], xr[1], xr[2], xr[3], sr), pack_e4m3(xr[4], xr[5], xr[6], xr[7], sr)};
+            u32x2{pack_e4m3(xr[0], xr[1], xr[2], xr[3], sr, top_r), pack_e4m3(xr[4], xr[5], xr[6], xr[7], sr, top_r)};
 }

@@ -58,3 +58,37 @@ def test_split_rows_of_the_largest_values(prefix, rows, keys, unit, spread):
         log(f"[gpu] {prefix} {rows}, chunk keys {k}, unit {u}")
         Attend(b, q, top_codes(data), scales).run().check("largest values", range(0, b.num_rows, 3))
     assert mla.device_flags() == 0
+
+
+@pytest.mark.parametrize("base", [0.0, BASE])
+def test_append8_of_the_largest_finite_values(base):
+    """bf16 values next to 2^128: codes whose values a bf16 holds, off by half a step at most."""
+    b = C.batch([0, 5, 16], [16, 2, 1], 16, seed=43)
+    new = C.new_latents(b, 4).copy()
+    tops = np.array([0x7F7F, 0xFF7F, 0x7F78, 0x7F77, 0xFF70, 0x7F6F, 0x7F00], dtype=np.uint16)
+    new[0, 3:3 + len(tops)] = tops
+    new[16, 100], new[18, 500] = 0x7F7F, 0xFF7F
+    new[9, 512:576:2], new[9, 513:576:2] = 0x7F7F, 0  # (one of a pair: rotated it stays below 2^128)
+    data, scales = C.cache8(b, 2)
+    c = mla.LatentCache8(num_pages=b.num_pages, page_size=16)
+    import torch
+    c.data.copy_(up8(data))
+    c.scales.view(torch.int16).copy_(to_dev(scales))
+    db = mla.DeviceBatch.from_batch(b)
+    mla.append_latent_kv8(db, to_dev(new), c, rope_base=base)
+    got, gs = down8(c)
+    if not base:
+        want, ws, _ = CO.append8(b, new, base, data, scales)
+        np.testing.assert_array_equal(gs.reshape(-1, 2), ws)
+        np.testing.assert_array_equal(got.reshape(-1, 576), want)
+    for r, x in enumerate(CO.rows(b, new, base)):
+        keys = CO.keys8(b, r, int(b.prefix_lens[r] + b.q_lens[r]), got, gs)[int(b.prefix_lens[r]):]
+        s = np.array([[CO.scale_value(gs.reshape(-1, 2)[CO.slot(b, r, int(b.prefix_lens[r]) + i) // 16, k]) for k in (0, 1)] for i in range(len(x))])
+        half = np.concatenate((np.repeat(s[:, :1], 512, 1), np.repeat(s[:, 1:], 64, 1)), 1) * 2.0 ** -10
+        m = np.zeros_like(x)  # (rotated in fp32: cos and sin within 2^-22, two products and a sum)
+        m[:, 512:] = np.repeat(np.abs(CO.bf16_value(new)[int(b.cu_q[r]):int(b.cu_q[r + 1]), 512:]).reshape(len(x), 32, 2).sum(2), 2, 1) * 2.0 ** -21
+        assert (np.abs(keys) < 2.0 ** 128).all()  # NaN and infinities fail it
+        assert (np.abs(keys - x) <= np.abs(x) * 2.0 ** -4 + half + m).all()
+    # and read back: attention gives finite rows
+    a = Attend(b, C.queries(b, 1).reshape(-1, 16, 576) * np.uint16(0), *down8(c))
+    a.run().check("largest values")
