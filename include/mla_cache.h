@@ -37,6 +37,11 @@
  *
  * Window.  With a window of W keys and S sinks, the row at position t sees the
  * keys j <= t with j > t - W or j < S.  W >= 1, so a row always sees itself.
+ *
+ * Values that are not finite.  Keys that a row does not see never reach it,
+ * whatever they hold.  Those that it sees count as the sums say: a score of NaN
+ * or +inf makes the row's output and lse of that head NaN, one of -inf has a
+ * weight of 0, and 0 x inf is NaN in the dims whose value is infinite.
  */
 #ifndef MLA_CACHE_H
 #define MLA_CACHE_H

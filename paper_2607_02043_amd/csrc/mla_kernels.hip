@@ -492,15 +492,17 @@ __device__ __forceinline__ void store_out4(const AttnArgs &a, int row, int head,
 // 15.1 and 6.9; 2048 rows of 7 parts 136.9, 119.7 and 94.3.  Only rows that have
 // partials get workgroups (the chain's launch had one per item and block row).
 //
-// MEAN (the 8-bit cache, whose values may be as large as fp32 holds): o_s is
+// Over the 8-bit cache, whose values may be as large as fp32 holds, o_s is
 // divided by l_s already, and the merge keeps an average with weights of at most 1,
-// so that no step is larger than the largest value.
+// so that no step is larger than the largest value.  With a window a part whose
+// visible scores are all -inf counts with weight 0 and is not left out: what it saw
+// may be infinite, and 0 x inf is NaN.
 struct SplitRef {
     const float *o, *ml;
 };
 
 // o, M, den += splits s0, s0 + SW, .. of head hh (B of them in flight).
-template <bool MEAN, int B, int SW, typename Slot>
+template <int F, int B, int SW, typename Slot>
 __device__ __forceinline__ void merge_splits(int s0, int nsplit, int hh, int lane, Slot slot, f32x4 (&o)[2], float &M,
                                              float &den) {
     for (; s0 < nsplit; s0 += B * SW) {
@@ -524,7 +526,7 @@ __device__ __forceinline__ void merge_splits(int s0, int nsplit, int hh, int lan
 #pragma unroll
         for (int q = 0; q < B; ++q) m_new = fmaxf(m_new, ms[q]);
         float c_old = (M == kNegInf) ? 0.f : exp2f(M - m_new);
-        if constexpr (MEAN) {
+        if constexpr (has_eight<F>) {
             const float d_old = den * c_old;
             den = d_old;
 #pragma unroll
@@ -543,9 +545,9 @@ __device__ __forceinline__ void merge_splits(int s0, int nsplit, int hh, int lan
         for (int k = 0; k < 2; ++k) o[k] = o[k] * c_old;
 #pragma unroll
         for (int q = 0; q < B; ++q) {
-            if (ms[q] == kNegInf) continue;  // a split that saw no key of this row
-            const float c = MEAN ? ls[q] : exp2f(ms[q] - m_new);
-            if constexpr (!MEAN) den += ls[q] * c;
+            if (F != kWindow && ms[q] == kNegInf) continue;  // a split that saw no key of this row
+            const float c = has_eight<F> ? ls[q] : ms[q] == kNegInf ? 0.f : exp2f(ms[q] - m_new);
+            if constexpr (!has_eight<F>) den += ls[q] * c;
 #pragma unroll
             for (int k = 0; k < 2; ++k) o[k] = o[k] + v[q][k] * c;
         }
@@ -553,23 +555,23 @@ __device__ __forceinline__ void merge_splits(int s0, int nsplit, int hh, int lan
     }
 }
 
-template <bool MEAN>
+template <int F>
 __device__ __forceinline__ void store_merged(const AttnArgs &a, int row, int hh, int lane, const f32x4 (&o)[2], float M,
                                              float den) {
-    const float inv = MEAN ? (den == 0.f ? NAN : 1.f) : 1.f / den;  // (no weight at all: NaN, as 0 / 0)
+    const float inv = has_eight<F> ? (den == 0.f ? NAN : 1.f) : 1.f / den;  // (no weight at all: NaN, as 0 / 0)
 #pragma unroll
     for (int k = 0; k < 2; ++k) store_out4(a, row, hh, 4 * lane + 256 * k, o[k] * inv);
     if (a.lse && lane == 0) a.lse[(size_t)row * kHeads + hh] = (M + log2f(den)) * kLn2;
 }
 
 // Heads hh0 .. hh0 + 4 / SW - 1 of a row with many splits; s_o holds 4 x 512 floats, s_ml 4 x 2.
-template <bool MEAN, int B, int SW, typename Slot>
+template <int F, int B, int SW, typename Slot>
 __device__ void merge_heads(const AttnArgs &a, int row, int hh0, int nsplit, Slot slot, float *s_o, float *s_ml) {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     const int hh = hh0 + wv / SW, part = wv % SW;
     f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
     float M = kNegInf, den = 0.f;
-    merge_splits<MEAN, B, SW>(part, nsplit, hh, lane, slot, o, M, den);
+    merge_splits<F, B, SW>(part, nsplit, hh, lane, slot, o, M, den);
     if constexpr (SW > 1) {
         if (part != 0) {
             f32x4 *dst = reinterpret_cast<f32x4 *>(s_o + wv * kDv) + lane;
@@ -585,11 +587,11 @@ __device__ void merge_heads(const AttnArgs &a, int row, int hh0, int nsplit, Slo
 #pragma unroll
         for (int w = 1; w < SW; ++w) {
             const float m = s_ml[2 * (wv + w)], l = s_ml[2 * (wv + w) + 1];
-            if (m == kNegInf) continue;  // fewer splits than wavefronts
+            if (F != kWindow && m == kNegInf) continue;  // fewer splits than wavefronts
             const float m_new = fmaxf(M, m);
-            float c_old = (M == kNegInf) ? 0.f : exp2f(M - m_new), c = exp2f(m - m_new);
+            float c_old = (M == kNegInf) ? 0.f : exp2f(M - m_new), c = (F == kWindow && m == kNegInf) ? 0.f : exp2f(m - m_new);
             const f32x4 *src = reinterpret_cast<const f32x4 *>(s_o + (wv + w) * kDv) + lane;
-            if constexpr (MEAN) {
+            if constexpr (has_eight<F>) {
                 c_old *= den;
                 c *= l;
                 den = c_old + c;
@@ -604,11 +606,11 @@ __device__ void merge_heads(const AttnArgs &a, int row, int hh0, int nsplit, Slo
             M = m_new;
         }
     }
-    store_merged<MEAN>(a, row, hh, lane, o, M, den);
+    store_merged<F>(a, row, hh, lane, o, M, den);
 }
 
 // A whole row of few parts, four heads per wavefront.
-template <bool MEAN, typename Slot>
+template <int F, typename Slot>
 __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
 #pragma unroll
@@ -616,8 +618,8 @@ __device__ void merge_row(const AttnArgs &a, int row, int nsplit, Slot slot) {
         const int hh = wv * (kHeads / 4) + k;
         f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         float M = kNegInf, den = 0.f;
-        merge_splits<MEAN, 2, 1>(0, nsplit, hh, lane, slot, o, M, den);
-        store_merged<MEAN>(a, row, hh, lane, o, M, den);
+        merge_splits<F, 2, 1>(0, nsplit, hh, lane, slot, o, M, den);
+        store_merged<F>(a, row, hh, lane, o, M, den);
     }
 }
 
@@ -869,14 +871,24 @@ __device__ __forceinline__ void group_barrier(int *ctr, int &epoch, int spin_lim
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Values that no row may read: a masked key has probability 0, but 0 times an
-// infinity or NaN is NaN.  Where some row masks a key, the forms of mla_cache.h zero
-// such values and leave it to the key's score, which is not finite either, to reach
-// the rows that see it.
-// (Two bf16 values a word.)
+// infinity or NaN is NaN.  The forms of mla_cache.h zero what is masked where a tile's
+// scores are not all finite, as those of a key with such a value never are.  Rows of a
+// block may differ in what they see: there such values are zeroed for all of
+// them, and a row that does see one gets its NaN apart (a score of NaN or +inf makes
+// the whole row NaN, one of -inf this value's dim, 0 x inf).
+// (Two bf16 values a word; all bits, a NaN, in place of those that are not finite.)
+__device__ __forceinline__ uint32_t not_finite_bf16x2(uint32_t w) {
+    return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
 __device__ __forceinline__ uint32_t finite_bf16x2(uint32_t w) {
     if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
     if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
     return w;
+}
+// c plus the sums over 16 keys of an operand's four NaNs or zeros a lane, times 0.
+__device__ __forceinline__ f32x4 mfma_f16_nan(uint32_t w0, uint32_t w1, f32x4 c) {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, u32x2{w0, w1}), f16x4{0, 0, 0, 0}, c, 0, 0, 0);
 }
 // Whether any of a wavefront's raw scores of a tile is not finite (a sum that overflows only costs time).
 __device__ __forceinline__ bool any_not_finite(f32x4 x) {
@@ -1061,11 +1073,14 @@ __device__ void decode_wg(const AttnArgs &a, int w, char *smem, int (*s_pages_g)
             vop[mt2] = u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
         if constexpr (F != kPlain) {
-            if (careful) {
+            if (careful) {  // (word i: keys 16 (i / 2) + 4 g + 2 (i & 1) and the next one)
 #pragma unroll
-                for (int mt2 = 0; mt2 < 8; ++mt2)
+                for (int i = 0; i < 4; ++i) {
+                    const int key = kbase + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
+                    const uint32_t seen = (row_sees<F>(a, key, sg.p) ? 0xffffu : 0u) | (row_sees<F>(a, key + 1, sg.p) ? 0xffff0000u : 0u);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) vop[mt2][i] = finite_bf16x2(vop[mt2][i]);
+                    for (int mt2 = 0; mt2 < 8; ++mt2) vop[mt2][i] &= seen;
+                }
             }
         }
         const u32x4 opb_h = {bh[0], bh[1], bh[2], bh[3]};
@@ -1183,9 +1198,9 @@ __device__ void decode_merge(const AttnArgs &a, int k, int part, float *s_o, flo
     };
     const int n = w1 - w0 + 1;
     if (MANY && a.merge_many)
-        merge_heads<has_eight<F>, 8, 4>(a, row, part, n, slot, s_o, s_ml);
+        merge_heads<F, 8, 4>(a, row, part, n, slot, s_o, s_ml);
     else
-        merge_heads<has_eight<F>, 4, 1>(a, row, 4 * part, n, slot, s_o, s_ml);
+        merge_heads<F, 4, 1>(a, row, 4 * part, n, slot, s_o, s_ml);
 }
 
 // The k-th row of the chunk requests whose keys are cut into ranges (requests
@@ -1260,11 +1275,11 @@ __device__ void chunk_merge(const AttnArgs &a, int k, int part, float *s_o, floa
     };
     const int row = it.row0 + it.i0 + j;
     if (MANY && a.chunk_merge_wgs == kHeads)
-        merge_heads<has_eight<F>, 8, 4>(a, row, part, it.nks_eff, slot, s_o, s_ml);
+        merge_heads<F, 8, 4>(a, row, part, it.nks_eff, slot, s_o, s_ml);
     else if (a.chunk_merge_wgs == kHeads / 4)
-        merge_heads<has_eight<F>, 4, 1>(a, row, 4 * part, it.nks_eff, slot, s_o, s_ml);
+        merge_heads<F, 4, 1>(a, row, 4 * part, it.nks_eff, slot, s_o, s_ml);
     else
-        merge_row<has_eight<F>>(a, row, it.nks_eff, slot);
+        merge_row<F>(a, row, it.nks_eff, slot);
 }
 
 // ------------------------------------------------------------- chunk path
@@ -1762,7 +1777,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto vconv = [&](bool careful) {
+    auto vconv = [&](int t, bool careful) {
         if constexpr (has_eight<F>) {
             // (half kt of the keys in word kt; a half whose scale is no number is not seen, or its scores are none either)
 #pragma unroll
@@ -1773,6 +1788,30 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         if constexpr (F != kPlain) {
             if (careful) {
+                // a NaN into the sums of every dim that has such a value among the keys that token tb sees
+#pragma unroll
+                for (int tb = 0; tb < kCT; ++tb) {
+                    const int at = it.p + it.i0 + tb, end = min(at + 1, k_end);
+                    const int kbase = ck.tile(t) + 4 * (opaque_lane() >> 4);
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt) {  // (keys 16 kt + 4 g .. + 3)
+                        uint32_t seen[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int key = kbase + 16 * kt + 2 * i;
+                            seen[i] = (key < end && row_sees<F>(a, key, at) ? 0xffffu : 0u) |
+                                      (key + 1 < end && row_sees<F>(a, key + 1, at) ? 0xffff0000u : 0u);
+                        }
+#pragma unroll
+                        for (int db = 0; db < 4; ++db) {
+                            // (found again for each token: sixteen kept words would spill)
+                            asm volatile("" : "+v"(av[db][2 * kt]), "+v"(av[db][2 * kt + 1]));
+                            acc[tb][db] = mfma_f16_nan(not_finite_bf16x2(av[db][2 * kt]) & seen[0],
+                                                       not_finite_bf16x2(av[db][2 * kt + 1]) & seen[1], acc[tb][db]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                }
 #pragma unroll
                 for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -1861,7 +1900,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         vload(0);
         softmax(0, 0, s0);
-        vconv(F == kWindow && hides(0) && any_not_finite(s0[0] + s0[1]));
+        vconv(0, F == kWindow && hides(0) && any_not_finite(s0[0] + s0[1]));
     }
     int slot = 0;  // ring slot of tile t (t % 3)
     [[maybe_unused]] int page_ahead = has_eight<F> ? page_of(min(2, ntiles - 1)) : 0;  // page of tile t + 2
@@ -1894,7 +1933,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             scores(slot1, s1);
             vload(slot1);
             softmax(t + 1, (t + 1) & 1, s1);
-            vconv(F == kWindow && hides(t + 1) && any_not_finite(s1[0] + s1[1]));
+            vconv(t + 1, F == kWindow && hides(t + 1) && any_not_finite(s1[0] + s1[1]));
         }
         slot = slot1;
         TRACE_TILE(t, 13);

@@ -92,3 +92,44 @@ def test_append8_of_the_largest_finite_values(base):
     # and read back: attention gives finite rows
     a = Attend(b, C.queries(b, 1).reshape(-1, 16, 576) * np.uint16(0), *down8(c))
     a.run().check("largest values")
+
+
+@pytest.mark.parametrize("keys,unit", [(0, 0), (64, 1)], ids=["whole", "split"])
+@pytest.mark.parametrize("window", [(16, 2), (70, 3), (1 << 20, 0)], ids=str)
+def test_infinities_of_a_windowed_cache(window, keys, unit):
+    """An infinite cached value whose score is -inf has a weight of 0, and 0 x inf is NaN: in that value's dim of every
+    row that sees the key, wherever its tile lies, and nowhere else.  Infinite rope dims have a weight of 0 alone."""
+    b = C.batch([50, 20, 33, 150], [1, 90, 1, 40], 32, seed=44)
+    pool, q = filled(b, 5), C.queries(b, 1).reshape(-1, 16, 576)
+    NEG, INF = 0xBF80, 0x7F80
+    q[:, :, 100], q[:, 5, 100] = NEG, 0x3F80  # scores of the values below: -inf, +inf for head 5
+    q[:, :, 300] = q[:, :, 7] = q[:, :, 530] = NEG
+    flat = pool.reshape(-1, 576)
+    for r, t, d in ((0, 45, 100), (0, 50, 300), (1, 30, 100), (1, 75, 300), (1, 75, 7), (2, 3, 100), (2, 1, 300), (3, 160, 300), (3, 0, 300), (3, 63, 100)):
+        flat[CO.slot(b, r, t), d] = INF
+    for r, t in ((1, 40), (0, 48), (3, 170)):
+        flat[CO.slot(b, r, t), 530] = INF
+    mla.debug_set(mla.MLA_DEBUG_CHUNK_KEYS, keys)
+    mla.debug_set(mla.MLA_DEBUG_DEC_UNIT, unit)
+    a = Attend(b, q, pool=pool, window=window).run()
+    out, lse = a.results()
+    qv = CO.bf16_value(q)
+    for row in range(b.num_rows):
+        r = int(np.searchsorted(b.cu_q, row, side="right")) - 1
+        pos = int(b.prefix_lens[r]) + row - int(b.cu_q[r])
+        k = CO.keys16(b, r, pos + 1, pool)
+        with np.errstate(invalid="ignore"):
+            ro, rl = CO.attend_row(qv[row], k, pos, SCALE, *window)
+        nan = np.isnan(ro)
+        np.testing.assert_array_equal(np.isnan(out[row]), nan, err_msg=str((r, pos)))
+        # what is finite, against bounds without the keys of weight 0
+        few = k[[j for j in CO.visible(pos, *window) if np.isfinite(k[j]).all()]]
+        to, tl = C.bounds(qv[row], few, len(few) - 1, SCALE, 0, 0, b.q_lens[r] > 1, True, np.where(nan, 0, ro), np.where(np.isnan(rl), 0, rl))
+        assert (np.where(nan, 0, np.abs(out[row] - ro)) <= to).all(), (r, pos)
+        assert (np.where(np.isnan(rl), 0, np.abs(lse[row] - rl)) <= tl).all(), (r, pos)
+
+
+def filled(b, seed):
+    """A bf16 pool with all of every request's tokens."""
+    rng = np.random.default_rng([seed, 4])
+    return W.f32_to_bf16_bits(rng.standard_normal((b.num_pages * b.page_size, 576), dtype=np.float32)).reshape(b.num_pages, b.page_size, 576)
