@@ -389,7 +389,8 @@ class LatentCache8:
     [num_pages][P][576], and `scales`, bf16 [num_pages][P / 16][2].
 
     LatentCache8(num_pages=n, page_size=P) allocates both (every code 0, every
-    scale 1); LatentCache8(data=.., scales=..) takes a program's own tensors."""
+    scale 1); LatentCache8(data=.., scales=..) takes a program's own tensors.
+    Both may be replaced later."""
 
     def __init__(self, num_pages: Optional[int] = None, page_size: Optional[int] = None, device="cuda", *, data=None, scales=None):
         import torch
@@ -401,14 +402,36 @@ class LatentCache8:
             # 4 bytes a block of 16 tokens, rounded up to 16
             whole = torch.ones(n // 2, dtype=torch.bfloat16, device=device)
             scales = whole[:num_pages * (page_size // MLA_CACHE8_BLOCK) * 2].view(num_pages, page_size // MLA_CACHE8_BLOCK, 2)
-        if data.dtype not in (torch.uint8, torch.float8_e4m3fn) or data.dim() != 3 or data.shape[2] != D_QK or not data.is_contiguous():
-            raise ValueError("data must be contiguous uint8 [num_pages][P][576]")
-        if (scales.dtype not in _bf16() or tuple(scales.shape) != (data.shape[0], data.shape[1] // MLA_CACHE8_BLOCK, 2) or
-                not scales.is_contiguous()):
-            raise ValueError("scales must be contiguous bf16 [num_pages][P / 16][2]")
-        self.data, self.scales = data, scales
-        self.num_pages, self.page_size = int(data.shape[0]), int(data.shape[1])
-        self.c = mla_cache8(data=_ptr(data), scales=_ptr(scales))
+        self.data, self.scales, self._of = data, scales, None
+        self._bound()
+
+    def _bound(self):
+        """(data, scales, their addresses, the C struct, pages, page size, device) of the tensors that `data` and `scales`
+        are now, checked again whenever they have changed."""
+        data, scales, of = self.data, self.scales, self._of
+        d, s = data.data_ptr(), scales.data_ptr()
+        if of is None or of[0] is not data or of[1] is not scales or of[2] != d or of[3] != s:
+            import torch
+            if data.dtype not in (torch.uint8, torch.float8_e4m3fn) or data.dim() != 3 or data.shape[2] != D_QK or not data.is_contiguous():
+                raise ValueError("data must be contiguous uint8 [num_pages][P][576]")
+            if (scales.dtype not in _bf16() or tuple(scales.shape) != (data.shape[0], data.shape[1] // MLA_CACHE8_BLOCK, 2) or
+                    not scales.is_contiguous()):
+                raise ValueError("scales must be contiguous bf16 [num_pages][P / 16][2]")
+            self._of = of = (data, scales, d, s, mla_cache8(data=d, scales=s), int(data.shape[0]), int(data.shape[1]),
+                             data.get_device() if data.device == scales.device else -1)
+        return of
+
+    @property
+    def c(self) -> mla_cache8:
+        return self._bound()[4]
+
+    @property
+    def num_pages(self) -> int:
+        return self._bound()[5]
+
+    @property
+    def page_size(self) -> int:
+        return self._bound()[6]
 
 
 def _window(window):
@@ -452,11 +475,13 @@ def _batch(batch: DeviceBatch, here):
 
 
 def _cache8(batch: DeviceBatch, cache: LatentCache8, here):
-    if cache.page_size != batch.page_size or cache.num_pages < batch.num_pages:
+    data, scales, _, _, c, pages, page_size, device = cache._bound()
+    if page_size != batch.page_size or pages < batch.num_pages:
         raise ValueError("the cache's pages do not match the batch's")
-    _on_device(cache.data, "the cache's data", here)
-    _on_device(cache.scales, "the cache's scales", here)
-    return ctypes.byref(cache.c)
+    if device != here:
+        _on_device(data, "the cache's data", here)
+        _on_device(scales, "the cache's scales", here)
+    return ctypes.byref(c)
 
 
 def _attend_args(batch: DeviceBatch, softmax_scale, out, lse, workspace, here):
