@@ -127,7 +127,8 @@ int mla_device_flags(int32_t clear, int32_t *flags, void *stream);
  *                         tuning and tests: results stay within rounding;
  *   MLA_DEBUG_WARM_PLAN   1 (the default; -1 restores it): a batch with as
  *                         many chunk requests as the last fully planned one
- *                         (same page size, table width and device), and
+ *                         (same page size, table width, device and form of
+ *                         the attention, see mla_cache.h), and
  *                         within 1/16 of its decode requests, decode tiles,
  *                         chunk query-key pairs and longest chunk, keeps
  *                         that plan's key split and decode unit size when

@@ -835,49 +835,77 @@ int make_plan_uncached(const mla_batch *b, const Shape &sh, int ncu, mla::ChunkR
     return MLA_OK;
 }
 
-// The plan depends only on the host lengths, the page size and the CU count;
-// the last one is kept per thread so a steady stream of identical steps
-// plans once.  The last full plan is kept too, as the warm start of batches
-// with nearly the same work (MLA_DEBUG_WARM_PLAN = 0 turns that off).
+// The plan depends only on the host lengths, the page size, the CU count and the
+// form; the last one is kept per thread and form so a steady stream of identical
+// steps plans once, also where a model's layers take turns between forms (full and
+// windowed attention, say).  The form's last full plan is kept too, as the warm
+// start of batches with nearly the same work (MLA_DEBUG_WARM_PLAN = 0 turns that off).
+constexpr size_t kPlanHdr = 12;
+constexpr int kKeptForms = 8;  // the form not planned for longest makes room
+struct KeptPlan {
+    unsigned long long used = 0;  // 0: free
+    int32_t form[3] = {};         // as the end of a header
+    std::vector<int32_t> key;     // header, query lengths, prefix lengths of `last`
+    Plan last, anchor;
+    int32_t anchor_hdr[kPlanHdr] = {};
+    bool have_anchor = false;
+};
+
+KeptPlan &kept_plan(const int32_t (&form)[3]) {
+    thread_local KeptPlan kept[kKeptForms];
+    thread_local unsigned long long clock = 0;
+    KeptPlan *k = kept;
+    for (KeptPlan &c : kept) {
+        if (c.used != 0 && std::memcmp(c.form, form, sizeof form) == 0) {
+            k = &c;
+            break;
+        }
+        if (c.used < k->used) k = &c;
+    }
+    if (k->used == 0 || std::memcmp(k->form, form, sizeof form) != 0) {
+        k->key.clear();
+        k->have_anchor = false;
+        std::memcpy(k->form, form, sizeof form);
+    }
+    k->used = ++clock;
+    return *k;
+}
+
 int make_plan(const mla_batch *b, const Shape &sh, Plan *pl, mla::ChunkRoute route = mla::kAbsorbAll, const mla::Form &form = {}) {
     *pl = Plan{};
     if (sh.R == 0) return MLA_OK;
     int st = MLA_OK;
     const int ncu = cu_count(&st);
     if (st != MLA_OK) return st;
-    constexpr size_t kHdr = 12;
-    const int32_t hdr[kHdr] = {b->page_size, ncu, sh.R, b->max_pages_per_req, route.min_rows, route.pair_keys,
-                               debug_value(MLA_DEBUG_CHUNK_KEYS).load(std::memory_order_relaxed),
-                               debug_value(MLA_DEBUG_DEC_UNIT).load(std::memory_order_relaxed),
-                               debug_value(MLA_DEBUG_DEC_FIRST).load(std::memory_order_relaxed),
-                               form.eight ? 1 : 0, form.band.window, form.band.sinks};
+    const int32_t of_form[3] = {form.eight ? 1 : 0, form.band.window, form.band.sinks};
+    const int32_t hdr[kPlanHdr] = {b->page_size, ncu, sh.R, b->max_pages_per_req, route.min_rows, route.pair_keys,
+                                   debug_value(MLA_DEBUG_CHUNK_KEYS).load(std::memory_order_relaxed),
+                                   debug_value(MLA_DEBUG_DEC_UNIT).load(std::memory_order_relaxed),
+                                   debug_value(MLA_DEBUG_DEC_FIRST).load(std::memory_order_relaxed),
+                                   of_form[0], of_form[1], of_form[2]};
     const size_t qbytes = (size_t)sh.R * sizeof(int32_t);
-    // key: header, query lengths, prefix lengths
-    thread_local std::vector<int32_t> key;
-    thread_local int32_t anchor_hdr[kHdr] = {};
-    thread_local bool have_anchor = false;
-    thread_local Plan cached, anchor;
-    if (key.size() == kHdr + 2 * (size_t)sh.R && std::memcmp(key.data(), hdr, sizeof hdr) == 0 &&
-        std::memcmp(key.data() + kHdr, b->q_lens, qbytes) == 0 &&
-        std::memcmp(key.data() + kHdr + sh.R, b->prefix_lens, qbytes) == 0) {
-        *pl = cached;
+    KeptPlan &k = kept_plan(of_form);
+    if (k.key.size() == kPlanHdr + 2 * (size_t)sh.R && std::memcmp(k.key.data(), hdr, sizeof hdr) == 0 &&
+        std::memcmp(k.key.data() + kPlanHdr, b->q_lens, qbytes) == 0 &&
+        std::memcmp(k.key.data() + kPlanHdr + sh.R, b->prefix_lens, qbytes) == 0) {
+        *pl = k.last;
         return MLA_OK;
     }
     // the anchor's header must match except for the request count
-    const bool warm = debug_value(MLA_DEBUG_WARM_PLAN).load(std::memory_order_relaxed) != 0 && have_anchor &&
-                      std::memcmp(anchor_hdr, hdr, 2 * sizeof(int32_t)) == 0 &&
-                      std::memcmp(anchor_hdr + 3, hdr + 3, (kHdr - 3) * sizeof(int32_t)) == 0;
-    st = make_plan_uncached(b, sh, ncu, route, pl, warm ? &anchor : nullptr, form);
+    const bool warm = debug_value(MLA_DEBUG_WARM_PLAN).load(std::memory_order_relaxed) != 0 && k.have_anchor &&
+                      std::memcmp(k.anchor_hdr, hdr, 2 * sizeof(int32_t)) == 0 &&
+                      std::memcmp(k.anchor_hdr + 3, hdr + 3, (kPlanHdr - 3) * sizeof(int32_t)) == 0;
+    st = make_plan_uncached(b, sh, ncu, route, pl, warm ? &k.anchor : nullptr, form);
     if (st != MLA_OK) return st;
-    key.resize(kHdr + 2 * (size_t)sh.R);
-    std::memcpy(key.data(), hdr, sizeof hdr);
-    std::memcpy(key.data() + kHdr, b->q_lens, qbytes);
-    std::memcpy(key.data() + kHdr + sh.R, b->prefix_lens, qbytes);
-    cached = *pl;
+    k.key.resize(kPlanHdr + 2 * (size_t)sh.R);
+    std::memcpy(k.key.data(), hdr, sizeof hdr);
+    std::memcpy(k.key.data() + kPlanHdr, b->q_lens, qbytes);
+    std::memcpy(k.key.data() + kPlanHdr + sh.R, b->prefix_lens, qbytes);
+    k.last = *pl;
     if (!pl->warm) {
-        anchor = *pl;
-        std::memcpy(anchor_hdr, hdr, sizeof hdr);
-        have_anchor = true;
+        k.anchor = *pl;
+        std::memcpy(k.anchor_hdr, hdr, sizeof hdr);
+        k.have_anchor = true;
     }
     return MLA_OK;
 }
