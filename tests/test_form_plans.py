@@ -4,6 +4,8 @@ and no form takes another's."""
 import os
 import subprocess
 
+import pytest
+
 from test_form_planner import FIELDS, check, harness, plans  # noqa: F401  (harness: a fixture)
 
 LAYERS = [dict(eight=0, window=0, sinks=0), dict(eight=1, window=0, sinks=0), dict(eight=1, window=500, sinks=64), dict(eight=0, window=500, sinks=64)]
@@ -36,6 +38,18 @@ def test_each_form_starts_warm_from_its_own_plan(harness):  # noqa: F811
         check(c, pl)
     for i, f in enumerate(LAYERS):  # as in a process that plans this form alone
         assert [pl for pl, _ in got[i::len(LAYERS)]] == [pl for pl, _ in plans(harness, [step(n, **f) for n in range(4)])]
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1000, 64), (3000, 0)])
+def test_no_form_takes_anothers_plan(harness, window, sinks):  # noqa: F811
+    """Neighbouring calls differ in one thing alone; each plan is that of a process of its own."""
+    near = [dict(eight=e, window=window, sinks=sinks) for e in (0, 1, 0, 1)]
+    if window:
+        near += [dict(eight=1, window=window, sinks=sinks + 32), dict(eight=1, window=window + 200, sinks=sinks + 32),
+                 dict(eight=0, window=window + 200, sinks=sinks + 32)]
+    alone = [plans(harness, [step(**f)])[0][0] for f in near]
+    assert alone[0] != alone[1], "lengths at which the caches' plans differ"
+    assert [pl for pl, _ in plans(harness, [step(**f) for f in near])] == alone
 
 
 def test_more_forms_than_are_kept(harness):  # noqa: F811
