@@ -37,6 +37,8 @@
  *
  * Window.  With a window of W keys and S sinks, the row at position t sees the
  * keys j <= t with j > t - W or j < S.  W >= 1, so a row always sees itself.
+ * Block-table entries of pages that hold no key that a row of the request sees
+ * may be anything, in appends as well.
  *
  * Values that are not finite.  Keys that a row does not see never reach it,
  * whatever they hold.  Those that it sees count as the sums say: a score of NaN
@@ -113,7 +115,7 @@ int mixed_step_attn8(const mla_batch *batch, const uint16_t *q, const mla_cache8
                      size_t workspace_bytes, void *stream);
 
 /* mixed_step_attn (bf16 cache) through a window.  Pages that hold no visible
- * key are not read, and their block-table entries may be anything.
+ * key are not read.
  * Errors: as mixed_step_attn, and MLA_ERR_INVALID_ARG for a bad window. */
 int mixed_step_attn_window(const mla_batch *batch, const uint16_t *q, const uint16_t *kv_cache, const mla_window *window,
                            float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace,

@@ -51,7 +51,9 @@
  *     environment when the library first runs): before launching, every entry
  *     point synchronises the stream and checks on the host that the device
  *     lengths equal the host ones, that every block-table entry a request uses
- *     lies in [0, num_pages) and that no written slot is aliased as above
+ *     (an append: those of the pages it writes into; attention: those of the
+ *     keys that its rows see) lies in [0, num_pages) and that no written slot is
+ *     written twice or, where the call attends, read as above
  *     (MLA_ERR_INVALID_ARG); after launching it synchronises again and turns
  *     the device flags into MLA_ERR_INVALID_ARG (bad page) or MLA_ERR_HIP
  *     (an expired wait).  For debugging: it makes every call synchronous.

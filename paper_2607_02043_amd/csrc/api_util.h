@@ -9,10 +9,12 @@
 namespace mla {
 
 // What a call uses of the cache, for check mode: writes in blocks of `block`
-// tokens, and, with a window (0: none), no key in [sinks, p - window].
+// tokens, and, with a window (0: none), no key in [sinks, p - window].  An append
+// reads no key before the first block that it writes into, as with a window of 1.
 struct CheckUse {
     long long block = 1, window = 0, sinks = 0;
 };
+inline CheckUse append_use(long long block) { return CheckUse{block, 1, 0}; }
 
 // Status and message of a failed HIP call.
 int hip_error(hipError_t e, const char *what);

@@ -134,7 +134,7 @@ int append_latent_kv_rope(const mla_batch *batch, const uint16_t *new_latents, f
         a.log2_page = log2_page;
         a.max_pages = batch->max_pages_per_req;
         a.num_pages = batch->num_pages;
-        if ((st = mla::check_before(batch, {}, stream)) != MLA_OK) return st;
+        if ((st = mla::check_before(batch, mla::append_use(1), stream)) != MLA_OK) return st;
         const hipError_t e = mla::launch_append_rope(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
         if (e != hipSuccess) return mla::hip_error(e, "append kernel launch");
         return mla::check_after("append_latent_kv_rope", stream);
@@ -170,8 +170,7 @@ int append_latent_kv8(const mla_batch *batch, const uint16_t *new_latents, float
         a.page_size = batch->page_size;
         a.max_pages = batch->max_pages_per_req;
         a.num_pages = batch->num_pages;
-        const mla::CheckUse use{MLA_CACHE8_BLOCK, 0, 0};
-        if ((st = mla::check_before(batch, use, stream)) != MLA_OK) return st;
+        if ((st = mla::check_before(batch, mla::append_use(MLA_CACHE8_BLOCK), stream)) != MLA_OK) return st;
         const hipError_t e = mla::launch_append8(a, rope_table(rope_base), static_cast<hipStream_t>(stream));
         if (e != hipSuccess) return mla::hip_error(e, "8-bit append kernel launch");
         return mla::check_after("append_latent_kv8", stream);

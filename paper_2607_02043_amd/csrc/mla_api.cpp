@@ -1076,7 +1076,7 @@ int append_latent_kv(const mla_batch *batch, const uint16_t *new_latents, uint16
     a.num_pages = batch->num_pages;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool chk = check_mode();
-    if (chk && (st = check_device_batch(batch, sh, s)) != MLA_OK) return st;
+    if (chk && (st = check_device_batch(batch, sh, s, mla::append_use(1))) != MLA_OK) return st;
     hipError_t e = mla::launch_append(a, s);
     if (e != hipSuccess) return hip_fail(e, "append kernel launch");
     return chk ? check_after_launch(s, "append_latent_kv") : MLA_OK;

@@ -133,3 +133,43 @@ def filled(b, seed):
     """A bf16 pool with all of every request's tokens."""
     rng = np.random.default_rng([seed, 4])
     return W.f32_to_bf16_bits(rng.standard_normal((b.num_pages * b.page_size, 576), dtype=np.float32)).reshape(b.num_pages, b.page_size, 576)
+
+
+@pytest.mark.parametrize("stale", ["outside the pool", "another request's"])
+@pytest.mark.parametrize("kind", ["8-bit", "rotated", "bf16"])
+def test_check_mode_of_a_windowed_program_that_gives_pages_back(kind, stale):
+    """Entries of pages that no row sees any more hold anything: an append then attends under check mode as without."""
+    import torch
+    window, P = (40, 5), 16
+    b = C.batch([300, 200, 90], [1, 33, 1], P, seed=45)
+    q, new = C.queries(b, 1), to_dev(C.new_latents(b, 3))
+    data, scales = C.cache8(b, 2)
+    bt = b.block_table.copy()
+    for r in range(b.num_reqs):
+        for lp in range(bt.shape[1]):
+            if lp * P >= window[1] and lp * P + P - 1 <= int(b.prefix_lens[r]) - window[0]:
+                # (the page that the next request writes its first new token into)
+                o = (r + 1) % b.num_reqs
+                bt[r, lp] = (-3, b.num_pages, 1 << 30)[lp % 3] if stale == "outside the pool" else b.block_table[o, int(b.prefix_lens[o]) // P]
+    results = []
+    for check, table in ((0, b.block_table), (0, bt), (1, bt)):
+        mla.debug_set(mla.MLA_DEBUG_CHECK, check)
+        a = Attend(b, q, data, scales, window=window) if kind == "8-bit" else Attend(b, q, pool=filled(b, 5), window=window)
+        a.db.bt_dev.copy_(torch.from_numpy(table))
+        if kind == "8-bit":
+            mla.append_latent_kv8(a.db, new, a.cache, rope_base=BASE)
+        elif kind == "rotated":
+            mla.append_latent_kv_rope(a.db, new, BASE, a.cache)
+        else:
+            mla.append_latent_kv(a.db, new, a.cache)
+        results.append(a.run().results())
+    for x in results[1:]:
+        for u, v in zip(results[0], x):
+            np.testing.assert_array_equal(u, v)
+    assert mla.device_flags() == 0
+    # what an append writes into is still looked at
+    a.db.bt_dev[1, 210 // P] = b.num_pages
+    call = {"8-bit": lambda: mla.append_latent_kv8(a.db, new, a.cache), "rotated": lambda: mla.append_latent_kv_rope(a.db, new, BASE, a.cache),
+            "bf16": lambda: mla.append_latent_kv(a.db, new, a.cache)}[kind]
+    with pytest.raises(mla.MlaError, match="outside"):
+        call()
