@@ -38,7 +38,10 @@
  * Window.  With a window of W keys and S sinks, the row at position t sees the
  * keys j <= t with j > t - W or j < S.  W >= 1, so a row always sees itself.
  * Block-table entries of pages that hold no key that a row of the request sees
- * may be anything, in appends as well.
+ * may be anything, in appends as well; page 0 is read in place of a page outside
+ * the pool.  Keys are read in tiles of 32: up to 31 hidden keys behind the sinks
+ * and as many before the window of a block of 8 rows are read with the seen ones
+ * (whatever they hold, it does not reach a result), the tiles between are not.
  *
  * Values that are not finite.  Keys that a row does not see never reach it,
  * whatever they hold.  Those that it sees count as the sums say: a score of NaN
@@ -114,8 +117,7 @@ int mixed_step_attn8(const mla_batch *batch, const uint16_t *q, const mla_cache8
                      float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace,
                      size_t workspace_bytes, void *stream);
 
-/* mixed_step_attn (bf16 cache) through a window.  Pages that hold no visible
- * key are not read.
+/* mixed_step_attn (bf16 cache) through a window.
  * Errors: as mixed_step_attn, and MLA_ERR_INVALID_ARG for a bad window. */
 int mixed_step_attn_window(const mla_batch *batch, const uint16_t *q, const uint16_t *kv_cache, const mla_window *window,
                            float softmax_scale, void *out, int32_t out_dtype, float *lse, void *workspace,
