@@ -57,10 +57,13 @@ struct Form {
 constexpr int kPlain = 0;
 constexpr int kWindow = 1;  // through AttnArgs::band
 constexpr int kEight = 2;   // over the 8-bit cache, AttnArgs::kv8
+constexpr int kFine = 4;    // either, fp32 output: chunk rows keep 22 bits of a probability
 template <int F>
 inline constexpr bool has_window = (F & kWindow) != 0;
 template <int F>
 inline constexpr bool has_eight = (F & kEight) != 0;
+template <int F>
+inline constexpr bool has_fine = (F & kFine) != 0;
 constexpr int kBlock8 = 16;  // tokens that share a pair of scales (MLA_CACHE8_BLOCK)
 
 struct AttnArgs {

@@ -1329,6 +1329,12 @@ template <int F>
 constexpr int q_reg_steps = F == kPlain ? 16 : has_eight<F> ? 16 : 15;
 constexpr int kChunkRing = 3;
 constexpr int kPTile = kCT * 64 * 16;                  // fp16 P of one tile: [token][lane] 16 bytes
+// P in LDS: two buffers, tile t in buffer t & 1.  kFine: hi and lo, twice over the 8-bit
+// cache and once over a bf16 one, whose tiles leave no room (a barrier more a tile).
+template <int F>
+constexpr int p_bytes = has_fine<F> && has_eight<F> ? 4 * kPTile : 2 * kPTile;
+template <int F>
+constexpr int p_stride = has_fine<F> ? (has_eight<F> ? 2 * kPTile : 0) : kPTile;  // between the buffers
 template <int F>
 constexpr int chunk_tile_bytes = has_eight<F> ? kTile8Bytes : kChunkTileBytes;
 // Forms other than the plain one raise a row's reference max as they go (see softmax): the factors [P buffer][token][head],
@@ -1338,11 +1344,19 @@ constexpr int kChunk8ScaleBytes = kChunkRing * 8;
 template <int F>
 constexpr int q_lds_bytes = (kQSteps - q_reg_steps<F>) * kCT * 64 * 16;  // query operands in LDS: [step][token][lane]
 template <int F>
-constexpr int chunk_lds = kChunkRing * chunk_tile_bytes<F> + 2 * kPTile + q_lds_bytes<F> + 2 * kCT * kHeads * 4 + 16 +
+constexpr int chunk_lds = kChunkRing * chunk_tile_bytes<F> + p_bytes<F> + q_lds_bytes<F> + 2 * kCT * kHeads * 4 + 16 +
                           (F != kPlain ? kRaiseBytes + kChunk8ScaleBytes : 0);
 // Largest exponent (log2 units) a probability may take against the reference
 // max: 2^15 stays inside fp16.
 constexpr float kMaxPExp = 15.f;
+// One fp16 of a probability (2^-11) leaves chunk rows 1e-4 off in the 2-norm: nothing
+// beside a bf16 output's own rounding (1.7e-3 with it and without), but a thousand
+// times an fp32 output's.  With fp32 output the forms of mla_cache.h (kFine) therefore
+// hold hi + lo, 1.2e-7 off: twice the value products, 2048 rows over 8192 keys in 8 bits
+// 548 -> 677 us, 4 x 1024 rows through a window of 1024 184 -> 223.  hi + lo is 22 bits
+// of a probability down to 2^-2 and off by 2^-25 below, so the reference is taken 2^6
+// below the max, as for decode rows.
+constexpr float kRefFine = 6.f;
 
 // Chunk tiles are laid out by octets of chunks: 16-byte chunk c (8 latent
 // dims) of tile key k (0..31) sits at position 256 (c >> 3) + 8 k +
@@ -1428,7 +1442,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     if (tid < min(npages, kPageWindow) && ck.logical_page(tid) < a.max_pages) pg = a.bt[(size_t)r * a.max_pages + ck.logical_page(tid)];
     constexpr int kQRegSteps = q_reg_steps<F>;
     u32x4 qreg[kQRegSteps], qr[kQSteps - kQRegSteps];
-    char *const s_q = smem + kChunkRing * chunk_tile_bytes<F> + 2 * kPTile;  // rope query operands
+    char *const s_q = smem + kChunkRing * chunk_tile_bytes<F> + p_bytes<F>;  // rope query operands
     {
         const uint16_t *qp = a.q + ((size_t)(it.row0 + it.i0 + tk) * kHeads + hd) * kDqk + (has_eight<F> ? 16 : 8) * g;
         const auto dim = [](int s) { return has_eight<F> ? 64 * (s / 2) + 8 * (s & 1) : 32 * s; };
@@ -1509,7 +1523,8 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
 #undef MLA_CHUNK_DMA_S
         } else {
             // keys past the item's range repeat its last key (a finite cached latent)
-            const int key = min(kbase + dkey, k_end - 1);
+            const int ln = F == kPlain ? lane : opaque_lane();  // (or an address is kept across the tiles, in scratch)
+            const int key = min(kbase + (has_fine<F> ? 8 * dw + (ln >> 3) : dkey), k_end - 1);
             const char *gs;
             if (fused && key >= it.p) {
                 gs = reinterpret_cast<const char *>(a.new_kv) + (size_t)(it.row0 + key - it.p) * kRowBytes;
@@ -1518,7 +1533,6 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
                 gs = reinterpret_cast<const char *>(a.kv) +
                      ((size_t)pg * a.page_size + (key & (a.page_size - 1))) * kRowBytes;
             }
-            const int ln = F == kPlain ? lane : opaque_lane();  // (or an address is kept across the tiles, in scratch)
             gs += 16 * ((ln & 7) ^ ((ln >> 3) & 7));
 #define MLA_CHUNK_DMA_V(r) lds_dma16_imm<128 * (r)>(gs, __builtin_amdgcn_readfirstlane(dst + 4096 * (r)))
             MLA_CHUNK_DMA_V(0); MLA_CHUNK_DMA_V(1); MLA_CHUNK_DMA_V(2); MLA_CHUNK_DMA_V(3); MLA_CHUNK_DMA_V(4);
@@ -1728,7 +1742,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
                     }
                 }
                 if (__builtin_amdgcn_ballot_w64(tm > m_ref + kMaxPExp) != 0) {
-                    const float m_new = fmaxf(m_ref, wave_max16(tm));
+                    const float m_new = fmaxf(m_ref, wave_max16(tm) - (has_fine<F> ? kRefFine : 0.f));
                     const float f = m_ref == kNegInf ? 0.f : exp2f(m_ref - m_new);
                     l_run *= f;
                     m_ref = m_new;
@@ -1750,8 +1764,15 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             p[e] = __builtin_amdgcn_exp2f(x[e] * a.scale_log2 - mref);
         }
         l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        *reinterpret_cast<u32x4 *>(s_pbuf + __builtin_amdgcn_readfirstlane(pbuf * kPTile) + (wv * 64 + lane) * 16) =
+        char *const dst = s_pbuf + __builtin_amdgcn_readfirstlane(pbuf * p_stride<F>) + (wv * 64 + lane) * 16;
+        *reinterpret_cast<u32x4 *>(dst) =
             u32x4{f16x2_bits(p[0], p[1]), f16x2_bits(p[2], p[3]), f16x2_bits(p[4], p[5]), f16x2_bits(p[6], p[7])};
+        if constexpr (has_fine<F>) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] -= (float)(_Float16)p[e];
+            *reinterpret_cast<u32x4 *>(dst + kPTile) =
+                u32x4{f16x2_bits(p[0], p[1]), f16x2_bits(p[2], p[3]), f16x2_bits(p[4], p[5]), f16x2_bits(p[6], p[7])};
+        }
     };
     // V^T operands of a tile for this wave's value dims, converted to fp16.
     // They are read and converted before the barrier that P waits for, so
@@ -1771,8 +1792,14 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         const char *tile = smem + __builtin_amdgcn_readfirstlane(slot * kChunkTileBytes);
 #pragma unroll
         for (int db = 0; db < 4; ++db) {
-            const u32x2 lo = lds_read_tr16(tile + vt_off[db]);
-            const u32x2 hi = lds_read_tr16(tile + vt_off[db] + 2048);
+            int off = vt_off[db];
+            if constexpr (has_fine<F>) {  // (db is bits 5 and 6: no registers for all four over the tiles)
+                off = vt_off[0];
+                asm volatile("" : "+v"(off));
+                off ^= 32 * db;
+            }
+            const u32x2 lo = lds_read_tr16(tile + off);
+            const u32x2 hi = lds_read_tr16(tile + off + 2048);
             av[db] = u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -1826,13 +1853,15 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     // O^T += V^T P^T for tile t (P from buffer t & 1)
     auto pv = [&](int t) {
         const int pbuf = t & 1;
-        const char *pb = s_pbuf + __builtin_amdgcn_readfirstlane(pbuf * kPTile) + lane * 16;
-        constexpr int PD = 3;  // P operands in flight
+        const char *pb = s_pbuf + __builtin_amdgcn_readfirstlane(pbuf * p_stride<F>) + lane * 16;
+        constexpr int PD = F == (kWindow | kEight | kFine) ? 2 : 3;  // P operands in flight
+        constexpr int parts = has_fine<F> ? 2 : 1, np = parts * kCT;
+        const auto p_at = [&](int k) { return pb + (k % parts) * kPTile + (k / parts) * 64 * 16; };
         u32x4 bp[PD];
         [[maybe_unused]] int raised_at = 0;
         if constexpr (F != kPlain) raised_at = s_raised[pbuf * kCT + (lane & 7)];
 #pragma unroll
-        for (int tb = 0; tb < PD; ++tb) bp[tb] = *reinterpret_cast<const u32x4 *>(pb + tb * 64 * 16);
+        for (int k = 0; k < PD; ++k) bp[k] = *reinterpret_cast<const u32x4 *>(p_at(k));
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (F != kPlain) {
             const uint64_t raised = __builtin_amdgcn_ballot_w64(raised_at == t) & 0xff;
@@ -1847,9 +1876,10 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             }
         }
 #pragma unroll
-        for (int tb = 0; tb < kCT; ++tb) {
-            const u32x4 cur = bp[tb % PD];
-            if (tb + PD < kCT) bp[tb % PD] = *reinterpret_cast<const u32x4 *>(pb + (tb + PD) * 64 * 16);
+        for (int k = 0; k < np; ++k) {
+            const u32x4 cur = bp[k % PD];
+            const int tb = k / parts;
+            if (k + PD < np) bp[k % PD] = *reinterpret_cast<const u32x4 *>(p_at(k + PD));
 #pragma unroll
             for (int db = 0; db < 4; ++db) acc[tb][db] = mfma_f16(av[db], cur, acc[tb][db]);
             __builtin_amdgcn_sched_barrier(0);
@@ -1900,7 +1930,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
         }
         vload(0);
         softmax(0, 0, s0);
-        vconv(0, F == kWindow && hides(0) && any_not_finite(s0[0] + s0[1]));
+        vconv(0, has_window<F> && !has_eight<F> && hides(0) && any_not_finite(s0[0] + s0[1]));
     }
     int slot = 0;  // ring slot of tile t (t % 3)
     [[maybe_unused]] int page_ahead = has_eight<F> ? page_of(min(2, ntiles - 1)) : 0;  // page of tile t + 2
@@ -1932,8 +1962,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
             if constexpr (has_eight<F>) scales8(w8);
             scores(slot1, s1);
             vload(slot1);
+            if constexpr (has_fine<F> && !has_eight<F>) lds_barrier();  // P of tile t is read
             softmax(t + 1, (t + 1) & 1, s1);
-            vconv(t + 1, F == kWindow && hides(t + 1) && any_not_finite(s1[0] + s1[1]));
+            vconv(t + 1, has_window<F> && !has_eight<F> && hides(t + 1) && any_not_finite(s1[0] + s1[1]));
         }
         slot = slot1;
         TRACE_TILE(t, 13);
@@ -2038,7 +2069,7 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attention_kernel(AttnArgs a) 
             }
         }
         else
-            decode_item<F>(a, item - a.n_chunk_items, smem, s_pages, s_seg, s_gbar);
+            decode_item<F & ~kFine>(a, item - a.n_chunk_items, smem, s_pages, s_seg, s_gbar);
         TRACE(7);
         int grid = a.grid;
         asm volatile("" : "+s"(grid));  // (computed again per item: kept across the items it would take registers from their loops)
@@ -2222,14 +2253,16 @@ hipError_t launch_attention(const AttnArgs &a, hipStream_t s) {
     const int grid = a.grid;
     if (grid == 0) return hipSuccess;
     const dim3 wgs(grid), threads(kAttnThreads);
+    const bool fine = a.out_bf16 == 0 && a.n_chunk_items > 0;
+    const auto launch = [&](auto *kernel) { hipLaunchKernelGGL(kernel, wgs, threads, 0, s, a); };
     if (a.kv8 == nullptr && a.band.window == 0)
-        hipLaunchKernelGGL(attention_kernel<kPlain>, wgs, threads, 0, s, a);
+        launch(attention_kernel<kPlain>);
     else if (a.kv8 == nullptr)
-        hipLaunchKernelGGL(attention_kernel<kWindow>, wgs, threads, 0, s, a);
+        launch(fine ? attention_kernel<kWindow | kFine> : attention_kernel<kWindow>);
     else if (a.band.window == 0)
-        hipLaunchKernelGGL(attention_kernel<kEight>, wgs, threads, 0, s, a);
+        launch(fine ? attention_kernel<kEight | kFine> : attention_kernel<kEight>);
     else
-        hipLaunchKernelGGL((attention_kernel<kEight | kWindow>), wgs, threads, 0, s, a);
+        launch(fine ? attention_kernel<kEight | kWindow | kFine> : attention_kernel<kEight | kWindow>);
     return hipGetLastError();
 }
 

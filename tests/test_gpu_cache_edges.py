@@ -173,3 +173,46 @@ def test_check_mode_of_a_windowed_program_that_gives_pages_back(kind, stale):
             "bf16": lambda: mla.append_latent_kv(a.db, new, a.cache)}[kind]
     with pytest.raises(mla.MlaError, match="outside"):
         call()
+
+
+def fine_bounds(x_max, n, v, top, ref):
+    """How far an fp32 output may be from the 64-bit one where a score is one exact product s: x = s scale log2(e) in
+    fp32 (two roundings of 2^-24 |x|, one more of the difference to the reference), exp2 within 2^-22, the sums of
+    cache_cases.bounds.  Probabilities as fp16 hi + lo: 2^-22 of p, and 2^-25 where lo is below fp16's normal
+    range, each key once; the largest p is at least 2^6, so 2^-31 of the sum.  A bf16 value goes to fp16 within
+    2^-24, one of the 8-bit cache within 2^-25 of `top`."""
+    delta = 2.0 ** -24 * 3 * x_max * np.log(2) + 2.0 ** -22
+    sums = 2.0 ** -24 * (n / 8 + 8)
+    return v * (2 * delta + 2.0 ** -22 + n * 2.0 ** -31 + 2 * sums) + (2.0 ** -25 * top if top else 2.0 ** -24) + 2.0 ** -24 * np.abs(ref)
+
+
+@pytest.mark.parametrize("keys", [0, 64], ids=["whole", "split"])
+@pytest.mark.parametrize("window", [None, (12, 3), (100, 0)], ids=str)
+@pytest.mark.parametrize("eight", [True, False], ids=["8-bit", "bf16"])
+def test_fp32_output_of_chunk_rows(eight, window, keys):
+    """Chunk rows with fp32 output hold more of a probability than an fp16 has."""
+    window = window if eight or window else (1 << 20, 0)
+    b = C.batch([0, 37, 150, 64], [40, 21, 30, 1], 16, seed=46)
+    q = np.zeros((b.num_rows, 16, 576), np.uint16)
+    q[:, :, 575] = W.f32_to_bf16_bits(np.random.default_rng(46).uniform(-32, 32, (b.num_rows, 16)).astype(np.float32))
+    mla.debug_set(mla.MLA_DEBUG_CHUNK_KEYS, keys)
+    if eight:
+        a = Attend(b, q, *C.cache8(b, 2, upto=lambda r: int(b.prefix_lens[r] + b.q_lens[r])), window=window)
+    else:
+        a = Attend(b, q, pool=filled(b, 5), window=window)
+    out, _ = a.run().results()
+    qv = CO.bf16_value(q)
+    off = base = 0.0
+    for row in range(b.num_rows - 1):
+        r = int(np.searchsorted(b.cu_q, row, side="right")) - 1
+        i = row - int(b.cu_q[r])
+        pos = int(b.prefix_lens[r]) + i
+        k = a.keys(r, pos + 1)
+        ro, _ = CO.attend_row(qv[row], k, pos, SCALE, *(window or (0, 0)))
+        seen = k[CO.visible(pos, *(window or (0, 0)))]
+        x = np.abs(qv[row, :, 575]).max() * np.abs(seen[:, 575]).max() * SCALE * np.log2(np.e)
+        lim = fine_bounds(x, len(seen), np.abs(seen[:, :512]).max(), a.top_scale(r, i), ro)
+        assert (np.abs(out[row] - ro) <= lim).all(), (r, pos, float((np.abs(out[row] - ro) / lim).max()))
+        off, base = off + ((out[row] - ro) ** 2).sum(), base + (ro ** 2).sum()
+    log(f"  relative error {np.sqrt(off / base):.2e}")
+    assert mla.device_flags() == 0
