@@ -124,7 +124,7 @@ def test_infinities_of_a_windowed_cache(window, keys, unit):
         np.testing.assert_array_equal(np.isnan(out[row]), nan, err_msg=str((r, pos)))
         # what is finite, against bounds without the keys of weight 0
         few = k[[j for j in CO.visible(pos, *window) if np.isfinite(k[j]).all()]]
-        to, tl = C.bounds(qv[row], few, len(few) - 1, SCALE, 0, 0, b.q_lens[r] > 1, True, np.where(nan, 0, ro), np.where(np.isnan(rl), 0, rl))
+        to, tl = C.bounds(qv[row], few, len(few) - 1, SCALE, 0, 0, b.q_lens[r] > 1, not a.bf16, np.where(nan, 0, ro), np.where(np.isnan(rl), 0, rl))
         assert (np.where(nan, 0, np.abs(out[row] - ro)) <= to).all(), (r, pos)
         assert (np.where(np.isnan(rl), 0, np.abs(lse[row] - rl)) <= tl).all(), (r, pos)
 
