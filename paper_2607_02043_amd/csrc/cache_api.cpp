@@ -24,7 +24,7 @@ int check_base(float base, bool zero_ok) {
     return MLA_OK;
 }
 
-// The last base's table is kept per thread (64 powers of 2, a microsecond).
+// The last base's table is kept per thread (32 powers of 2, a microsecond).
 const mla::RopeTable &rope_table(float base) {
     thread_local mla::RopeTable t;
     thread_local float of = 0.f;

@@ -23,14 +23,14 @@
 //     through its own 2-slot ring.
 // Rows whose keys are split across items leave fp32 partials (the
 // unnormalised sum, over the 8-bit cache the average; the max and sum in log2
-// units); a second, small merge
-// kernel combines them in a fixed order.  Results are therefore run-to-run
-// deterministic and do not depend on the physical page order.
+// units); a second, small merge kernel combines them in a fixed order.  Results are
+// therefore run-to-run deterministic and do not depend on the physical page order.
 //
 // The attention and merge kernels are templates over the forms of mla_cache.h: plain,
-// through a window of keys with sinks, over a cache held in 8 bits, or both.
-// cache_tile.h holds that cache's tiles, cache_decode.h its decode items and
-// cache_append.h the appends that rotate or round on the way.
+// through a window of keys with sinks, over a cache held in 8 bits, or both, and those
+// with fp32 output and chunk rows once more with finer probabilities.  cache_tile.h
+// holds that cache's tiles, cache_decode.h its decode items and cache_append.h the
+// appends that rotate or round on the way.
 #include "mla_kernels.h"
 
 #include <limits.h>
@@ -65,15 +65,16 @@ constexpr int kDecRing = 2;                                   // ring slots of e
 constexpr int kDecGroupBytes = kDecRing * kDecTileBytes;
 constexpr int kDecXBytes = 4 * kHeads * 20 * 4;               // partial score blocks of a group
 constexpr int kDecLds = 2 * kDecGroupBytes + 2 * kDecXBytes;  // two groups: rings, then score blocks
-// chunk path
+// over the 8-bit cache
 constexpr int kTile8Bytes = kKeysPerTile * kDqk;        // 18432: a tile of the 8-bit cache, also a query block
 constexpr int kDec8SlotBytes = 2 * kTile8Bytes;         // its decode path: two tiles a ring slot
 constexpr int kDec8GroupBytes = kDecRing * kDec8SlotBytes;
-constexpr int kDec8XBytes = 4 * 64 * 16;                // score blocks of a group
+constexpr int kDec8XBytes = 4 * 64 * 16;                // a unit's probabilities in a group, fp16 hi and lo
 constexpr int kDec8ScaleBytes = kDecRing * 16;          // pairs of scales, four a slot
 constexpr int kDec8StatBytes = 4 * kHeads * 4 + 16;     // a float of each wave and head, a word of each wave
 constexpr int kDec8Lds = 2 * (kDec8GroupBytes + kDec8XBytes + kDec8ScaleBytes + kDec8StatBytes);
 static_assert(kTile8Bytes == kHeads * kRowBytes, "a query block fills a slot");
+// chunk path
 constexpr int kChunkKeys = kKeysPerTile;  // 32
 constexpr int kChunkTileBytes = kChunkKeys * kRowBytes;  // 36864
 

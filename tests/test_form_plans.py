@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from test_form_planner import FIELDS, check, harness, plans  # noqa: F401  (harness: a fixture)
+from test_form_planner import check, harness, plans  # noqa: F401  (harness: a fixture)
 
 LAYERS = [dict(eight=0, window=0, sinks=0), dict(eight=1, window=0, sinks=0), dict(eight=1, window=500, sinks=64), dict(eight=0, window=500, sinks=64)]
 
