@@ -48,9 +48,8 @@
  * or +inf makes the row's output and lse of that head NaN, one of -inf has a
  * weight of 0, and 0 x inf is NaN in the dims whose value is infinite.
  *
- * Probabilities meet the values with 22 bits (8-bit cache) or 16 (bf16 cache) in
- * decode rows.  Chunk rows hold 22 bits where the output is fp32 and 11 where it
- * is bf16 and rounds more than that.  Sums are fp32.
+ * Probabilities meet the values with 22 bits or more; in chunk rows with bf16
+ * output, which rounds to fewer, with 11.  Sums are fp32.
  */
 #ifndef MLA_CACHE_H
 #define MLA_CACHE_H

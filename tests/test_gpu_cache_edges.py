@@ -216,3 +216,24 @@ def test_fp32_output_of_chunk_rows(eight, window, keys):
         off, base = off + ((out[row] - ro) ** 2).sum(), base + (ro ** 2).sum()
     log(f"  relative error {np.sqrt(off / base):.2e}")
     assert mla.device_flags() == 0
+
+
+@pytest.mark.parametrize("eight,window", [(True, None), (True, (1 << 20, 0)), (False, (1 << 20, 0))], ids=str)
+@pytest.mark.parametrize("prefix", [1, 3, 9, 40])
+def test_fp32_output_of_decode_rows(prefix, eight, window):
+    """Decode rows in the 2-norm.  A weight off by e_j moves the output by w_j e_j (v_j - out); the values here are
+    independent with mean 0, so over many rows and dims the error's norm is at most max |e| of the output's.
+    e, in 2^-24: the score, one product and x = s scale log2(e), three roundings of |x| ln 2 (|x| < 1.6 but for a few:
+    4 x 3.5 x SCALE log2 e); exp2 within an ulp, 2; the probability's parts 2^-22, 4; the sum, its inverse and the output, 3."""
+    b = C.batch([prefix] * 40, [1] * 40, 16, seed=47)
+    q = np.zeros((b.num_rows, 16, 576), np.uint16)
+    q[:, :, 575] = W.f32_to_bf16_bits(np.random.default_rng(47).uniform(-4, 4, (b.num_rows, 16)).astype(np.float32))
+    if eight:
+        a = Attend(b, q, *C.cache8(b, 2, upto=lambda r: prefix + 1), window=window)
+    else:
+        a = Attend(b, q, pool=filled(b, 5), window=window)
+    out, _ = a.run().results()
+    want = np.stack([CO.attend_row(CO.bf16_value(q[r]), a.keys(r, prefix + 1), prefix, SCALE)[0] for r in range(40)])
+    rel = np.sqrt(((out - want) ** 2).sum() / (want ** 2).sum())
+    log(f"  relative error {rel:.2e}")
+    assert rel <= 2.0 ** -24 * (3 * 1.6 * np.log(2) + 2 + 4 + 3)
