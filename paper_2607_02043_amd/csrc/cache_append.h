@@ -21,7 +21,7 @@ __device__ __forceinline__ SinCos rope_angle(int t, double turns) {
 
 // One wavefront a row, as append_kernel; lanes 0 .. 31 rotate a pair each.
 // Bound by latency like it: lengths -> page id -> store, with the row's loads and
-// the angles beside them (4 tokens 1.9 us, 4160 tokens 4.3 us, 2.2 TB/s).
+// the angles beside them (4 tokens 2.0 us, 4160 tokens 4.5 us, 2.1 TB/s).
 __global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendArgs a, RopeTable rope) {
     const int lane = threadIdx.x & 63;
     const int row = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -77,8 +77,8 @@ struct Block8Count {
 };
 
 // Bound by latency: the lengths, then the page id and the rows, then the old scales,
-// then the stores, a round trip each (256 tokens of 256 requests 5.6 us, with the
-// turns of the rotation found in the kernel 6.0).
+// then the stores, a round trip each (256 tokens of 256 requests 5.2 us, with the
+// turns of the rotation found in the kernel 0.4 more).
 // One workgroup a block: thread (wave w, lane l) takes the compressed chunk l
 // (8 dims) of its rows w, w + 4, .., and the first 128 threads one rope chunk (4
 // pairs) each.  The two maxima meet in LDS; then everything is scaled, rounded and

@@ -71,7 +71,7 @@ __device__ __forceinline__ void issue8(const Source8 &s, uint32_t slot, uint32_t
 // each wave scores 16 keys over all dims, takes their probabilities against the
 // reference so far and passes those on (the scores passed on instead, whose softmax
 // every wave then repeats: 329, so 307), and then accumulates its 128 value dims over
-// the 64 keys.  That size now takes 269 us with the merge, 4.7 TB/s.
+// the 64 keys.  That size now takes 261 us with the merge, 4.9 TB/s.
 // Keys are converted at the matrix instruction (two values an instruction, the scale of
 // the 16 keys applied on the way: bf16 holds the result exactly).  Values become fp16
 // relative to v_ref, the scale of the first blocks (raised, rarely, to what fp16

@@ -1365,7 +1365,7 @@ constexpr float kMaxPExp = 15.f;
 // beside a bf16 output's own rounding (1.7e-3 with it and without), but a thousand
 // times an fp32 output's.  With fp32 output the forms of mla_cache.h (kFine) therefore
 // hold hi + lo, 1.2e-7 off: twice the value products, 2048 rows over 8192 keys in 8 bits
-// 548 -> 677 us, 4 x 1024 rows through a window of 1024 184 -> 223.  hi + lo is 22 bits
+// 540 -> 657 us, 4 x 1024 rows through a window of 1024 182 -> 220.  hi + lo is 22 bits
 // of a probability down to 2^-2 and off by 2^-25 below, so the reference is taken 2^6
 // below the max, as for decode rows.
 constexpr float kRefFine = 6.f;
@@ -1555,7 +1555,7 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
 
     // The same over the 8-bit cache: five DMAs of each of the four waves, the scales among them.  A wave's 16 keys are in
     // one page (16 tokens at least).  The lanes' offsets wait in the page window that chunk items leave free: computed
-    // for each tile they make 2048 rows over 8192 keys 540 us, not 533, and no register is left to keep one.
+    // for each tile they cost 1.3 % of 2048 rows over 8192 keys, and no register is left to keep one.
     [[maybe_unused]] int *const s_voff8 = s_pages + kPageWindow;  // [wave of four][lane]
     [[maybe_unused]] auto issue8 = [&](int t, int slot, int page) {
         const int kbase = ck.tile(t);
@@ -1592,8 +1592,9 @@ __device__ bool chunk_item(const AttnArgs &a, int item, char *smem, int *s_pages
     f32x4 acc[kCT][4];  // [token][value block db]
 
     // Over the 8-bit cache: one 16-byte piece of a key a lane feeds two steps, converted on the way (exactly, scale
-    // included).  2048 rows over 8192 keys take 533 us, 960 TFLOP/s; the eight waves' conversions are half of the vector
-    // instructions (two tokens a wave, half of the conversions and more query operands in LDS: 567 us).
+    // included).  2048 rows over 8192 keys beside 128 decodes take 540 us, 980 TFLOP/s; the eight waves' conversions are
+    // half of the vector instructions (two tokens a wave, half of the conversions and more query operands in LDS: 6 %
+    // slower).
     [[maybe_unused]] auto scores8 = [&](const char *tile, f32x4 (&s)[2]) {
         s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
         constexpr int D = 2, kGroups = kDqk / 64;  // groups of 64 dims, those whose pieces are in flight
