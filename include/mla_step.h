@@ -166,8 +166,10 @@ const char *mla_last_error(void);
 
 /* Device workspace (bytes) that mixed_step_attn / mixed_step need for this
  * batch, or 0 on invalid arguments (then mla_last_error says why; an empty
- * batch also needs 0 bytes).  Depends only on the host arrays, the
- * device's CU count and the debug knobs that force the plan (a workspace
+ * batch also needs 0 bytes).  Depends on the host arrays, the device's CU
+ * count, where a warm start applies (MLA_DEBUG_WARM_PLAN) the thread's last full
+ * plan, by a few per cent, so ask on the thread that calls, for the batch that it
+ * calls next; and on the debug knobs that force the plan (a workspace
  * sized under one setting of MLA_DEBUG_CHUNK_KEYS, MLA_DEBUG_DEC_UNIT or
  * MLA_DEBUG_DEC_FIRST may be too small under another: the call then fails
  * with MLA_ERR_WORKSPACE).  The first 256 bytes hold the work-queue counters of the
