@@ -45,6 +45,10 @@ HIDDEN = 2048
 EXPORTED_CACHE = ("mla_cache8_scale_bytes", "append_latent_kv_rope", "append_latent_kv8", "mixed_step_attn8_workspace_bytes",
                   "mixed_step_attn_window_workspace_bytes", "mixed_step_attn8", "mixed_step_attn_window")
 MLA_CACHE8_BLOCK = 16
+# include/mla_ffn.h
+EXPORTED_FFN = ("mla_linear4_workspace_bytes", "mla_linear4", "mla_gated_ffn_workspace_bytes", "mla_gated_ffn", "mla_gated_ffn4")
+MLA_MX4_GROUP = 32
+MLA_FFN_COUNTER_BYTES = 4096
 
 
 class MlaError(RuntimeError):
@@ -87,6 +91,19 @@ class mla_cache8(ctypes.Structure):
 
 class mla_window(ctypes.Structure):
     _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
+class mla_mx4(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class mla_ffn_weights(ctypes.Structure):
+    _fields_ = [("w_gate", ctypes.c_void_p), ("w_up", ctypes.c_void_p), ("w_down", ctypes.c_void_p),
+                ("hidden", ctypes.c_int32), ("inner", ctypes.c_int32)]
+
+
+class mla_ffn4_weights(ctypes.Structure):
+    _fields_ = [("w_gate", mla_mx4), ("w_up", mla_mx4), ("w_down", mla_mx4), ("hidden", ctypes.c_int32), ("inner", ctypes.c_int32)]
 
 
 _lib = None
@@ -154,6 +171,14 @@ def lib() -> ctypes.CDLL:
             f.argtypes = [bp, np_]
             f.restype = sz
         L.mla_cache8_scale_bytes.restype = sz
+        L.mla_linear4.argtypes = [i32, vp, ctypes.POINTER(mla_mx4), i32, i32, vp, i32, vp, sz, vp]
+        L.mla_gated_ffn.argtypes = [i32, vp, ctypes.POINTER(mla_ffn_weights), vp, i32, vp, sz, vp]
+        L.mla_gated_ffn4.argtypes = [i32, vp, ctypes.POINTER(mla_ffn4_weights), vp, i32, vp, sz, vp]
+        for f in (L.mla_linear4, L.mla_gated_ffn, L.mla_gated_ffn4):
+            f.restype = ctypes.c_int
+        for f in (L.mla_linear4_workspace_bytes, L.mla_gated_ffn_workspace_bytes):
+            f.argtypes = [i32, i32, i32]
+            f.restype = sz
         _lib = L
     return _lib
 
@@ -552,3 +577,120 @@ def workspace_for_cache8(batch: DeviceBatch, window=None, device="cuda"):
 def workspace_for_window(batch: DeviceBatch, window, device="cuda"):
     """A zeroed workspace for mixed_step_attn_window (None if it needs none)."""
     return _workspace(lib().mixed_step_attn_window_workspace_bytes, batch, window, device)
+
+
+# --------------------------------------------------------------------------
+# The feed-forward half of a layer (include/mla_ffn.h)
+# --------------------------------------------------------------------------
+class Weights4:
+    """A weight matrix [N][K] in 4 bits: `codes`, uint8 [N][K / 2] (two e2m1 codes a byte, the even one in the low half),
+    and `scales`, uint8 [N][K / 32] (b stands for 2^(b - 127)).  K is a multiple of 32.  The tensors stay those it was
+    made of."""
+
+    def __init__(self, codes, scales):
+        import torch
+        if codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_contiguous() or codes.shape[1] == 0 or codes.shape[1] % 16:
+            raise ValueError("codes must be contiguous uint8 [N][K / 2], K a multiple of 32")
+        if (scales.dtype != torch.uint8 or not scales.is_contiguous() or
+                tuple(scales.shape) != (codes.shape[0], codes.shape[1] * 2 // MLA_MX4_GROUP)):
+            raise ValueError("scales must be contiguous uint8 [N][K / 32]")
+        if scales.device != codes.device:
+            raise ValueError(f"codes are on {codes.device}, scales on {scales.device}")
+        self._tensors = (codes, scales)
+        self.out_features, self.in_features = int(codes.shape[0]), int(codes.shape[1]) * 2
+        self.device_index = codes.get_device()
+
+    codes = property(lambda self: self._tensors[0])
+    scales = property(lambda self: self._tensors[1])
+
+    @property
+    def c(self) -> mla_mx4:
+        return mla_mx4(self._tensors[0].data_ptr(), self._tensors[1].data_ptr())
+
+
+class FfnWeights:
+    """The weights of a gated feed-forward block: `gate` and `up` [inner][hidden], `down` [hidden][inner], each a
+    contiguous bf16 tensor, or each a Weights4.  They stay those it was made of."""
+
+    def __init__(self, gate, up, down):
+        self._weights = (gate, up, down)
+        self.four_bit = isinstance(gate, Weights4)
+        if any(isinstance(w, Weights4) != self.four_bit for w in (up, down)):
+            raise ValueError("gate, up and down must be of one kind")
+        if self.four_bit:
+            shapes = [(w.out_features, w.in_features) for w in self._weights]
+            devices = {w.device_index for w in self._weights}
+        else:
+            for name, w in zip(("gate", "up", "down"), self._weights):
+                if w.dtype not in _bf16() or w.dim() != 2 or not w.is_contiguous():
+                    raise ValueError(f"{name} must be a contiguous bf16 matrix")
+            shapes = [tuple(int(n) for n in w.shape) for w in self._weights]
+            devices = {w.get_device() for w in self._weights}
+        self.inner, self.hidden = shapes[0]
+        if shapes[1] != shapes[0] or shapes[2] != (self.hidden, self.inner):
+            raise ValueError(f"gate and up must be [inner][hidden], down [hidden][inner]: got {shapes}")
+        if len(devices) > 1:
+            raise ValueError("gate, up and down must be on one device")
+        self.device_index = devices.pop()
+
+    gate = property(lambda self: self._weights[0])
+    up = property(lambda self: self._weights[1])
+    down = property(lambda self: self._weights[2])
+
+    @property
+    def c(self):
+        if self.four_bit:
+            return mla_ffn4_weights(*(w.c for w in self._weights), self.hidden, self.inner)
+        return mla_ffn_weights(*(w.data_ptr() for w in self._weights), self.hidden, self.inner)
+
+
+def _ffn_args(x, weights, width_in, width_out, out, workspace):
+    import torch
+    here = _here()
+    if weights.device_index != here:
+        raise ValueError("the weights are not on the current CUDA device")
+    if x.dim() != 2:
+        raise ValueError(f"x must be [T][{width_in}]")
+    T = int(x.shape[0])
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        _on_device(workspace, "workspace", here)
+    return ((T, _dev(x, "x", (T, width_in), _bf16(), here), ctypes.byref(weights.c)),
+            (_dev(out, "out", (T, width_out), (torch.float32, *_bf16()), here), _out_mode(out), _ptr(workspace), _nbytes(workspace)))
+
+
+def linear4(x, weights: Weights4, out, workspace, stream=None) -> None:
+    """out = x W^T with 4-bit weights: x bf16 [T][K], out [T][N] float32 or bf16 (dtype picks the mode)."""
+    a, b = _ffn_args(x, weights, weights.in_features, weights.out_features, out, workspace)
+    _check(lib().mla_linear4(*a, weights.in_features, weights.out_features, *b, _stream(stream)))
+
+
+def gated_ffn(x, weights: FfnWeights, out, workspace, stream=None) -> None:
+    """out = (silu(x gate^T) * (x up^T)) down^T: x bf16 [T][hidden], out [T][hidden] float32 or bf16 (dtype picks the mode)."""
+    a, b = _ffn_args(x, weights, weights.hidden, weights.hidden, out, workspace)
+    call = lib().mla_gated_ffn4 if weights.four_bit else lib().mla_gated_ffn
+    _check(call(*a, *b, _stream(stream)))
+
+
+def _ffn_workspace(n, num_rows, what, device):
+    import torch
+    if num_rows == 0:
+        return None
+    if n == 0:
+        raise ValueError(f"{num_rows} rows of {what}: not sizes that the library takes")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:MLA_FFN_COUNTER_BYTES].zero_()
+    return ws
+
+
+def workspace_for_linear4(num_rows: int, weights: Weights4, device="cuda"):
+    """A workspace for linear4 of up to num_rows rows, its counters zeroed (None for 0 rows)."""
+    n = int(lib().mla_linear4_workspace_bytes(int(num_rows), weights.in_features, weights.out_features))
+    return _ffn_workspace(n, num_rows, f"{weights.out_features} x {weights.in_features} weights", device)
+
+
+def workspace_for_ffn(num_rows: int, weights: FfnWeights, device="cuda"):
+    """A workspace for gated_ffn of up to num_rows rows and either output type, its counters zeroed (None for 0 rows)."""
+    n = int(lib().mla_gated_ffn_workspace_bytes(int(num_rows), weights.hidden, weights.inner))
+    return _ffn_workspace(n, num_rows, f"hidden {weights.hidden}, inner {weights.inner}", device)
