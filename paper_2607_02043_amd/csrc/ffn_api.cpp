@@ -4,6 +4,9 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include "api_util.h"
 #include "ffn_kernels.h"
 
@@ -12,6 +15,7 @@ namespace {
 using mla::set_error;
 
 constexpr int kMaxSize = 1 << 24;
+constexpr int kMaxRows = 1 << 28;
 
 size_t a256(size_t v) { return (v + 255) & ~size_t(255); }
 bool bad_ptr(const void *p) { return !p || (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
@@ -27,6 +31,7 @@ int check_size(const char *name, int32_t v, int32_t step) {
 int check_rows(int32_t T, const void *x, const void *out, int32_t out_dtype) {
     if (out_dtype != MLA_OUT_F32 && out_dtype != MLA_OUT_BF16)
         return set_error(MLA_ERR_INVALID_ARG, "out_dtype = %d is neither MLA_OUT_F32 nor MLA_OUT_BF16", out_dtype);
+    if (T > kMaxRows) return set_error(MLA_ERR_UNSUPPORTED, "num_rows = %d > %d", T, kMaxRows);
     if (bad_ptr(x) || bad_ptr(out)) return set_error(MLA_ERR_INVALID_ARG, "x / out must be non-NULL and 16-byte aligned");
     return MLA_OK;
 }
@@ -49,10 +54,15 @@ int check_workspace(const void *ws, size_t have, size_t need, int32_t T) {
 // Planes of h: one bf16 where the output is rounded to bf16 anyway, three (24 bits) in front of fp32.
 int planes_of(int32_t out_dtype) { return out_dtype == MLA_OUT_F32 ? 3 : 1; }
 
-// Workspace: the counters, then h (room for three planes).
-size_t h_at() { return MLA_FFN_COUNTER_BYTES; }
+// Workspace: the counters, room for the parts of split sums, then h (room for three planes).
+size_t h_at() { return MLA_FFN_COUNTER_BYTES + ffn::kPartBytes; }
 size_t ffn_bytes(int32_t T, int32_t inner) { return h_at() + a256((size_t)T * (size_t)inner * 3 * 2); }
-size_t linear_bytes() { return MLA_FFN_COUNTER_BYTES; }
+size_t linear_bytes() { return MLA_FFN_COUNTER_BYTES + ffn::kPartBytes; }
+static_assert(MLA_FFN_COUNTER_BYTES == ffn::kMaxSplitTiles * 4, "a counter for each tile of a split launch");
+void use_workspace(ffn::GemmArgs *g, char *ws) {
+    g->counters = reinterpret_cast<uint32_t *>(ws);
+    g->parts = reinterpret_cast<float *>(ws + MLA_FFN_COUNTER_BYTES);
+}
 
 int cu_count() {
     int ncu = 256, dev = 0, v = 0;
@@ -62,20 +72,108 @@ int cu_count() {
     return ncu;
 }
 
-ffn::Shape pick_shape(const ffn::GemmArgs &g, ffn::Epilogue epi) {
-    static const ffn::Shape shapes[] = {{256, 256}, {128, 128}, {64, 128}, {32, 128}};
-    const long long need = cu_count() * 85LL / 100;
-    ffn::Shape t{};
-    for (const ffn::Shape &c : shapes) {
-        t = c;
-        const int cols = epi == ffn::kGate ? c.bn / 2 : c.bn;
-        if ((long long)((g.M + c.bm - 1) / c.bm) * ((g.N + cols - 1) / cols) >= need) break;
-    }
-    return t;
+// What a launch takes, in us: sweeps of every kernel and number of parts over 45 products of 1 to 4160 rows (an
+// MI355X, weights from memory).  A workgroup walks its stages of 64 k (1 / groups of them) at `stage` us each; with
+// more than one workgroup a CU a stage takes `share` us for each of them.  In the kernels for many rows, one
+// workgroup a CU, further rounds follow each other.  Joining parts adds `join` and `join_part` a part.
+struct Cost {
+    float fixed, stage, share;
+    int groups;
+    float join, join_part;
+};
+constexpr Cost kCostBf16[ffn::kVariants] = {
+    {3.f, .95f, 1.84f, 8, 2.f, .9f},
+    {3.5f, .5f, .5f, 1, 6.f, .4f}, {3.5f, .63f, .53f, 1, 5.f, .75f}, {3.5f, .9f, .57f, 1, 8.f, .9f},
+    {}, {}, {}, {}, {}, {}, {}, {},
+    {5.f, 1.f, 0.f, 1, 12.f, 2.5f}, {7.f, 1.32f, 0.f, 1, 25.f, 6.f},
+};
+constexpr Cost kCost4[ffn::kVariants] = {
+    {3.f, .45f, .9f, 8, .2f, 1.5f},
+    {}, {}, {},
+    {3.f, .7f, .64f, 4, 3.5f, .7f}, {3.f, .9f, .85f, 4, 3.5f, .7f}, {3.f, 1.15f, 1.2f, 4, 4.f, .4f}, {3.f, 1.25f, 1.3f, 4, 4.f, 1.f},
+    {3.f, .75f, .61f, 1, 4.f, 1.f}, {3.f, .9f, .65f, 1, 5.f, 3.f}, {3.f, .9f, .5f, 1, 4.f, 1.f}, {3.f, 1.3f, 1.1f, 2, 12.f, 2.f},
+    {5.f, 1.04f, 0.f, 1, 12.f, 2.5f}, {8.f, 1.45f, 0.f, 1, 25.f, 6.f},
+};
+
+float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::Shape &t, int ncu) {
+    const Cost &c = (four ? kCost4 : kCostBf16)[t.variant];
+    const ffn::VariantSize &v = ffn::kSizes[t.variant];
+    const int cols = epi == ffn::kGate ? v.bn / 2 : v.bn;
+    const double tiles = std::ceil((double)g.M / v.bm) * std::ceil((double)g.N / cols);
+    const double chain = std::ceil(std::ceil(g.K / 64.0) * g.a_planes / t.splits / c.groups), load = tiles * t.splits / ncu;
+    const double joined = t.splits > 1 ? c.join + c.join_part * t.splits : 0.0;
+    if (c.share == 0.f) return (float)(std::ceil(load) * (c.fixed + chain * c.stage) + joined);
+    const double shared = load > 2.0 ? load : std::ceil(load);
+    return (float)(c.fixed + chain * std::max<double>(c.stage, shared * c.share) + joined);
 }
 
-int launch(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, hipStream_t s, const char *what) {
-    const hipError_t e = ffn::launch_gemm(g, four, epi, pick_shape(g, epi), s);
+struct Plan {
+    ffn::Shape shape{};
+    int rest = 0;  // rows at the end that a launch of their own takes
+    float us = 0;
+};
+
+// The cheapest kernel and number of parts for these rows.
+Plan best_whole(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, int ncu) {
+    Plan best;
+    best.us = INFINITY;
+    for (int v = 0; v < ffn::kVariants; ++v) {
+        ffn::Shape t{static_cast<ffn::Variant>(v), 1};
+        if (!ffn::fits(g, four, epi, t)) continue;
+        const int cols = epi == ffn::kGate ? ffn::kSizes[v].bn / 2 : ffn::kSizes[v].bn;
+        const double tiles = std::ceil((double)g.M / ffn::kSizes[v].bm) * std::ceil((double)g.N / cols);
+        for (; t.splits <= 32; ++t.splits) {
+            if (t.splits > 1 && (tiles * t.splits > 2.0 * ncu || !ffn::fits(g, four, epi, t))) break;
+            const float us = cost_of(g, four, epi, t, ncu);
+            if (us < best.us) best = {t, 0, us};
+        }
+    }
+    return best;
+}
+
+// One launch for all rows, or one for a multiple of 128 or 256 and one for the rows behind it, which would
+// cost the first a round of workgroups (4160 rows x 2048 of K = 10944: 217 us, as 4096 and 64 rows 153 + 27).
+// Kept for the last sizes of a thread: a step calls with the same ones for every layer.
+const Plan &plan_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi) {
+    struct Entry {
+        int dev = -1, M = 0, N = 0, K = 0, kind = 0;
+        Plan plan;
+    };
+    thread_local Entry kept[16];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) dev = 0;
+    const int kind = (four ? 1 : 0) + 2 * epi + 8 * g.a_planes;
+    Entry &e = kept[((unsigned)g.M * 31u + (unsigned)g.N * 7u + (unsigned)g.K + (unsigned)kind) % 16u];
+    if (e.dev == dev && e.M == g.M && e.N == g.N && e.K == g.K && e.kind == kind) return e.plan;
+    const int ncu = cu_count();
+    Plan best = best_whole(g, four, epi, ncu);
+    for (int step : {128, 256}) {
+        ffn::GemmArgs part = g;
+        const int rest = g.M % step;
+        if (rest == 0 || g.M < 2 * step) continue;
+        part.M = g.M - rest;
+        Plan p = best_whole(part, four, epi, ncu);
+        part.M = rest;
+        p.us = 1.05f * (p.us + best_whole(part, four, epi, ncu).us);  // not for a few per cent
+        p.rest = rest;
+        if (p.us < best.us) best = p;
+    }
+    e = {dev, g.M, g.N, g.K, kind, best};
+    return e.plan;
+}
+
+int launch(ffn::GemmArgs g, bool four, ffn::Epilogue epi, hipStream_t s, const char *what) {
+    const Plan plan = plan_of(g, four, epi);
+    const int rows = g.M;
+    g.M = rows - plan.rest;
+    hipError_t e = ffn::launch_gemm(g, four, epi, plan.shape, s);
+    if (e == hipSuccess && plan.rest > 0) {
+        const size_t width = epi == ffn::kStoreF32 ? 4 : 2;
+        g.a += (size_t)g.M * g.K;
+        g.out = static_cast<char *>(g.out) + (size_t)g.M * g.N * width;
+        g.M = plan.rest;
+        e = ffn::launch_gemm(g, four, epi, best_whole(g, four, epi, cu_count()).shape, s);
+    }
     return e == hipSuccess ? MLA_OK : mla::hip_error(e, what);
 }
 
@@ -89,20 +187,22 @@ int ffn_run(int32_t T, const uint16_t *x, const ffn::Weights (&w)[3], bool four,
     g.a_planes = 1;
     g.b = w[0];
     g.up = w[1];
-    g.M = T;
+    g.M = g.plane_rows = T;
     g.N = I;
     g.K = H;
     g.out = ws + h_at();
     g.h_planes = planes_of(out_dtype);
+    use_workspace(&g, ws);
     if ((st = launch(g, four, ffn::kGate, s, "gate and up projection")) != MLA_OK) return st;
     ffn::GemmArgs d{};
     d.a = reinterpret_cast<const uint16_t *>(ws + h_at());
     d.a_planes = g.h_planes;
     d.b = w[2];
-    d.M = T;
+    d.M = d.plane_rows = T;
     d.N = H;
     d.K = I;
     d.out = out;
+    use_workspace(&d, ws);
     return launch(d, four, out_dtype == MLA_OUT_F32 ? ffn::kStoreF32 : ffn::kStoreBf16, s, "down projection");
 }
 
@@ -111,7 +211,7 @@ int ffn_run(int32_t T, const uint16_t *x, const ffn::Weights (&w)[3], bool four,
 extern "C" {
 
 size_t mla_linear4_workspace_bytes(int32_t num_rows, int32_t in_features, int32_t out_features) {
-    if (num_rows <= 0 || bad_size(in_features, MLA_MX4_GROUP) || bad_size(out_features, 8)) return 0;
+    if (num_rows <= 0 || num_rows > kMaxRows || bad_size(in_features, MLA_MX4_GROUP) || bad_size(out_features, 8)) return 0;
     return linear_bytes();
 }
 
@@ -129,16 +229,17 @@ int mla_linear4(int32_t num_rows, const uint16_t *x, const mla_mx4 *w, int32_t i
     g.a = x;
     g.a_planes = 1;
     g.b = ffn::Weights{nullptr, w->codes, w->scales};
-    g.M = num_rows;
+    g.M = g.plane_rows = num_rows;
     g.N = out_features;
     g.K = in_features;
     g.out = out;
+    use_workspace(&g, static_cast<char *>(workspace));
     return launch(g, true, out_dtype == MLA_OUT_F32 ? ffn::kStoreF32 : ffn::kStoreBf16, static_cast<hipStream_t>(stream),
                   "product with 4-bit weights");
 }
 
 size_t mla_gated_ffn_workspace_bytes(int32_t num_rows, int32_t hidden, int32_t inner) {
-    if (num_rows <= 0 || bad_size(hidden, 8) || bad_size(inner, 8)) return 0;
+    if (num_rows <= 0 || num_rows > kMaxRows || bad_size(hidden, 8) || bad_size(inner, 8)) return 0;
     return ffn_bytes(num_rows, inner);
 }
 

@@ -8,6 +8,9 @@
 // included, two an instruction), so both formats share the products.
 #include "ffn_kernels.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace ffn {
 namespace {
 
@@ -15,6 +18,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -35,9 +39,16 @@ __device__ __forceinline__ u32x4 mx_values(uint32_t codes, float scale) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
 
-// h = silu(g) u.  exp(-g) overflows to infinity where silu(g) is below the smallest
-// fp32: the quotient is then 0, as it should.
-__device__ __forceinline__ float gated(float g, float u) { return g / (1.f + expf(-g)) * u; }
+// h = silu(g) u = g u / (1 + exp(-g)), silu off by less than 2^-21 of itself or 2^-120: exp(-g) as 2^(-g log2 e) with
+// the product's own rounding put back, then the hardware's quotient (1 ulp).  From |g| = 200 on exp(-g) is 0 or infinite,
+// and silu g or 0.  (The library's expf and division: a sixth of a 256 x 256 tile's time, 9 of 57 us.)
+__device__ __forceinline__ float gated(float g, float u) {
+    constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147182f;
+    const float c = __builtin_amdgcn_fmed3f(g, -200.f, 200.f), t = c * kLog2e;
+    const float rest = __builtin_fmaf(c, kLog2e, -t) + c * kLog2eRest;
+    const float e = __builtin_amdgcn_exp2f(-t);
+    return g * __builtin_amdgcn_rcpf(1.f + e * (1.f - rest * kLn2)) * u;
+}
 
 // v as the sum of bf16 values, most significant first: the next plane takes what the
 // last one left.  A value whose first rounding is not finite has zeros behind it.
@@ -48,10 +59,30 @@ __device__ __forceinline__ uint32_t next_plane(float &v) {
     return b;
 }
 
+// A wave-uniform pointer, in scalar registers.
+template <class T>
+__device__ __forceinline__ const T *uniform(const T *p) {
+    const uint64_t b = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const T *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32 |
+                                       (uint32_t)__builtin_amdgcn_readfirstlane((int)b));
+}
+
 // One 16-byte global -> LDS load per lane: lane i writes LDS bytes [lds + 16 i, lds + 16 i + 16); `lds` must be
 // wave-uniform.  Completion is tracked by hand with vmcnt (the compiler does not see these loads).
 __device__ __forceinline__ void dma16(const void *gsrc, uint32_t lds) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds), "v"(gsrc) : "memory");
+}
+
+// The same from base + off (base wave-uniform).  Where a vector instruction has written the base's registers (readfirstlane),
+// five wait states have to pass before a vector load reads them; the compiler does not look inside and places none.
+__device__ __forceinline__ void dma16_at(uint32_t off, const void *base, uint32_t lds) {
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(uniform(static_cast<const char *>(base))) : "memory");
+}
+// Ends a half phase: nothing moves across, and no wait beside those written out.
+__device__ __forceinline__ void half_phase() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" : : : "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int N>
@@ -81,13 +112,16 @@ __device__ __forceinline__ int swz_a(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int swz_b(int row) { return ((row >> 1) & 1) | (((row >> 3) & 3) << 1); }
 __device__ __forceinline__ int pair_column(int lane, int nb) { return 32 * (nb >> 1) + 8 * ((lane & 15) >> 2) + 4 * (nb & 1) + (lane & 3); }
 
-// Tile of workgroup blockIdx.x: groups of kGroup row tiles, row tile fastest, and each
-// XCD (workgroups are dealt to the 8 XCDs in turn) a contiguous run of that order.
+// Place of workgroup b in an order of n: workgroups are dealt to the 8 XCDs in turn, and each
+// XCD gets a contiguous run of the order.
+__device__ __forceinline__ int xcd_run(int b, int n) {
+    const int per = n >> 3;
+    return b < per * 8 ? (b & 7) * per + (b >> 3) : b;
+}
+// The tile at place t: groups of kGroup row tiles, row tile fastest, so that a run covers a block of
+// about 8 x 4 tiles whose rows and weights stay in its XCD's L2.
 constexpr int kGroup = 8;
-__device__ __forceinline__ void tile_of(int mtiles, int ntiles, int *mt, int *nt) {
-    const int tiles = mtiles * ntiles, per = tiles >> 3;
-    int t = blockIdx.x;
-    if (t < per * 8) t = (t & 7) * per + (t >> 3);
+__device__ __forceinline__ void tile_at(int t, int mtiles, int ntiles, int *mt, int *nt) {
     const int g = t / (kGroup * ntiles), first = g * kGroup, gm = min(kGroup, mtiles - first), r = t - g * kGroup * ntiles;
     *mt = first + r % gm;
     *nt = r / gm;
@@ -114,7 +148,7 @@ __device__ __forceinline__ void store_h(const GemmArgs &g, f32x4 g0, f32x4 g1, f
         h[4 + i] = gated(g1[i], u1[i]);
     }
     uint16_t *dst = static_cast<uint16_t *>(g.out) + (size_t)row * g.N + n;
-    for (int p = 0; p < g.h_planes; ++p, dst += (size_t)g.M * g.N) {
+    for (int p = 0; p < g.h_planes; ++p, dst += (size_t)g.plane_rows * g.N) {
         u32x4 v;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -125,28 +159,379 @@ __device__ __forceinline__ void store_h(const GemmArgs &g, f32x4 g0, f32x4 g1, f
     }
 }
 
+// Split sums.  Every workgroup of a tile has stored its part; true in all threads of
+// the one that comes last, which then sees the parts of the others.  The counter is
+// left as it was found, zero.
+__device__ __forceinline__ bool last_of_tile(uint32_t *counter, int splits) {
+    __shared__ bool last;
+    __syncthreads();  // this workgroup's parts are stored
+    if (threadIdx.x == 0) {
+        last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)splits - 1;
+        if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(last);  // one branch for the whole wave
+}
+
+// Four consecutive columns of a row.
+template <int EPI>
+__device__ __forceinline__ void store_four(const GemmArgs &g, f32x4 v, int row, int n) {
+    const size_t at = (size_t)row * g.N + n;
+    if constexpr (EPI == kStoreF32)
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(g.out) + at) = v;
+    else
+        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(g.out) + at) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+}
+__device__ __forceinline__ void store_h4(const GemmArgs &g, f32x4 gate, f32x4 up, int row, int n) {
+    float h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = gated(gate[i], up[i]);
+    uint16_t *dst = static_cast<uint16_t *>(g.out) + (size_t)row * g.N + n;
+    for (int p = 0; p < g.h_planes; ++p, dst += (size_t)g.plane_rows * g.N) {
+        u32x2 v;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t lo = next_plane(h[2 * k]), hi = next_plane(h[2 * k + 1]);
+            v[k] = lo | (hi << 16);
+        }
+        *reinterpret_cast<u32x2 *>(dst) = v;
+    }
+}
+
+// Few rows: the call is bound by reading the weights once, so they go straight from
+// memory to registers.  A workgroup takes 16 MB rows and CB blocks of 16 weight rows
+// (kGate: the first half gate, the second the same columns of up); its eight waves
+// share K in slices of 128, a slice ahead in registers, and meet in LDS.  Within a
+// slice a lane holds 32 neighbouring k of its row (lane / 16 picks which), 64 bytes in
+// bf16 or 16 in 4 bits under one scale; the products' order of k is that of both
+// operands, so nothing is moved.  gridDim.z cuts K further where the columns are too
+// few for the chip.
+template <int MB, int CB, bool FOUR, int EPI>
+__global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
+    constexpr int NB = FOUR ? 1 : 4, JB = EPI == kGate ? CB / 2 : CB, UNITS = MB * JB;
+    __shared__ f32x4 red[4][MB * CB][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
+    const int n0 = blockIdx.x * 16 * JB, m0 = blockIdx.y * 16 * MB;
+    const int ns = (g.K + 127) >> 7, total = ns * g.a_planes, step = 8 * g.splits;
+    const size_t plane = (size_t)g.plane_rows * g.K;
+
+    const uint16_t *arow[MB], *brow[CB];
+    const uint8_t *crow[CB], *srow[CB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) arow[mb] = g.a + (size_t)min(m0 + 16 * mb + (lane & 15), g.M - 1) * g.K;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {  // columns past the end repeat the last one, never stored
+        const Weights &w = EPI == kGate && cb >= JB ? g.up : g.b;
+        const size_t n = min(n0 + 16 * (cb % JB) + (lane & 15), g.N - 1);
+        if constexpr (FOUR) {
+            crow[cb] = w.codes + n * (g.K / 2);
+            srow[cb] = w.scales + n * (g.K / kMxGroup);
+        } else {
+            brow[cb] = w.w + n * g.K;
+        }
+    }
+    // k of the lane's chunk i: with 4-bit weights 32 neighbouring k, as their codes are loaded; in bf16 the four lanes of a row
+    // take 64 neighbouring bytes at a time
+    const auto at_k = [&](int k0, int i) { return k0 + (FOUR ? 32 * grp + 8 * i : 32 * i + 8 * grp); };
+    struct Slice {
+        u32x4 b[CB][NB], a[MB][4];
+        uint32_t scale[CB];
+    };
+    // chunks behind the last k are read from the row's start, and dropped in use()
+    const auto load = [&](Slice &s, int j) {
+        const int p = j / ns, k0 = (j - p * ns) * 128;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            if constexpr (FOUR) {
+                const int k = k0 + 32 * grp, at = k < g.K ? k : 0;
+                s.b[cb][0] = *reinterpret_cast<const u32x4 *>(crow[cb] + at / 2);
+                s.scale[cb] = srow[cb][at / kMxGroup];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s.b[cb][i] = *reinterpret_cast<const u32x4 *>(brow[cb] + (at_k(k0, i) < g.K ? at_k(k0, i) : 0));
+            }
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s.a[mb][i] = *reinterpret_cast<const u32x4 *>(arow[mb] + p * plane + (at_k(k0, i) < g.K ? at_k(k0, i) : 0));
+    };
+    f32x4 acc[MB][CB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) acc[mb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto use = [&](Slice &s, int j) {
+        const int k0 = j % ns * 128;
+        if (k0 + 128 > g.K) {
+            const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool in = at_k(k0, i) < g.K;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) s.a[mb][i] = in ? s.a[mb][i] : zero;
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    if constexpr (!FOUR) s.b[cb][i] = in ? s.b[cb][i] : zero;
+                    else if (i == 0) {
+                        s.b[cb][0] = in ? s.b[cb][0] : zero;
+                        s.scale[cb] = in ? s.scale[cb] : 0u;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                u32x4 b;
+                if constexpr (FOUR) b = mx_values(s.b[cb][0][i], mx_scale(s.scale[cb]));
+                else b = s.b[cb][i];
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) acc[mb][cb] = mfma(b, s.a[mb][i], acc[mb][cb]);
+            }
+        }
+    };
+    Slice s0, s1;
+    int j = blockIdx.z * 8 + wave;
+    if (j < total) load(s0, j);
+    while (j < total) {
+        if (j + step < total) load(s1, j + step);
+        use(s0, j);
+        if ((j += step) >= total) break;
+        if (j + step < total) load(s0, j + step);
+        use(s1, j);
+        j += step;
+    }
+
+    // the eight waves' sums: (w, w + 4), then 0 .. 3 in order
+    if (wave >= 4) {
+#pragma unroll
+        for (int b = 0; b < MB * CB; ++b) red[wave - 4][b][lane] = acc[b / CB][b % CB];
+    }
+    __syncthreads();
+    if (wave < 4) {
+#pragma unroll
+        for (int b = 0; b < MB * CB; ++b) red[wave][b][lane] += acc[b / CB][b % CB];
+    }
+    __syncthreads();
+    const int tile = blockIdx.y * gridDim.x + blockIdx.x;
+    f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * (MB * CB * 64) + lane;
+    const auto block_sum = [&](int b) { return red[0][b][lane] + red[1][b][lane] + red[2][b][lane] + red[3][b][lane]; };
+    if (g.splits > 1) {
+        for (int b = wave; b < MB * CB; b += 8) parts[((size_t)blockIdx.z * (MB * CB) + b) * 64] = block_sum(b);
+        if (!last_of_tile(g.counters + tile, g.splits)) return;
+    }
+    const auto total_sum = [&](int b) {
+        if (g.splits == 1) return block_sum(b);
+        f32x4 v = parts[(size_t)b * 64];
+        for (int z = 1; z < g.splits; ++z) v += parts[((size_t)z * (MB * CB) + b) * 64];
+        return v;
+    };
+    // D[16 mb + lane % 16][16 jb + 4 (lane / 16) + i]
+    for (int u = wave; u < UNITS; u += 8) {
+        const int mb = u / JB, jb = u % JB, row = m0 + 16 * mb + (lane & 15), n = n0 + 16 * jb + 4 * grp;
+        const f32x4 v = total_sum(mb * CB + jb);
+        if constexpr (EPI == kGate) {
+            const f32x4 up = total_sum(mb * CB + JB + jb);
+            if (row < g.M && n < g.N) store_h4(g, v, up, row, n);
+        } else {
+            if (row < g.M && n < g.N) store_four<EPI>(g, v, row, n);
+        }
+    }
+}
+
+// A middling number of rows: bound by the weights, which go straight from memory to
+// registers as above, or by the products.  WC waves share the rows of x through LDS
+// (slices of 128 k, one ahead: loaded to registers before a slice's products, stored
+// to the other buffer after them) and take CB blocks of 16 weight rows each (kGate:
+// the first half gate, the second the same columns of up); KG such groups take K's
+// slices in turn and meet in LDS.  gridDim.z cuts K further.
+template <int MB, int CB, int WC, int KG, int EPI>
+__global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
+    constexpr int JB = EPI == kGate ? CB / 2 : CB, COLS = 16 * JB * WC;
+    constexpr int BUF = MB * 16 * 16;               // 16-byte slots of one buffer
+    constexpr int LPT = (BUF + 64 * WC - 1) / (64 * WC);
+    static_assert(BUF % (64 * WC) == 0 || LPT == 1, "loads of a slice");
+    static_assert(KG == 1 || KG * 2 * BUF >= (KG / 2) * WC * MB * CB * 64, "partial sums fit the buffers");
+    __shared__ u32x4 sm[KG * 2 * BUF];
+    const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 4, l16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wc = wave % WC, kg = wave / WC, gt = tid % (64 * WC);
+    int mt, nt;
+    tile_at(xcd_run(blockIdx.x, gridDim.x), (g.M + 16 * MB - 1) / (16 * MB), (g.N + COLS - 1) / COLS, &mt, &nt);
+    const int m0 = mt * 16 * MB, n0 = nt * COLS + wc * 16 * JB;
+    const int ns = (g.K + 127) >> 7, total = ns * g.a_planes;
+    const int j0 = (int)((long long)total * blockIdx.z / g.splits), j1 = (int)((long long)total * (blockIdx.z + 1) / g.splits);
+    const int rounds = (j1 - j0 + KG - 1) / KG;
+    const size_t plane = (size_t)g.plane_rows * g.K;
+    u32x4 *const buf = sm + kg * 2 * BUF;
+
+    // column of block jb that lane l16 loads: pairs of blocks are interleaved (pair_column) so that a lane ends up with 8
+    // neighbouring columns
+    const auto column = [&](int jb) { return JB % 2 == 0 ? pair_column(lane, jb) : 16 * jb + l16; };
+    const uint8_t *crow[CB], *srow[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        const Weights &w = EPI == kGate && cb >= JB ? g.up : g.b;
+        const size_t n = min(n0 + column(cb % JB), g.N - 1);
+        crow[cb] = w.codes + n * (g.K / 2);
+        srow[cb] = w.scales + n * (g.K / kMxGroup);
+    }
+    const uint16_t *arow[LPT];
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) arow[i] = g.a + (size_t)min(m0 + min((gt + 64 * WC * i) >> 4, 16 * MB - 1), g.M - 1) * g.K;
+
+    u32x4 areg[LPT];
+    const auto load_a = [&](int j) {
+        const int p = j / ns, k = (j - p * ns) * 128 + (gt & 15) * 8;
+#pragma unroll
+        for (int i = 0; i < LPT; ++i) areg[i] = *reinterpret_cast<const u32x4 *>(arow[i] + p * plane + (k < g.K ? k : 0));
+    };
+    const auto put_a = [&](int j, u32x4 *to) {
+        const bool in = j % ns * 128 + (gt & 15) * 8 < g.K;
+#pragma unroll
+        for (int i = 0; i < LPT; ++i) {
+            const int row = (gt + 64 * WC * i) >> 4;
+            if (BUF % (64 * WC) == 0 || row < 16 * MB) to[row * 16 + ((gt ^ row) & 15)] = in ? areg[i] : u32x4{0u, 0u, 0u, 0u};
+        }
+    };
+    struct Slice {
+        u32x4 codes[CB];
+        uint32_t scale[CB];
+    };
+    const auto load_b = [&](Slice &s, int j) {
+        const int k = j % ns * 128 + 32 * grp, at = k < g.K ? k : 0;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            s.codes[cb] = *reinterpret_cast<const u32x4 *>(crow[cb] + at / 2);
+            s.scale[cb] = srow[cb][at / kMxGroup];
+        }
+    };
+    f32x4 acc[MB][CB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) acc[mb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto use = [&](Slice &s, int j, const u32x4 *from) {
+        const int k0 = j % ns * 128;
+        if (k0 + 128 > g.K) {  // groups behind the last k count as zeros, on both sides
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const bool in = k0 + 32 * grp < g.K;
+                s.codes[cb] = in ? s.codes[cb] : u32x4{0u, 0u, 0u, 0u};
+                s.scale[cb] = in ? s.scale[cb] : 0u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32x4 fa[MB];
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) fa[mb] = from[(16 * mb + l16) * 16 + ((4 * grp + i) ^ l16)];
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const u32x4 b = mx_values(s.codes[cb][i], mx_scale(s.scale[cb]));
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) acc[mb][cb] = mfma(b, fa[mb], acc[mb][cb]);
+            }
+        }
+    };
+    Slice s0, s1;
+    int j = j0 + kg;
+    if (j < j1) {
+        load_a(j);
+        load_b(s0, j);
+        put_a(j, buf);
+    }
+    __syncthreads();
+    const auto round = [&](Slice &now, Slice &next, u32x4 *from, u32x4 *to) {
+        if (j + KG < j1) {
+            load_a(j + KG);
+            load_b(next, j + KG);
+        }
+        if (j < j1) use(now, j, from);
+        if (j + KG < j1) put_a(j + KG, to);
+        __syncthreads();
+        j += KG;
+    };
+    for (int r = 0; r < rounds; r += 2) {
+        round(s0, s1, buf, buf + BUF);
+        if (r + 1 < rounds) round(s1, s0, buf + BUF, buf);
+    }
+
+    // the groups' sums, halved in order
+    if constexpr (KG > 1) {
+        f32x4 *const part = reinterpret_cast<f32x4 *>(sm);
+#pragma unroll
+        for (int half = KG / 2; half >= 1; half /= 2) {
+            if (kg >= half && kg < 2 * half) {
+#pragma unroll
+                for (int b = 0; b < MB * CB; ++b) part[(((kg - half) * WC + wc) * MB * CB + b) * 64 + lane] = acc[b / CB][b % CB];
+            }
+            __syncthreads();
+            if (kg < half) {
+#pragma unroll
+                for (int b = 0; b < MB * CB; ++b) acc[b / CB][b % CB] += part[((kg * WC + wc) * MB * CB + b) * 64 + lane];
+            }
+            if (half > 1) __syncthreads();
+        }
+    }
+    if (g.splits > 1) {
+        const int tile = nt * ((g.M + 16 * MB - 1) / (16 * MB)) + mt;
+        constexpr int PART = WC * MB * CB * 64;
+        f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * PART + wc * MB * CB * 64 + lane;
+        if (kg == 0) {
+#pragma unroll
+            for (int b = 0; b < MB * CB; ++b) parts[(size_t)blockIdx.z * PART + b * 64] = acc[b / CB][b % CB];
+        }
+        if (!last_of_tile(g.counters + tile, g.splits) || kg > 0) return;
+#pragma unroll
+        for (int b = 0; b < MB * CB; ++b) acc[b / CB][b % CB] = parts[b * 64];
+        for (int z = 1; z < g.splits; ++z)
+#pragma unroll
+            for (int b = 0; b < MB * CB; ++b) acc[b / CB][b % CB] += parts[(size_t)z * PART + b * 64];
+    }
+    if (kg > 0) return;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const int row = m0 + 16 * mb + l16;
+        if (row >= g.M) continue;
+#pragma unroll
+        for (int jb = 0; jb < JB; jb += JB % 2 == 0 ? 2 : 1) {
+            if constexpr (JB % 2 == 0) {
+                const int n = n0 + 16 * jb + 8 * grp;
+                if (n >= g.N) continue;
+                if constexpr (EPI == kGate) store_h(g, acc[mb][jb], acc[mb][jb + 1], acc[mb][JB + jb], acc[mb][JB + jb + 1], row, n);
+                else store_eight<EPI>(g, acc[mb][jb], acc[mb][jb + 1], row, n);
+            } else {
+                const int n = n0 + 16 * jb + 4 * grp;
+                if (n >= g.N) continue;
+                if constexpr (EPI == kGate) store_h4(g, acc[mb][jb], acc[mb][JB + jb], row, n);
+                else store_four<EPI>(g, acc[mb][jb], row, n);
+            }
+        }
+    }
+}
+
 // BM x BN tile on WR x WC waves, K in stages of 64 through a ring of D LDS stages
-// that direct global -> LDS loads fill ahead.  4-bit weights pass through registers,
-// a stage ahead.  With kGate the BN weight rows are, for each column of waves, 32
+// that direct global -> LDS loads fill ahead.  With kGate the BN weight rows are, for each column of waves, 32
 // rows of the gate and the same 32 of the up projection, so that a lane ends up with
 // both products of its columns.
-template <int BM, int BN, int D, int WR, int WC, bool FOUR, int EPI>
+template <int BM, int BN, int D, int WR, int WC, int EPI>
 __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
     constexpr int NT = 64 * WR * WC, NW = WR * WC;
     constexpr int STAGE = (BM + BN) * 8;                       // 16-byte slots per stage
-    constexpr int LOADED = FOUR ? BM * 8 : STAGE;              // those that direct loads fill
-    constexpr int NPW = LOADED / 64 / NW;                      // loads per wave per stage
+    constexpr int NPW = STAGE / 64 / NW;                      // loads per wave per stage
     constexpr int WM = BM / WR, MB = WM / 16, WN = BN / WC, NB = WN / 16;
-    static_assert(LOADED % NT == 0 && WN == 64 && MB >= 1 && NB == 4, "shape");
-    static_assert(!FOUR || BN * 2 == NT, "one group of codes a thread and stage");
+    static_assert(STAGE % NT == 0 && WN == 64 && MB >= 1 && NB == 4, "shape");
     __shared__ __attribute__((aligned(1024))) u32x4 ring[D * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     constexpr int COLS = EPI == kGate ? BN / 2 : BN;           // output columns of a tile
     int mt, nt;
-    tile_of((g.M + BM - 1) / BM, (g.N + COLS - 1) / COLS, &mt, &nt);
+    tile_at(xcd_run(blockIdx.x, gridDim.x), (g.M + BM - 1) / BM, (g.N + COLS - 1) / COLS, &mt, &nt);
     const int m0 = mt * BM, n0 = nt * COLS;
-    const int nk = (g.K + kBK - 1) / kBK, stages = nk * g.a_planes;
+    const int nk = (g.K + kBK - 1) / kBK, all = nk * g.a_planes;
+    const int first = (int)((long long)all * blockIdx.z / g.splits), stages = (int)((long long)all * (blockIdx.z + 1) / g.splits) - first;
 
     // weight row of the tile's B row rb: (second matrix?, row); rows past the end repeat the last, never stored
     const auto weight_row = [&](int rb, bool *second) {
@@ -166,9 +551,9 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
         }
     }
     const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
-    const size_t plane = (size_t)g.M * g.K;
+    const size_t plane = (size_t)g.plane_rows * g.K;
     const auto issue = [&](int st) {
-        const int p = st / nk, k0 = (st - p * nk) * kBK;
+        const int p = (first + st) / nk, k0 = (first + st - p * nk) * kBK;
         const uint32_t dst = ring_lds + (uint32_t)((st % D) * STAGE * 16 + wave * NPW * 1024);
         const bool tail = k0 + kBK > g.K;
 #pragma unroll
@@ -179,30 +564,6 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
             dma16(from, __builtin_amdgcn_readfirstlane(dst + i * 1024));
         }
     };
-    // 4-bit weights: thread t holds group t % 2 of B row t / 2
-    const uint8_t *codes = nullptr, *scales = nullptr;
-    if constexpr (FOUR) {
-        bool second;
-        const size_t n = weight_row(tid >> 1, &second);
-        codes = (second ? g.up.codes : g.b.codes) + n * (g.K / 2) + (tid & 1) * 16;
-        scales = (second ? g.up.scales : g.b.scales) + n * (g.K / kMxGroup) + (tid & 1);
-    }
-    u32x4 held = {0u, 0u, 0u, 0u};
-    uint32_t held_scale = 0u;
-    const auto load_codes = [&](int st) {
-        const int k0 = st % nk * kBK;
-        const bool in = k0 + (tid & 1) * kMxGroup < g.K;
-        held = in ? *reinterpret_cast<const u32x4 *>(codes + k0 / 2) : u32x4{0u, 0u, 0u, 0u};
-        held_scale = in ? scales[k0 / kMxGroup] : 0u;
-    };
-    const auto put_codes = [&](int st) {
-        u32x4 *const to = ring + (st % D) * STAGE;
-        const int row = BM + (tid >> 1);
-        const float s = mx_scale(held_scale);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) to[row * 8 + (((tid & 1) * 4 + c) ^ swz_b(row))] = mx_values(held[c], s);
-    };
-
     f32x4 acc[MB][NB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
@@ -210,10 +571,6 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
         for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int wr = (wave / WC) * WM, wc = BM + (wave % WC) * WN;
 
-    if constexpr (FOUR) {
-        load_codes(0);
-        put_codes(0);
-    }
 #pragma unroll
     for (int st = 0; st < D - 1; ++st)
         if (st < stages) issue(st);
@@ -222,7 +579,6 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
         // stage kt has landed once no more than the stages issued after it are in flight
         wait_stages<NPW, D - 1>(min(D - 1, stages - 1 - kt));
         __syncthreads();
-        if (FOUR && kt + 1 < stages) load_codes(kt + 1);
         const u32x4 *cur = ring + (kt % D) * STAGE;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -243,8 +599,20 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma(fb[nb], fa[mb], acc[mb][nb]);
         }
-        if (FOUR && kt + 1 < stages) put_codes(kt + 1);
         __syncthreads();  // the slot of stage kt is refilled by the next iteration's loads
+    }
+
+    if (g.splits > 1) {
+        const int tile = nt * ((g.M + BM - 1) / BM) + mt;
+        f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * (BM * BN / 4) + (size_t)wave * MB * NB * 64 + lane;
+#pragma unroll
+        for (int b = 0; b < MB * NB; ++b) parts[(size_t)blockIdx.z * (BM * BN / 4) + b * 64] = acc[b / NB][b % NB];
+        if (!last_of_tile(g.counters + tile, g.splits)) return;
+#pragma unroll
+        for (int b = 0; b < MB * NB; ++b) acc[b / NB][b % NB] = parts[b * 64];
+        for (int z = 1; z < g.splits; ++z)
+#pragma unroll
+            for (int b = 0; b < MB * NB; ++b) acc[b / NB][b % NB] += parts[(size_t)z * (BM * BN / 4) + b * 64];
     }
 
     // acc[mb][2 p + b][i] = C[16 mb + lane % 16][32 p + 8 (lane / 16) + 4 b + i]
@@ -263,34 +631,388 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
     }
 }
 
-template <int BM, int BN, int D, int WR, int WC, bool FOUR>
-hipError_t launch_tiles(const GemmArgs &g, Epilogue epi, hipStream_t s) {
-    const int cols = epi == kGate ? BN / 2 : BN;
-    const long long tiles = (long long)((g.M + BM - 1) / BM) * ((g.N + cols - 1) / cols);
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)tiles);
-    constexpr int NT = 64 * WR * WC;
-    if (epi == kStoreBf16) tile_kernel<BM, BN, D, WR, WC, FOUR, kStoreBf16><<<grid, NT, 0, s>>>(g);
-    else if (epi == kStoreF32) tile_kernel<BM, BN, D, WR, WC, FOUR, kStoreF32><<<grid, NT, 0, s>>>(g);
-    else tile_kernel<BM, BN, D, WR, WC, FOUR, kGate><<<grid, NT, 0, s>>>(g);
-    return hipGetLastError();
+// Many rows: bound by the products.  A tile of 64 Q rows and 256 weight rows on eight
+// waves of 32 Q x 64, K in stages of 64, two of them in LDS.  A stage has four regions:
+// Ah, the h-th 16 Q rows of both row halves, and Bp, the p-th 32 weight rows of the four
+// columns of waves (kGate: B0 gate, B1 up).  Its products are four phases of 4 Q matrix
+// instructions:
+//     phase   products    reads for them                refills (of two stages on)
+//       0      A0 x B0      A0                            A1 (of the next stage)
+//       1      A0 x B1      B1                            B0
+//       2      A1 x B1      A1                            A0
+//       3      A1 x B0      B0 of the next stage          B1
+// where a phase first reads and refills, then multiplies.  Waves 4 .. 7 run half a phase
+// behind waves 0 .. 3, the other wave of their SIMD, so that one multiplies while the other
+// reads: LDS and the matrix unit both are busy all the time.  A region is refilled two
+// phases after its last read (a barrier ends every half phase, and a wave's reads have
+// arrived when its phase ends) and read six phases after that: a wave waits for all but its
+// last five refills, never for all.
+//   4-bit weights: B0 and B1 are one region of codes, refilled and read at B0's places.  A
+// lane's 16 codes of a stage are 16 neighbouring k under one scale, the operands of both
+// 32-k steps (the rows' chunks are read in that order); phases 0 and 1 make them bf16.  The
+// scales of up to kRunStages stages wait in LDS from before the first, a longer K is run in
+// parts.
+constexpr int kRunStages = 128;
+enum Region : int { kB0, kA0, kB1, kA1 };  // in the order that they are filled
+// Loads that a wave makes for a region.
+template <int Q, bool FOUR>
+struct Fills {
+    static constexpr int of(Region r) { return r == kA0 || r == kA1 ? Q / 2 : FOUR ? (r == kB0 ? 1 : 0) : 2; }
+    static constexpr int all() { return of(kB0) + of(kA0) + of(kB1) + of(kA1); }
+    static constexpr int last_five(Region newest) { return all() + of(newest); }
+};
+template <int Q, bool FOUR, int EPI>
+__global__ __launch_bounds__(512) void big_kernel(const GemmArgs g) {
+    static_assert(Q == 2 || Q == 4, "whole loads of a region");
+    constexpr int BM = 64 * Q;
+    using F = Fills<Q, FOUR>;
+    // 16-byte slots of the regions and their places in a stage
+    constexpr int B0_SLOTS = FOUR ? 512 : 1024, B1_SLOTS = FOUR ? 0 : 1024;
+    constexpr int AT_A0 = B0_SLOTS, AT_A1 = AT_A0 + 256 * Q, AT_B1 = AT_A1 + 256 * Q, STAGE = AT_B1 + B1_SLOTS;
+    constexpr int SCALE_ROW = kRunStages * 2 + 4;         // bytes of a weight row's scales: 4 beside the banks of the next row
+    __shared__ __attribute__((aligned(1024))) u32x4 ring[2 * STAGE];
+    __shared__ uint32_t scales[FOUR ? 256 * SCALE_ROW / 4 : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int COLS = EPI == kGate ? 128 : 256;
+    // the parts of one z follow each other: an XCD's tiles are then at the same stages
+    const int mtiles = (g.M + BM - 1) / BM, ntiles = (g.N + COLS - 1) / COLS, tiles = mtiles * ntiles;
+    const int place = xcd_run(blockIdx.x, gridDim.x), z = __builtin_amdgcn_readfirstlane(place / tiles);
+    int mt, nt;
+    tile_at(place - z * tiles, mtiles, ntiles, &mt, &nt);
+    const int m0 = __builtin_amdgcn_readfirstlane(mt * BM), n0 = __builtin_amdgcn_readfirstlane(nt * COLS);
+    const int nk = (g.K + kBK - 1) / kBK;
+    const int wr = wave >> 2, wc = wave & 3, l16 = lane & 15, g4 = lane >> 4;
+
+    // Filling.  A wave's i-th load fills rows 64 i + 8 w .. + 7 of a region, which are neighbours in x or the weights: their first
+    // one is wave-uniform, this lane's place behind it is the same for all (with 4-bit weights a load is 32 rows' codes).  Rows
+    // past the end repeat the last one; never stored.
+    const int kin_a = ((lane & 7) ^ swz_a(8 * wave + (lane >> 3))) * 8;
+    const int kin_b = FOUR ? (lane & 1) * 32 : ((lane & 7) ^ swz_b(8 * wave + (lane >> 3))) * 8;
+    const uint32_t lane_a = (uint32_t)(lane >> 3) * (uint32_t)g.K * 2u + (uint32_t)kin_a * 2u;
+    uint32_t lane_b = (uint32_t)(lane >> 3) * (uint32_t)g.K * 2u + (uint32_t)kin_b * 2u;
+    const char *row_b[2][2] = {{nullptr, nullptr}, {nullptr, nullptr}};  // [p][i]; FOUR: [0][0] alone
+    const auto column = [&](int rb) {  // of weight row rb of the tile
+        return min(n0 + (EPI == kGate ? (rb >> 6) * 32 + (rb & 31) : rb), g.N - 1) - n0;
+    };
+    if constexpr (FOUR) {
+        const uint8_t *const codes = (EPI == kGate && (wave & 1) ? g.up.codes : g.b.codes) + (size_t)n0 * (g.K / 2);
+        row_b[0][0] = uniform(reinterpret_cast<const char *>(codes));
+        lane_b = (uint32_t)column(32 * wave + (lane >> 1)) * (uint32_t)(g.K / 2) + (uint32_t)kin_b / 2u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = 64 * i + 8 * wave;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {  // (widths are multiples of 8: the eight columns exist or none of them)
+                const int col = min(n0 + (EPI == kGate ? (r >> 5) * 32 + (r & 31) : (r >> 5) * 64 + 32 * p + (r & 31)), g.N - 8);
+                row_b[p][i] = uniform(reinterpret_cast<const char *>((EPI == kGate && p == 1 ? g.up.w : g.b.w) + (size_t)col * g.K));
+            }
+        }
+    }
+    const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
+    const char *a_run = nullptr;  // rows of x of this run's plane
+    int st_run = 0;               // and its first stage
+    const auto zeros_or = [](bool in, const char *from) { return in ? from : reinterpret_cast<const char *>(&kZeros); };
+    const auto fill = [&](auto region_, int st, int slot) {  // into stage slot `slot`
+        constexpr int region = decltype(region_)::value;
+        const int k0 = (st_run + st) * kBK;
+        const bool whole = k0 + kBK <= g.K;  // (not so: the last stage of a K that is no multiple of 64)
+        const uint32_t stage = ring_lds + (uint32_t)slot * (STAGE * 16) + wave * 1024;
+        if constexpr (region == kA0 || region == kA1) {
+#pragma unroll
+            for (int i = 0; i < Q / 2; ++i) {
+                const int r = 64 * i + 8 * wave, half = r / (16 * Q);
+                const int row = m0 + half * (BM / 2) + (region == kA0 ? 0 : 16 * Q) + r % (16 * Q);
+                const uint32_t dst = stage + (region == kA0 ? AT_A0 : AT_A1) * 16 + i * 8192;
+                if (whole && row + 8 <= g.M) {
+                    dma16_at(lane_a, a_run + ((size_t)row * g.K + k0) * 2, dst);
+                } else {
+                    const size_t at = (size_t)min(row + (lane >> 3), g.M - 1) * g.K + k0 + kin_a;
+                    dma16(zeros_or(k0 + kin_a < g.K, a_run + at * 2), dst);
+                }
+            }
+        } else if constexpr (!FOUR) {
+            constexpr int p = region == kB0 ? 0 : 1;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t dst = stage + (p == 0 ? 0 : AT_B1) * 16 + i * 8192;
+                const char *base = row_b[p][i] + (size_t)k0 * 2;
+                if (whole) dma16_at(lane_b, base, dst);
+                else dma16(zeros_or(k0 + kin_b < g.K, base + lane_b), dst);
+            }
+        } else if constexpr (region == kB0) {
+            const char *base = row_b[0][0] + (size_t)k0 / 2;
+            if (whole) dma16_at(lane_b, base, stage);
+            else dma16(zeros_or(k0 + kin_b < g.K, base + lane_b), stage);
+        }
+    };
+
+    f32x4 acc[2][Q][4];      // [h][mb][2 p + nb]
+    u32x4 fa[Q][2];           // [mb][k step]
+    u32x4 fb0[2][2][2], fb1[2][2];  // B0 of two stages (4-bit: of one), B1: [nb][k step]
+    typedef uint32_t codes2 __attribute__((ext_vector_type(2)));
+    codes2 code[2][2];        // [p][nb]
+    uint32_t scale[2][2];
+    // this lane's slots in a region for the two k steps
+    int at_a[2], at_b[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        at_a[s] = (16 * Q * wr + l16) * 8 + ((FOUR ? 2 * g4 + s : 4 * s + g4) ^ swz_a(l16));
+        at_b[s] = (32 * wc + pair_column(lane, 0)) * 8 + ((4 * s + g4) ^ swz_b(pair_column(lane, 0)));  // (the pair's other block: 4 rows on)
+    }
+    const auto read_a = [&](int slot, int at) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int mb = 0; mb < Q; ++mb) fa[mb][s] = ring[slot * STAGE + at + mb * 128 + at_a[s]];
+    };
+    const auto read_b = [&](u32x4(&fb)[2][2], int slot, int at) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb) fb[nb][s] = ring[slot * STAGE + at + nb * 32 + at_b[s]];
+    };
+    const auto read_codes = [&](int slot, int st) {
+        const codes2 *const from = reinterpret_cast<const codes2 *>(ring + slot * STAGE);
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb) {
+                const int r = 64 * wc + 32 * p + pair_column(lane, nb);
+                code[p][nb] = from[r * 4 + g4];
+                scale[p][nb] = scales[r * (SCALE_ROW / 4) + (st >> 1)];
+            }
+    };
+    const auto convert = [&](u32x4(&fb)[2][2], int p, int st) {
+        if constexpr (FOUR) {
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb) {
+                const float f = mx_scale((scale[p][nb] >> ((st & 1) * 16 + (g4 >> 1) * 8)) & 0xffu);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) fb[nb][s] = mx_values(code[p][nb][s], f);
+            }
+        }
+    };
+    const auto multiply = [&](int h, const u32x4(&fb)[2][2], int p) {
+        half_phase();
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int mb = 0; mb < Q; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < 2; ++nb) acc[h][mb][2 * p + nb] = mfma(fb[nb][s], fa[mb][s], acc[h][mb][2 * p + nb]);
+        __builtin_amdgcn_s_setprio(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // what this phase read has arrived, used already or not
+        half_phase();
+    };
+    const std::integral_constant<int, kB0> B0{};
+    const std::integral_constant<int, kB1> B1{};
+    const std::integral_constant<int, kA0> A0{};
+    const std::integral_constant<int, kA1> A1{};
+    // One stage, in slot SLOT; behind it LEFT more (2: any number, which are refilled).
+    const auto stage = [&](auto slot_, auto left_, int st) {
+        constexpr int SLOT = decltype(slot_)::value, LEFT = decltype(left_)::value, FB = FOUR ? 0 : SLOT;
+        read_a(SLOT, AT_A0);
+        if constexpr (LEFT >= 1) fill(A1, st + 1, SLOT ^ 1);
+        convert(fb0[FB], 0, st);
+        wait_vm<LEFT >= 1 ? F::last_five(kA1) : F::of(kA1)>();
+        multiply(0, fb0[FB], 0);
+        if constexpr (!FOUR) read_b(fb1, SLOT, AT_B1);
+        if constexpr (LEFT >= 2) fill(B0, st + 2, SLOT);
+        convert(fb1, 1, st);
+        wait_vm<LEFT >= 2 ? F::last_five(kB0) : LEFT == 1 ? F::all() : 0>();
+        multiply(0, fb1, 1);
+        read_a(SLOT, AT_A1);
+        if constexpr (LEFT >= 2) fill(A0, st + 2, SLOT);
+        if constexpr (LEFT >= 1) wait_vm<LEFT >= 2 ? F::last_five(kA0) : F::all() - F::of(kB0)>();
+        multiply(1, fb1, 1);
+        if constexpr (LEFT >= 1) {
+            if constexpr (FOUR) read_codes(SLOT ^ 1, st + 1);
+            else read_b(fb0[FB ^ 1], SLOT ^ 1, 0);
+        }
+        if constexpr (LEFT >= 2) fill(B1, st + 2, SLOT);
+        if constexpr (LEFT >= 1) wait_vm<LEFT >= 2 ? F::last_five(kB1) : F::of(kB1) + F::of(kA1)>();
+        multiply(1, fb0[FB], 0);
+    };
+    // The scales of a run's stages, four (of two stages) a word, 0 behind the last group: two threads a weight row, eight
+    // words of a thread in flight.  (One after the other they cost each tile 8 us.)
+    const auto load_scales = [&](int stages) {
+        const int rb = tid >> 1, groups = g.K / kMxGroup - 2 * st_run, words = (stages + 1) / 2, mine = (words + 1) / 2;
+        const uint8_t *const from = (EPI == kGate && (rb & 32) ? g.up.scales : g.b.scales) + ((size_t)n0 + column(rb)) * (g.K / kMxGroup) + 2 * st_run;
+        uint32_t *const to = scales + rb * (SCALE_ROW / 4);
+        const int rest = groups & 3, full = groups >> 2;
+        for (int i0 = 0; i0 < mine; i0 += 8) {
+            uint32_t v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int w = (tid & 1) * mine + i0 + i;
+                v[i] = 0;
+                if (w < full) __builtin_memcpy(&v[i], from + 4 * w, 4);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int w = (tid & 1) * mine + i0 + i;
+                if (w == full)
+                    for (int k = 0; k < rest; ++k) v[i] |= (uint32_t)from[4 * w + k] << (8 * k);
+                if (i0 + i < mine && w < words) to[w] = v[i];
+            }
+        }
+        __syncthreads();
+    };
+    const auto run = [&](int stages) {
+        const int first = stages & 1;  // slot of the first stage: the last but one is in slot 0
+        fill(B0, 0, first);
+        fill(A0, 0, first);
+        fill(B1, 0, first);
+        fill(A1, 0, first);
+        fill(B0, 1, first ^ 1);
+        fill(A0, 1, first ^ 1);
+        fill(B1, 1, first ^ 1);
+        if constexpr (FOUR) load_scales(stages);
+        wait_vm<F::last_five(kB1)>();
+        half_phase();
+        if constexpr (FOUR) {
+            read_codes(first, 0);
+        } else {  // into both: a choice between them would put them into memory
+            read_b(fb0[0], first, 0);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) fb0[1][b / 2][b % 2] = fb0[0][b / 2][b % 2];
+        }
+        if (wr == 1) half_phase();
+        int st = 0;
+        if (first == 1) stage(std::integral_constant<int, 1>(), std::integral_constant<int, 2>(), st++);
+        for (; st < stages - 2; st += 2) {
+            stage(std::integral_constant<int, 0>(), std::integral_constant<int, 2>(), st);
+            stage(std::integral_constant<int, 1>(), std::integral_constant<int, 2>(), st + 1);
+        }
+        stage(std::integral_constant<int, 0>(), std::integral_constant<int, 1>(), st);
+        stage(std::integral_constant<int, 1>(), std::integral_constant<int, 0>(), st + 1);
+        if (wr == 0) half_phase();
+    };
+    // Stages [s0, s1) of the tile, counted over all planes of x.
+    const auto sums = [&](int s0, int s1) {
+#pragma unroll
+        for (int b = 0; b < 8 * Q; ++b) acc[b / (4 * Q)][b / 4 % Q][b % 4] = f32x4{0.f, 0.f, 0.f, 0.f};
+        while (s0 < s1) {
+            const int p = s0 / nk, left = min(s1, (p + 1) * nk) - s0;
+            // with 4-bit weights at most kRunStages of them: in parts of equal length, so of two stages at least
+            const int stages = FOUR ? left / ((left + kRunStages - 1) / kRunStages) : left;
+            a_run = uniform(reinterpret_cast<const char *>(g.a + (size_t)p * g.plane_rows * g.K));
+            st_run = s0 - p * nk;
+            run(stages);
+            s0 += stages;
+        }
+    };
+    // K cut into parts: in units of four stages (the last of a plane up to seven), so that none is shorter than two
+    const int per_plane = max(nk / kUnitStages, 1), units = per_plane * g.a_planes;
+    const auto stage_of = [&](int u) { return u / per_plane * nk + u % per_plane * kUnitStages; };
+    sums(__builtin_amdgcn_readfirstlane(stage_of((int)((long long)units * z / g.splits))),
+         __builtin_amdgcn_readfirstlane(stage_of((int)((long long)units * (z + 1) / g.splits))));
+    if (g.splits > 1) {
+        constexpr size_t PART = BM * 64;  // f32x4 of a part
+        const int tile = nt * mtiles + mt;
+        f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * PART + (size_t)wave * (8 * Q) * 64 + lane;
+#pragma unroll
+        for (int b = 0; b < 8 * Q; ++b) parts[(size_t)z * PART + b * 64] = acc[b / (4 * Q)][b / 4 % Q][b % 4];
+        if (!last_of_tile(g.counters + tile, g.splits)) return;
+        for (int w = 0; w < g.splits; ++w)
+#pragma unroll
+            for (int b = 0; b < 8 * Q; ++b) {
+                f32x4 &v = acc[b / (4 * Q)][b / 4 % Q][b % 4];
+                const f32x4 part = parts[(size_t)w * PART + b * 64];
+                v = w == 0 ? part : v + part;
+                if (b % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // loads of more at once would cost the loop its registers
+            }
+    }
+    // acc[h][mb][2 p + b][i] = C[BM / 2 wr + 16 Q h + 16 mb + lane % 16][column 8 (lane / 16) + 4 b + i of the wave's p-th 32]
+    const int cw = n0 + wc * (EPI == kGate ? 32 : 64) + 8 * g4;
+#pragma unroll
+    for (int b = 0; b < 2 * Q; ++b) {
+        const f32x4(&v)[4] = acc[b / Q][b % Q];
+        const int row = m0 + BM / 2 * wr + 16 * b + l16;
+        if (row >= g.M) continue;
+        if constexpr (EPI == kGate) {
+            if (cw < g.N) store_h(g, v[0], v[1], v[2], v[3], row, cw);
+        } else {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+                if (cw + 32 * p < g.N) store_eight<EPI>(g, v[2 * p], v[2 * p + 1], row, cw + 32 * p);
+        }
+    }
 }
 
+// Workgroups: the tiles of every part, those of a part behind each other.
+template <class... A, class... B>
+hipError_t launch_epilogue(Epilogue epi, void (*bf16)(A...), void (*f32)(A...), void (*gate)(A...), dim3 grid, int threads, hipStream_t s, B... args) {
+    (epi == kStoreBf16 ? bf16 : epi == kStoreF32 ? f32 : gate)<<<grid, threads, 0, s>>>(args...);
+    return hipGetLastError();
+}
+template <int MB, int CB, int WC, int KG>
+hipError_t launch_mid(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
+    return launch_epilogue(epi, mid_kernel<MB, CB, WC, KG, kStoreBf16>, mid_kernel<MB, CB, WC, KG, kStoreF32>, mid_kernel<MB, CB, WC, KG, kGate>,
+                           dim3(grid.x * grid.y, 1, grid.z), 64 * WC * KG, s, g);
+}
+template <int BM, int D>
+hipError_t launch_tile(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
+    return launch_epilogue(epi, tile_kernel<BM, 128, D, 2, 2, kStoreBf16>, tile_kernel<BM, 128, D, 2, 2, kStoreF32>, tile_kernel<BM, 128, D, 2, 2, kGate>,
+                           dim3(grid.x * grid.y, 1, grid.z), 256, s, g);
+}
+template <int Q, bool FOUR>
+hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
+    return launch_epilogue(epi, big_kernel<Q, FOUR, kStoreBf16>, big_kernel<Q, FOUR, kStoreF32>, big_kernel<Q, FOUR, kGate>,
+                           dim3(grid.x * grid.y * grid.z), 512, s, g);
+}
 template <bool FOUR>
-hipError_t launch_shape(const GemmArgs &g, Epilogue epi, const Shape &t, hipStream_t s) {
-    if (t.bm == 256 && t.bn == 256) return launch_tiles<256, 256, 2, 2, 4, FOUR>(g, epi, s);
-    if (t.bm == 128 && t.bn == 128) return launch_tiles<128, 128, 2, 2, 2, FOUR>(g, epi, s);
-    if (t.bm == 64 && t.bn == 128) return launch_tiles<64, 128, 3, 2, 2, FOUR>(g, epi, s);
-    if (t.bm == 32 && t.bn == 128) return launch_tiles<32, 128, 4, 2, 2, FOUR>(g, epi, s);
-    return hipErrorInvalidValue;
+hipError_t launch_rows(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
+    return launch_epilogue(epi, rows_kernel<1, 2, FOUR, kStoreBf16>, rows_kernel<1, 2, FOUR, kStoreF32>, rows_kernel<1, 2, FOUR, kGate>, grid, 512, s, g);
+}
+
+struct Tiles {
+    long long m, n;
+};
+Tiles tiles_of(const GemmArgs &g, Epilogue epi, Variant v) {
+    const int cols = epi == kGate ? kSizes[v].bn / 2 : kSizes[v].bn;
+    return {((long long)g.M + kSizes[v].bm - 1) / kSizes[v].bm, ((long long)g.N + cols - 1) / cols};
 }
 
 }  // namespace
 
-hipError_t launch_gemm(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t, hipStream_t s) {
-    if (g.M <= 0) return hipSuccess;
-    if (g.N <= 0 || g.N % 8 != 0 || g.K <= 0 || g.K % (four_bit ? kMxGroup : 8) != 0 || g.a_planes < 1) return hipErrorInvalidValue;
-    return four_bit ? launch_shape<true>(g, epi, t, s) : launch_shape<false>(g, epi, t, s);
+bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t) {
+    if (t.variant < 0 || t.variant >= kVariants || !(four_bit ? kSizes[t.variant].four : kSizes[t.variant].bf16)) return false;
+    if (g.M < 1 || g.N < 8 || g.N % 8 != 0 || g.K < 1 || g.K % (four_bit ? kMxGroup : 8) != 0 || g.a_planes < 1 || t.splits < 1) return false;
+    const Tiles n = tiles_of(g, epi, t.variant);
+    if (n.m * n.n > 0x7fffffff || (t.variant == kRows16 && n.m > 0xffff)) return false;
+    const int stages = (g.K + kBK - 1) / kBK;
+    const bool big = t.variant == kBig128 || t.variant == kBig256;
+    if (big && stages < 2) return false;
+    if (t.splits == 1) return true;
+    return n.m * n.n <= kMaxSplitTiles && (size_t)(n.m * n.n) * t.splits * kSizes[t.variant].bm * kSizes[t.variant].bn * 4 <= kPartBytes &&
+           t.splits <= (big ? std::max(stages / kUnitStages, 1) : (g.K + 127) / 128) * g.a_planes;
+}
+
+hipError_t launch_gemm(GemmArgs g, bool four_bit, Epilogue epi, const Shape &t, hipStream_t s) {
+    if (!fits(g, four_bit, epi, t) || (t.splits > 1 && (!g.parts || !g.counters))) return hipErrorInvalidValue;
+    const Tiles n = tiles_of(g, epi, t.variant);
+    g.splits = t.splits;
+    const dim3 grid((unsigned)n.n, (unsigned)n.m, (unsigned)t.splits);
+    switch (t.variant) {
+        case kRows16: return four_bit ? launch_rows<true>(g, epi, grid, s) : launch_rows<false>(g, epi, grid, s);
+        case kTile32: return launch_tile<32, 4>(g, epi, grid, s);
+        case kTile64: return launch_tile<64, 3>(g, epi, grid, s);
+        case kTile128: return launch_tile<128, 2>(g, epi, grid, s);
+        case kMid16: return launch_mid<1, 2, 2, 4>(g, epi, grid, s);
+        case kMid32: return launch_mid<2, 2, 2, 4>(g, epi, grid, s);
+        case kMid48: return launch_mid<3, 2, 2, 4>(g, epi, grid, s);
+        case kMid64: return launch_mid<4, 2, 2, 4>(g, epi, grid, s);
+        case kMid32Wide: return launch_mid<2, 2, 8, 1>(g, epi, grid, s);
+        case kMid64Wide: return launch_mid<4, 4, 4, 1>(g, epi, grid, s);
+        case kMid64Cols: return launch_mid<4, 2, 4, 1>(g, epi, grid, s);
+        case kMid64Pair: return launch_mid<4, 2, 4, 2>(g, epi, grid, s);
+        case kBig128: return four_bit ? launch_big<2, true>(g, epi, grid, s) : launch_big<2, false>(g, epi, grid, s);
+        case kBig256: return four_bit ? launch_big<4, true>(g, epi, grid, s) : launch_big<4, false>(g, epi, grid, s);
+        default: return hipErrorInvalidValue;
+    }
 }
 
 }  // namespace ffn
