@@ -41,7 +41,7 @@ enum Variant : int {
     kRows16,                                      // few rows, either kind of weights
     kTile32, kTile64, kTile128,                   // bf16 weights
     kMid16, kMid32, kMid48, kMid64,               // 4-bit weights, four wave groups on K
-    kMid32Wide, kMid64Wide, kMid64Cols, kMid64Pair,  // 4-bit weights, one or two
+    kMid32Wide, kMid64Wide, kMid64Cols, kMid64Pair, kMid64Long,  // 4-bit weights, one or two
     kBig128, kBig256,                             // many rows, either kind
     kVariants
 };
@@ -53,7 +53,7 @@ constexpr VariantSize kSizes[kVariants] = {
     {16, 32, true, true},
     {32, 128, true, false}, {64, 128, true, false}, {128, 128, true, false},
     {16, 64, false, true}, {32, 64, false, true}, {48, 64, false, true}, {64, 64, false, true},
-    {32, 256, false, true}, {64, 256, false, true}, {64, 128, false, true}, {64, 128, false, true},
+    {32, 256, false, true}, {64, 256, false, true}, {64, 128, false, true}, {64, 128, false, true}, {64, 128, false, true},
     {128, 256, true, true}, {256, 256, true, true},
 };
 constexpr int kUnitStages = 4;  // stages of 64 k that a part of K has at least in the kernels for many rows

@@ -343,14 +343,15 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
 
 // A middling number of rows: bound by the weights, which go straight from memory to
 // registers as above, or by the products.  WC waves share the rows of x through LDS
-// (slices of 128 k, one ahead: loaded to registers before a slice's products, stored
+// (slices of 128 SL k, one ahead: loaded to registers before a slice's products, stored
 // to the other buffer after them) and take CB blocks of 16 weight rows each (kGate:
 // the first half gate, the second the same columns of up); KG such groups take K's
 // slices in turn and meet in LDS.  gridDim.z cuts K further.
-template <int MB, int CB, int WC, int KG, int EPI>
+template <int MB, int CB, int WC, int KG, int SL, int EPI>
 __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
     constexpr int JB = EPI == kGate ? CB / 2 : CB, COLS = 16 * JB * WC;
-    constexpr int BUF = MB * 16 * 16;               // 16-byte slots of one buffer
+    constexpr int CH = 16 * SL;                     // 16-byte chunks of a row's slice
+    constexpr int BUF = MB * 16 * CH;               // and of one buffer
     constexpr int LPT = (BUF + 64 * WC - 1) / (64 * WC);
     static_assert(BUF % (64 * WC) == 0 || LPT == 1, "loads of a slice");
     static_assert(KG == 1 || KG * 2 * BUF >= (KG / 2) * WC * MB * CB * 64, "partial sums fit the buffers");
@@ -360,7 +361,7 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
     int mt, nt;
     tile_at(xcd_run(blockIdx.x, gridDim.x), (g.M + 16 * MB - 1) / (16 * MB), (g.N + COLS - 1) / COLS, &mt, &nt);
     const int m0 = mt * 16 * MB, n0 = nt * COLS + wc * 16 * JB;
-    const int ns = (g.K + 127) >> 7, total = ns * g.a_planes;
+    const int ns = (g.K + 128 * SL - 1) / (128 * SL), total = ns * g.a_planes;
     const int j0 = (int)((long long)total * blockIdx.z / g.splits), j1 = (int)((long long)total * (blockIdx.z + 1) / g.splits);
     const int rounds = (j1 - j0 + KG - 1) / KG;
     const size_t plane = (size_t)g.plane_rows * g.K;
@@ -379,32 +380,42 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
     }
     const uint16_t *arow[LPT];
 #pragma unroll
-    for (int i = 0; i < LPT; ++i) arow[i] = g.a + (size_t)min(m0 + min((gt + 64 * WC * i) >> 4, 16 * MB - 1), g.M - 1) * g.K;
+    for (int i = 0; i < LPT; ++i) arow[i] = g.a + (size_t)min(m0 + min((gt + 64 * WC * i) / CH, 16 * MB - 1), g.M - 1) * g.K;
 
     u32x4 areg[LPT];
     const auto load_a = [&](int j) {
-        const int p = j / ns, k = (j - p * ns) * 128 + (gt & 15) * 8;
+        const int p = j / ns, k = (j - p * ns) * (128 * SL) + gt % CH * 8;
 #pragma unroll
         for (int i = 0; i < LPT; ++i) areg[i] = *reinterpret_cast<const u32x4 *>(arow[i] + p * plane + (k < g.K ? k : 0));
     };
     const auto put_a = [&](int j, u32x4 *to) {
-        const bool in = j % ns * 128 + (gt & 15) * 8 < g.K;
+        const bool in = j % ns * (128 * SL) + gt % CH * 8 < g.K;
 #pragma unroll
         for (int i = 0; i < LPT; ++i) {
-            const int row = (gt + 64 * WC * i) >> 4;
-            if (BUF % (64 * WC) == 0 || row < 16 * MB) to[row * 16 + ((gt ^ row) & 15)] = in ? areg[i] : u32x4{0u, 0u, 0u, 0u};
+            const int row = (gt + 64 * WC * i) / CH;
+            if (BUF % (64 * WC) == 0 || row < 16 * MB) to[row * CH + (gt % CH ^ (row & 15))] = in ? areg[i] : u32x4{0u, 0u, 0u, 0u};
         }
     };
+    // a lane's SL groups of a slice are neighbours, as its codes are loaded; behind the last k they are read from the row's
+    // start, and dropped in use()
     struct Slice {
-        u32x4 codes[CB];
-        uint32_t scale[CB];
+        u32x4 codes[CB][SL];
+        uint32_t scales[CB];
     };
     const auto load_b = [&](Slice &s, int j) {
-        const int k = j % ns * 128 + 32 * grp, at = k < g.K ? k : 0;
+        const int k = j % ns * (128 * SL) + 32 * SL * grp;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            s.codes[cb] = *reinterpret_cast<const u32x4 *>(crow[cb] + at / 2);
-            s.scale[cb] = srow[cb][at / kMxGroup];
+#pragma unroll
+            for (int t = 0; t < SL; ++t) s.codes[cb][t] = *reinterpret_cast<const u32x4 *>(crow[cb] + (k + 32 * t < g.K ? k + 32 * t : 0) / 2);
+            const uint8_t *const from = srow[cb] + (k < g.K ? k : 0) / kMxGroup;
+            if (SL == 1 || k + 32 >= g.K) {
+                s.scales[cb] = *from;
+            } else {
+                uint16_t two;
+                __builtin_memcpy(&two, from, 2);
+                s.scales[cb] = two;
+            }
         }
     };
     f32x4 acc[MB][CB];
@@ -413,23 +424,25 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) acc[mb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
     const auto use = [&](Slice &s, int j, const u32x4 *from) {
-        const int k0 = j % ns * 128;
-        if (k0 + 128 > g.K) {  // groups behind the last k count as zeros, on both sides
+        const int k0 = j % ns * (128 * SL);
+        if (k0 + 128 * SL > g.K) {  // groups behind the last k count as zeros, on both sides
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-                const bool in = k0 + 32 * grp < g.K;
-                s.codes[cb] = in ? s.codes[cb] : u32x4{0u, 0u, 0u, 0u};
-                s.scale[cb] = in ? s.scale[cb] : 0u;
-            }
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int t = 0; t < SL; ++t)
+                    if (k0 + 32 * (SL * grp + t) >= g.K) {
+                        s.codes[cb][t] = u32x4{0u, 0u, 0u, 0u};
+                        s.scales[cb] &= ~(0xffu << (8 * t));
+                    }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4 * SL; ++i) {
             u32x4 fa[MB];
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) fa[mb] = from[(16 * mb + l16) * 16 + ((4 * grp + i) ^ l16)];
+            for (int mb = 0; mb < MB; ++mb) fa[mb] = from[(16 * mb + l16) * CH + ((4 * SL * grp + i) ^ l16)];
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                const u32x4 b = mx_values(s.codes[cb][i], mx_scale(s.scale[cb]));
+                const u32x4 b = mx_values(s.codes[cb][i / 4][i % 4], mx_scale((s.scales[cb] >> (i / 4 * 8)) & 0xffu));
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb) acc[mb][cb] = mfma(b, fa[mb], acc[mb][cb]);
             }
@@ -512,56 +525,66 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
     }
 }
 
-// BM x BN tile on WR x WC waves, K in stages of 64 through a ring of D LDS stages
-// that direct global -> LDS loads fill ahead.  With kGate the BN weight rows are, for each column of waves, 32
-// rows of the gate and the same 32 of the up projection, so that a lane ends up with
-// both products of its columns.
+// A middling number of rows, bf16 weights: a BM x BN tile on WR x WC waves, K in stages of
+// 64 through a ring of D LDS stages that direct global -> LDS loads fill ahead.  A stage's
+// operands are read while the products of the one before run, so that one barrier a stage
+// is all that the waves wait for together: behind it a stage has landed for all of them
+// and the slot of the one before is free.  With kGate the BN weight rows are, for each
+// column of waves, 32 rows of the gate and the same 32 of the up projection, so that a lane
+// ends up with both products of its columns.
 template <int BM, int BN, int D, int WR, int WC, int EPI>
 __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
-    constexpr int NT = 64 * WR * WC, NW = WR * WC;
-    constexpr int STAGE = (BM + BN) * 8;                       // 16-byte slots per stage
+    constexpr int NW = WR * WC;
+    constexpr int STAGE = (BM + BN) * 8;                      // 16-byte slots per stage
     constexpr int NPW = STAGE / 64 / NW;                      // loads per wave per stage
     constexpr int WM = BM / WR, MB = WM / 16, WN = BN / WC, NB = WN / 16;
-    static_assert(STAGE % NT == 0 && WN == 64 && MB >= 1 && NB == 4, "shape");
+    static_assert(STAGE % (64 * NW) == 0 && WN == 64 && MB >= 1 && NB == 4 && D >= 2, "shape");
     __shared__ __attribute__((aligned(1024))) u32x4 ring[D * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    constexpr int COLS = EPI == kGate ? BN / 2 : BN;           // output columns of a tile
+    constexpr int COLS = EPI == kGate ? BN / 2 : BN;          // output columns of a tile
     int mt, nt;
     tile_at(xcd_run(blockIdx.x, gridDim.x), (g.M + BM - 1) / BM, (g.N + COLS - 1) / COLS, &mt, &nt);
-    const int m0 = mt * BM, n0 = nt * COLS;
+    const int m0 = __builtin_amdgcn_readfirstlane(mt * BM), n0 = __builtin_amdgcn_readfirstlane(nt * COLS);
     const int nk = (g.K + kBK - 1) / kBK, all = nk * g.a_planes;
     const int first = (int)((long long)all * blockIdx.z / g.splits), stages = (int)((long long)all * (blockIdx.z + 1) / g.splits) - first;
 
-    // weight row of the tile's B row rb: (second matrix?, row); rows past the end repeat the last, never stored
-    const auto weight_row = [&](int rb, bool *second) {
-        *second = EPI == kGate && (rb & 32) != 0;
-        return min(n0 + (EPI == kGate ? (rb >> 6) * 32 + (rb & 31) : rb), g.N - 1);
-    };
-    const uint16_t *src[NPW];
+    // The wave's i-th load fills 8 neighbouring rows of x or the weights: the first one is wave-uniform.  Rows past the end
+    // repeat the last one (the widths are multiples of 8: of weight rows all eight exist or none); never stored.
+    const char *base[NPW];
+    uint32_t off[NPW];
+    int kin[NPW];
 #pragma unroll
     for (int i = 0; i < NPW; ++i) {
-        const int s = (wave * NPW + i) * 64 + lane, row = s >> 3;
-        if (row < BM) {
-            src[i] = g.a + (size_t)min(m0 + row, g.M - 1) * g.K + ((s & 7) ^ swz_a(row)) * 8;
+        const int at = 8 * (wave * NPW + i), row = at + (lane >> 3);
+        kin[i] = ((lane & 7) ^ (at < BM ? swz_a(row) : swz_b(row))) * 8;
+        if (at < BM) {
+            const int r = min(m0 + at, g.M - 1);
+            base[i] = uniform(reinterpret_cast<const char *>(g.a + (size_t)r * g.K));
+            off[i] = (uint32_t)min(lane >> 3, g.M - 1 - r) * (uint32_t)g.K * 2u + (uint32_t)kin[i] * 2u;
         } else {
-            bool second;
-            const size_t n = weight_row(row - BM, &second);
-            src[i] = (second ? g.up.w : g.b.w) + n * g.K + ((s & 7) ^ swz_b(row)) * 8;
+            const int rb = at - BM, n = min(n0 + (EPI == kGate ? (rb >> 6) * 32 + (rb & 31) : rb), g.N - 8);
+            base[i] = uniform(reinterpret_cast<const char *>((EPI == kGate && (rb & 32) ? g.up.w : g.b.w) + (size_t)n * g.K));
+            off[i] = (uint32_t)(lane >> 3) * (uint32_t)g.K * 2u + (uint32_t)kin[i] * 2u;
         }
     }
-    const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
-    const size_t plane = (size_t)g.plane_rows * g.K;
-    const auto issue = [&](int st) {
-        const int p = (first + st) / nk, k0 = (first + st - p * nk) * kBK;
-        const uint32_t dst = ring_lds + (uint32_t)((st % D) * STAGE * 16 + wave * NPW * 1024);
-        const bool tail = k0 + kBK > g.K;
+    const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring)) + wave * NPW * 1024;
+    const size_t plane = (size_t)g.plane_rows * g.K * 2;
+    int p = first / nk, k0 = (first - p * nk) * kBK, slot_in = 0;  // of the stage to load next
+    const auto issue = [&] {
+        const uint32_t dst = ring_lds + (uint32_t)(slot_in * STAGE * 16);
+        const bool whole = k0 + kBK <= g.K;
 #pragma unroll
         for (int i = 0; i < NPW; ++i) {
-            const int s = (wave * NPW + i) * 64 + lane, row = s >> 3;
-            const void *from = src[i] + k0 + (row < BM ? p * plane : 0);
-            if (tail && k0 + ((s & 7) ^ (row < BM ? swz_a(row) : swz_b(row))) * 8 >= g.K) from = &kZeros;
-            dma16(from, __builtin_amdgcn_readfirstlane(dst + i * 1024));
+            const char *const from = base[i] + (size_t)k0 * 2 + (8 * (wave * NPW + i) < BM ? p * plane : 0);
+            if (whole) dma16_at(off[i], from, dst + i * 1024);
+            else dma16(k0 + kin[i] < g.K ? from + off[i] : reinterpret_cast<const char *>(&kZeros), dst + i * 1024);
+        }
+        slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
+        k0 += kBK;
+        if (k0 >= g.K) {
+            k0 = 0;
+            ++p;
         }
     };
     f32x4 acc[MB][NB];
@@ -570,36 +593,56 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int wr = (wave / WC) * WM, wc = BM + (wave % WC) * WN;
-
+    struct Operands {
+        u32x4 a[2][MB], b[2][NB];
+    };
+    int at_a[2], at_b[2];  // this lane's slots in a stage for the two steps of 32 k
 #pragma unroll
-    for (int st = 0; st < D - 1; ++st)
-        if (st < stages) issue(st);
-    for (int kt = 0; kt < stages; ++kt) {
-        if (kt + D - 1 < stages) issue(kt + D - 1);
-        // stage kt has landed once no more than the stages issued after it are in flight
-        wait_stages<NPW, D - 1>(min(D - 1, stages - 1 - kt));
-        __syncthreads();
-        const u32x4 *cur = ring + (kt % D) * STAGE;
+    for (int s = 0; s < 2; ++s) {
+        const int kc = s * 4 + (lane >> 4), ra = wr + (lane & 15), rb = wc + pair_column(lane, 0);
+        at_a[s] = ra * 8 + (kc ^ swz_a(ra));
+        at_b[s] = rb * 8 + (kc ^ swz_b(rb));
+    }
+    const auto read = [&](Operands &o, int slot) {
+        const u32x4 *const cur = ring + slot * STAGE;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int kc = s * 4 + (lane >> 4);
-            u32x4 fa[MB], fb[NB];
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                const int row = wr + mb * 16 + (lane & 15);
-                fa[mb] = cur[row * 8 + (kc ^ swz_a(row))];
-            }
+            for (int mb = 0; mb < MB; ++mb) o.a[s][mb] = cur[at_a[s] + mb * 128];
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const int row = wc + pair_column(lane, nb);
-                fb[nb] = cur[row * 8 + (kc ^ swz_b(row))];
-            }
+            for (int nb = 0; nb < NB; ++nb) o.b[s][nb] = cur[at_b[s] + pair_column(0, nb) * 8];  // (rows 4 and 32 on: same swizzle)
+        }
+    };
+    const auto multiply = [&](const Operands &o) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma(fb[nb], fa[mb], acc[mb][nb]);
-        }
-        __syncthreads();  // the slot of stage kt is refilled by the next iteration's loads
+                for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma(o.b[s][nb], o.a[s][mb], acc[mb][nb]);
+    };
+#pragma unroll
+    for (int st = 0; st < D; ++st)
+        if (st < stages) issue();
+    wait_stages<NPW, D - 1>(min(D - 1, stages - 1));
+    half_phase();
+    Operands o0, o1;
+    read(o0, 0);
+    int slot = 0;
+    const auto step = [&](Operands &now, Operands &next, int kt) {
+        // stage kt + 1 has landed once no more than the D - 2 stages issued after it are in flight; this wave's operands of
+        // stage kt have arrived, behind the barrier those of all waves: its slot is free
+        if (kt + 1 < stages) wait_stages<NPW, D - 2>(min(D - 2, stages - 2 - kt));
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        half_phase();
+        if (kt + D < stages) issue();
+        slot = slot + 1 == D ? 0 : slot + 1;
+        if (kt + 1 < stages) read(next, slot);
+        multiply(now);
+    };
+    for (int kt = 0; kt < stages; kt += 2) {
+        step(o0, o1, kt);
+        if (kt + 1 < stages) step(o1, o0, kt + 1);
     }
 
     if (g.splits > 1) {
@@ -948,15 +991,15 @@ hipError_t launch_epilogue(Epilogue epi, void (*bf16)(A...), void (*f32)(A...), 
     (epi == kStoreBf16 ? bf16 : epi == kStoreF32 ? f32 : gate)<<<grid, threads, 0, s>>>(args...);
     return hipGetLastError();
 }
-template <int MB, int CB, int WC, int KG>
+template <int MB, int CB, int WC, int KG, int SL>
 hipError_t launch_mid(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
-    return launch_epilogue(epi, mid_kernel<MB, CB, WC, KG, kStoreBf16>, mid_kernel<MB, CB, WC, KG, kStoreF32>, mid_kernel<MB, CB, WC, KG, kGate>,
+    return launch_epilogue(epi, mid_kernel<MB, CB, WC, KG, SL, kStoreBf16>, mid_kernel<MB, CB, WC, KG, SL, kStoreF32>, mid_kernel<MB, CB, WC, KG, SL, kGate>,
                            dim3(grid.x * grid.y, 1, grid.z), 64 * WC * KG, s, g);
 }
-template <int BM, int D>
+template <int BM, int D, int WR = 2>
 hipError_t launch_tile(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
-    return launch_epilogue(epi, tile_kernel<BM, 128, D, 2, 2, kStoreBf16>, tile_kernel<BM, 128, D, 2, 2, kStoreF32>, tile_kernel<BM, 128, D, 2, 2, kGate>,
-                           dim3(grid.x * grid.y, 1, grid.z), 256, s, g);
+    return launch_epilogue(epi, tile_kernel<BM, 128, D, WR, 2, kStoreBf16>, tile_kernel<BM, 128, D, WR, 2, kStoreF32>,
+                           tile_kernel<BM, 128, D, WR, 2, kGate>, dim3(grid.x * grid.y, 1, grid.z), 128 * WR, s, g);
 }
 template <int Q, bool FOUR>
 hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
@@ -999,16 +1042,17 @@ hipError_t launch_gemm(GemmArgs g, bool four_bit, Epilogue epi, const Shape &t, 
     switch (t.variant) {
         case kRows16: return four_bit ? launch_rows<true>(g, epi, grid, s) : launch_rows<false>(g, epi, grid, s);
         case kTile32: return launch_tile<32, 4>(g, epi, grid, s);
-        case kTile64: return launch_tile<64, 3>(g, epi, grid, s);
-        case kTile128: return launch_tile<128, 2>(g, epi, grid, s);
-        case kMid16: return launch_mid<1, 2, 2, 4>(g, epi, grid, s);
-        case kMid32: return launch_mid<2, 2, 2, 4>(g, epi, grid, s);
-        case kMid48: return launch_mid<3, 2, 2, 4>(g, epi, grid, s);
-        case kMid64: return launch_mid<4, 2, 2, 4>(g, epi, grid, s);
-        case kMid32Wide: return launch_mid<2, 2, 8, 1>(g, epi, grid, s);
-        case kMid64Wide: return launch_mid<4, 4, 4, 1>(g, epi, grid, s);
-        case kMid64Cols: return launch_mid<4, 2, 4, 1>(g, epi, grid, s);
-        case kMid64Pair: return launch_mid<4, 2, 4, 2>(g, epi, grid, s);
+        case kTile64: return launch_tile<64, 3, 4>(g, epi, grid, s);
+        case kTile128: return launch_tile<128, 4, 4>(g, epi, grid, s);
+        case kMid16: return launch_mid<1, 2, 2, 4, 2>(g, epi, grid, s);
+        case kMid32: return launch_mid<2, 2, 2, 4, 1>(g, epi, grid, s);
+        case kMid48: return launch_mid<3, 2, 2, 4, 1>(g, epi, grid, s);
+        case kMid64: return launch_mid<4, 2, 2, 4, 1>(g, epi, grid, s);
+        case kMid32Wide: return launch_mid<2, 2, 8, 1, 2>(g, epi, grid, s);
+        case kMid64Wide: return launch_mid<4, 4, 4, 1, 1>(g, epi, grid, s);
+        case kMid64Cols: return launch_mid<4, 2, 4, 1, 2>(g, epi, grid, s);
+        case kMid64Pair: return launch_mid<4, 2, 4, 2, 1>(g, epi, grid, s);
+        case kMid64Long: return launch_mid<4, 2, 4, 2, 2>(g, epi, grid, s);
         case kBig128: return four_bit ? launch_big<2, true>(g, epi, grid, s) : launch_big<2, false>(g, epi, grid, s);
         case kBig256: return four_bit ? launch_big<4, true>(g, epi, grid, s) : launch_big<4, false>(g, epi, grid, s);
         default: return hipErrorInvalidValue;
