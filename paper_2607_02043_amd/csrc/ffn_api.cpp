@@ -75,26 +75,25 @@ int cu_count() {
 // What a launch takes, in us: sweeps of every kernel and number of parts over 45 products of 1 to 4160 rows (an
 // MI355X, weights from memory).  A workgroup walks its stages of 64 k (1 / groups of them) at `stage` us each; where
 // `resident` workgroups of a CU run at once, a stage takes `share` us for each of them, and rounds of them follow
-// each other.  Joining parts adds `join` and `join_part` a part.  The rule's choice is within a tenth of the best
+// each other.  Parts are stored at 2.5 TB/s by all, and read by the workgroup that joins a tile's at 60 GB/s.  The rule's choice is within a tenth of the best
 // for 37 of the 45, within a quarter for all.
 struct Cost {
     float fixed, stage, share;
     int resident, groups;
-    float join, join_part;
 };
 constexpr Cost kCostBf16[ffn::kVariants] = {
-    {3.f, .95f, 1.84f, 4, 8, 2.f, .9f},
-    {3.5f, .5f, .5f, 2, 1, 6.f, .4f}, {3.5f, .57f, .48f, 2, 1, 5.f, .75f}, {3.5f, .75f, .8f, 1, 1, 6.f, 1.2f},
+    {3.f, 1.4f, 1.7f, 4, 8},
+    {3.5f, .5f, .5f, 2, 1}, {3.5f, .57f, .48f, 2, 1}, {3.5f, .75f, .8f, 1, 1},
     {}, {}, {}, {}, {}, {}, {}, {}, {},
-    {5.f, 1.f, 1.f, 1, 1, 2.f, 4.f}, {7.f, 1.32f, 1.32f, 1, 1, 25.f, 6.f},
+    {5.f, 1.f, 1.f, 1, 1}, {7.f, 1.32f, 1.32f, 1, 1},
 };
 constexpr Cost kCost4[ffn::kVariants] = {
-    {3.f, .45f, .9f, 4, 8, .2f, 2.f},
+    {3.f, .62f, .9f, 4, 8},
     {}, {}, {},
-    {3.f, .7f, .6f, 4, 4, 3.5f, .7f}, {3.f, .9f, .85f, 4, 4, 3.5f, .7f}, {3.f, 1.15f, 1.2f, 2, 4, 4.f, .4f}, {3.f, 1.25f, 1.3f, 1, 4, 4.f, 1.f},
-    {3.f, .7f, .57f, 2, 1, 4.f, 1.f}, {3.f, .9f, .6f, 2, 1, 6.f, 4.f}, {3.f, .72f, .34f, 2, 1, 6.f, 2.f}, {3.f, 1.2f, .7f, 2, 2, 4.f, 2.f},
-    {3.f, .85f, .9f, 1, 2, 6.f, 1.f},
-    {5.f, 1.04f, 1.04f, 1, 1, 16.f, 2.5f}, {8.f, 1.45f, 1.45f, 1, 1, 25.f, 6.f},
+    {3.f, .7f, .6f, 4, 4}, {3.f, .9f, .85f, 4, 4}, {3.f, 1.15f, 1.2f, 2, 4}, {3.f, 1.25f, 1.3f, 1, 4},
+    {3.f, .7f, .57f, 2, 1}, {3.f, .9f, .6f, 2, 1}, {3.f, .6f, .3f, 2, 1}, {3.f, 1.2f, 1.f, 2, 2},
+    {3.f, .85f, .9f, 1, 2},
+    {5.f, 1.04f, 1.04f, 1, 1}, {8.f, 1.45f, 1.45f, 1, 1},
 };
 
 float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::Shape &t, int ncu) {
@@ -103,13 +102,15 @@ float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::S
     const int cols = epi == ffn::kGate ? v.bn / 2 : v.bn;
     const double tiles = std::ceil((double)g.M / v.bm) * std::ceil((double)g.N / cols);
     const double chain = std::ceil(std::ceil(g.K / 64.0) * g.a_planes / t.splits / c.groups), load = tiles * t.splits / ncu;
-    const double joined = t.splits > 1 ? c.join + c.join_part * t.splits : 0.0;
-    // workgroups a CU has at once, and how many times (past three rounds they no longer end together)
-    const double once = std::min<double>(c.resident, std::ceil(load)), rounds = load > 3.0 * c.resident && c.resident > 1 ? load / c.resident : std::ceil(load / once);
-    const double walk = rounds * (c.fixed + chain * std::max<double>(c.stage, once * c.share)) + joined;
-    // what the weights take to arrive: 4.3 TB/s in bf16, 2.8 in 4 bits
+    const double part = 4.0 * v.bm * v.bn, joined = t.splits > 1 ? 2.0 + t.splits * part / 6e4 + tiles * t.splits * part / 2.5e6 : 0.0;
+    // workgroups a CU has at once, and how many times (past one and a half rounds they no longer end together)
+    const double once = std::min<double>(c.resident, std::ceil(load)), rounds = load > 1.5 * c.resident && c.resident > 1 ? load / c.resident : std::ceil(load / once);
+    // (the few-row kernel reads each row of x for itself: a single one costs it less)
+    const double rows = t.variant == ffn::kRows16 ? .7 + .3 * std::min(g.M, 16) / 16 : 1.0;
+    const double walk = rounds * (c.fixed + chain * rows * (once > 1 ? std::max<double>(c.stage, once * c.share) : c.stage)) + joined;
+    // what the weights take to arrive: 4.3 TB/s in bf16, in 4 bits 3.4 where wave groups share K and 2.4 where they do not
     const double bytes = (epi == ffn::kGate ? 2.0 : 1.0) * g.N * (double)g.K * (four ? .53 : 2.0);
-    return (float)std::max(walk, bytes / (four ? 2.8e6 : 4.3e6) + c.fixed);
+    return (float)std::max(walk, bytes / (!four ? 4.3e6 : c.groups >= 4 ? 3.4e6 : 2.4e6) + c.fixed);
 }
 
 struct Plan {

@@ -19,6 +19,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -159,18 +160,72 @@ __device__ __forceinline__ void store_h(const GemmArgs &g, f32x4 g0, f32x4 g1, f
     }
 }
 
-// Split sums.  Every workgroup of a tile has stored its part; true in all threads of
-// the one that comes last, which then sees the parts of the others.  The counter is
-// left as it was found, zero.
+// Split sums.  Parts meet in memory; the XCDs do not share their L2 caches.  THROUGH: they are written and read as
+// device-wide atomics, past the L2s, which costs a part 4 TB/s for the chip but no more; otherwise as plain values, and
+// a workgroup writes back what its L2 holds before it is counted (some 3 us, more with more of them).  So small tiles
+// go through (a row of K = 10944 in 4 bits 10.6 -> 7.3 us, 16 rows in bf16 19.3 -> 13.7), those of 64 KB and more do
+// not (1500 rows, parts of 256 KB: 102 against 116 us).
+template <bool THROUGH>
+__device__ __forceinline__ void put_part(f32x4 *to, f32x4 v) {
+    if constexpr (THROUGH) {
+        const u64x2 w = __builtin_bit_cast(u64x2, v);
+        uint64_t *const p = reinterpret_cast<uint64_t *>(to);
+        __hip_atomic_store(p, w[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(p + 1, w[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else {
+        *to = v;
+    }
+}
+template <bool THROUGH>
+__device__ __forceinline__ f32x4 get_part(const f32x4 *from) {
+    if constexpr (THROUGH) {
+        const uint64_t *const p = reinterpret_cast<const uint64_t *>(from);
+        return __builtin_bit_cast(f32x4, u64x2{__hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                               __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)});
+    } else {
+        return *from;
+    }
+}
+// Every workgroup of a tile has put its part: true in all threads of the one that comes last, which then gets those of
+// the others.  The counter is left as it was found, zero.
+template <bool THROUGH>
 __device__ __forceinline__ bool last_of_tile(uint32_t *counter, int splits) {
     __shared__ bool last;
-    __syncthreads();  // this workgroup's parts are stored
+    // THROUGH: each wave waits until its own stores have arrived in memory; else the release below covers the workgroup's
+    if constexpr (THROUGH) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    __syncthreads();
     if (threadIdx.x == 0) {
-        last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)splits - 1;
+        const uint32_t before = __hip_atomic_fetch_add(counter, 1u, THROUGH ? __ATOMIC_RELAXED : __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        last = before == (uint32_t)splits - 1;
         if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(last);  // one branch for the whole wave
+}
+
+// sums[b] = the parts' b-th values, part 0 first.  Four parts of eight values are in flight at a time: one after the
+// other, each would cost a trip to memory (a 64 x 128 tile's 16 parts are half a megabyte, which
+// one CU takes 10 us to read).
+template <bool THROUGH, int N>
+__device__ __forceinline__ void join_parts(f32x4 (&sums)[N], const f32x4 *parts, size_t stride, int splits) {
+    constexpr int C = N < 8 ? N : 8;
+    static_assert(N % C == 0, "whole chunks");
+#pragma unroll
+    for (int b0 = 0; b0 < N; b0 += C) {
+        for (int z = 0; z < splits; z += 4) {
+            f32x4 v[4][C];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int b = 0; b < C; ++b) v[i][b] = get_part<THROUGH>(parts + (size_t)min(z + i, splits - 1) * stride + (b0 + b) * 64);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (z + i < splits) {
+#pragma unroll
+                    for (int b = 0; b < C; ++b) sums[b0 + b] = z + i == 0 ? v[i][b] : sums[b0 + b] + v[i][b];
+                }
+        }
+    }
 }
 
 // Four consecutive columns of a row.
@@ -319,14 +374,14 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
     f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * (MB * CB * 64) + lane;
     const auto block_sum = [&](int b) { return red[0][b][lane] + red[1][b][lane] + red[2][b][lane] + red[3][b][lane]; };
     if (g.splits > 1) {
-        for (int b = wave; b < MB * CB; b += 8) parts[((size_t)blockIdx.z * (MB * CB) + b) * 64] = block_sum(b);
-        if (!last_of_tile(g.counters + tile, g.splits)) return;
+        for (int b = wave; b < MB * CB; b += 8) put_part<true>(parts + ((size_t)blockIdx.z * (MB * CB) + b) * 64, block_sum(b));
+        if (!last_of_tile<true>(g.counters + tile, g.splits)) return;
     }
     const auto total_sum = [&](int b) {
         if (g.splits == 1) return block_sum(b);
-        f32x4 v = parts[(size_t)b * 64];
-        for (int z = 1; z < g.splits; ++z) v += parts[((size_t)z * (MB * CB) + b) * 64];
-        return v;
+        f32x4 v[1];
+        join_parts<true>(v, parts + (size_t)b * 64, MB * CB * 64, g.splits);
+        return v[0];
     };
     // D[16 mb + lane % 16][16 jb + 4 (lane / 16) + i]
     for (int u = wave; u < UNITS; u += 8) {
@@ -350,6 +405,7 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
 template <int MB, int CB, int WC, int KG, int SL, int EPI>
 __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
     constexpr int JB = EPI == kGate ? CB / 2 : CB, COLS = 16 * JB * WC;
+    constexpr bool kThrough = MB * CB * WC < 64;
     constexpr int CH = 16 * SL;                     // 16-byte chunks of a row's slice
     constexpr int BUF = MB * 16 * CH;               // and of one buffer
     constexpr int LPT = (BUF + 64 * WC - 1) / (64 * WC);
@@ -494,14 +550,10 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
         f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * PART + wc * MB * CB * 64 + lane;
         if (kg == 0) {
 #pragma unroll
-            for (int b = 0; b < MB * CB; ++b) parts[(size_t)blockIdx.z * PART + b * 64] = acc[b / CB][b % CB];
+            for (int b = 0; b < MB * CB; ++b) put_part<kThrough>(parts + (size_t)blockIdx.z * PART + b * 64, acc[b / CB][b % CB]);
         }
-        if (!last_of_tile(g.counters + tile, g.splits) || kg > 0) return;
-#pragma unroll
-        for (int b = 0; b < MB * CB; ++b) acc[b / CB][b % CB] = parts[b * 64];
-        for (int z = 1; z < g.splits; ++z)
-#pragma unroll
-            for (int b = 0; b < MB * CB; ++b) acc[b / CB][b % CB] += parts[(size_t)z * PART + b * 64];
+        if (!last_of_tile<kThrough>(g.counters + tile, g.splits) || kg > 0) return;
+        join_parts<kThrough>(reinterpret_cast<f32x4(&)[MB * CB]>(acc), parts, PART, g.splits);
     }
     if (kg > 0) return;
 #pragma unroll
@@ -649,13 +701,9 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
         const int tile = nt * ((g.M + BM - 1) / BM) + mt;
         f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * (BM * BN / 4) + (size_t)wave * MB * NB * 64 + lane;
 #pragma unroll
-        for (int b = 0; b < MB * NB; ++b) parts[(size_t)blockIdx.z * (BM * BN / 4) + b * 64] = acc[b / NB][b % NB];
-        if (!last_of_tile(g.counters + tile, g.splits)) return;
-#pragma unroll
-        for (int b = 0; b < MB * NB; ++b) acc[b / NB][b % NB] = parts[b * 64];
-        for (int z = 1; z < g.splits; ++z)
-#pragma unroll
-            for (int b = 0; b < MB * NB; ++b) acc[b / NB][b % NB] += parts[(size_t)z * (BM * BN / 4) + b * 64];
+        for (int b = 0; b < MB * NB; ++b) put_part<true>(parts + (size_t)blockIdx.z * (BM * BN / 4) + b * 64, acc[b / NB][b % NB]);
+        if (!last_of_tile<true>(g.counters + tile, g.splits)) return;
+        join_parts<true>(reinterpret_cast<f32x4(&)[MB * NB]>(acc), parts, BM * BN / 4, g.splits);
     }
 
     // acc[mb][2 p + b][i] = C[16 mb + lane % 16][32 p + 8 (lane / 16) + 4 b + i]
@@ -957,16 +1005,9 @@ __global__ __launch_bounds__(512) void big_kernel(const GemmArgs g) {
         const int tile = nt * mtiles + mt;
         f32x4 *const parts = reinterpret_cast<f32x4 *>(g.parts) + (size_t)tile * g.splits * PART + (size_t)wave * (8 * Q) * 64 + lane;
 #pragma unroll
-        for (int b = 0; b < 8 * Q; ++b) parts[(size_t)z * PART + b * 64] = acc[b / (4 * Q)][b / 4 % Q][b % 4];
-        if (!last_of_tile(g.counters + tile, g.splits)) return;
-        for (int w = 0; w < g.splits; ++w)
-#pragma unroll
-            for (int b = 0; b < 8 * Q; ++b) {
-                f32x4 &v = acc[b / (4 * Q)][b / 4 % Q][b % 4];
-                const f32x4 part = parts[(size_t)w * PART + b * 64];
-                v = w == 0 ? part : v + part;
-                if (b % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // loads of more at once would cost the loop its registers
-            }
+        for (int b = 0; b < 8 * Q; ++b) put_part<false>(parts + (size_t)z * PART + b * 64, acc[b / (4 * Q)][b / 4 % Q][b % 4]);
+        if (!last_of_tile<false>(g.counters + tile, g.splits)) return;
+        join_parts<false>(reinterpret_cast<f32x4(&)[8 * Q]>(acc), parts, PART, g.splits);
     }
     // acc[h][mb][2 p + b][i] = C[BM / 2 wr + 16 Q h + 16 mb + lane % 16][column 8 (lane / 16) + 4 b + i of the wave's p-th 32]
     const int cw = n0 + wc * (EPI == kGate ? 32 : 64) + 8 * g4;
