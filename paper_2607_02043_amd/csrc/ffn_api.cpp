@@ -108,9 +108,9 @@ float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::S
     // (the few-row kernel reads each row of x for itself: a single one costs it less)
     const double rows = t.variant == ffn::kRows16 ? .7 + .3 * std::min(g.M, 16) / 16 : 1.0;
     const double walk = rounds * (c.fixed + chain * rows * (once > 1 ? std::max<double>(c.stage, once * c.share) : c.stage)) + joined;
-    // what the weights take to arrive: 4.3 TB/s in bf16, in 4 bits 3.4 where wave groups share K and 2.4 where they do not
+    // what the weights take to arrive: 4.3 TB/s in bf16, in 4 bits 3.4 where wave groups share K and 2.7 where they do not
     const double bytes = (epi == ffn::kGate ? 2.0 : 1.0) * g.N * (double)g.K * (four ? .53 : 2.0);
-    return (float)std::max(walk, bytes / (!four ? 4.3e6 : c.groups >= 4 ? 3.4e6 : 2.4e6) + c.fixed);
+    return (float)std::max(walk, bytes / (!four ? 4.3e6 : c.groups >= 4 ? 3.4e6 : 2.7e6) + c.fixed);
 }
 
 struct Plan {
