@@ -75,8 +75,8 @@ int cu_count() {
 // What a launch takes, in us: sweeps of every kernel and number of parts over 45 products of 1 to 4160 rows (an
 // MI355X, weights from memory).  A workgroup walks its stages of 64 k (1 / groups of them) at `stage` us each; where
 // `resident` workgroups of a CU run at once, a stage takes `share` us for each of them, and rounds of them follow
-// each other.  Parts are stored at 2.5 TB/s by all, and read by the workgroup that joins a tile's at 60 GB/s.  The rule's choice is within a tenth of the best
-// for 37 of the 45, within a quarter for all.
+// each other.  Parts are stored at 2.5 TB/s by all, and read by the workgroup that joins a tile's at 60 GB/s.  The
+// rule's choice is within 12 % of the best for each of the 45.
 struct Cost {
     float fixed, stage, share;
     int resident, groups;
@@ -84,14 +84,14 @@ struct Cost {
 constexpr Cost kCostBf16[ffn::kVariants] = {
     {3.f, 1.4f, 1.7f, 4, 8},
     {3.5f, .5f, .5f, 2, 1}, {3.5f, .57f, .48f, 2, 1}, {3.5f, .75f, .8f, 1, 1},
-    {}, {}, {}, {}, {}, {}, {}, {}, {},
+    {}, {}, {}, {}, {}, {}, {}, {},
     {5.f, 1.f, 1.f, 1, 1}, {7.f, 1.32f, 1.32f, 1, 1},
 };
 constexpr Cost kCost4[ffn::kVariants] = {
     {3.f, .62f, .9f, 4, 8},
     {}, {}, {},
     {3.f, .7f, .6f, 4, 4}, {3.f, .9f, .85f, 4, 4}, {3.f, 1.15f, 1.2f, 2, 4}, {3.f, 1.25f, 1.3f, 1, 4},
-    {3.f, .7f, .57f, 2, 1}, {3.f, .9f, .6f, 2, 1}, {3.f, .6f, .3f, 2, 1}, {3.f, 1.2f, 1.f, 2, 2},
+    {3.f, .7f, .57f, 2, 1}, {3.f, .9f, .6f, 2, 1}, {3.f, .6f, .3f, 2, 1},
     {3.f, .85f, .9f, 1, 2},
     {5.f, 1.04f, 1.04f, 1, 1}, {8.f, 1.45f, 1.45f, 1, 1},
 };
@@ -99,8 +99,8 @@ constexpr Cost kCost4[ffn::kVariants] = {
 float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::Shape &t, int ncu) {
     const Cost &c = (four ? kCost4 : kCostBf16)[t.variant];
     const ffn::VariantSize &v = ffn::kSizes[t.variant];
-    const int cols = epi == ffn::kGate ? v.bn / 2 : v.bn;
-    const double tiles = std::ceil((double)g.M / v.bm) * std::ceil((double)g.N / cols);
+    const ffn::Tiles n = ffn::tiles_of(g, epi, t.variant);
+    const double tiles = (double)(n.m * n.n);
     const double chain = std::ceil(std::ceil(g.K / 64.0) * g.a_planes / t.splits / c.groups), load = tiles * t.splits / ncu;
     const double part = 4.0 * v.bm * v.bn, joined = t.splits > 1 ? 2.0 + t.splits * part / 6e4 + tiles * t.splits * part / 2.5e6 : 0.0;
     // workgroups a CU has at once, and how many times (past one and a half rounds they no longer end together)
@@ -115,8 +115,9 @@ float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::S
 
 struct Plan {
     ffn::Shape shape{};
-    int rest = 0;  // rows at the end that a launch of their own takes
     float us = 0;
+    int rest = 0;  // rows at the end that a launch of their own takes
+    ffn::Shape rest_shape{};
 };
 
 // The cheapest kernel and number of parts for these rows.
@@ -126,12 +127,11 @@ Plan best_whole(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, int ncu) {
     for (int v = 0; v < ffn::kVariants; ++v) {
         ffn::Shape t{static_cast<ffn::Variant>(v), 1};
         if (!ffn::fits(g, four, epi, t)) continue;
-        const int cols = epi == ffn::kGate ? ffn::kSizes[v].bn / 2 : ffn::kSizes[v].bn;
-        const double tiles = std::ceil((double)g.M / ffn::kSizes[v].bm) * std::ceil((double)g.N / cols);
+        const ffn::Tiles n = ffn::tiles_of(g, epi, t.variant);
         for (; t.splits <= 32; ++t.splits) {
-            if (t.splits > 1 && (tiles * t.splits > 2.0 * ncu || !ffn::fits(g, four, epi, t))) break;
+            if (t.splits > 1 && (n.m * n.n * t.splits > 2LL * ncu || !ffn::fits(g, four, epi, t))) break;
             const float us = cost_of(g, four, epi, t, ncu);
-            if (us < best.us) best = {t, 0, us};
+            if (us < best.us) best = {t, us};
         }
     }
     return best;
@@ -160,8 +160,10 @@ const Plan &plan_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi) {
         part.M = g.M - rest;
         Plan p = best_whole(part, four, epi, ncu);
         part.M = rest;
-        p.us = 1.05f * (p.us + best_whole(part, four, epi, ncu).us);  // not for a few per cent
+        const Plan behind = best_whole(part, four, epi, ncu);
+        p.us = 1.05f * (p.us + behind.us);  // not for a few per cent
         p.rest = rest;
+        p.rest_shape = behind.shape;
         if (p.us < best.us) best = p;
     }
     e = {dev, g.M, g.N, g.K, kind, best};
@@ -170,6 +172,7 @@ const Plan &plan_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi) {
 
 int launch(ffn::GemmArgs g, bool four, ffn::Epilogue epi, hipStream_t s, const char *what) {
     const Plan plan = plan_of(g, four, epi);
+    if (plan.shape.splits < 1) return set_error(MLA_ERR_UNSUPPORTED, "%s: %d x %d outputs are more tiles than a launch takes", what, g.M, g.N);
     const int rows = g.M;
     g.M = rows - plan.rest;
     hipError_t e = ffn::launch_gemm(g, four, epi, plan.shape, s);
@@ -178,7 +181,7 @@ int launch(ffn::GemmArgs g, bool four, ffn::Epilogue epi, hipStream_t s, const c
         g.a += (size_t)g.M * g.K;
         g.out = static_cast<char *>(g.out) + (size_t)g.M * g.N * width;
         g.M = plan.rest;
-        e = ffn::launch_gemm(g, four, epi, best_whole(g, four, epi, cu_count()).shape, s);
+        e = ffn::launch_gemm(g, four, epi, plan.rest_shape, s);
     }
     return e == hipSuccess ? MLA_OK : mla::hip_error(e, what);
 }

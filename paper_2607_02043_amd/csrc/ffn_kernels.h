@@ -1,6 +1,7 @@
 // Launch-side description of the feed-forward kernels of libmlastep (host <-> device).
 #pragma once
 #include <hip/hip_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 namespace ffn {
@@ -41,7 +42,7 @@ enum Variant : int {
     kRows16,                                      // few rows, either kind of weights
     kTile32, kTile64, kTile128,                   // bf16 weights
     kMid16, kMid32, kMid48, kMid64,               // 4-bit weights, four wave groups on K
-    kMid32Wide, kMid64Wide, kMid64Cols, kMid64Pair, kMid64Long,  // 4-bit weights, one or two
+    kMid32Wide, kMid64Wide, kMid64Cols, kMid64Long,  // 4-bit weights, one or two
     kBig128, kBig256,                             // many rows, either kind
     kVariants
 };
@@ -53,7 +54,7 @@ constexpr VariantSize kSizes[kVariants] = {
     {16, 32, true, true},
     {32, 128, true, false}, {64, 128, true, false}, {128, 128, true, false},
     {16, 64, false, true}, {32, 64, false, true}, {48, 64, false, true}, {64, 64, false, true},
-    {32, 256, false, true}, {64, 256, false, true}, {64, 128, false, true}, {64, 128, false, true}, {64, 128, false, true},
+    {32, 256, false, true}, {64, 256, false, true}, {64, 128, false, true}, {64, 128, false, true},
     {128, 256, true, true}, {256, 256, true, true},
 };
 constexpr int kUnitStages = 4;  // stages of 64 k that a part of K has at least in the kernels for many rows
@@ -67,8 +68,28 @@ struct Shape {
 constexpr int kMaxSplitTiles = 1024;
 constexpr size_t kPartBytes = size_t(64) << 20;
 
+struct Tiles {
+    long long m, n;
+};
+inline Tiles tiles_of(const GemmArgs &g, Epilogue epi, Variant v) {
+    const int cols = epi == kGate ? kSizes[v].bn / 2 : kSizes[v].bn;
+    return {((long long)g.M + kSizes[v].bm - 1) / kSizes[v].bm, ((long long)g.N + cols - 1) / cols};
+}
 // Whether the launch is one that the kernels take.
-bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t);
+inline bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t) {
+    if (t.variant < 0 || t.variant >= kVariants || !(four_bit ? kSizes[t.variant].four : kSizes[t.variant].bf16)) return false;
+    if (g.M < 1 || g.N < 8 || g.N % 8 != 0 || g.K < 1 || g.K % (four_bit ? kMxGroup : 8) != 0 || g.a_planes < 1 || t.splits < 1) return false;
+    const Tiles n = tiles_of(g, epi, t.variant);
+    if (n.m * n.n > 0x7fffffff || (t.variant == kRows16 && n.m > 0xffff)) return false;
+    const int stages = (g.K + kBK - 1) / kBK;
+    const bool big = t.variant == kBig128 || t.variant == kBig256;
+    if (big && stages < 2) return false;
+    if (t.splits == 1) return true;
+    // no part is empty: the kernels for many rows count in units of stages, the others in stages or in slices of up to four
+    const long long pieces = (long long)(big ? (stages < kUnitStages ? 1 : stages / kUnitStages) : (stages + 3) / 4) * g.a_planes;
+    return n.m * n.n <= kMaxSplitTiles && t.splits <= pieces &&
+           (size_t)(n.m * n.n) * t.splits * kSizes[t.variant].bm * kSizes[t.variant].bn * 4 <= kPartBytes;
+}
 hipError_t launch_gemm(GemmArgs g, bool four_bit, Epilogue epi, const Shape &t, hipStream_t s);
 
 }  // namespace ffn

@@ -8,7 +8,6 @@
 // included, two an instruction), so both formats share the products.
 #include "ffn_kernels.h"
 
-#include <algorithm>
 #include <type_traits>
 
 namespace ffn {
@@ -1052,28 +1051,7 @@ hipError_t launch_rows(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s
     return launch_epilogue(epi, rows_kernel<1, 2, FOUR, kStoreBf16>, rows_kernel<1, 2, FOUR, kStoreF32>, rows_kernel<1, 2, FOUR, kGate>, grid, 512, s, g);
 }
 
-struct Tiles {
-    long long m, n;
-};
-Tiles tiles_of(const GemmArgs &g, Epilogue epi, Variant v) {
-    const int cols = epi == kGate ? kSizes[v].bn / 2 : kSizes[v].bn;
-    return {((long long)g.M + kSizes[v].bm - 1) / kSizes[v].bm, ((long long)g.N + cols - 1) / cols};
-}
-
 }  // namespace
-
-bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t) {
-    if (t.variant < 0 || t.variant >= kVariants || !(four_bit ? kSizes[t.variant].four : kSizes[t.variant].bf16)) return false;
-    if (g.M < 1 || g.N < 8 || g.N % 8 != 0 || g.K < 1 || g.K % (four_bit ? kMxGroup : 8) != 0 || g.a_planes < 1 || t.splits < 1) return false;
-    const Tiles n = tiles_of(g, epi, t.variant);
-    if (n.m * n.n > 0x7fffffff || (t.variant == kRows16 && n.m > 0xffff)) return false;
-    const int stages = (g.K + kBK - 1) / kBK;
-    const bool big = t.variant == kBig128 || t.variant == kBig256;
-    if (big && stages < 2) return false;
-    if (t.splits == 1) return true;
-    return n.m * n.n <= kMaxSplitTiles && (size_t)(n.m * n.n) * t.splits * kSizes[t.variant].bm * kSizes[t.variant].bn * 4 <= kPartBytes &&
-           t.splits <= (big ? std::max(stages / kUnitStages, 1) : (g.K + 127) / 128) * g.a_planes;
-}
 
 hipError_t launch_gemm(GemmArgs g, bool four_bit, Epilogue epi, const Shape &t, hipStream_t s) {
     if (!fits(g, four_bit, epi, t) || (t.splits > 1 && (!g.parts || !g.counters))) return hipErrorInvalidValue;
@@ -1092,7 +1070,6 @@ hipError_t launch_gemm(GemmArgs g, bool four_bit, Epilogue epi, const Shape &t, 
         case kMid32Wide: return launch_mid<2, 2, 8, 1, 2>(g, epi, grid, s);
         case kMid64Wide: return launch_mid<4, 4, 4, 1, 1>(g, epi, grid, s);
         case kMid64Cols: return launch_mid<4, 2, 4, 1, 2>(g, epi, grid, s);
-        case kMid64Pair: return launch_mid<4, 2, 4, 2, 1>(g, epi, grid, s);
         case kMid64Long: return launch_mid<4, 2, 4, 2, 2>(g, epi, grid, s);
         case kBig128: return four_bit ? launch_big<2, true>(g, epi, grid, s) : launch_big<2, false>(g, epi, grid, s);
         case kBig256: return four_bit ? launch_big<4, true>(g, epi, grid, s) : launch_big<4, false>(g, epi, grid, s);

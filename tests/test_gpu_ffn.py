@@ -30,8 +30,12 @@ def test_linear4_rows(T, dtype):
 
 
 # widths: one group and odd numbers of them, ends inside a stage and a slice; outputs from 8 columns on
-@pytest.mark.parametrize("T", [1, 5, 40, 70, 300])
-@pytest.mark.parametrize("k,n", [(32, 8), (64, 24), (96, 40), (160, 1000), (416, 136), (2048, 72), (1376, 264), (10944, 16)])
+FEW = (1, 5, 40, 70, 300)
+LINEAR_SIZES = [(32, 8), (64, 24), (96, 40), (160, 1000), (416, 136), (2048, 72), (1376, 264), (10944, 16)]
+
+
+@pytest.mark.parametrize("T", FEW)
+@pytest.mark.parametrize("k,n", LINEAR_SIZES)
 def test_linear4_sizes(T, k, n):
     log(f"[gpu] linear4 {T} x {k} -> {n}")
     x, w = rows(3, T, k), Matrix(4, n, k, True)
@@ -52,13 +56,51 @@ SIZES = [(8, 8), (24, 40), (40, 8), (72, 1368), (2048, 24), (1000, 200)]
 SIZES4 = [(32, 32), (96, 32), (32, 160), (2048, 96), (160, 1376), (1024, 224)]
 
 
-@pytest.mark.parametrize("T", [1, 5, 40, 70, 300])
+@pytest.mark.parametrize("T", FEW)
 @pytest.mark.parametrize("four,hidden,inner", [(False, *s) for s in SIZES] + [(True, *s) for s in SIZES4])
 def test_ffn_sizes(T, four, hidden, inner):
     log(f"[gpu] ffn {T} x {hidden} x {inner} {four}")
     x, mats = rows(7, T, hidden), block(8, hidden, inner, four)
     ref = O.ffn(x.double().numpy(), *(m.values for m in mats), 3)
     assert_within(ffn(x, mats, F32), *ref, F32, f"{T} x {hidden} x {inner}")
+
+
+# (0 product with 4-bit weights, 1 block in bf16, 2 block in 4 bits; rows; in or hidden; out or inner; fp32 output): calls
+# that between them choose every kernel, whole and in parts, in every product that it takes, and rows left to a second launch
+EVERY_KERNEL = [
+    (0, 2169, 96, 40, 0), (0, 2207, 2656, 40, 0), (0, 2249, 5344, 952, 1), (0, 2759, 3744, 72, 1), (0, 2775, 2720, 40, 0),
+    (0, 2912, 6784, 752, 0), (0, 3258, 160, 200, 1), (0, 4253, 3968, 8, 0), (0, 4447, 192, 80, 0), (0, 4461, 160, 8, 1),
+    (0, 4479, 2304, 8, 1), (1, 4, 8, 328, 1), (1, 10, 8, 1056, 0), (1, 1048, 112, 200, 1), (1, 1361, 3152, 728, 1),
+    (1, 1925, 2128, 8, 1), (1, 2121, 1128, 24, 0), (1, 2503, 904, 4200, 0), (1, 2552, 3160, 72, 1), (1, 2773, 712, 1072, 1),
+    (1, 2892, 8, 136, 0), (1, 3368, 72, 624, 1), (1, 3596, 1272, 1600, 1), (1, 3695, 1064, 72, 0), (1, 3714, 10504, 320, 0),
+    (1, 3882, 80, 1192, 0), (1, 4173, 8, 1864, 0), (1, 4186, 952, 5440, 0), (1, 4225, 3504, 8, 0), (1, 4253, 16, 8448, 0),
+    (1, 4302, 1552, 8, 1), (1, 4305, 8, 200, 1), (1, 4339, 8, 2560, 1), (1, 4426, 3648, 96, 0), (2, 341, 128, 2080, 1),
+    (2, 393, 2720, 32, 1), (2, 408, 9504, 96, 1), (2, 451, 4256, 1920, 1), (2, 480, 128, 4192, 1), (2, 684, 5184, 32, 1),
+    (2, 801, 64, 7424, 0), (2, 1155, 32, 4000, 1), (2, 1238, 7584, 32, 0), (2, 1413, 7328, 128, 1), (2, 1420, 5440, 768, 1),
+    (2, 1532, 96, 32, 1), (2, 1693, 2432, 160, 1), (2, 1812, 2720, 288, 1), (2, 2103, 96, 32, 1), (2, 2186, 2368, 32, 1),
+    (2, 2220, 64, 800, 1), (2, 2699, 1472, 32, 0), (2, 2700, 1696, 5184, 0), (2, 2743, 160, 4320, 0), (2, 2935, 5312, 768, 1),
+    (2, 3380, 1216, 800, 0), (2, 3421, 672, 2240, 1), (2, 3458, 1248, 2048, 1), (2, 3546, 8256, 288, 1), (2, 3737, 160, 1664, 1),
+    (2, 4101, 3424, 256, 0), (2, 4187, 96, 32, 1), (2, 4213, 2112, 32, 1), (2, 4234, 32, 1088, 1), (2, 4255, 96, 864, 1),
+    (2, 4313, 160, 96, 0), (2, 4473, 160, 32, 1),
+    (0, 21, 2944, 16752, 0), (2, 19, 8704, 3264, 1), (2, 21, 2080, 8704, 0),
+]
+
+
+@pytest.mark.parametrize("what,T,k,n,f32", EVERY_KERNEL)
+def test_every_kernel(what, T, k, n, f32):
+    log(f"[gpu] every kernel {what} {T} {k} {n} {f32}")
+    dtype, four = (F32 if f32 else BF16), what != 1
+    x = rows(31, T, k)
+    # the first and last rows, those at each multiple of 128 (tiles and second launches begin there), 64 more
+    edge = np.arange(0, T, 128)
+    at = np.unique(np.concatenate((np.arange(min(T, 8)), np.arange(max(0, T - 8), T), edge, edge[1:] - 1, np.random.default_rng(1).integers(0, T, 64))))
+    if what == 0:
+        w = Matrix(32, n, k, True)
+        got, ref = linear4(x, w, dtype), O.linear(x[at].double().numpy(), w.values)
+    else:
+        mats = block(33, k, n, four)
+        got, ref = ffn(x, mats, dtype), O.ffn(x[at].double().numpy(), *(m.values for m in mats), 3 if f32 else 1)
+    assert_within(got[at], *ref, dtype, f"{what} {T} x {k} x {n}")
 
 
 @pytest.mark.parametrize("four", [False, True], ids=["bf16w", "mx4"])
