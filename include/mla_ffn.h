@@ -86,7 +86,8 @@ size_t mla_linear4_workspace_bytes(int32_t num_rows, int32_t in_features, int32_
  *   out           DEVICE [T][N] fp32 or bf16 (out_dtype).
  * Errors: MLA_ERR_INVALID_ARG (a null or misaligned pointer with T > 0, T < 0,
  * an unknown out_dtype, a size < 1), MLA_ERR_UNSUPPORTED (sizes that are not
- * such multiples, or above 2^24), MLA_ERR_WORKSPACE, MLA_ERR_HIP. */
+ * such multiples, or above 2^24, more than 2^28 rows, more tiles of outputs
+ * than a launch takes), MLA_ERR_WORKSPACE, MLA_ERR_HIP. */
 int mla_linear4(int32_t num_rows, const uint16_t *x, const mla_mx4 *w, int32_t in_features, int32_t out_features, void *out,
                 int32_t out_dtype, void *workspace, size_t workspace_bytes, void *stream);
 

@@ -76,11 +76,12 @@ inline Tiles tiles_of(const GemmArgs &g, Epilogue epi, Variant v) {
     return {((long long)g.M + kSizes[v].bm - 1) / kSizes[v].bm, ((long long)g.N + cols - 1) / cols};
 }
 // Whether the launch is one that the kernels take.
+constexpr long long kMaxTiles = (1 << 23) - 1;  // (of up to 512 threads: a grid has fewer than 2^32)
 inline bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t) {
     if (t.variant < 0 || t.variant >= kVariants || !(four_bit ? kSizes[t.variant].four : kSizes[t.variant].bf16)) return false;
     if (g.M < 1 || g.N < 8 || g.N % 8 != 0 || g.K < 1 || g.K % (four_bit ? kMxGroup : 8) != 0 || g.a_planes < 1 || t.splits < 1) return false;
     const Tiles n = tiles_of(g, epi, t.variant);
-    if (n.m * n.n > 0x7fffffff || (t.variant == kRows16 && n.m > 0xffff)) return false;
+    if (n.m * n.n > kMaxTiles || (t.variant == kRows16 && n.m > 0xffff)) return false;
     const int stages = (g.K + kBK - 1) / kBK;
     const bool big = t.variant == kBig128 || t.variant == kBig256;
     if (big && stages < 2) return false;

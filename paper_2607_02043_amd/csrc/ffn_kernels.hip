@@ -160,10 +160,10 @@ __device__ __forceinline__ void store_h(const GemmArgs &g, f32x4 g0, f32x4 g1, f
 }
 
 // Split sums.  Parts meet in memory; the XCDs do not share their L2 caches.  THROUGH: they are written and read as
-// device-wide atomics, past the L2s, which costs a part 4 TB/s for the chip but no more; otherwise as plain values, and
-// a workgroup writes back what its L2 holds before it is counted (some 3 us, more with more of them).  So small tiles
-// go through (a row of K = 10944 in 4 bits 10.6 -> 7.3 us, 16 rows in bf16 19.3 -> 13.7), those of 64 KB and more do
-// not (1500 rows, parts of 256 KB: 102 against 116 us).
+// device-wide atomics, past the L2s, at 4 TB/s for the whole chip; otherwise as plain values, and a workgroup writes
+// back what its L2 holds before it is counted (some 3 us, more with more of them).  So small tiles go through (a row of
+// K = 10944 in 4 bits 10.6 -> 7.3 us, 16 rows in bf16 19.3 -> 13.7), those of 4-bit weights with 64 KB a part and the
+// tiles for many rows do not (1500 rows, parts of 256 KB: 102 against 116 us).
 template <bool THROUGH>
 __device__ __forceinline__ void put_part(f32x4 *to, f32x4 v) {
     if constexpr (THROUGH) {
@@ -190,8 +190,8 @@ __device__ __forceinline__ f32x4 get_part(const f32x4 *from) {
 template <bool THROUGH>
 __device__ __forceinline__ bool last_of_tile(uint32_t *counter, int splits) {
     __shared__ bool last;
-    // THROUGH: each wave waits until its own stores have arrived in memory; else the release below covers the workgroup's
-    if constexpr (THROUGH) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    // each wave waits for its own stores, which have then arrived: THROUGH in memory, else in the L2 that the release writes back
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     __syncthreads();
     if (threadIdx.x == 0) {
         const uint32_t before = __hip_atomic_fetch_add(counter, 1u, THROUGH ? __ATOMIC_RELAXED : __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
@@ -202,9 +202,9 @@ __device__ __forceinline__ bool last_of_tile(uint32_t *counter, int splits) {
     return __builtin_amdgcn_readfirstlane(last);  // one branch for the whole wave
 }
 
-// sums[b] = the parts' b-th values, part 0 first.  Four parts of eight values are in flight at a time: one after the
-// other, each would cost a trip to memory (a 64 x 128 tile's 16 parts are half a megabyte, which
-// one CU takes 10 us to read).
+// sums[b] = the parts' b-th values, part 0 first: the order, and so the result, is the same whoever comes last.  Four
+// parts of eight values are in flight at a time; one after the other, each would cost a trip to memory (one CU reads
+// some 60 GB/s: the 16 parts of a 64 x 128 tile, half a megabyte, take it 9 us).
 template <bool THROUGH, int N>
 __device__ __forceinline__ void join_parts(f32x4 (&sums)[N], const f32x4 *parts, size_t stride, int splits) {
     constexpr int C = N < 8 ? N : 8;
@@ -1025,7 +1025,6 @@ __global__ __launch_bounds__(512) void big_kernel(const GemmArgs g) {
     }
 }
 
-// Workgroups: the tiles of every part, those of a part behind each other.
 template <class... A, class... B>
 hipError_t launch_epilogue(Epilogue epi, void (*bf16)(A...), void (*f32)(A...), void (*gate)(A...), dim3 grid, int threads, hipStream_t s, B... args) {
     (epi == kStoreBf16 ? bf16 : epi == kStoreF32 ? f32 : gate)<<<grid, threads, 0, s>>>(args...);
@@ -1042,7 +1041,7 @@ hipError_t launch_tile(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s
                            tile_kernel<BM, 128, D, WR, 2, kGate>, dim3(grid.x * grid.y, 1, grid.z), 128 * WR, s, g);
 }
 template <int Q, bool FOUR>
-hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
+hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {  // the tiles of every part, those of a part behind each other
     return launch_epilogue(epi, big_kernel<Q, FOUR, kStoreBf16>, big_kernel<Q, FOUR, kStoreF32>, big_kernel<Q, FOUR, kGate>,
                            dim3(grid.x * grid.y * grid.z), 512, s, g);
 }

@@ -18,6 +18,8 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SRC = os.path.join(ROOT, "tests", "planner", "ffn_harness.cpp")
 NAMES = ["rows16", "tile32", "tile64", "tile128", "mid16", "mid32", "mid48", "mid64", "mid32wide", "mid64wide", "mid64cols", "mid64long",
          "big128", "big256"]
+SIZES = dict(zip(NAMES, [(16, 32), (32, 128), (64, 128), (128, 128), (16, 64), (32, 64), (48, 64), (64, 64), (32, 256), (64, 256), (64, 128),
+                         (64, 128), (128, 256), (256, 256)]))
 BF16 = {"rows16", "tile32", "tile64", "tile128", "big128", "big256"}
 FOUR = set(NAMES) - {"tile32", "tile64", "tile128"}
 
@@ -54,6 +56,12 @@ def plans(exe, calls):
 def check(call, launches):
     what, rows, k, n, f32 = call
     assert all(x["fits"] for x in launches), (call, launches)
+    for x in launches:  # a grid has fewer than 2^32 threads along x; 2^16 along y, z
+        bm, bn = SIZES[NAMES[x["variant"]]]
+        m, c = -(-x["M"] // bm), -(-x["N"] // (bn // 2 if x["gate"] else bn))
+        assert m * c * 512 < 1 << 32 and x["splits"] < 1 << 16 and (x["variant"] > 0 or m < 1 << 16)
+        if x["splits"] > 1:
+            assert m * c <= 1024 and m * c * x["splits"] * bm * bn * 4 <= 64 << 20
     products = [(n, k, 1, 0)] if what == 0 else [(n, k, 1, 1), (k, n, 3 if f32 else 1, 0)]
     for N, K, planes, gate in products:
         mine = [x for x in launches if (x["N"], x["K"], x["planes"], x["gate"]) == (N, K, planes, gate)]
@@ -75,7 +83,7 @@ def every_use():
 def test_calls_over_the_whole_range(harness):
     rng = random.Random(5)
     log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))  # noqa: E731
-    calls = [(0, 1, 32, 8, 0), (1, 1, 8, 8, 1), (2, 1 << 20, 32, 32, 0), (0, 1 << 28, 32, 8, 0), (0, 1, 1 << 24, 1 << 24, 1), (1, 70000, 8, 102400, 0)]
+    calls = [(0, 1, 32, 8, 0), (1, 1, 8, 8, 1), (2, 1 << 20, 32, 32, 0), (0, 1 << 28, 32, 8, 0), (0, 1 << 28, 64, 8, 0), (2, 1 << 28, 64, 32, 1), (0, 1, 1 << 24, 1 << 24, 1), (1, 70000, 8, 102400, 0)]
     for _ in range(4000):
         what = rng.randrange(3)
         step = 8 if what == 1 else 32

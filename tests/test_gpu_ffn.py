@@ -1,4 +1,6 @@
 """The feed-forward operators against their definition in 64 bits (needs an MI355X)."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -101,6 +103,51 @@ def test_every_kernel(what, T, k, n, f32):
         mats = block(33, k, n, four)
         got, ref = ffn(x, mats, dtype), O.ffn(x[at].double().numpy(), *(m.values for m in mats), 3 if f32 else 1)
     assert_within(got[at], *ref, dtype, f"{what} {T} x {k} x {n}")
+
+
+@pytest.mark.parametrize("what,T,k,n,f32", EVERY_KERNEL)
+def test_rows_keep_to_themselves(what, T, k, n, f32):
+    """Rows that are not finite change no bit of the others, in every kernel."""
+    log(f"[gpu] rows apart {what} {T} {k} {n} {f32}")
+    dtype, four = (F32 if f32 else BF16), what != 1
+    x = rows(41, T, k)
+    bad = torch.from_numpy(np.unique(np.random.default_rng([T, k]).integers(0, T, 1 + T // 50)))
+    y = x.clone()
+    y[bad, 0], y[bad, k - 1] = math.nan, math.inf
+    if what == 0:
+        w = Matrix(42, n, k, True)
+        one, two = linear4(x, w, dtype), linear4(y, w, dtype)
+    else:
+        mats = block(43, k, n, four)
+        one, two = ffn(x, mats, dtype), ffn(y, mats, dtype)
+    assert np.isfinite(one).all() and np.isnan(two[bad]).all()
+    others = np.setdiff1d(np.arange(T), bad.numpy())
+    assert np.array_equal(one[others], two[others])
+
+
+@pytest.mark.parametrize("four", [False, True], ids=["bf16w", "mx4"])
+def test_calls_at_once(four):
+    """Calls on two streams, each with a workspace of its own, as often as they may meet."""
+    mats = block(44, 2048, 1376, four)
+    W, L = mla.FfnWeights(*(m.device() for m in mats)), Matrix(45, 1000, 2048, True).device()
+    xs = [rows(46, T, 2048).cuda() for T in (40, 130)]
+    spaces = [(mla.workspace_for_ffn(130, W), mla.workspace_for_linear4(130, L)) for _ in xs]
+
+    def both(i, stream=None):
+        outs = torch.empty((len(xs[i]), 2048), dtype=F32, device="cuda"), torch.empty((len(xs[i]), 1000), dtype=BF16, device="cuda")
+        mla.gated_ffn(xs[i], W, outs[0], spaces[i][0], stream=stream)
+        mla.linear4(xs[i], L, outs[1], spaces[i][1], stream=stream)
+        return outs
+
+    want = [both(0), both(1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(20):
+        for i in (0, 1):
+            got.append((i, both(i, streams[i])))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i, outs in got for a, b in zip(outs, want[i]))
 
 
 @pytest.mark.parametrize("four", [False, True], ids=["bf16w", "mx4"])
@@ -265,6 +312,56 @@ def test_offsets_beyond_32_bits():
     at = np.array([0, 1, 32_537, 65_073, 65_074, T - 257, T - 1])
     ref = O.linear(x[at].double().numpy(), w.values)
     assert_within(out[torch.from_numpy(at).cuda()].double().cpu().numpy(), *ref, BF16, "sampled rows")
+
+
+@pytest.mark.parametrize("T", [2, 40, 400])
+def test_weights4_beyond_32_bits(T):
+    """Codes of more than 2^32 bytes; the last output columns of them."""
+    k, n = 131_072, 66_000
+    log(f"[gpu] linear4 {T} x {k} -> {n}")
+    gen = torch.Generator(device="cuda").manual_seed(51)
+    W = mla.Weights4(torch.randint(0, 256, (n, k // 2), dtype=torch.uint8, device="cuda", generator=gen),
+                     torch.randint(118, 122, (n, k // 32), dtype=torch.uint8, device="cuda", generator=gen))
+    x = rows(52, T, k)
+    out = torch.empty((T, n), dtype=F32, device="cuda")
+    mla.linear4(x.cuda(), W, out, mla.workspace_for_linear4(T, W))
+    cols, at = torch.tensor([0, 1, 32_767, 32_768, 65_537, n - 2, n - 1]), np.unique([0, T // 2, T - 1])
+    values = O.mx4_values(W.codes[cols.cuda()].cpu().numpy(), W.scales[cols.cuda()].cpu().numpy())
+    got = out[:, cols.cuda()].double().cpu().numpy()[at]
+    assert_within(got, *O.linear(x[at].double().numpy(), values), F32, "sampled columns")
+
+
+@pytest.mark.parametrize("T", [2, 40, 400])
+def test_block_beyond_32_bits(T):
+    """bf16 weights of more than 2^32 bytes each: of the inner width only the last 64 count, the other rows of gate and
+    up are zero."""
+    hidden, inner, last = 32_768, 66_000, 64
+    log(f"[gpu] ffn {T} x {hidden} x {inner}")
+    mats = block(53, hidden, last, False)
+    gate, up = (torch.zeros((inner, hidden), dtype=BF16, device="cuda") for _ in range(2))
+    gate[-last:], up[-last:] = mats[0].w.cuda(), mats[1].w.cuda()
+    down = torch.ones((hidden, inner), dtype=BF16, device="cuda")
+    down[:, -last:] = mats[2].w.cuda()
+    W = mla.FfnWeights(gate, up, down)
+    x = rows(54, T, hidden)
+    out = torch.empty((T, hidden), dtype=F32, device="cuda")
+    mla.gated_ffn(x.cuda(), W, out, mla.workspace_for_ffn(T, W))
+    at = np.unique([0, T // 2, T - 1])
+    assert_within(out.double().cpu().numpy()[at], *O.ffn(x[at].double().numpy(), *(m.values for m in mats), 3), F32, "sampled rows")
+
+
+def test_rows_beyond_32_bits():
+    """x of more than 2^32 bytes, and more rows than a launch counts in 16-row tiles along one of its axes."""
+    T, k, n = 1_100_000, 2048, 32
+    log(f"[gpu] linear4 {T} x {k} -> {n}")
+    gen = torch.Generator(device="cuda").manual_seed(55)
+    x = torch.randn((T, k), device="cuda", generator=gen, dtype=BF16)
+    w = Matrix(56, n, k, True)
+    W = w.device()
+    out = torch.empty((T, n), dtype=F32, device="cuda")
+    mla.linear4(x, W, out, mla.workspace_for_linear4(T, W))
+    at = torch.tensor([0, 1, 1_048_575, 1_048_576, T - 2, T - 1], device="cuda")
+    assert_within(out[at].double().cpu().numpy(), *O.linear(x[at].double().cpu().numpy(), w.values), F32, "sampled rows")
 
 
 def test_rows_and_weights_at_other_alignments():
