@@ -96,12 +96,17 @@ constexpr Cost kCost4[ffn::kVariants] = {
     {5.f, 1.04f, 1.04f, 1, 1}, {8.f, 1.45f, 1.45f, 1, 1},
 };
 
+// The kernels that take three planes of x together (9 more products).
+constexpr Cost kCostBf16x3[] = {{3.f, 2.f, 2.f, 1, 8}, {5.f, .86f, .53f, 2, 1}, {5.f, .8f, .8f, 1, 1}, {6.f, 1.4f, 1.4f, 1, 1}};
+constexpr Cost kCost4x3[] = {{3.f, 1.55f, 1.55f, 1, 8}, {}, {}, {}};
+
 float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::Shape &t, int ncu) {
-    const Cost &c = (four ? kCost4 : kCostBf16)[t.variant];
+    const bool together = g.a_planes == 3 && ffn::planes_together(t.variant);
+    const Cost &c = together ? (four ? kCost4x3 : kCostBf16x3)[t.variant] : (four ? kCost4 : kCostBf16)[t.variant];
     const ffn::VariantSize &v = ffn::kSizes[t.variant];
     const ffn::Tiles n = ffn::tiles_of(g, epi, t.variant);
     const double tiles = (double)(n.m * n.n);
-    const double chain = std::ceil(std::ceil(g.K / 64.0) * g.a_planes / t.splits / c.groups), load = tiles * t.splits / ncu;
+    const double chain = std::ceil(std::ceil(g.K / 64.0) * (together ? 1 : g.a_planes) / t.splits / c.groups), load = tiles * t.splits / ncu;
     const double part = 4.0 * v.bm * v.bn, joined = t.splits > 1 ? 2.0 + t.splits * part / 6e4 + tiles * t.splits * part / 2.5e6 : 0.0;
     // workgroups a CU has at once, and how many times (past one and a half rounds they no longer end together)
     const double once = std::min<double>(c.resident, std::ceil(load)), rounds = load > 1.5 * c.resident && c.resident > 1 ? load / c.resident : std::ceil(load / once);

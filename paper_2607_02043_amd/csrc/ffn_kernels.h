@@ -75,11 +75,16 @@ inline Tiles tiles_of(const GemmArgs &g, Epilogue epi, Variant v) {
     const int cols = epi == kGate ? kSizes[v].bn / 2 : kSizes[v].bn;
     return {((long long)g.M + kSizes[v].bm - 1) / kSizes[v].bm, ((long long)g.N + cols - 1) / cols};
 }
+// Whether a kernel takes the planes of x together, each weight read once; else one after the other, as a longer K.
+inline bool planes_together(Variant v) { return v <= kTile128; }
 // Whether the launch is one that the kernels take.
 constexpr long long kMaxTiles = (1 << 23) - 1;  // (of up to 512 threads: a grid has fewer than 2^32)
 inline bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t) {
     if (t.variant < 0 || t.variant >= kVariants || !(four_bit ? kSizes[t.variant].four : kSizes[t.variant].bf16)) return false;
-    if (g.M < 1 || g.N < 8 || g.N % 8 != 0 || g.K < 1 || g.K % (four_bit ? kMxGroup : 8) != 0 || g.a_planes < 1 || t.splits < 1) return false;
+    if (g.M < 1 || g.N < 8 || g.N % 8 != 0 || g.K < 1 || g.K % (four_bit ? kMxGroup : 8) != 0 || t.splits < 1) return false;
+    // three planes in front of fp32, with bf16 weights always
+    if (g.a_planes != 1 && (g.a_planes != 3 || epi != kStoreF32)) return false;
+    if (!four_bit && epi == kStoreF32 && g.a_planes != 3) return false;
     const Tiles n = tiles_of(g, epi, t.variant);
     if (n.m * n.n > kMaxTiles || (t.variant == kRows16 && n.m > 0xffff)) return false;
     const int stages = (g.K + kBK - 1) / kBK;
@@ -87,7 +92,7 @@ inline bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t)
     if (big && stages < 2) return false;
     if (t.splits == 1) return true;
     // no part is empty: the kernels for many rows count in units of stages, the others in stages or in slices of up to four
-    const long long pieces = (long long)(big ? (stages < kUnitStages ? 1 : stages / kUnitStages) : (stages + 3) / 4) * g.a_planes;
+    const long long pieces = (long long)(big ? (stages < kUnitStages ? 1 : stages / kUnitStages) : (stages + 3) / 4) * (planes_together(t.variant) ? 1 : g.a_planes);
     return n.m * n.n <= kMaxSplitTiles && t.splits <= pieces &&
            (size_t)(n.m * n.n) * t.splits * kSizes[t.variant].bm * kSizes[t.variant].bn * 4 <= kPartBytes;
 }

@@ -258,15 +258,15 @@ __device__ __forceinline__ void store_h4(const GemmArgs &g, f32x4 gate, f32x4 up
 // share K in slices of 128, a slice ahead in registers, and meet in LDS.  Within a
 // slice a lane holds 32 neighbouring k of its row (lane / 16 picks which), 64 bytes in
 // bf16 or 16 in 4 bits under one scale; the products' order of k is that of both
-// operands, so nothing is moved.  gridDim.z cuts K further where the columns are too
-// few for the chip.
-template <int MB, int CB, bool FOUR, int EPI>
+// operands, so nothing is moved.  The P planes of x meet a weight where it is loaded.
+// gridDim.z cuts K further where the columns are too few for the chip.
+template <int MB, int CB, bool FOUR, int EPI, int P>
 __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
     constexpr int NB = FOUR ? 1 : 4, JB = EPI == kGate ? CB / 2 : CB, UNITS = MB * JB;
     __shared__ f32x4 red[4][MB * CB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
     const int n0 = blockIdx.x * 16 * JB, m0 = blockIdx.y * 16 * MB;
-    const int ns = (g.K + 127) >> 7, total = ns * g.a_planes, step = 8 * g.splits;
+    const int total = (g.K + 127) >> 7, step = 8 * g.splits;
     const size_t plane = (size_t)g.plane_rows * g.K;
 
     const uint16_t *arow[MB], *brow[CB];
@@ -288,12 +288,12 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
     // take 64 neighbouring bytes at a time
     const auto at_k = [&](int k0, int i) { return k0 + (FOUR ? 32 * grp + 8 * i : 32 * i + 8 * grp); };
     struct Slice {
-        u32x4 b[CB][NB], a[MB][4];
+        u32x4 b[CB][NB], a[P][MB][4];
         uint32_t scale[CB];
     };
     // chunks behind the last k are read from the row's start, and dropped in use()
     const auto load = [&](Slice &s, int j) {
-        const int p = j / ns, k0 = (j - p * ns) * 128;
+        const int k0 = j * 128;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             if constexpr (FOUR) {
@@ -306,9 +306,11 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
             }
         }
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.a[mb][i] = *reinterpret_cast<const u32x4 *>(arow[mb] + p * plane + (at_k(k0, i) < g.K ? at_k(k0, i) : 0));
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s.a[p][mb][i] = *reinterpret_cast<const u32x4 *>(arow[mb] + p * plane + (at_k(k0, i) < g.K ? at_k(k0, i) : 0));
     };
     f32x4 acc[MB][CB];
 #pragma unroll
@@ -316,14 +318,14 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) acc[mb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
     const auto use = [&](Slice &s, int j) {
-        const int k0 = j % ns * 128;
+        const int k0 = j * 128;
         if (k0 + 128 > g.K) {
             const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool in = at_k(k0, i) < g.K;
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) s.a[mb][i] = in ? s.a[mb][i] : zero;
+                for (int b = 0; b < P * MB; ++b) s.a[b / MB][b % MB][i] = in ? s.a[b / MB][b % MB][i] : zero;
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) {
                     if constexpr (!FOUR) s.b[cb][i] = in ? s.b[cb][i] : zero;
@@ -342,7 +344,7 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
                 if constexpr (FOUR) b = mx_values(s.b[cb][0][i], mx_scale(s.scale[cb]));
                 else b = s.b[cb][i];
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) acc[mb][cb] = mfma(b, s.a[mb][i], acc[mb][cb]);
+                for (int m = 0; m < P * MB; ++m) acc[m % MB][cb] = mfma(b, s.a[m / MB][m % MB][i], acc[m % MB][cb]);
             }
         }
     };
@@ -577,16 +579,17 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
 }
 
 // A middling number of rows, bf16 weights: a BM x BN tile on WR x WC waves, K in stages of
-// 64 through a ring of D LDS stages that direct global -> LDS loads fill ahead.  A stage's
+// 64 through a ring of D LDS stages that direct global -> LDS loads fill ahead; all P planes of
+// x are in a stage, so the weights are loaded once.  A stage's
 // operands are read while the products of the one before run, so that one barrier a stage
 // is all that the waves wait for together: behind it a stage has landed for all of them
 // and the slot of the one before is free.  With kGate the BN weight rows are, for each
 // column of waves, 32 rows of the gate and the same 32 of the up projection, so that a lane
 // ends up with both products of its columns.
-template <int BM, int BN, int D, int WR, int WC, int EPI>
+template <int BM, int BN, int D, int WR, int WC, int EPI, int P>
 __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
-    constexpr int NW = WR * WC;
-    constexpr int STAGE = (BM + BN) * 8;                      // 16-byte slots per stage
+    constexpr int NW = WR * WC, AR = P * BM;
+    constexpr int STAGE = (AR + BN) * 8;                      // 16-byte slots per stage
     constexpr int NPW = STAGE / 64 / NW;                      // loads per wave per stage
     constexpr int WM = BM / WR, MB = WM / 16, WN = BN / WC, NB = WN / 16;
     static_assert(STAGE % (64 * NW) == 0 && WN == 64 && MB >= 1 && NB == 4 && D >= 2, "shape");
@@ -597,7 +600,7 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
     int mt, nt;
     tile_at(xcd_run(blockIdx.x, gridDim.x), (g.M + BM - 1) / BM, (g.N + COLS - 1) / COLS, &mt, &nt);
     const int m0 = __builtin_amdgcn_readfirstlane(mt * BM), n0 = __builtin_amdgcn_readfirstlane(nt * COLS);
-    const int nk = (g.K + kBK - 1) / kBK, all = nk * g.a_planes;
+    const int all = (g.K + kBK - 1) / kBK;
     const int first = (int)((long long)all * blockIdx.z / g.splits), stages = (int)((long long)all * (blockIdx.z + 1) / g.splits) - first;
 
     // The wave's i-th load fills 8 neighbouring rows of x or the weights: the first one is wave-uniform.  Rows past the end
@@ -608,58 +611,53 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
 #pragma unroll
     for (int i = 0; i < NPW; ++i) {
         const int at = 8 * (wave * NPW + i), row = at + (lane >> 3);
-        kin[i] = ((lane & 7) ^ (at < BM ? swz_a(row) : swz_b(row))) * 8;
-        if (at < BM) {
-            const int r = min(m0 + at, g.M - 1);
-            base[i] = uniform(reinterpret_cast<const char *>(g.a + (size_t)r * g.K));
+        kin[i] = ((lane & 7) ^ (at < AR ? swz_a(row) : swz_b(row - AR))) * 8;
+        if (at < AR) {
+            const int r = min(m0 + at % BM, g.M - 1);
+            base[i] = uniform(reinterpret_cast<const char *>(g.a + ((size_t)(at / BM) * g.plane_rows + r) * g.K));
             off[i] = (uint32_t)min(lane >> 3, g.M - 1 - r) * (uint32_t)g.K * 2u + (uint32_t)kin[i] * 2u;
         } else {
-            const int rb = at - BM, n = min(n0 + (EPI == kGate ? (rb >> 6) * 32 + (rb & 31) : rb), g.N - 8);
+            const int rb = at - AR, n = min(n0 + (EPI == kGate ? (rb >> 6) * 32 + (rb & 31) : rb), g.N - 8);
             base[i] = uniform(reinterpret_cast<const char *>((EPI == kGate && (rb & 32) ? g.up.w : g.b.w) + (size_t)n * g.K));
             off[i] = (uint32_t)(lane >> 3) * (uint32_t)g.K * 2u + (uint32_t)kin[i] * 2u;
         }
     }
     const uint32_t ring_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring)) + wave * NPW * 1024;
-    const size_t plane = (size_t)g.plane_rows * g.K * 2;
-    int p = first / nk, k0 = (first - p * nk) * kBK, slot_in = 0;  // of the stage to load next
+    int k0 = first * kBK, slot_in = 0;  // of the stage to load next
     const auto issue = [&] {
         const uint32_t dst = ring_lds + (uint32_t)(slot_in * STAGE * 16);
         const bool whole = k0 + kBK <= g.K;
 #pragma unroll
         for (int i = 0; i < NPW; ++i) {
-            const char *const from = base[i] + (size_t)k0 * 2 + (8 * (wave * NPW + i) < BM ? p * plane : 0);
+            const char *const from = base[i] + (size_t)k0 * 2;
             if (whole) dma16_at(off[i], from, dst + i * 1024);
             else dma16(k0 + kin[i] < g.K ? from + off[i] : reinterpret_cast<const char *>(&kZeros), dst + i * 1024);
         }
         slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
         k0 += kBK;
-        if (k0 >= g.K) {
-            k0 = 0;
-            ++p;
-        }
     };
     f32x4 acc[MB][NB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int wr = (wave / WC) * WM, wc = BM + (wave % WC) * WN;
+    const int wr = (wave / WC) * WM, wc = (wave % WC) * WN;
     struct Operands {
-        u32x4 a[2][MB], b[2][NB];
+        u32x4 a[2][P * MB], b[2][NB];
     };
     int at_a[2], at_b[2];  // this lane's slots in a stage for the two steps of 32 k
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int kc = s * 4 + (lane >> 4), ra = wr + (lane & 15), rb = wc + pair_column(lane, 0);
         at_a[s] = ra * 8 + (kc ^ swz_a(ra));
-        at_b[s] = rb * 8 + (kc ^ swz_b(rb));
+        at_b[s] = (AR + rb) * 8 + (kc ^ swz_b(rb));
     }
     const auto read = [&](Operands &o, int slot) {
         const u32x4 *const cur = ring + slot * STAGE;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) o.a[s][mb] = cur[at_a[s] + mb * 128];
+            for (int m = 0; m < P * MB; ++m) o.a[s][m] = cur[at_a[s] + (m / MB * BM + m % MB * 16) * 8];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) o.b[s][nb] = cur[at_b[s] + pair_column(0, nb) * 8];  // (rows 4 and 32 on: same swizzle)
         }
@@ -668,9 +666,9 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
+            for (int m = 0; m < P * MB; ++m)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma(o.b[s][nb], o.a[s][mb], acc[mb][nb]);
+                for (int nb = 0; nb < NB; ++nb) acc[m % MB][nb] = mfma(o.b[s][nb], o.a[s][m], acc[m % MB][nb]);
     };
 #pragma unroll
     for (int st = 0; st < D; ++st)
@@ -1035,10 +1033,10 @@ hipError_t launch_mid(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s)
     return launch_epilogue(epi, mid_kernel<MB, CB, WC, KG, SL, kStoreBf16>, mid_kernel<MB, CB, WC, KG, SL, kStoreF32>, mid_kernel<MB, CB, WC, KG, SL, kGate>,
                            dim3(grid.x * grid.y, 1, grid.z), 64 * WC * KG, s, g);
 }
-template <int BM, int D, int WR = 2>
+template <int BM, int D, int D3, int WR>
 hipError_t launch_tile(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
-    return launch_epilogue(epi, tile_kernel<BM, 128, D, WR, 2, kStoreBf16>, tile_kernel<BM, 128, D, WR, 2, kStoreF32>,
-                           tile_kernel<BM, 128, D, WR, 2, kGate>, dim3(grid.x * grid.y, 1, grid.z), 128 * WR, s, g);
+    return launch_epilogue(epi, tile_kernel<BM, 128, D, WR, 2, kStoreBf16, 1>, tile_kernel<BM, 128, D3, WR, 2, kStoreF32, 3>,
+                           tile_kernel<BM, 128, D, WR, 2, kGate, 1>, dim3(grid.x * grid.y, 1, grid.z), 128 * WR, s, g);
 }
 template <int Q, bool FOUR>
 hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {  // the tiles of every part, those of a part behind each other
@@ -1047,7 +1045,9 @@ hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s)
 }
 template <bool FOUR>
 hipError_t launch_rows(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
-    return launch_epilogue(epi, rows_kernel<1, 2, FOUR, kStoreBf16>, rows_kernel<1, 2, FOUR, kStoreF32>, rows_kernel<1, 2, FOUR, kGate>, grid, 512, s, g);
+    constexpr int kAlone = FOUR ? 1 : 3;  // planes in front of fp32: a product on its own has one (and 4-bit weights)
+    return launch_epilogue(epi, rows_kernel<1, 2, FOUR, kStoreBf16, 1>, g.a_planes == 3 ? rows_kernel<1, 2, FOUR, kStoreF32, 3> : rows_kernel<1, 2, FOUR, kStoreF32, kAlone>,
+                           rows_kernel<1, 2, FOUR, kGate, 1>, grid, 512, s, g);
 }
 
 }  // namespace
@@ -1059,9 +1059,9 @@ hipError_t launch_gemm(GemmArgs g, bool four_bit, Epilogue epi, const Shape &t, 
     const dim3 grid((unsigned)n.n, (unsigned)n.m, (unsigned)t.splits);
     switch (t.variant) {
         case kRows16: return four_bit ? launch_rows<true>(g, epi, grid, s) : launch_rows<false>(g, epi, grid, s);
-        case kTile32: return launch_tile<32, 4>(g, epi, grid, s);
-        case kTile64: return launch_tile<64, 3, 4>(g, epi, grid, s);
-        case kTile128: return launch_tile<128, 4, 4>(g, epi, grid, s);
+        case kTile32: return launch_tile<32, 4, 2, 2>(g, epi, grid, s);
+        case kTile64: return launch_tile<64, 3, 3, 4>(g, epi, grid, s);
+        case kTile128: return launch_tile<128, 4, 2, 4>(g, epi, grid, s);
         case kMid16: return launch_mid<1, 2, 2, 4, 2>(g, epi, grid, s);
         case kMid32: return launch_mid<2, 2, 2, 4, 1>(g, epi, grid, s);
         case kMid48: return launch_mid<3, 2, 2, 4, 1>(g, epi, grid, s);

@@ -85,6 +85,8 @@ EVERY_KERNEL = [
     (2, 4101, 3424, 256, 0), (2, 4187, 96, 32, 1), (2, 4213, 2112, 32, 1), (2, 4234, 32, 1088, 1), (2, 4255, 96, 864, 1),
     (2, 4313, 160, 96, 0), (2, 4473, 160, 32, 1),
     (0, 21, 2944, 16752, 0), (2, 19, 8704, 3264, 1), (2, 21, 2080, 8704, 0),
+    (1, 2378, 40, 520, 1), (1, 3265, 1240, 72, 1), (1, 4387, 408, 3456, 1), (2, 2125, 64, 672, 1), (1, 4310, 8, 1040, 1),
+    (1, 3791, 1224, 2000, 1), (1, 4180, 16, 10728, 1),
 ]
 
 
