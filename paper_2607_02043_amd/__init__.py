@@ -644,33 +644,54 @@ class FfnWeights:
         return mla_ffn_weights(*(w.data_ptr() for w in self._weights), self.hidden, self.inner)
 
 
-def _ffn_args(x, weights, width_in, width_out, out, workspace):
-    import torch
+_ffn_modes = None  # {type of an output: its mode}
+
+
+def _ffn_args(x, weights, width_in, width_out, out, workspace, stream):
+    """The call's arguments before and behind the sizes.  What is right passes in a few comparisons (a product of one row
+    takes 4 us on the device); the checks that name what is wrong run only where something is."""
+    global _ffn_modes
+    if _ffn_modes is None:
+        import torch
+        _ffn_modes = {torch.float32: MLA_OUT_F32, **{t: MLA_OUT_BF16 for t in _bf16()}}
     here = _here()
+    mode, shape, to = _ffn_modes.get(out.dtype), x.shape, out.shape
+    if not (mode is not None and len(shape) == 2 == len(to) and shape[1] == width_in and to[1] == width_out and shape[0] == to[0]
+            and _ffn_modes.get(x.dtype) == MLA_OUT_BF16 and x.is_contiguous() and out.is_contiguous()
+            and x.get_device() == out.get_device() == weights.device_index == here
+            and (workspace is None or (workspace.get_device() == here and workspace.is_contiguous()))):
+        _ffn_refuse(x, weights, width_in, width_out, out, workspace, here)
+    stream = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
+    return ((shape[0], x.data_ptr(), ctypes.byref(weights.c)),
+            (out.data_ptr(), mode, *((0, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)), stream))
+
+
+def _ffn_refuse(x, weights, width_in, width_out, out, workspace, here):
+    import torch
     if weights.device_index != here:
         raise ValueError("the weights are not on the current CUDA device")
     if x.dim() != 2:
         raise ValueError(f"x must be [T][{width_in}]")
-    T = int(x.shape[0])
+    _dev(x, "x", (int(x.shape[0]), width_in), _bf16(), here)
     if workspace is not None:
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
         _on_device(workspace, "workspace", here)
-    return ((T, _dev(x, "x", (T, width_in), _bf16(), here), ctypes.byref(weights.c)),
-            (_dev(out, "out", (T, width_out), (torch.float32, *_bf16()), here), _out_mode(out), _ptr(workspace), _nbytes(workspace)))
+    _dev(out, "out", (int(x.shape[0]), width_out), (torch.float32, *_bf16()), here)
+    raise ValueError("x, out or workspace is not what the call takes")
 
 
 def linear4(x, weights: Weights4, out, workspace, stream=None) -> None:
     """out = x W^T with 4-bit weights: x bf16 [T][K], out [T][N] float32 or bf16 (dtype picks the mode)."""
-    a, b = _ffn_args(x, weights, weights.in_features, weights.out_features, out, workspace)
-    _check(lib().mla_linear4(*a, weights.in_features, weights.out_features, *b, _stream(stream)))
+    a, b = _ffn_args(x, weights, weights.in_features, weights.out_features, out, workspace, stream)
+    _check(lib().mla_linear4(*a, weights.in_features, weights.out_features, *b))
 
 
 def gated_ffn(x, weights: FfnWeights, out, workspace, stream=None) -> None:
     """out = (silu(x gate^T) * (x up^T)) down^T: x bf16 [T][hidden], out [T][hidden] float32 or bf16 (dtype picks the mode)."""
-    a, b = _ffn_args(x, weights, weights.hidden, weights.hidden, out, workspace)
+    a, b = _ffn_args(x, weights, weights.hidden, weights.hidden, out, workspace, stream)
     call = lib().mla_gated_ffn4 if weights.four_bit else lib().mla_gated_ffn
-    _check(call(*a, *b, _stream(stream)))
+    _check(call(*a, *b))
 
 
 def _ffn_workspace(n, num_rows, what, device):

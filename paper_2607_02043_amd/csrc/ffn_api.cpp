@@ -72,23 +72,23 @@ int cu_count() {
     return ncu;
 }
 
-// What a launch takes, in us: sweeps of every kernel and number of parts over 45 products of 1 to 4160 rows (an
+// What a launch takes, in us: sweeps of the kernels and numbers of parts over 180 products of 1 to 4160 rows (an
 // MI355X, weights from memory).  A workgroup walks its stages of 64 k (1 / groups of them) at `stage` us each; where
 // `resident` workgroups of a CU run at once, a stage takes `share` us for each of them, and rounds of them follow
 // each other.  Parts are stored at 2.5 TB/s by all, and read by the workgroup that joins a tile's at 60 GB/s.  The
-// rule's choice is within 12 % of the best for each of the 45.
+// rule's choice is within 12 % of the best for each product, and 0.5 % off it in the mean.
 struct Cost {
     float fixed, stage, share;
     int resident, groups;
 };
 constexpr Cost kCostBf16[ffn::kVariants] = {
-    {3.f, 1.4f, 1.7f, 4, 8},
-    {3.5f, .5f, .5f, 2, 1}, {3.5f, .57f, .48f, 2, 1}, {3.5f, .75f, .8f, 1, 1},
+    {3.f, 1.4f, 1.7f, 4, 8}, {2.3f, 1.f, .94f, 3, 8},
+    {3.5f, .5f, .5f, 2, 1}, {4.5f, .48f, .4f, 2, 1}, {4.5f, .65f, .65f, 1, 1},
     {}, {}, {}, {}, {}, {}, {}, {},
     {5.f, 1.f, 1.f, 1, 1}, {7.f, 1.32f, 1.32f, 1, 1},
 };
 constexpr Cost kCost4[ffn::kVariants] = {
-    {3.f, .62f, .9f, 4, 8},
+    {3.f, .77f, 1.f, 4, 8}, {2.3f, .68f, .72f, 4, 8},
     {}, {}, {},
     {3.f, .7f, .6f, 4, 4}, {3.f, .9f, .85f, 4, 4}, {3.f, 1.15f, 1.2f, 2, 4}, {3.f, 1.25f, 1.3f, 1, 4},
     {3.f, .7f, .57f, 2, 1}, {3.f, .9f, .6f, 2, 1}, {3.f, .6f, .3f, 2, 1},
@@ -96,9 +96,9 @@ constexpr Cost kCost4[ffn::kVariants] = {
     {5.f, 1.04f, 1.04f, 1, 1}, {8.f, 1.45f, 1.45f, 1, 1},
 };
 
-// The kernels that take three planes of x together (9 more products).
-constexpr Cost kCostBf16x3[] = {{3.f, 2.f, 2.f, 1, 8}, {5.f, .86f, .53f, 2, 1}, {5.f, .8f, .8f, 1, 1}, {6.f, 1.4f, 1.4f, 1, 1}};
-constexpr Cost kCost4x3[] = {{3.f, 1.55f, 1.55f, 1, 8}, {}, {}, {}};
+// The kernels that take three planes of x together.
+constexpr Cost kCostBf16x3[] = {{3.f, 2.f, 2.f, 1, 8}, {2.3f, 1.75f, 1.75f, 1, 8}, {5.f, .86f, .53f, 2, 1}, {5.f, .8f, .8f, 1, 1}, {6.f, 1.4f, 1.4f, 1, 1}};
+constexpr Cost kCost4x3[] = {{3.f, 1.5f, 1.5f, 1, 8}, {2.3f, 1.3f, 1.3f, 1, 8}, {}, {}, {}};
 
 float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::Shape &t, int ncu) {
     const bool together = g.a_planes == 3 && ffn::planes_together(t.variant);
@@ -111,11 +111,11 @@ float cost_of(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, const ffn::S
     // workgroups a CU has at once, and how many times (past one and a half rounds they no longer end together)
     const double once = std::min<double>(c.resident, std::ceil(load)), rounds = load > 1.5 * c.resident && c.resident > 1 ? load / c.resident : std::ceil(load / once);
     // (the few-row kernel reads each row of x for itself: a single one costs it less)
-    const double rows = t.variant == ffn::kRows16 ? .7 + .3 * std::min(g.M, 16) / 16 : 1.0;
+    const double rows = t.variant > ffn::kRows16Narrow ? 1.0 : four ? .55 + .45 * std::min(g.M, 16) / 16 : .7 + .3 * std::min(g.M, 16) / 16;
     const double walk = rounds * (c.fixed + chain * rows * (once > 1 ? std::max<double>(c.stage, once * c.share) : c.stage)) + joined;
-    // what the weights take to arrive: 4.3 TB/s in bf16, in 4 bits 3.4 where wave groups share K and 2.7 where they do not
+    // what the weights take to arrive: 5 TB/s in bf16, in 4 bits 3.4 where wave groups share K and 2.7 where they do not
     const double bytes = (epi == ffn::kGate ? 2.0 : 1.0) * g.N * (double)g.K * (four ? .53 : 2.0);
-    return (float)std::max(walk, bytes / (!four ? 4.3e6 : c.groups >= 4 ? 3.4e6 : 2.7e6) + c.fixed);
+    return (float)std::max(walk, bytes / (!four ? 5e6 : c.groups >= 4 ? 3.4e6 : 2.7e6) + c.fixed);
 }
 
 struct Plan {

@@ -39,7 +39,7 @@ struct GemmArgs {
 
 // The kernels: bm rows x bn weight rows a workgroup (kGate: bn / 2 columns of h).
 enum Variant : int {
-    kRows16,                                      // few rows, either kind of weights
+    kRows16, kRows16Narrow,                       // few rows, either kind of weights
     kTile32, kTile64, kTile128,                   // bf16 weights
     kMid16, kMid32, kMid48, kMid64,               // 4-bit weights, four wave groups on K
     kMid32Wide, kMid64Wide, kMid64Cols, kMid64Long,  // 4-bit weights, one or two
@@ -51,7 +51,7 @@ struct VariantSize {
     bool bf16, four;
 };
 constexpr VariantSize kSizes[kVariants] = {
-    {16, 32, true, true},
+    {16, 32, true, true}, {16, 16, true, true},
     {32, 128, true, false}, {64, 128, true, false}, {128, 128, true, false},
     {16, 64, false, true}, {32, 64, false, true}, {48, 64, false, true}, {64, 64, false, true},
     {32, 256, false, true}, {64, 256, false, true}, {64, 128, false, true}, {64, 128, false, true},
@@ -86,7 +86,7 @@ inline bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t)
     if (g.a_planes != 1 && (g.a_planes != 3 || epi != kStoreF32)) return false;
     if (!four_bit && epi == kStoreF32 && g.a_planes != 3) return false;
     const Tiles n = tiles_of(g, epi, t.variant);
-    if (n.m * n.n > kMaxTiles || (t.variant == kRows16 && n.m > 0xffff)) return false;
+    if (n.m * n.n > kMaxTiles || (t.variant <= kRows16Narrow && n.m > 0xffff)) return false;
     const int stages = (g.K + kBK - 1) / kBK;
     const bool big = t.variant == kBig128 || t.variant == kBig256;
     if (big && stages < 2) return false;

@@ -254,18 +254,23 @@ __device__ __forceinline__ void store_h4(const GemmArgs &g, f32x4 gate, f32x4 up
 
 // Few rows: the call is bound by reading the weights once, so they go straight from
 // memory to registers.  A workgroup takes 16 MB rows and CB blocks of 16 weight rows
-// (kGate: the first half gate, the second the same columns of up); its eight waves
-// share K in slices of 128, a slice ahead in registers, and meet in LDS.  Within a
-// slice a lane holds 32 neighbouring k of its row (lane / 16 picks which), 64 bytes in
-// bf16 or 16 in 4 bits under one scale; the products' order of k is that of both
-// operands, so nothing is moved.  The P planes of x meet a weight where it is loaded.
-// gridDim.z cuts K further where the columns are too few for the chip.
+// (kGate: the first half gate, the second the same columns of up; half and half of a
+// single block); its eight waves share K in slices of 128, a slice ahead in registers,
+// and meet in LDS.  Within a slice a lane holds 32 neighbouring k of its row (lane / 16
+// picks which), 64 bytes in bf16 or 16 in 4 bits under one scale; the products' order of
+// k is that of both operands, so nothing is moved.  The P planes of x meet a weight where
+// it is loaded.  gridDim.z cuts K further where the columns are too few for the chip.
+//   One block a workgroup is twice as many of them: 2048 x 2048 in 4 bits, one row 4.9 ->
+// 3.9 us (2.4 an empty launch), gate and up of 4 x 1408 in bf16 7.3 -> 5.7 (2.0 TB/s);
+// two read x half as often: 16 rows of 10944 columns in 4 bits 19.4 against 14.4.  Of many
+// columns they read 4.3 to 4.9 TB/s in bf16 (K = 2048, 10944 columns of gate and up).
 template <int MB, int CB, bool FOUR, int EPI, int P>
 __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
-    constexpr int NB = FOUR ? 1 : 4, JB = EPI == kGate ? CB / 2 : CB, UNITS = MB * JB;
+    constexpr bool kHalves = EPI == kGate && CB == 1;  // rows 0 .. 7 of the block gate, 8 .. 15 the same columns of up
+    constexpr int NB = FOUR ? 1 : 4, JB = EPI == kGate && !kHalves ? CB / 2 : CB, UNITS = MB * JB, COLS = kHalves ? 8 : 16 * JB;
     __shared__ f32x4 red[4][MB * CB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
-    const int n0 = blockIdx.x * 16 * JB, m0 = blockIdx.y * 16 * MB;
+    const int n0 = blockIdx.x * COLS, m0 = blockIdx.y * 16 * MB;
     const int total = (g.K + 127) >> 7, step = 8 * g.splits;
     const size_t plane = (size_t)g.plane_rows * g.K;
 
@@ -275,8 +280,8 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
     for (int mb = 0; mb < MB; ++mb) arow[mb] = g.a + (size_t)min(m0 + 16 * mb + (lane & 15), g.M - 1) * g.K;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {  // columns past the end repeat the last one, never stored
-        const Weights &w = EPI == kGate && cb >= JB ? g.up : g.b;
-        const size_t n = min(n0 + 16 * (cb % JB) + (lane & 15), g.N - 1);
+        const Weights &w = (kHalves ? (lane & 8) != 0 : EPI == kGate && cb >= JB) ? g.up : g.b;
+        const size_t n = min(n0 + 16 * (cb % JB) + (lane & (kHalves ? 7 : 15)), g.N - 1);
         if constexpr (FOUR) {
             crow[cb] = w.codes + n * (g.K / 2);
             srow[cb] = w.scales + n * (g.K / kMxGroup);
@@ -388,7 +393,12 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
     for (int u = wave; u < UNITS; u += 8) {
         const int mb = u / JB, jb = u % JB, row = m0 + 16 * mb + (lane & 15), n = n0 + 16 * jb + 4 * grp;
         const f32x4 v = total_sum(mb * CB + jb);
-        if constexpr (EPI == kGate) {
+        if constexpr (kHalves) {
+            f32x4 up;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) up[i] = __shfl(v[i], lane ^ 32);
+            if (row < g.M && grp < 2) store_h4(g, v, up, row, n);
+        } else if constexpr (EPI == kGate) {
             const f32x4 up = total_sum(mb * CB + JB + jb);
             if (row < g.M && n < g.N) store_h4(g, v, up, row, n);
         } else {
@@ -1043,11 +1053,11 @@ hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s)
     return launch_epilogue(epi, big_kernel<Q, FOUR, kStoreBf16>, big_kernel<Q, FOUR, kStoreF32>, big_kernel<Q, FOUR, kGate>,
                            dim3(grid.x * grid.y * grid.z), 512, s, g);
 }
-template <bool FOUR>
+template <int CB, bool FOUR>
 hipError_t launch_rows(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
     constexpr int kAlone = FOUR ? 1 : 3;  // planes in front of fp32: a product on its own has one (and 4-bit weights)
-    return launch_epilogue(epi, rows_kernel<1, 2, FOUR, kStoreBf16, 1>, g.a_planes == 3 ? rows_kernel<1, 2, FOUR, kStoreF32, 3> : rows_kernel<1, 2, FOUR, kStoreF32, kAlone>,
-                           rows_kernel<1, 2, FOUR, kGate, 1>, grid, 512, s, g);
+    return launch_epilogue(epi, rows_kernel<1, CB, FOUR, kStoreBf16, 1>, g.a_planes == 3 ? rows_kernel<1, CB, FOUR, kStoreF32, 3> : rows_kernel<1, CB, FOUR, kStoreF32, kAlone>,
+                           rows_kernel<1, CB, FOUR, kGate, 1>, grid, 512, s, g);
 }
 
 }  // namespace
@@ -1058,7 +1068,8 @@ hipError_t launch_gemm(GemmArgs g, bool four_bit, Epilogue epi, const Shape &t, 
     g.splits = t.splits;
     const dim3 grid((unsigned)n.n, (unsigned)n.m, (unsigned)t.splits);
     switch (t.variant) {
-        case kRows16: return four_bit ? launch_rows<true>(g, epi, grid, s) : launch_rows<false>(g, epi, grid, s);
+        case kRows16: return four_bit ? launch_rows<2, true>(g, epi, grid, s) : launch_rows<2, false>(g, epi, grid, s);
+        case kRows16Narrow: return four_bit ? launch_rows<1, true>(g, epi, grid, s) : launch_rows<1, false>(g, epi, grid, s);
         case kTile32: return launch_tile<32, 4, 2, 2>(g, epi, grid, s);
         case kTile64: return launch_tile<64, 3, 3, 4>(g, epi, grid, s);
         case kTile128: return launch_tile<128, 4, 2, 4>(g, epi, grid, s);

@@ -16,11 +16,11 @@ import test_gpu_ffn as G
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SRC = os.path.join(ROOT, "tests", "planner", "ffn_harness.cpp")
-NAMES = ["rows16", "tile32", "tile64", "tile128", "mid16", "mid32", "mid48", "mid64", "mid32wide", "mid64wide", "mid64cols", "mid64long",
+NAMES = ["rows16", "rows16narrow", "tile32", "tile64", "tile128", "mid16", "mid32", "mid48", "mid64", "mid32wide", "mid64wide", "mid64cols", "mid64long",
          "big128", "big256"]
-SIZES = dict(zip(NAMES, [(16, 32), (32, 128), (64, 128), (128, 128), (16, 64), (32, 64), (48, 64), (64, 64), (32, 256), (64, 256), (64, 128),
+SIZES = dict(zip(NAMES, [(16, 32), (16, 16), (32, 128), (64, 128), (128, 128), (16, 64), (32, 64), (48, 64), (64, 64), (32, 256), (64, 256), (64, 128),
                          (64, 128), (128, 256), (256, 256)]))
-BF16 = {"rows16", "tile32", "tile64", "tile128", "big128", "big256"}
+BF16 = {"rows16", "rows16narrow", "tile32", "tile64", "tile128", "big128", "big256"}
 FOUR = set(NAMES) - {"tile32", "tile64", "tile128"}
 
 
@@ -59,7 +59,7 @@ def check(call, launches):
     for x in launches:  # a grid has fewer than 2^32 threads along x; 2^16 along y, z
         bm, bn = SIZES[NAMES[x["variant"]]]
         m, c = -(-x["M"] // bm), -(-x["N"] // (bn // 2 if x["gate"] else bn))
-        assert m * c * 512 < 1 << 32 and x["splits"] < 1 << 16 and (x["variant"] > 0 or m < 1 << 16)
+        assert m * c * 512 < 1 << 32 and x["splits"] < 1 << 16 and (x["variant"] > 1 or m < 1 << 16)
         if x["splits"] > 1:
             assert m * c <= 1024 and m * c * x["splits"] * bm * bn * 4 <= 64 << 20
     products = [(n, k, 1, 0)] if what == 0 else [(n, k, 1, 1), (k, n, 3 if f32 else 1, 0)]

@@ -87,6 +87,10 @@ EVERY_KERNEL = [
     (0, 21, 2944, 16752, 0), (2, 19, 8704, 3264, 1), (2, 21, 2080, 8704, 0),
     (1, 2378, 40, 520, 1), (1, 3265, 1240, 72, 1), (1, 4387, 408, 3456, 1), (2, 2125, 64, 672, 1), (1, 4310, 8, 1040, 1),
     (1, 3791, 1224, 2000, 1), (1, 4180, 16, 10728, 1),
+    (1, 1552, 64, 1344, 0), (1, 952, 64, 2376, 0), (0, 4180, 2080, 32, 0), (1, 1040, 24, 2680, 0), (1, 1636, 1088, 40, 0), (1, 1781, 72, 520, 1), (1, 2590, 1728, 4944, 0),
+    (1, 2785, 24, 528, 0), (1, 2954, 656, 4320, 0), (1, 4212, 160, 3048, 0), (1, 4256, 24, 2104, 0), (1, 4262, 24, 11160, 1),
+    (1, 4303, 4104, 208, 0), (1, 4355, 4560, 496, 0), (1, 4366, 8, 2264, 1), (1, 737, 3184, 16, 0), (2, 1037, 544, 32, 0),
+    (2, 369, 3136, 32, 1), (2, 56, 416, 2304, 1), (2, 677, 32, 3232, 0),
 ]
 
 
