@@ -449,6 +449,11 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
 #pragma unroll
     for (int i = 0; i < LPT; ++i) arow[i] = g.a + (size_t)min(m0 + min((gt + 64 * WC * i) / CH, 16 * MB - 1), g.M - 1) * g.K;
 
+    // Place of a row's chunk 4 SL q + i (the i-th that lanes of quarter q multiply), before the XOR with the row.  A read of 16
+    // bytes a lane is served 16 lanes at a time, rows 0 .. 3 and 12 .. 15 of one quarter with rows 4 .. 11 of the next: the
+    // quarters of such a pair differ in the lowest bit, so that the XOR leaves them apart (as their chunks lie in memory: 8
+    // cycles a read for 4).
+    const auto place = [](int q, int i) { return (q & 1) + 2 * i + 8 * SL * (q >> 1); };
     u32x4 areg[LPT];
     const auto load_a = [&](int j) {
         const int p = j / ns, k = (j - p * ns) * (128 * SL) + gt % CH * 8;
@@ -460,7 +465,7 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
 #pragma unroll
         for (int i = 0; i < LPT; ++i) {
             const int row = (gt + 64 * WC * i) / CH;
-            if (BUF % (64 * WC) == 0 || row < 16 * MB) to[row * CH + (gt % CH ^ (row & 15))] = in ? areg[i] : u32x4{0u, 0u, 0u, 0u};
+            if (BUF % (64 * WC) == 0 || row < 16 * MB) to[row * CH + (place(gt % CH / (4 * SL), gt % (4 * SL)) ^ (row & 15))] = in ? areg[i] : u32x4{0u, 0u, 0u, 0u};
         }
     };
     // a lane's SL groups of a slice are neighbours, as its codes are loaded; behind the last k they are read from the row's
@@ -506,7 +511,7 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
         for (int i = 0; i < 4 * SL; ++i) {
             u32x4 fa[MB];
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) fa[mb] = from[(16 * mb + l16) * CH + ((4 * SL * grp + i) ^ l16)];
+            for (int mb = 0; mb < MB; ++mb) fa[mb] = from[(16 * mb + l16) * CH + (place(grp, i) ^ l16)];
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
                 const u32x4 b = mx_values(s.codes[cb][i / 4][i % 4], mx_scale((s.scales[cb] >> (i / 4 * 8)) & 0xffu));
@@ -747,7 +752,7 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
 // last five refills, never for all.
 //   4-bit weights: B0 and B1 are one region of codes, refilled and read at B0's places.  A
 // lane's 16 codes of a stage are 16 neighbouring k under one scale, the operands of both
-// 32-k steps (the rows' chunks are read in that order); phases 0 and 1 make them bf16.  The
+// 32-k steps (the rows' chunks lie in that order); phases 0 and 1 make them bf16.  The
 // scales of up to kRunStages stages wait in LDS from before the first, a longer K is run in
 // parts.
 constexpr int kRunStages = 128;
@@ -784,8 +789,9 @@ __global__ __launch_bounds__(512) void big_kernel(const GemmArgs g) {
     // Filling.  A wave's i-th load fills rows 64 i + 8 w .. + 7 of a region, which are neighbours in x or the weights: their first
     // one is wave-uniform, this lane's place behind it is the same for all (with 4-bit weights a load is 32 rows' codes).  Rows
     // past the end repeat the last one; never stored.
-    const int kin_a = ((lane & 7) ^ swz_a(8 * wave + (lane >> 3))) * 8;
-    const int kin_b = FOUR ? (lane & 1) * 32 : ((lane & 7) ^ swz_b(8 * wave + (lane >> 3))) * 8;
+    const int at_k = (lane & 7) ^ swz_a(8 * wave + (lane >> 3));
+    const int kin_a = (FOUR ? 2 * (at_k & 3) + (at_k >> 2) : at_k) * 8;  // (4-bit: chunk 2 q + s at the place of 4 s + q, which is read conflict-free)
+    const int kin_b = FOUR ? ((lane ^ (lane >> 4)) & 1) * 32 : ((lane & 7) ^ swz_b(8 * wave + (lane >> 3))) * 8;
     const uint32_t lane_a = (uint32_t)(lane >> 3) * (uint32_t)g.K * 2u + (uint32_t)kin_a * 2u;
     uint32_t lane_b = (uint32_t)(lane >> 3) * (uint32_t)g.K * 2u + (uint32_t)kin_b * 2u;
     const char *row_b[2][2] = {{nullptr, nullptr}, {nullptr, nullptr}};  // [p][i]; FOUR: [0][0] alone
@@ -795,7 +801,10 @@ __global__ __launch_bounds__(512) void big_kernel(const GemmArgs g) {
     if constexpr (FOUR) {
         const uint8_t *const codes = (EPI == kGate && (wave & 1) ? g.up.codes : g.b.codes) + (size_t)n0 * (g.K / 2);
         row_b[0][0] = uniform(reinterpret_cast<const char *>(codes));
-        lane_b = (uint32_t)column(32 * wave + (lane >> 1)) * (uint32_t)(g.K / 2) + (uint32_t)kin_b / 2u;
+        // Codes of 32 rows: those of an operand's 16 rows follow each other, and the two halves of a row change places in
+        // every other eight rows, so that 32 lanes read all 64 banks.
+        const int at = lane >> 1, row = 8 * ((at >> 2) & 3) + 4 * (at >> 4) + (at & 3);
+        lane_b = (uint32_t)column(32 * wave + row) * (uint32_t)(g.K / 2) + (uint32_t)kin_b / 2u;
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -855,7 +864,7 @@ __global__ __launch_bounds__(512) void big_kernel(const GemmArgs g) {
     int at_a[2], at_b[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        at_a[s] = (16 * Q * wr + l16) * 8 + ((FOUR ? 2 * g4 + s : 4 * s + g4) ^ swz_a(l16));
+        at_a[s] = (16 * Q * wr + l16) * 8 + ((4 * s + g4) ^ swz_a(l16));
         at_b[s] = (32 * wc + pair_column(lane, 0)) * 8 + ((4 * s + g4) ^ swz_b(pair_column(lane, 0)));  // (the pair's other block: 4 rows on)
     }
     const auto read_a = [&](int slot, int at) {
@@ -877,7 +886,7 @@ __global__ __launch_bounds__(512) void big_kernel(const GemmArgs g) {
 #pragma unroll
             for (int nb = 0; nb < 2; ++nb) {
                 const int r = 64 * wc + 32 * p + pair_column(lane, nb);
-                code[p][nb] = from[r * 4 + g4];
+                code[p][nb] = from[(64 * wc + 32 * p + 16 * nb + l16) * 4 + (((g4 >> 1) ^ (l16 >> 3)) * 2 + (g4 & 1))];
                 scale[p][nb] = scales[r * (SCALE_ROW / 4) + (st >> 1)];
             }
     };
