@@ -413,6 +413,12 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
 // to the other buffer after them) and take CB blocks of 16 weight rows each (kGate:
 // the first half gate, the second the same columns of up); KG such groups take K's
 // slices in turn and meet in LDS.  gridDim.z cuts K further.
+//   Four groups make a short chain where columns are few (48 rows of 2 x 5504 columns, K =
+// 2048: 12.9 us, 0.9 TB/s; 64 rows of 5000: 12.9), eight waves side by side read x least
+// where they are many (32 rows of 102400 columns: 33 us from the L2s and the memory-side
+// cache, 40 from memory, 2.8 TB/s), and 64 x 128 tiles carry up to some 2000 rows (2048 x
+// 2048 of K = 5504: 53 us, 870 TFLOP/s).  The chain of a slice bounds it: its rows through
+// LDS, 32 conversions a block, then the products.
 template <int MB, int CB, int WC, int KG, int SL, int EPI>
 __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
     constexpr int JB = EPI == kGate ? CB / 2 : CB, COLS = 16 * JB * WC;
@@ -594,13 +600,17 @@ __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
 }
 
 // A middling number of rows, bf16 weights: a BM x BN tile on WR x WC waves, K in stages of
-// 64 through a ring of D LDS stages that direct global -> LDS loads fill ahead; all P planes of
-// x are in a stage, so the weights are loaded once.  A stage's
-// operands are read while the products of the one before run, so that one barrier a stage
-// is all that the waves wait for together: behind it a stage has landed for all of them
-// and the slot of the one before is free.  With kGate the BN weight rows are, for each
-// column of waves, 32 rows of the gate and the same 32 of the up projection, so that a lane
-// ends up with both products of its columns.
+// 64 through a ring of D LDS stages that direct global -> LDS loads fill ahead; all P planes
+// of x are in a stage, so that the weights are loaded once (64 rows, K = 10944: 26 us, where
+// planes one after the other as a longer K took 39).  A stage's operands are read while the
+// products of the one before run, so that one barrier a stage is all that the waves wait
+// for together: behind it a stage has landed for all of them and the slot of the one before
+// is free.  With kGate the BN weight rows are, for each column of waves, 32 rows of the gate
+// and the same 32 of the up projection, so that a lane ends up with both products of its
+// columns.
+//   The loads bound it: a CU takes 18 to 27 ns for each KB of them whatever else it does (a
+// stage of 64 x 128: 24 KB, 0.48 us; deeper rings, loads through registers and loads between
+// the products are no faster).  544 rows of 2 x 1368 columns, K = 2048: 18.4 us, 330 TFLOP/s.
 template <int BM, int BN, int D, int WR, int WC, int EPI, int P>
 __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
     constexpr int NW = WR * WC, AR = P * BM;
@@ -755,6 +765,9 @@ __global__ __launch_bounds__(64 * WR * WC) void tile_kernel(const GemmArgs g) {
 // 32-k steps (the rows' chunks lie in that order); phases 0 and 1 make them bf16.  The
 // scales of up to kRunStages stages wait in LDS from before the first, a longer K is run in
 // parts.
+//   bf16: 4160 x 2 x 10944 columns of K = 2048 in 310 us, 1200 TFLOP/s (4096 x 4096 of K =
+// 16384: 1460; a tile's start and end cost 8 us, its 32 stages 46); 4 bits: 4096 x 8192 of
+// K = 2048 in 118 us, 1165 TFLOP/s, the conversions beside the products.
 constexpr int kRunStages = 128;
 enum Region : int { kB0, kA0, kB1, kA1 };  // in the order that they are filled
 // Loads that a wave makes for a region.
