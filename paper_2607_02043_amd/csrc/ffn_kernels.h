@@ -91,8 +91,10 @@ inline bool fits(const GemmArgs &g, bool four_bit, Epilogue epi, const Shape &t)
     const bool big = t.variant == kBig128 || t.variant == kBig256;
     if (big && stages < 2) return false;
     if (t.splits == 1) return true;
-    // no part is empty: the kernels for many rows count in units of stages, the others in stages or in slices of up to four
-    const long long pieces = (long long)(big ? (stages < kUnitStages ? 1 : stages / kUnitStages) : (stages + 3) / 4) * (planes_together(t.variant) ? 1 : g.a_planes);
+    // no part is empty: those for few rows deal out slices of two stages to eight waves, those for many count in units of
+    // stages, the others in stages or in slices of up to four
+    const int once = t.variant <= kRows16Narrow ? ((stages + 1) / 2 + 7) / 8 : big ? (stages < kUnitStages ? 1 : stages / kUnitStages) : (stages + 3) / 4;
+    const long long pieces = (long long)once * (planes_together(t.variant) ? 1 : g.a_planes);
     return n.m * n.n <= kMaxSplitTiles && t.splits <= pieces &&
            (size_t)(n.m * n.n) * t.splits * kSizes[t.variant].bm * kSizes[t.variant].bn * 4 <= kPartBytes;
 }

@@ -70,27 +70,26 @@ def test_ffn_sizes(T, four, hidden, inner):
 # (0 product with 4-bit weights, 1 block in bf16, 2 block in 4 bits; rows; in or hidden; out or inner; fp32 output): calls
 # that between them choose every kernel, whole and in parts, in every product that it takes, and rows left to a second launch
 EVERY_KERNEL = [
-    (0, 2169, 96, 40, 0), (0, 2207, 2656, 40, 0), (0, 2249, 5344, 952, 1), (0, 2759, 3744, 72, 1), (0, 2775, 2720, 40, 0),
-    (0, 2912, 6784, 752, 0), (0, 3258, 160, 200, 1), (0, 4253, 3968, 8, 0), (0, 4447, 192, 80, 0), (0, 4461, 160, 8, 1),
-    (0, 4479, 2304, 8, 1), (1, 4, 8, 328, 1), (1, 10, 8, 1056, 0), (1, 1048, 112, 200, 1), (1, 1361, 3152, 728, 1),
-    (1, 1925, 2128, 8, 1), (1, 2121, 1128, 24, 0), (1, 2503, 904, 4200, 0), (1, 2552, 3160, 72, 1), (1, 2773, 712, 1072, 1),
-    (1, 2892, 8, 136, 0), (1, 3368, 72, 624, 1), (1, 3596, 1272, 1600, 1), (1, 3695, 1064, 72, 0), (1, 3714, 10504, 320, 0),
-    (1, 3882, 80, 1192, 0), (1, 4173, 8, 1864, 0), (1, 4186, 952, 5440, 0), (1, 4225, 3504, 8, 0), (1, 4253, 16, 8448, 0),
-    (1, 4302, 1552, 8, 1), (1, 4305, 8, 200, 1), (1, 4339, 8, 2560, 1), (1, 4426, 3648, 96, 0), (2, 341, 128, 2080, 1),
-    (2, 393, 2720, 32, 1), (2, 408, 9504, 96, 1), (2, 451, 4256, 1920, 1), (2, 480, 128, 4192, 1), (2, 684, 5184, 32, 1),
-    (2, 801, 64, 7424, 0), (2, 1155, 32, 4000, 1), (2, 1238, 7584, 32, 0), (2, 1413, 7328, 128, 1), (2, 1420, 5440, 768, 1),
-    (2, 1532, 96, 32, 1), (2, 1693, 2432, 160, 1), (2, 1812, 2720, 288, 1), (2, 2103, 96, 32, 1), (2, 2186, 2368, 32, 1),
-    (2, 2220, 64, 800, 1), (2, 2699, 1472, 32, 0), (2, 2700, 1696, 5184, 0), (2, 2743, 160, 4320, 0), (2, 2935, 5312, 768, 1),
-    (2, 3380, 1216, 800, 0), (2, 3421, 672, 2240, 1), (2, 3458, 1248, 2048, 1), (2, 3546, 8256, 288, 1), (2, 3737, 160, 1664, 1),
-    (2, 4101, 3424, 256, 0), (2, 4187, 96, 32, 1), (2, 4213, 2112, 32, 1), (2, 4234, 32, 1088, 1), (2, 4255, 96, 864, 1),
-    (2, 4313, 160, 96, 0), (2, 4473, 160, 32, 1),
-    (0, 21, 2944, 16752, 0), (2, 19, 8704, 3264, 1), (2, 21, 2080, 8704, 0),
-    (1, 2378, 40, 520, 1), (1, 3265, 1240, 72, 1), (1, 4387, 408, 3456, 1), (2, 2125, 64, 672, 1), (1, 4310, 8, 1040, 1),
-    (1, 3791, 1224, 2000, 1), (1, 4180, 16, 10728, 1),
-    (1, 1552, 64, 1344, 0), (1, 952, 64, 2376, 0), (0, 4180, 2080, 32, 0), (1, 1040, 24, 2680, 0), (1, 1636, 1088, 40, 0), (1, 1781, 72, 520, 1), (1, 2590, 1728, 4944, 0),
-    (1, 2785, 24, 528, 0), (1, 2954, 656, 4320, 0), (1, 4212, 160, 3048, 0), (1, 4256, 24, 2104, 0), (1, 4262, 24, 11160, 1),
-    (1, 4303, 4104, 208, 0), (1, 4355, 4560, 496, 0), (1, 4366, 8, 2264, 1), (1, 737, 3184, 16, 0), (2, 1037, 544, 32, 0),
-    (2, 369, 3136, 32, 1), (2, 56, 416, 2304, 1), (2, 677, 32, 3232, 0),
+    (0, 21, 2944, 16752, 0), (0, 2169, 96, 40, 0), (0, 2207, 2656, 40, 0), (0, 2249, 5344, 952, 1), (0, 2759, 3744, 72, 1),
+    (0, 2775, 2720, 40, 0), (0, 2912, 6784, 752, 0), (0, 3258, 160, 200, 1), (0, 4180, 2080, 32, 0), (0, 4253, 3968, 8, 0),
+    (0, 4447, 192, 80, 0), (0, 4461, 160, 8, 1), (0, 4479, 2304, 8, 1), (1, 2, 2056, 8, 0), (1, 4, 8, 328, 1), (1, 10, 8, 1056, 0),
+    (1, 703, 24, 2440, 1), (1, 737, 3184, 16, 0), (1, 952, 64, 2376, 0), (1, 1040, 24, 2680, 0), (1, 1048, 112, 200, 1),
+    (1, 1361, 3152, 728, 1), (1, 1552, 64, 1344, 0), (1, 1636, 1088, 40, 0), (1, 1781, 72, 520, 1), (1, 1925, 2128, 8, 1),
+    (1, 2121, 1128, 24, 0), (1, 2378, 40, 520, 1), (1, 2503, 904, 4200, 0), (1, 2552, 3160, 72, 1), (1, 2590, 1728, 4944, 0),
+    (1, 2773, 712, 1072, 1), (1, 2785, 24, 528, 0), (1, 2892, 8, 136, 0), (1, 2954, 656, 4320, 0), (1, 3265, 1240, 72, 1),
+    (1, 3368, 72, 624, 1), (1, 3596, 1272, 1600, 1), (1, 3695, 1064, 72, 0), (1, 3714, 10504, 320, 0), (1, 3791, 1224, 2000, 1),
+    (1, 3882, 80, 1192, 0), (1, 4173, 8, 1864, 0), (1, 4180, 16, 10728, 1), (1, 4186, 952, 5440, 0), (1, 4212, 160, 3048, 0),
+    (1, 4225, 3504, 8, 0), (1, 4253, 16, 8448, 0), (1, 4256, 24, 2104, 0), (1, 4262, 24, 11160, 1), (1, 4302, 1552, 8, 1),
+    (1, 4303, 4104, 208, 0), (1, 4305, 8, 200, 1), (1, 4310, 8, 1040, 1), (1, 4339, 8, 2560, 1), (1, 4355, 4560, 496, 0),
+    (1, 4366, 8, 2264, 1), (1, 4387, 408, 3456, 1), (1, 4426, 3648, 96, 0), (2, 18, 32, 1568, 1), (2, 19, 8704, 3264, 1),
+    (2, 21, 2080, 8704, 0), (2, 56, 416, 2304, 1), (2, 341, 128, 2080, 1), (2, 369, 3136, 32, 1), (2, 393, 2720, 32, 1),
+    (2, 408, 9504, 96, 1), (2, 451, 4256, 1920, 1), (2, 480, 128, 4192, 1), (2, 677, 32, 3232, 0), (2, 684, 5184, 32, 1),
+    (2, 801, 64, 7424, 0), (2, 1037, 544, 32, 0), (2, 1155, 32, 4000, 1), (2, 1238, 7584, 32, 0), (2, 1413, 7328, 128, 1),
+    (2, 1420, 5440, 768, 1), (2, 1532, 96, 32, 1), (2, 1693, 2432, 160, 1), (2, 1812, 2720, 288, 1), (2, 2103, 96, 32, 1),
+    (2, 2125, 64, 672, 1), (2, 2186, 2368, 32, 1), (2, 2220, 64, 800, 1), (2, 2699, 1472, 32, 0), (2, 2700, 1696, 5184, 0),
+    (2, 2743, 160, 4320, 0), (2, 2935, 5312, 768, 1), (2, 3380, 1216, 800, 0), (2, 3421, 672, 2240, 1), (2, 3458, 1248, 2048, 1),
+    (2, 3546, 8256, 288, 1), (2, 3737, 160, 1664, 1), (2, 4101, 3424, 256, 0), (2, 4187, 96, 32, 1), (2, 4213, 2112, 32, 1),
+    (2, 4234, 32, 1088, 1), (2, 4255, 96, 864, 1), (2, 4313, 160, 96, 0), (2, 4473, 160, 32, 1),
 ]
 
 
