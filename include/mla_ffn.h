@@ -24,8 +24,8 @@
  *   the values from 2^128 on (b = 253 and 254 only) count as infinite.
  *
  * Precision: bf16 inputs, fp32 sums.  h is computed in fp32 and meets w_down
- * as one bf16, rounded to nearest even, where out is bf16, and as the sum of
- * three (24 bits) where out is fp32.  Values that are not finite count as the
+ * as one bf16, rounded to nearest even, where out is bf16, and with all its 24
+ * bits, as the sum of three, where out is fp32.  Values that are not finite count as the
  * formulas say, in every row that they belong to and no other.
  *
  * Conventions, errors and streams are those of mla_step.h.  Device arrays are

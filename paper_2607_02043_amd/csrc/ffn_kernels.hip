@@ -50,13 +50,15 @@ __device__ __forceinline__ float gated(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.f + e * (1.f - rest * kLn2)) * u;
 }
 
-// v as the sum of bf16 values, most significant first: the next plane takes what the
-// last one left.  A value whose first rounding is not finite has zeros behind it.
-__device__ __forceinline__ uint32_t next_plane(float &v) {
-    const uint32_t b = bf16_of(v);
+// h as the sum of three bf16 values, most significant first: each takes the eight leading bits of what the last one left,
+// so the sum is h itself.  None has the other sign, and none is zero unless h is (the least value of h's sign stands for
+// it, 2^-133), so that an infinite weight, or an infinite h, makes a sum infinite as it should and not inf - inf or 0 inf.
+__device__ __forceinline__ uint32_t least_plane(float h) { return h != 0.f ? (__float_as_uint(h) >> 31 << 15) | 1u : 0u; }
+__device__ __forceinline__ uint32_t next_plane(float &v, uint32_t least) {
+    const uint32_t b = __float_as_uint(v) >> 16;
     const float r = v - bf16_value(b);
     v = fabsf(r) < INFINITY ? r : 0.f;
-    return b;
+    return (b & 0x7fffu) != 0u ? b : least;
 }
 
 // A wave-uniform pointer, in scalar registers.
@@ -148,11 +150,18 @@ __device__ __forceinline__ void store_h(const GemmArgs &g, f32x4 g0, f32x4 g1, f
         h[4 + i] = gated(g1[i], u1[i]);
     }
     uint16_t *dst = static_cast<uint16_t *>(g.out) + (size_t)row * g.N + n;
+    if (g.h_planes == 1) {  // rounded to nearest
+        *reinterpret_cast<u32x4 *>(dst) = u32x4{pack2(h[0], h[1]), pack2(h[2], h[3]), pack2(h[4], h[5]), pack2(h[6], h[7])};
+        return;
+    }
+    uint32_t least[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) least[i] = least_plane(h[i]);
     for (int p = 0; p < g.h_planes; ++p, dst += (size_t)g.plane_rows * g.N) {
         u32x4 v;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = next_plane(h[2 * k]), hi = next_plane(h[2 * k + 1]);
+            const uint32_t lo = next_plane(h[2 * k], least[2 * k]), hi = next_plane(h[2 * k + 1], least[2 * k + 1]);
             v[k] = lo | (hi << 16);
         }
         *reinterpret_cast<u32x4 *>(dst) = v;
@@ -241,11 +250,18 @@ __device__ __forceinline__ void store_h4(const GemmArgs &g, f32x4 gate, f32x4 up
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = gated(gate[i], up[i]);
     uint16_t *dst = static_cast<uint16_t *>(g.out) + (size_t)row * g.N + n;
+    if (g.h_planes == 1) {
+        *reinterpret_cast<u32x2 *>(dst) = u32x2{pack2(h[0], h[1]), pack2(h[2], h[3])};
+        return;
+    }
+    uint32_t least[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) least[i] = least_plane(h[i]);
     for (int p = 0; p < g.h_planes; ++p, dst += (size_t)g.plane_rows * g.N) {
         u32x2 v;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const uint32_t lo = next_plane(h[2 * k]), hi = next_plane(h[2 * k + 1]);
+            const uint32_t lo = next_plane(h[2 * k], least[2 * k]), hi = next_plane(h[2 * k + 1], least[2 * k + 1]);
             v[k] = lo | (hi << 16);
         }
         *reinterpret_cast<u32x2 *>(dst) = v;
@@ -1077,7 +1093,7 @@ hipError_t launch_big(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s)
 }
 template <int CB, bool FOUR>
 hipError_t launch_rows(const GemmArgs &g, Epilogue epi, dim3 grid, hipStream_t s) {
-    constexpr int kAlone = FOUR ? 1 : 3;  // planes in front of fp32: a product on its own has one (and 4-bit weights)
+    constexpr int kAlone = FOUR ? 1 : 3;  // in front of fp32 one plane is a product on its own, which has 4-bit weights
     return launch_epilogue(epi, rows_kernel<1, CB, FOUR, kStoreBf16, 1>, g.a_planes == 3 ? rows_kernel<1, CB, FOUR, kStoreF32, 3> : rows_kernel<1, CB, FOUR, kStoreF32, kAlone>,
                            rows_kernel<1, CB, FOUR, kGate, 1>, grid, 512, s, g);
 }

@@ -231,6 +231,42 @@ def test_large_gates_and_infinite_h(T, dtype):
     assert np.all(np.abs(got[:, 0] - 6000.0) <= (0.0 if dtype == F32 else 2 * 2.0 ** -8 * 6000.0)) and not got[:, 1:].any()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=_name)
+@pytest.mark.parametrize("T", [2, 40, 300, 1100])
+def test_infinite_weights_of_the_down_projection(T, dtype):
+    """An infinite weight makes its column infinite with the sign of h, whatever the bits of h; beside others of the same
+    sign too, and an infinite h beside it."""
+    hidden, inner = 128, 160
+    x, mats = rows(61, T, hidden), block(62, hidden, inner, False)
+    mats[2].w[7, 3] = math.inf
+    mats[2].w[9, 100] = -math.inf
+    assert_within(ffn(x, mats, dtype), *O.ffn(x.double().numpy(), *(m.values for m in mats), 3 if dtype == F32 else 1), dtype, "random h")
+    for m in mats:
+        m.w[:] = 0
+    x[:] = 0
+    x[:, 0] = 1.0
+    gate, up, down = (m.w for m in mats)
+    gate[0, 0], up[0, 0] = 1000.0, 3.0     # h = 3000: two planes and nothing behind them
+    gate[1, 0], up[1, 0] = 1024.0, -2.0    # h = -2048: one
+    gate[2, 0], up[2, 0] = 1e30, 1e30      # h infinite
+    down[:, 2] = 1.0
+    down[:2, 0], down[2:4, 1], down[4, 2] = math.inf, -math.inf, math.inf
+    down[5:7, 0], down[5, 1], down[6, 1] = math.inf, -math.inf, math.inf
+    down[:, 3:] = 1.0
+    got = ffn(x, mats, dtype)
+    assert np.all(got[:, [0, 1, 2, 3, 4, 5, 7]] == np.inf) and np.isnan(got[:, 6]).all()
+
+
+@pytest.mark.parametrize("T", [2, 40, 300])
+def test_infinite_4_bit_weights_of_the_down_projection(T):
+    x, mats = rows(63, T, 64), block(64, 64, 96, True)
+    mats[2].codes[5, 16:32], mats[2].scales[5, 1] = 0, 254
+    mats[2].codes[5, 20] = 0x50  # 3 x 2^127 at k = 41 of column 5: infinite, nothing else of its group
+    ref = O.ffn(x.double().numpy(), *(m.values for m in mats), 3)
+    assert np.isinf(ref[0][:, 5]).all()
+    assert_within(ffn(x, mats, F32), *ref, F32, f"{T} rows")
+
+
 @pytest.mark.parametrize("four", [False, True], ids=["bf16w", "mx4"])
 @pytest.mark.parametrize("T", [1, 50, 200, 700])
 def test_same_call_same_bits_on_another_stream_and_a_larger_workspace(T, four):
