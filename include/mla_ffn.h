@@ -24,9 +24,11 @@
  *   the values from 2^128 on (b = 253 and 254 only) count as infinite.
  *
  * Precision: bf16 inputs, fp32 sums.  h is computed in fp32 and meets w_down
- * as one bf16, rounded to nearest even, where out is bf16, and with all its 24
- * bits, as the sum of three, where out is fp32.  Values that are not finite count as the
- * formulas say, in every row that they belong to and no other.
+ * as one bf16, rounded to nearest even, where out is bf16.  Where out is fp32 it
+ * meets it as the sum of three bf16: with all its 24 bits from 2^-110 on, below
+ * that as the nearest multiple of 2^-133, and no smaller than 3 x 2^-133 unless
+ * it is 0.  Values that are not finite count as the formulas say, in every row
+ * that they belong to and no other.
  *
  * Conventions, errors and streams are those of mla_step.h.  Device arrays are
  * contiguous and 16-byte aligned; out overlaps no input and no workspace.

@@ -50,15 +50,35 @@ __device__ __forceinline__ float gated(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.f + e * (1.f - rest * kLn2)) * u;
 }
 
-// h as the sum of three bf16 values, most significant first: each takes the eight leading bits of what the last one left,
-// so the sum is h itself.  None has the other sign, and none is zero unless h is (the least value of h's sign stands for
-// it, 2^-133), so that an infinite weight, or an infinite h, makes a sum infinite as it should and not inf - inf or 0 inf.
-__device__ __forceinline__ uint32_t least_plane(float h) { return h != 0.f ? (__float_as_uint(h) >> 31 << 15) | 1u : 0u; }
-__device__ __forceinline__ uint32_t next_plane(float &v, uint32_t least) {
-    const uint32_t b = __float_as_uint(v) >> 16;
-    const float r = v - bf16_value(b);
-    v = fabsf(r) < INFINITY ? r : 0.f;
-    return (b & 0x7fffu) != 0u ? b : least;
+// h as the sum of three bf16 values of one sign, most significant first: h itself from 2^-110 on, below that the nearest
+// multiple of kLeast = 2^-133, the least bf16.  None is zero unless h is, so that an infinite weight, or an infinite h, makes
+// a sum infinite as it should and not inf - inf or 0 inf.  So the first two leave `room` for each one behind them: h's last
+// bit, at least kLeast.  Then the first leaves at most 2^16 + 1 of h's last bits and the second at most 2^8, which the third
+// holds; every partial sum is a multiple of that bit, and exact in fp32.  A nonzero h counts as 3 kLeast at least.
+// (Planes filled up with kLeast, which the others did not make room for, put h off by up to 2 kLeast: 1.6 % at 2^-126.)
+constexpr float kLeast = 0x1p-133f;
+__device__ __forceinline__ float least_plane(float h) { return h != 0.f ? kLeast : 0.f; }
+__device__ __forceinline__ float plane_room(float h, float least) { return fmaxf(__uint_as_float(__float_as_uint(h) & 0x7f800000u) * 0x1p-23f, least); }
+// One of the first two of v = |h| or what the one before left, and v what it leaves.  (Of an infinite v the largest number,
+// and v stays as it is; so does a NaN.)
+__device__ __forceinline__ uint32_t next_plane(float &v, float room, float least) {
+    const float most = fminf(v - room, 3.40282347e38f);  // negative where v < room
+    const int b = max((int)__float_as_uint(most) >> 16, (int)__float_as_uint(least) >> 16);
+    v -= bf16_value((uint32_t)b);
+    return (uint32_t)b;
+}
+// N values h, in pairs, as the P-th plane takes them; `v` holds |h| before the first.
+template <int P, int N>
+__device__ __forceinline__ void plane_of(uint32_t (&to)[N / 2], const float (&h)[N], float (&v)[N]) {
+    uint32_t b[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float least = least_plane(h[i]);
+        b[i] = P < 2 ? next_plane(v[i], (2 - P) * plane_room(h[i], least), least) : bf16_of(v[i] < least ? least : v[i]);
+        b[i] |= __float_as_uint(h[i]) >> 16 & 0x8000u;
+    }
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) to[k] = b[2 * k] | (b[2 * k + 1] << 16);
 }
 
 // A wave-uniform pointer, in scalar registers.
@@ -154,18 +174,17 @@ __device__ __forceinline__ void store_h(const GemmArgs &g, f32x4 g0, f32x4 g1, f
         *reinterpret_cast<u32x4 *>(dst) = u32x4{pack2(h[0], h[1]), pack2(h[2], h[3]), pack2(h[4], h[5]), pack2(h[6], h[7])};
         return;
     }
-    uint32_t least[8];
+    float v[8];
+    uint32_t b[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) least[i] = least_plane(h[i]);
-    for (int p = 0; p < g.h_planes; ++p, dst += (size_t)g.plane_rows * g.N) {
-        u32x4 v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = next_plane(h[2 * k], least[2 * k]), hi = next_plane(h[2 * k + 1], least[2 * k + 1]);
-            v[k] = lo | (hi << 16);
-        }
-        *reinterpret_cast<u32x4 *>(dst) = v;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = fabsf(h[i]);
+    const size_t plane = (size_t)g.plane_rows * g.N;
+    plane_of<0>(b, h, v);
+    *reinterpret_cast<u32x4 *>(dst) = u32x4{b[0], b[1], b[2], b[3]};
+    plane_of<1>(b, h, v);
+    *reinterpret_cast<u32x4 *>(dst + plane) = u32x4{b[0], b[1], b[2], b[3]};
+    plane_of<2>(b, h, v);
+    *reinterpret_cast<u32x4 *>(dst + 2 * plane) = u32x4{b[0], b[1], b[2], b[3]};
 }
 
 // Split sums.  Parts meet in memory; the XCDs do not share their L2 caches.  THROUGH: they are written and read as
@@ -254,18 +273,17 @@ __device__ __forceinline__ void store_h4(const GemmArgs &g, f32x4 gate, f32x4 up
         *reinterpret_cast<u32x2 *>(dst) = u32x2{pack2(h[0], h[1]), pack2(h[2], h[3])};
         return;
     }
-    uint32_t least[4];
+    float v[4];
+    uint32_t b[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) least[i] = least_plane(h[i]);
-    for (int p = 0; p < g.h_planes; ++p, dst += (size_t)g.plane_rows * g.N) {
-        u32x2 v;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const uint32_t lo = next_plane(h[2 * k], least[2 * k]), hi = next_plane(h[2 * k + 1], least[2 * k + 1]);
-            v[k] = lo | (hi << 16);
-        }
-        *reinterpret_cast<u32x2 *>(dst) = v;
-    }
+    for (int i = 0; i < 4; ++i) v[i] = fabsf(h[i]);
+    const size_t plane = (size_t)g.plane_rows * g.N;
+    plane_of<0>(b, h, v);
+    *reinterpret_cast<u32x2 *>(dst) = u32x2{b[0], b[1]};
+    plane_of<1>(b, h, v);
+    *reinterpret_cast<u32x2 *>(dst + plane) = u32x2{b[0], b[1]};
+    plane_of<2>(b, h, v);
+    *reinterpret_cast<u32x2 *>(dst + 2 * plane) = u32x2{b[0], b[1]};
 }
 
 // Few rows: the call is bound by reading the weights once, so they go straight from
