@@ -39,15 +39,17 @@ __device__ __forceinline__ u32x4 mx_values(uint32_t codes, float scale) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
 
-// h = silu(g) u = g u / (1 + exp(-g)), silu off by less than 2^-21 of itself or 2^-120: exp(-g) as 2^(-g log2 e) with
-// the product's own rounding put back, then the hardware's quotient (1 ulp).  From |g| = 200 on exp(-g) is 0 or infinite,
-// and silu g or 0.  (The library's expf and division: a sixth of a 256 x 256 tile's time, 9 of 57 us.)
+// h = silu(g) u = g u / (1 + exp(-g)), silu off by less than 2^-21 of itself where exp(-g) is a number, down to g = -88.72:
+// exp(-g) as 2^(-g log2 e) with the product's own rounding put back, then the hardware's reciprocal (1 ulp).  That gives
+// no subnormal numbers, so it takes a quarter of the sum, which stays below 2^126, and a quarter of g (whose last bits count
+// below 2^-124 alone, 2^-149 of the result).  Further down exp(-g) is infinite and silu, less than 2^-121, is -0; from 200 on
+// silu is g.  (The library's expf and division: a sixth of a 256 x 256 tile's time, 9 of 57 us.)
 __device__ __forceinline__ float gated(float g, float u) {
     constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147182f;
     const float c = __builtin_amdgcn_fmed3f(g, -200.f, 200.f), t = c * kLog2e;
     const float rest = __builtin_fmaf(c, kLog2e, -t) + c * kLog2eRest;
     const float e = __builtin_amdgcn_exp2f(-t);
-    return g * __builtin_amdgcn_rcpf(1.f + e * (1.f - rest * kLn2)) * u;
+    return .25f * g * __builtin_amdgcn_rcpf(.25f + e * (.25f - rest * (.25f * kLn2))) * u;
 }
 
 // h as the sum of three bf16 values of one sign, most significant first: h itself from 2^-110 on, below that the nearest
