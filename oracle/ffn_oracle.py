@@ -61,3 +61,20 @@ def ffn(x, gate, up, down, planes):
 def rounded_bound(out, bound, bf16):
     """The bound with the output's own rounding: half a step, 2^-8 or 2^-24 of the value."""
     return bound + (2.0 ** -8 if bf16 else 2.0 ** -24) * (np.abs(out) + bound)
+
+
+def _sums_norm(k, planes=1):
+    """As _sums, of all outputs together in the 2-norm, where products have random signs: each of the roundings is off by a step
+    (2^-23) at most of a partial sum, which is no larger than the result in the mean, and they are independent."""
+    return np.sqrt(64.0 + planes * k / 32.0) * 2.0 ** -23
+
+
+def linear_norm(k):
+    """Bound on |got - out| / |out| in the 2-norm for an fp32 result of random values."""
+    return _sums_norm(k)
+
+
+def ffn_norm(hidden, inner):
+    """The same for a block whose h meets w_down with 24 bits: errors of g (|silu'| < 1.1) and u, the gate's 2^-21, h's
+    2^-24, then those of the down projection."""
+    return 2.1 * _sums_norm(hidden) + 2.0 ** -21 + 2.0 ** -24 + _sums_norm(inner, 3)
