@@ -37,10 +37,12 @@
  * Workspaces are caller-allocated device memory.  The first
  * MLA_FFN_COUNTER_BYTES bytes are counters: they must be zero when a workspace
  * is first used, and every completed call leaves them zero again.  The rest is
- * ignored on entry.  A workspace for T rows serves calls of fewer rows with
- * weights of the same sizes, and the same workspace may serve all entry points
- * in turn; calls that overlap in time need distinct ones.  Results do not depend
- * on what ran before: sums that are cut into parts are joined in one order.
+ * ignored on entry: 64 MiB for parts of sums whatever the sizes, and in a
+ * block's 6 T I bytes more whatever out's type.  A workspace for T rows serves
+ * calls of fewer rows with weights of the same sizes, and the same workspace may
+ * serve all entry points in turn; calls that overlap in time need distinct ones.
+ * Results do not depend on what ran before: sums that are cut into parts are
+ * joined in one order.
  */
 #ifndef MLA_FFN_H
 #define MLA_FFN_H

@@ -54,7 +54,8 @@ int check_workspace(const void *ws, size_t have, size_t need, int32_t T) {
 // Planes of h: one bf16 where the output is rounded to bf16 anyway, three (24 bits) in front of fp32.
 int planes_of(int32_t out_dtype) { return out_dtype == MLA_OUT_F32 ? 3 : 1; }
 
-// Workspace: the counters, room for the parts of split sums, then h (room for three planes).
+// Workspace: the counters, room for the parts of split sums (as much as any launch takes: the choice for fewer rows may
+// split where that for more does not), then h (room for three planes, as the output's type is not known here).
 size_t h_at() { return MLA_FFN_COUNTER_BYTES + ffn::kPartBytes; }
 size_t ffn_bytes(int32_t T, int32_t inner) { return h_at() + a256((size_t)T * (size_t)inner * 3 * 2); }
 size_t linear_bytes() { return MLA_FFN_COUNTER_BYTES + ffn::kPartBytes; }
@@ -72,11 +73,14 @@ int cu_count() {
     return ncu;
 }
 
-// What a launch takes, in us: sweeps of the kernels and numbers of parts over 180 products of 1 to 4160 rows (an
-// MI355X, weights from memory).  A workgroup walks its stages of 64 k (1 / groups of them) at `stage` us each; where
-// `resident` workgroups of a CU run at once, a stage takes `share` us for each of them, and rounds of them follow
-// each other.  Parts are stored at 2.5 TB/s by all, and read by the workgroup that joins a tile's at 60 GB/s.  The
-// rule's choice is within 12 % of the best for each product, and 0.5 % off it in the mean.
+// What a launch takes, in us, fitted to sweeps of the kernels and numbers of parts on an MI355X with weights from memory.
+// A workgroup walks its stages of 64 k (1 / groups of them) at `stage` us each; where a CU gets up to `resident` workgroups,
+// a stage takes `share` us for each of them, and rounds of them follow each other.  All five are numbers of the fit:
+// `resident` is not what registers and LDS let a CU hold (one to three workgroups, fewer than `resident` for the few-row
+// kernels, kTile32 and kMid16 to kMid48).  Parts are stored at 2.5 TB/s by all, and read by the workgroup that joins a
+// tile's at 60 GB/s.  Of 143 products of 1 to 2200 rows the choice takes 1.7 % longer than the best in the mean, 18 more
+// than 6 % and seven more than 12 %, all seven with 4-bit weights (64 rows of 2048 columns, K = 5504 in three planes:
+// 20.6 against 16.4 us).
 struct Cost {
     float fixed, stage, share;
     int resident, groups;
@@ -143,7 +147,7 @@ Plan best_whole(const ffn::GemmArgs &g, bool four, ffn::Epilogue epi, int ncu) {
 }
 
 // One launch for all rows, or one for a multiple of 128 or 256 and one for the rows behind it, which would
-// cost the first a round of workgroups (4160 rows x 2048 of K = 10944: 217 us, as 4096 and 64 rows 153 + 27).
+// cost the first a round of workgroups (4160 rows x 2048 of K = 10944: 219 us, as 4096 and 64 rows 156 + 20).
 // A thread keeps those of the last kKeptPlans sizes that it planned: a step calls with the same ones for every layer.
 // (On the host planning a launch takes 1 to 4 us, finding it 0.03: products of 1 to 4160 rows, 8 sizes in turn.)
 constexpr int kKeptPlans = 16;

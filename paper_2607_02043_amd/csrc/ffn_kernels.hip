@@ -190,7 +190,10 @@ __device__ __forceinline__ void store_h(const GemmArgs &g, f32x4 g0, f32x4 g1, f
 }
 
 // Split sums.  Parts meet in memory; the XCDs do not share their L2 caches.  THROUGH: they are written and read as
-// device-wide atomics, past the L2s, at 4 TB/s for the whole chip; otherwise as plain values, and a workgroup writes
+// device-wide atomics, past the L2s, at 4 TB/s for the whole chip, and counted with a relaxed one.  That order is the
+// instructions', not the language's (a release would write back the L2, which this is to avoid): vmcnt counts a device-wide
+// store once every XCD sees it, all waves have waited for theirs when the counter is raised, and a device-wide load takes
+// nothing from a cache that others do not see.  Otherwise the parts are stored as plain values, and a workgroup writes
 // back what its L2 holds before it is counted (some 3 us, more with more of them).  So small tiles go through (a row of
 // K = 10944 in 4 bits 10.6 -> 7.3 us, 16 rows in bf16 19.3 -> 13.7), those of 4-bit weights with 64 KB a part and the
 // tiles for many rows do not (1500 rows, parts of 256 KB: 102 against 116 us).
@@ -454,7 +457,8 @@ __global__ __launch_bounds__(512) void rows_kernel(const GemmArgs g) {
 // where they are many (32 rows of 102400 columns: 33 us from the L2s and the memory-side
 // cache, 40 from memory, 2.8 TB/s), and 64 x 128 tiles carry up to some 2000 rows (2048 x
 // 2048 of K = 5504: 53 us, 870 TFLOP/s).  The chain of a slice bounds it: its rows through
-// LDS, 32 conversions a block, then the products.
+// LDS, 32 conversions a block, then the products.  Planes of x follow each other as a longer
+// K, so a weight is loaded and converted once for each of them.
 template <int MB, int CB, int WC, int KG, int SL, int EPI>
 __global__ __launch_bounds__(64 * WC * KG) void mid_kernel(const GemmArgs g) {
     constexpr int JB = EPI == kGate ? CB / 2 : CB, COLS = 16 * JB * WC;
