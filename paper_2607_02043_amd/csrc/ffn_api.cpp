@@ -75,7 +75,7 @@ int cu_count() {
 
 // What a launch takes, in us, fitted to sweeps of the kernels and numbers of parts on an MI355X with weights from memory.
 // A workgroup walks its stages of 64 k (1 / groups of them) at `stage` us each; where a CU gets up to `resident` workgroups,
-// a stage takes `share` us for each of them, and rounds of them follow each other.  All five are numbers of the fit:
+// a stage takes `share` us for each of them, and rounds of them follow each other.  All but `groups` are numbers of the fit:
 // `resident` is not what registers and LDS let a CU hold (one to three workgroups, fewer than `resident` for the few-row
 // kernels, kTile32 and kMid16 to kMid48).  Parts are stored at 2.5 TB/s by all, and read by the workgroup that joins a
 // tile's at 60 GB/s.  Of 143 products of 1 to 2200 rows the choice takes 1.7 % longer than the best in the mean, 18 more
